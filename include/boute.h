@@ -45,6 +45,9 @@ typedef enum {
 
 typedef enum { BOUTE_ACQ_EHVI2D = 0, BOUTE_ACQ_MC_HVI = 1, BOUTE_ACQ_NEHVI = 2 } boute_acq_mode;
 
+/* Element types of the arrays that take more than one (logits). */
+typedef enum { BOUTE_F32 = 0, BOUTE_F16 = 1, BOUTE_BF16 = 2 } boute_dtype;
+
 /* Human-readable name of a status code (static string). */
 const char *boute_status_string(int status);
 
@@ -348,8 +351,8 @@ int boute_selftest_wait(int complete, unsigned long long limit_ns, void *stream)
  * its extent per source unit and skips the access (the bulk copies, the
  * operand images, the outputs, the strips and boxes, the selection). This
  * call waits for the device, returns 1 and fills rec (4 words: the source
- * unit 1 posterior, 2 in-sample, 3 acquisition, 4 front, 5 fit, 6 top-k;
- * the source line; the index; the extent) when some unit recorded one since
+ * unit 1 posterior, 2 in-sample, 3 acquisition, 4 front, 5 fit, 6 top-k,
+ * 7 log-probabilities, 8 answer scores, 9 routing; the source line; the index; the extent) when some unit recorded one since
  * the last call, else 0; it clears the records. The product library returns
  * BOUTE_ERR_UNSUPPORTED (its checks compile to nothing). */
 int boute_bounds_report(long long *rec);
@@ -575,6 +578,109 @@ int boute_mobo_run(const boute_mobo_config *cfg, int d, int m, const float *cand
                    const double *cons, int d_tau, double *kc, double *ls, double *s2,
                    double *noise, double *X, double *Y, int n0, boute_objective_fn f, void *user,
                    long long *sel, double *theta_hist, int *n_out, int *converged);
+
+/* ---- what a model's answers say ---------------------------------------------------
+ * Sec. 4.1: a query goes to a model by a routing score, and the observations of
+ * the search (quality, load) come from routing queries under a configuration.
+ * These calls evaluate that side on the device: the log-probabilities of the
+ * tokens of an answer, the scores of an answer, the choice of models or
+ * replicas for a query, and the gradients with which such a router is trained.
+ * Logits may be fp32, fp16 or bf16 (boute_dtype) and have their own row pitch
+ * (ld >= the row's length, in elements); any element-aligned address will do.
+ * Sums, maxima and softmax statistics are held in fp32.
+ *
+ * Per position of an answer, with z = scale * logits rounded once to fp32 (scale =
+ * 1 / temperature, finite and > 0), over the V tokens of a vocabulary:
+ *   lse = ln sum_j exp(z_j),  logprob = z_target - lse,
+ *   entropy = -sum_j p_j ln p_j with p_j = exp(z_j - lse) and 0 ln 0 = 0,
+ *   the k tokens of the largest z in the order (value descending, -0 as +0,
+ *   equal values by ascending index) and their log-probabilities.
+ * A token with z = -inf is masked: it has no probability and is never an
+ * alternative; alternatives that do not exist have index -1 and log-probability
+ * -inf. A row without a token left has lse = logprob = -inf and entropy 0. A
+ * row that holds a NaN or +inf has no distribution: its floats are NaN and its
+ * indices -1.
+ *   logits: T rows of V; targets: T int64; a target < 0 marks a position that
+ *   holds no token (logprob 0, whatever the row), one >= V gives logprob NaN;
+ *   logprob, entropy, lse: T fp32; top_idx: T x k int64, top_logprob: T x k
+ *   fp32 (both may be NULL when k = 0).
+ * 0 <= T < 2^31, 1 <= V <= BOUTE_MAX_VOCAB, 0 <= k <= min(V, BOUTE_MAX_ALTERNATIVES). */
+#define BOUTE_MAX_VOCAB (1 << 20)
+#define BOUTE_MAX_ALTERNATIVES 32
+int boute_token_logprobs(const void *logits, int dtype, long long T, int V, long long ld,
+                         const long long *targets, float scale, int k, float *logprob,
+                         float *entropy, float *lse, long long *top_idx, float *top_logprob,
+                         void *stream);
+/* Its gradient with respect to the logits, from the forward call's lse and
+ * entropy and the outputs' gradients g_logprob and g_entropy (T fp32 each;
+ * g_entropy, and entropy with it, may be NULL):
+ *   dlogits_j = scale (g_logprob ([j = target] - p_j) - g_entropy p_j (ln p_j + entropy)),
+ * rounded once to the logits' type. A position without a token takes g_logprob
+ * as 0; a row without a token left (lse = -inf) has gradient 0; a target >= V
+ * and a row without a distribution (lse NaN) have gradient NaN. dlogits: T rows
+ * of V with pitch ldd; it may be logits itself (with ldd = ld). */
+int boute_token_logprobs_grad(const void *logits, int dtype, long long T, int V, long long ld,
+                              const long long *targets, float scale, const float *lse,
+                              const float *entropy, const float *g_logprob,
+                              const float *g_entropy, void *dlogits, long long ldd, void *stream);
+
+/* The scores of Q answers, the features that a router reads: answer q holds
+ * the positions offsets[q] .. offsets[q + 1] - 1 of the T positions (offsets:
+ * Q + 1 int64, ascending, within [0, T]; what lies outside is not read), of
+ * which those with targets >= 0 count (targets NULL: all):
+ *   scores (Q x 4 fp32): mean logprob, lowest logprob, mean entropy, highest
+ *   entropy; counts (Q int32): the positions counted. An answer without any
+ *   has scores 0. NaN passes through to the mean and the extreme.
+ * 0 <= T < 2^31, 0 <= Q < 2^31. */
+int boute_answer_scores(const float *logprob, const float *entropy, const long long *targets,
+                        const long long *offsets, long long T, long long Q, float *scores,
+                        int *counts, void *stream);
+/* Its gradient: with g_scores (Q x 4) and n the positions that count,
+ *   g_logprob_t = g_0 / n + g_1 [t is the first with the lowest logprob],
+ *   g_entropy_t = g_2 / n + g_3 [t is the first with the highest entropy]
+ * (NaN before every number), 0 for positions that do not count or lie in no
+ * answer. g_logprob, g_entropy: T fp32. */
+int boute_answer_scores_grad(const float *logprob, const float *entropy,
+                             const long long *targets, const long long *offsets, long long T,
+                             long long Q, const float *g_scores, float *g_logprob,
+                             float *g_entropy, void *stream);
+
+/* Queries to experts (the models, or the replicas of their deployments), Sec.
+ * 4.1 and App. C: for each of T queries with logits x over E experts,
+ *   s = softmax(x) or 1 / (1 + exp(-x)) (mode; fp32: what underflows is 0), c = s + bias,
+ * the experts in G groups of E / G neighbours (models with their replicas): a
+ * group's score is the sum of its group_top (1 or 2) largest c, the keep groups
+ * with the largest scores stay, and of their experts the k with the largest c
+ * are chosen (in this order; equal values by ascending index). The bias moves
+ * choices (load balance), not weights: with the chosen s,
+ *   weight_i = factor s_i, or factor s_i / sum_chosen s (renorm; 0 when the sum is 0).
+ * An expert with x = -inf or with a bias of -inf or NaN is out of service: it is
+ * never chosen (x = -inf has no share of the softmax either), and a group
+ * without one in service is not kept; choices that do not exist have index -1
+ * and weight 0. A query whose logits hold a NaN (or, with softmax, +inf) has no
+ * choice: index -1, weights NaN.
+ *   logits: T rows of E with pitch ld; bias: E fp32 or NULL;
+ *   idx: T x k int32, weight: T x k fp32; load (E int32 or NULL): the queries
+ *   that chose each expert, written (not added to) by the call.
+ * E <= 1024, k <= 32, G <= 32, E a multiple of G, 1 <= keep <= G,
+ * k <= keep E / G, 0 <= T < 2^31, T k < 2^31. */
+typedef enum { BOUTE_ROUTE_SOFTMAX = 0, BOUTE_ROUTE_SIGMOID = 1 } boute_route_mode;
+#define BOUTE_MAX_EXPERTS 1024
+#define BOUTE_MAX_CHOICES 32
+#define BOUTE_MAX_GROUPS 32
+int boute_route(const void *logits, int dtype, long long T, int E, long long ld,
+                const float *bias, int mode, int G, int keep, int group_top, int k, int renorm,
+                float factor, int *idx, float *weight, int *load, void *stream);
+/* The gradient of the weights with respect to the logits, for the choices idx
+ * (T x k, -1 for none) held fixed; g_weight: T x k fp32. With S the sum of the
+ * chosen s,
+ *   ds_i = factor (g_i - sum_j g_j s_j / S) / S (renorm; 0 when S = 0) or factor g_i,
+ *   dlogits = ds s (1 - s) (sigmoid), dlogits_j = s_j (ds_j - sum_i ds_i s_i) (softmax),
+ * rounded once to the logits' type; a query without a choice has gradient 0.
+ * dlogits: T rows of E with pitch ldd; it may be logits itself (with ldd = ld). */
+int boute_route_grad(const void *logits, int dtype, long long T, int E, long long ld, int mode,
+                     int k, int renorm, float factor, const int *idx, const float *g_weight,
+                     void *dlogits, long long ldd, void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,8 @@ from . import build as _build
 BOUTE_OK, BOUTE_ERR_INVALID_ARG, BOUTE_ERR_NOT_PD, BOUTE_ERR_CUDA = 0, 1, 2, 3
 BOUTE_ERR_OOM, BOUTE_ERR_UNSUPPORTED, BOUTE_ERR_TIMEOUT = 4, 5, 6
 BOUTE_ACQ_EHVI2D, BOUTE_ACQ_MC_HVI, BOUTE_ACQ_NEHVI = 0, 1, 2
+BOUTE_F32, BOUTE_F16, BOUTE_BF16 = 0, 1, 2
+BOUTE_ROUTE_SOFTMAX, BOUTE_ROUTE_SIGMOID = 0, 1
 BOUTE_TF_IDENTITY, BOUTE_TF_LOG, BOUTE_TF_LOGIT, BOUTE_TF_NEGATE = 0, 1, 2, 4
 
 #: exported symbols declared in include/boute.h
@@ -37,6 +39,8 @@ SYMBOLS = (
     "boute_gp_learn", "boute_gp_learn_k", "boute_mobo_run", "boute_base_normals",
     "boute_engine_set_normals", "boute_engine_set_n", "boute_selftest_wait",
     "boute_engine_free",
+    "boute_token_logprobs", "boute_token_logprobs_grad", "boute_answer_scores",
+    "boute_answer_scores_grad", "boute_route", "boute_route_grad",
 )
 #: stage names of boute_engine_stage_times, in order
 STAGES = ("fit", "front", "posterior", "acquisition", "topk")
@@ -45,6 +49,7 @@ _lib = None
 _vp = ctypes.c_void_p
 _i = ctypes.c_int
 _ll = ctypes.c_longlong
+_f = ctypes.c_float
 
 
 class MoboConfig(ctypes.Structure):
@@ -135,6 +140,16 @@ def load(path: str | None = None):
                             _vp, _vp, _vp, _vp, _vp, _vp, _i, ObjectiveFn, _vp, _vp, _vp,
                             ctypes.POINTER(_i), ctypes.POINTER(_i)], _i),
         "boute_engine_free": ([_vp], None),
+        "boute_token_logprobs": ([_vp, _i, _ll, _i, _ll, _vp, _f, _i, _vp, _vp, _vp, _vp, _vp,
+                                  _vp], _i),
+        "boute_token_logprobs_grad": ([_vp, _i, _ll, _i, _ll, _vp, _f, _vp, _vp, _vp, _vp, _vp,
+                                       _ll, _vp], _i),
+        "boute_answer_scores": ([_vp, _vp, _vp, _vp, _ll, _ll, _vp, _vp, _vp], _i),
+        "boute_answer_scores_grad": ([_vp, _vp, _vp, _vp, _ll, _ll, _vp, _vp, _vp, _vp], _i),
+        "boute_route": ([_vp, _i, _ll, _i, _ll, _vp, _i, _i, _i, _i, _i, _i, _f, _vp, _vp, _vp,
+                         _vp], _i),
+        "boute_route_grad": ([_vp, _i, _ll, _i, _ll, _i, _i, _i, _f, _vp, _vp, _vp, _ll, _vp],
+                             _i),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -602,3 +617,108 @@ def boute_engine_set_constraints(e: Engine, cons=None):
 
 def boute_engine_free(e: Engine):
     e.free()
+
+
+_DTYPES = {torch.float32: BOUTE_F32, torch.float16: BOUTE_F16, torch.bfloat16: BOUTE_BF16}
+
+
+def _rows(t, like=None):
+    """(pointer, dtype code, pitch) of a 2-dimensional CUDA tensor whose rows are contiguous."""
+    code = _DTYPES.get(t.dtype)
+    if code is None or (like is not None and t.dtype != like.dtype):
+        raise TypeError(f"unsupported or different dtype {t.dtype}")
+    if t.dim() != 2 or (like is not None and t.shape != like.shape):
+        raise ValueError("expected a matrix" + ("" if like is None else " of the logits' shape"))
+    T, V = t.shape
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError("rows must be contiguous")
+    if T > 1 and t.stride(0) < V:
+        raise ValueError("rows must not overlap")
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    return t.data_ptr(), code, t.stride(0) if T > 1 else V
+
+
+def _pn(t, dtype, *shape):
+    """Pointer of a contiguous CUDA tensor of this dtype and shape, or None."""
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
+    return _p(t, dtype)
+
+
+def boute_token_logprobs(logits, targets, scale, logprob, entropy, lse, top_idx=None,
+                         top_logprob=None, stream=None):
+    """logits: T x V (fp32, fp16 or bf16, rows contiguous); targets: T int64
+    (< 0: no token); logprob, entropy, lse: T fp32; top_idx: T x k int64 and
+    top_logprob: T x k fp32, the k alternatives (both or neither)."""
+    f32 = torch.float32
+    x, code, ld = _rows(logits)
+    T, V = logits.shape
+    k = 0 if top_idx is None else top_idx.shape[-1]
+    _check(load().boute_token_logprobs(x, code, T, V, ld, _pn(targets, torch.int64, T),
+                                       scale, k, _pn(logprob, f32, T), _pn(entropy, f32, T),
+                                       _pn(lse, f32, T), _pn(top_idx, torch.int64, T, k),
+                                       _pn(top_logprob, f32, T, k), _s(stream)),
+           "boute_token_logprobs")
+
+
+def boute_token_logprobs_grad(logits, targets, scale, lse, entropy, g_logprob, g_entropy, dlogits,
+                              stream=None):
+    """entropy and g_entropy may be None; dlogits: T x V of the logits' dtype, may be logits."""
+    f32 = torch.float32
+    x, code, ld = _rows(logits)
+    dx, _, ldd = _rows(dlogits, logits)
+    T, V = logits.shape
+    _check(load().boute_token_logprobs_grad(x, code, T, V, ld, _pn(targets, torch.int64, T),
+                                            scale, _pn(lse, f32, T), _pn(entropy, f32, T),
+                                            _pn(g_logprob, f32, T), _pn(g_entropy, f32, T), dx,
+                                            ldd, _s(stream)), "boute_token_logprobs_grad")
+
+
+def boute_answer_scores(logprob, entropy, targets, offsets, scores, counts, stream=None):
+    """logprob, entropy: T fp32; targets: T int64 or None; offsets: Q + 1 int64;
+    scores: Q x 4 fp32; counts: Q int32."""
+    f32, i64 = torch.float32, torch.int64
+    T, Q = logprob.shape[0], offsets.shape[0] - 1
+    _check(load().boute_answer_scores(_pn(logprob, f32, T), _pn(entropy, f32, T),
+                                      _pn(targets, i64, T), _pn(offsets, i64, Q + 1), T, Q,
+                                      _pn(scores, f32, Q, 4), _pn(counts, torch.int32, Q),
+                                      _s(stream)), "boute_answer_scores")
+
+
+def boute_answer_scores_grad(logprob, entropy, targets, offsets, g_scores, g_logprob, g_entropy,
+                             stream=None):
+    """g_scores: Q x 4 fp32 in; g_logprob, g_entropy: T fp32 out."""
+    f32, i64 = torch.float32, torch.int64
+    T, Q = logprob.shape[0], offsets.shape[0] - 1
+    _check(load().boute_answer_scores_grad(_pn(logprob, f32, T), _pn(entropy, f32, T),
+                                           _pn(targets, i64, T), _pn(offsets, i64, Q + 1), T, Q,
+                                           _pn(g_scores, f32, Q, 4), _pn(g_logprob, f32, T),
+                                           _pn(g_entropy, f32, T), _s(stream)),
+           "boute_answer_scores_grad")
+
+
+def boute_route(logits, bias, mode, G, keep, group_top, renorm, factor, idx, weight, load_=None,
+                stream=None):
+    """logits: T x E (fp32, fp16 or bf16, rows contiguous); bias: E fp32 or None;
+    mode: BOUTE_ROUTE_*; idx: T x k int32; weight: T x k fp32; load_: E int32 or None."""
+    x, code, ld = _rows(logits)
+    T, E = logits.shape
+    k = idx.shape[-1]
+    _check(load().boute_route(x, code, T, E, ld, _pn(bias, torch.float32, E), mode, G, keep,
+                              group_top, k, bool(renorm), factor, _pn(idx, torch.int32, T, k),
+                              _pn(weight, torch.float32, T, k), _pn(load_, torch.int32, E),
+                              _s(stream)), "boute_route")
+
+
+def boute_route_grad(logits, mode, renorm, factor, idx, g_weight, dlogits, stream=None):
+    """idx: T x k int32 (-1: none); g_weight: T x k fp32; dlogits: T x E of the
+    logits' dtype, may be logits."""
+    x, code, ld = _rows(logits)
+    dx, _, ldd = _rows(dlogits, logits)
+    T, E = logits.shape
+    k = idx.shape[-1]
+    _check(load().boute_route_grad(x, code, T, E, ld, mode, k, bool(renorm), factor,
+                                   _pn(idx, torch.int32, T, k),
+                                   _pn(g_weight, torch.float32, T, k), dx, ldd, _s(stream)),
+           "boute_route_grad")

@@ -1192,7 +1192,8 @@ int boute_bounds_report(long long *rec) {
 #else
   if (cudaDeviceSynchronize() != cudaSuccess) return last_launch_status();
   int (*readers[])(long long *) = {bounds_read_posterior, bounds_read_insample, bounds_read_acq,
-                                   bounds_read_front,     bounds_read_fit,      bounds_read_topk};
+                                   bounds_read_front,     bounds_read_fit,      bounds_read_topk,
+                                   bounds_read_logprobs,  bounds_read_scores,   bounds_read_route};
   int found = 0;
   rec[0] = rec[1] = rec[2] = rec[3] = 0;
   for (int u = 0; u < (int)(sizeof(readers) / sizeof(readers[0])); ++u) {

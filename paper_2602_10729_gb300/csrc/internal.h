@@ -136,6 +136,9 @@ int bounds_read_acq(long long *out);
 int bounds_read_front(long long *out);
 int bounds_read_fit(long long *out);
 int bounds_read_topk(long long *out);
+int bounds_read_logprobs(long long *out);
+int bounds_read_scores(long long *out);
+int bounds_read_route(long long *out);
 // codes: outcome transforms before standardising (objective_code)
 int launch_standardize(const double *Y, int B, int n, int m, int codes, double *Ys,
                        cudaStream_t s);
