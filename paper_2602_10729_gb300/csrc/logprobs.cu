@@ -4,9 +4,9 @@
 // With z = scale x, m = max z, s = sum exp(z - m) and u = sum (z - m) exp(z - m):
 //   lse = m + ln s,  logprob = z_t - m - ln s,  entropy = ln s - u / s.
 // One pass over a row: each warp keeps a running maximum and s and u relative to
-// it, and leaves the maximum of every chunk of 256 logits. The k-th largest of
-// the lanes' own maxima is reached by k logits at least, and by few others; only
-// the chunks whose maximum reaches it are read again, and what reaches it there
+// it, and every lane leaves the maximum of each 64 bytes of logits it saw. The k-th
+// largest of the lanes' own maxima is reached by k logits at least, and by few others;
+// only the 64 bytes whose maximum reaches it are read again, and what reaches it there
 // is ranked. A row is a block's, or a cluster's when there are few rows.
 #include <float.h>
 #include <math.h>
@@ -18,9 +18,10 @@ namespace boute {
 namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kThreads = 256;   // of a block that has as many chunks
-constexpr int kChunk = 256;     // logits a warp reads at a time
+constexpr int kThreads = 256, kWarps = 4;  // a block's most; its warps when rows are many
 constexpr int kMaxCluster = 8;
+constexpr int kTops = 256;  // maxima from which the alternatives' bound is taken
+constexpr int kList = 256;  // candidates ranked at once, 32 a warp at least
 constexpr float kLowest = -200.f;  // exp(kLowest) = 2^kLowest = 0 in fp32
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -38,6 +39,11 @@ __device__ __forceinline__ float warp_max_nan(float v) {
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 __device__ __forceinline__ float exp2_fast(float y) {  // (2 ulp; what is below 2^-126 is 0)
@@ -69,61 +75,43 @@ __device__ __forceinline__ int add_peer(uint32_t a, int v) {
   return old;
 }
 
-// ---- a row in chunks -----------------------------------------------------------------
-// Chunk c holds the logits [256 c - off, 256 c - off + 256) of a row whose first logit lies
-// `off` elements after a 16-byte boundary, so that every chunk starts on one. A lane holds one
-// 16-byte vector of it (16-bit logits) or two (fp32).
+// ---- a row in pieces -----------------------------------------------------------------
+// A piece is 2 KB of a row, of which a lane holds four 16-byte vectors 512 bytes apart. Piece q
+// holds the logits [q SPAN - off, (q + 1) SPAN - off) of a row whose first logit lies `off` logits
+// after a 16-byte boundary, so that every vector starts on one.
 template <class T>
-struct Chunk {
-  static constexpr int E = 16 / sizeof(T), VPL = kChunk / (32 * E);
-  uint4 v[VPL];
-  static __device__ __forceinline__ int index(int i, int e) {  // within the chunk
-    return (i * 32 + (threadIdx.x & 31)) * E + e;
+struct Piece {
+  static constexpr int E = 16 / sizeof(T), N = 4 * E, SPAN = 32 * N;
+  uint4 v[4];
+  // of a lane's j-th logit, within the piece
+  static __device__ __forceinline__ int index(int j) {
+    return (j / E * 32 + (threadIdx.x & 31)) * E + j % E;
   }
+  static __host__ __device__ int count(int off, int V) { return (off + V + SPAN - 1) / SPAN; }
 };
 
+// A whole piece; at: its first logit.
 template <class T>
-struct Row {
-  const T *x;
-  int off, V;
-  __device__ __forceinline__ Row(const T *row, int V_) : x(row), V(V_) {
-    off = (int)((uintptr_t)row % 16 / sizeof(T));
-  }
-  static __host__ __device__ int chunks(int off, int V) { return (off + V + kChunk - 1) / kChunk; }
-  // -inf outside the row; nothing outside the row is read
-  __device__ __forceinline__ Chunk<T> load(int c) const {
-    Chunk<T> r;
-    const int first = c * kChunk - off;
-    if (first >= 0 && first + kChunk <= V) {
+__device__ __forceinline__ Piece<T> load_whole(const T *at) {
+  Piece<T> r;
+  const uint4 *p = (const uint4 *)at + (threadIdx.x & 31);
 #pragma unroll
-      for (int i = 0; i < Chunk<T>::VPL; ++i)
-        r.v[i] = *(const uint4 *)(x + first + Chunk<T>::index(i, 0));
-    } else {
-      T t[Chunk<T>::E];
-#pragma unroll
-      for (int i = 0; i < Chunk<T>::VPL; ++i) {
-#pragma unroll
-        for (int e = 0; e < Chunk<T>::E; ++e) {
-          const int j = first + Chunk<T>::index(i, e);
-          t[e] = j >= 0 && j < V ? x[j] : from_float<T>(-INFINITY);
-        }
-        memcpy(&r.v[i], t, 16);
-      }
-    }
-    return r;
-  }
-};
-
-// The chunk of another row y of the same length whose chunks lie elsewhere: from the logit y
-// holds at `first` on, `shift` bytes after a 16-byte boundary in y.
+  for (int i = 0; i < 4; ++i) r.v[i] = p[32 * i];
+  return r;
+}
+// The piece of a row y of V logits from its logit `first` on, `shift` bytes after a 16-byte
+// boundary: -inf outside the row, of which nothing is read.
 template <class T>
-__device__ __forceinline__ Chunk<T> load_shifted(const T *y, int V, int first, int shift) {
-  constexpr int E = Chunk<T>::E;
-  Chunk<T> r;
-  if (first >= E && first + kChunk + E <= V) {
+__device__ __forceinline__ Piece<T> load_piece(const T *y, int V, int first, int shift) {
+  constexpr int E = Piece<T>::E;
+  Piece<T> r;
 #pragma unroll
-    for (int i = 0; i < Chunk<T>::VPL; ++i) {
-      const char *p = (const char *)(y + first + Chunk<T>::index(i, 0)) - shift;
+  for (int i = 0; i < 4; ++i) {
+    const int j0 = first + Piece<T>::index(i * E);
+    if (shift == 0 && j0 >= 0 && j0 + E <= V) {
+      r.v[i] = *(const uint4 *)(y + j0);
+    } else if (j0 >= E && j0 + 2 * E <= V) {  // two vectors, of which these 16 bytes
+      const char *p = (const char *)(y + j0) - shift;
       const uint4 a = *(const uint4 *)p, b = *(const uint4 *)(p + 16);
       uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
       if (shift & 8)
@@ -135,106 +123,91 @@ __device__ __forceinline__ Chunk<T> load_shifted(const T *y, int V, int first, i
       const int bits = 8 * (shift & 3);
       r.v[i] = {__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
                 __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits)};
-    }
-  } else {
-    T t[E];
+    } else {
+      T t[E];
 #pragma unroll
-    for (int i = 0; i < Chunk<T>::VPL; ++i) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int j = first + Chunk<T>::index(i, e);
-        t[e] = j >= 0 && j < V ? y[j] : from_float<T>(-INFINITY);
-      }
+      for (int e = 0; e < E; ++e)
+        t[e] = j0 + e >= 0 && j0 + e < V ? y[j0 + e] : from_float<T>(-INFINITY);
       memcpy(&r.v[i], t, 16);
     }
   }
   return r;
 }
-// Chunk c of the row at y (off elements after a boundary); nothing outside the row is written.
+// The piece of the row y from its logit `first` (on a boundary) on; nothing outside is written.
 template <class T>
-__device__ __forceinline__ void store(T *y, int off, int V, int c, const Chunk<T> &r) {
-  const int first = c * kChunk - off;
-  if (first >= 0 && first + kChunk <= V) {
+__device__ __forceinline__ void store_piece(T *y, int V, int first, const Piece<T> &r) {
+  constexpr int E = Piece<T>::E;
+  if (first >= 0 && first + Piece<T>::SPAN <= V) {
+    uint4 *p = (uint4 *)(y + first) + (threadIdx.x & 31);
 #pragma unroll
-    for (int i = 0; i < Chunk<T>::VPL; ++i)
-      *(uint4 *)(y + first + Chunk<T>::index(i, 0)) = r.v[i];
-  } else {
-    T t[Chunk<T>::E];
+    for (int i = 0; i < 4; ++i) p[32 * i] = r.v[i];
+    return;
+  }
 #pragma unroll
-    for (int i = 0; i < Chunk<T>::VPL; ++i) {
-      memcpy(t, &r.v[i], 16);
+  for (int i = 0; i < 4; ++i) {
+    const int j0 = first + Piece<T>::index(i * E);
+    T t[E];
+    memcpy(t, &r.v[i], 16);
 #pragma unroll
-      for (int e = 0; e < Chunk<T>::E; ++e) {
-        const int j = first + Chunk<T>::index(i, e);
-        if (j >= 0 && j < V) y[j] = t[e];
-      }
-    }
+    for (int e = 0; e < E; ++e)
+      if (j0 + e >= 0 && j0 + e < V) y[j0 + e] = t[e];
   }
 }
 
-// A lane's 8 (VPL x E) logits of a chunk as floats, and back (one rounding).
-__device__ __forceinline__ void unpack2(uint32_t w, float &a, float &b, __nv_bfloat16) {
-  a = __uint_as_float(w << 16);
-  b = __uint_as_float(w & 0xffff0000u);
+// Logits 2 j and 2 j + 1 of a lane's piece as a pair of floats, and back (one rounding).
+__device__ __forceinline__ uint32_t word(const uint4 (&v)[4], int j) {
+  const uint4 a = v[j / 4];
+  return j % 4 == 0 ? a.x : j % 4 == 1 ? a.y : j % 4 == 2 ? a.z : a.w;
 }
-__device__ __forceinline__ void unpack2(uint32_t w, float &a, float &b, __half) {
-  unpack_f16x2(w, a, b);
+__device__ __forceinline__ void set_word(uint4 (&v)[4], int j, uint32_t w) {
+  uint4 &a = v[j / 4];
+  (j % 4 == 0 ? a.x : j % 4 == 1 ? a.y : j % 4 == 2 ? a.z : a.w) = w;
 }
-template <class T>
-__device__ __forceinline__ void values(const Chunk<T> &c, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < Chunk<T>::VPL; ++i) {
-    const uint32_t w[4] = {c.v[i].x, c.v[i].y, c.v[i].z, c.v[i].w};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (sizeof(T) == 4) x[4 * i + q] = __uint_as_float(w[q]);
-      else unpack2(w[q], x[2 * q], x[2 * q + 1], T{});
-    }
-  }
+__device__ __forceinline__ void pair(const Piece<float> &p, int j, float &a, float &b) {
+  a = __uint_as_float(word(p.v, 2 * j));
+  b = __uint_as_float(word(p.v, 2 * j + 1));
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b, __half) { return pack_f16x2(a, b); }
-__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
+__device__ __forceinline__ void pair(const Piece<__nv_bfloat16> &p, int j, float &a, float &b) {
+  a = __uint_as_float(word(p.v, j) << 16);
+  b = __uint_as_float(word(p.v, j) & 0xffff0000u);
+}
+__device__ __forceinline__ void pair(const Piece<__half> &p, int j, float &a, float &b) {
+  unpack_f16x2(word(p.v, j), a, b);
+}
+__device__ __forceinline__ void set_pair(Piece<float> &p, int j, float a, float b) {
+  set_word(p.v, 2 * j, __float_as_uint(a));
+  set_word(p.v, 2 * j + 1, __float_as_uint(b));
+}
+__device__ __forceinline__ void set_pair(Piece<__nv_bfloat16> &p, int j, float a, float b) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
+  set_word(p.v, j, r);
 }
-template <class T>
-__device__ __forceinline__ Chunk<T> chunk_of(const float (&x)[8]) {
-  Chunk<T> c;
-#pragma unroll
-  for (int i = 0; i < Chunk<T>::VPL; ++i) {
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(x[4 * i + q]);
-      else w[q] = pack2(x[2 * q], x[2 * q + 1], T{});
-    }
-    c.v[i] = {w[0], w[1], w[2], w[3]};
-  }
-  return c;
+__device__ __forceinline__ void set_pair(Piece<__half> &p, int j, float a, float b) {
+  set_word(p.v, j, pack_f16x2(a, b));
 }
-// A lane's largest logit of a chunk, NaN if it holds one.
-__device__ __forceinline__ float lane_max(const Chunk<float> &c) {
-  float x[8];
-  values(c, x);
+
+// A lane's largest logit of a piece, NaN if it holds one.
+__device__ __forceinline__ float lane_max(const Piece<float> &p) {
+  float m = __uint_as_float(word(p.v, 15));
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1)
-#pragma unroll
-    for (int i = 0; i < o; ++i) x[i] = max_nan(x[i], x[i + o]);
-  return x[0];
+  for (int j = 0; j < 14; j += 2)
+    m = max_nan(m, __uint_as_float(word(p.v, j)), __uint_as_float(word(p.v, j + 1)));
+  return max_nan(m, __uint_as_float(word(p.v, 14)));
 }
 template <class H2, class T>
-__device__ __forceinline__ float lane_max16(const Chunk<T> &c) {
-  H2 h[4];
-  memcpy(h, &c.v[0], 16);
-  const H2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  return max_nan(to_float(m.x), to_float(m.y));
+__device__ __forceinline__ float lane_max16(const Piece<T> &p) {
+  H2 h[16];
+  memcpy(h, p.v, 64);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < o; ++i) h[i] = __hmax2_nan(h[i], h[i + o]);
+  return max_nan(to_float(h[0].x), to_float(h[0].y));
 }
-__device__ __forceinline__ float lane_max(const Chunk<__half> &c) {
-  return lane_max16<__half2>(c);
-}
-__device__ __forceinline__ float lane_max(const Chunk<__nv_bfloat16> &c) {
-  return lane_max16<__nv_bfloat162>(c);
+__device__ __forceinline__ float lane_max(const Piece<__half> &p) { return lane_max16<__half2>(p); }
+__device__ __forceinline__ float lane_max(const Piece<__nv_bfloat16> &p) {
+  return lane_max16<__nv_bfloat162>(p);
 }
 
 // ---- sums ----------------------------------------------------------------------------
@@ -261,7 +234,31 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   return {m, a.s + b.s, a.u + b.u};
 }
 
-// Order-preserving bits; of -inf at least, which is below every logit.
+// Adds a piece to pairs of partial sums; CLAMP: with logits so far below m that (x - m) c
+// overflows (-inf, masks of the type's lowest value), whose y 2^y is else a NaN.
+template <bool CLAMP, class T>
+__device__ __forceinline__ void add_piece(const Piece<T> &p, float m, float c,
+                                          unsigned long long &s2, unsigned long long &u2) {
+  const unsigned long long m2 = f2_dup(m), c2 = f2_dup(c);
+#pragma unroll
+  for (int j = 0; j < Piece<T>::N / 2; ++j) {
+    float a, b;
+    pair(p, j, a, b);
+    unsigned long long y = f2_mul(f2_sub(f2_pack(a, b), m2), c2);
+    f2_split(y, a, b);
+    if (CLAMP) {
+      a = fmaxf(a, kLowest);
+      b = fmaxf(b, kLowest);
+      y = f2_pack(a, b);
+    }
+    const unsigned long long e = f2_pack(exp2_fast(a), exp2_fast(b));
+    s2 = f2_add(s2, e);
+    u2 = f2_fma(y, e, u2);
+  }
+}
+
+// ---- alternatives --------------------------------------------------------------------
+// Order-preserving bits of a float, and their upper half, which stands for a lower bound of it.
 __device__ __forceinline__ unsigned order_bits(float v) {
   const unsigned u = __float_as_uint(v);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
@@ -270,17 +267,23 @@ __device__ __forceinline__ float from_order_bits(unsigned o) {
   return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
 
-// A value that k of the block's threads reach with theirs, close to the largest such one: built
-// bit by bit until exactly k reach it. -inf where fewer than k have one.
-__device__ __forceinline__ float kth_bound(float mine, int k) {
-  const unsigned o = order_bits(mine);
-  unsigned t = 0u;
-  for (unsigned bit = 1u << 31; bit; bit >>= 1) {
-    const int n = __syncthreads_count(o >= (t | bit));
-    if (n >= k) t |= bit;
-    if (n == k) break;
+// An upper half of order bits that k of n floats reach (n a multiple of 32, at most kTops), close
+// to the largest such one: built bit by bit until exactly k reach it; by one warp. That of -inf
+// where fewer than k are above it.
+__device__ __forceinline__ unsigned kth_bound(const float *v, int n, int k) {
+  const int lane = threadIdx.x & 31;
+  unsigned o[kTops / 32], t = 0u;
+#pragma unroll
+  for (int i = 0; i < kTops / 32; ++i) o[i] = 32 * i < n ? order_bits(v[32 * i + lane]) >> 16 : 0u;
+  for (unsigned bit = 1u << 15; bit; bit >>= 1) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < kTops / 32; ++i) c += o[i] >= (t | bit);
+    c = __reduce_add_sync(kAll, c);
+    if (c >= k) t |= bit;
+    if (c == k) break;
   }
-  return from_order_bits(max(t, order_bits(-INFINITY)));
+  return max(t, order_bits(-INFINITY) >> 16);
 }
 
 // A warp's best 32 keys, fed with those above a bound that rises with the k-th of them.
@@ -299,43 +302,52 @@ struct WarpBest {
   }
 };
 
-// A row per cluster of CS blocks; chunk c is warp (c mod CS W)'s, in order.
+// A row per cluster of CS blocks; piece q is warp (q mod CS W)'s.
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4)
     token_logprobs_kernel(const T *logits, int V, long long ld, const long long *targets,
-                          float scale, int k, int CS, int per_warp, float *logprob,
-                          float *entropy, float *lse, long long *top_idx, float *top_logprob) {
-  constexpr int U = sizeof(T) == 4 ? 2 : 4;  // chunks in flight: 64 bytes a lane
-  extern __shared__ unsigned long long list[];  // the leader's: CS W 32 candidates' keys
+                          float scale, int k, int CS, float *logprob, float *entropy, float *lse,
+                          long long *top_idx, float *top_logprob) {
+  constexpr int N = Piece<T>::N, SPAN = Piece<T>::SPAN;
+  // a bound this much lower lets no logit slip that the scale rounds onto the bound (16-bit
+  // logits are too far apart for that)
+  constexpr unsigned kSlack = sizeof(T) == 4 ? 1 : 0;
+  extern __shared__ unsigned short most[];  // upper order bits of each piece's lanes' maxima
+  __shared__ unsigned long long list[kList];  // (the leader's) candidates' keys
+  __shared__ float tops[kTops], lanes[kThreads];
   __shared__ Sums wsum[kThreads / 32];
-  __shared__ float csum[kMaxCluster][3], ctau[kMaxCluster];
+  __shared__ float csum[kMaxCluster][3];
+  __shared__ unsigned bound;
   __shared__ int nlist;
-  const int W = blockDim.x / 32, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int NT = blockDim.x, W = NT / 32, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = CS > 1 ? blockIdx.x % CS : 0;
   const long long row = blockIdx.x / CS;
-  const Row<T> r(logits + row * ld, V);
+  const T *x = logits + row * ld;
+  const int off = (int)((uintptr_t)x % 16 / sizeof(T));
   const float c = fminf(scale * kLog2e, FLT_MAX);
-  float *cmax = (float *)(list + CS * W * 32) + warp * per_warp;  // this warp's chunks' maxima
-  if (tid == 0) nlist = 0;
+  long long t = -1;
+  float xt = 0.f;
+  if (tid == 0) {
+    nlist = 0;
+    if (rank == 0) t = targets[row];
+    if (t >= 0 && t < V) xt = to_float(x[t]);
+  }
 
-  const int C = Row<T>::chunks(r.off, V), step = CS * W, first = rank * W + warp;
+  const int Q = Piece<T>::count(off, V), step = CS * W, first = rank * W + warp;
+  const int whole0 = off ? 1 : 0, whole1 = (off + V) / SPAN;  // pieces within the row
   float m = -INFINITY, top = -INFINITY;
   unsigned long long s2 = 0ull, u2 = 0ull;  // pairs of partial sums
-  for (int i = 0; i < per_warp; i += U) {
-    Chunk<T> v[U];
-    float cm[U], g = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = r.load(first + (i + u) * step);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float l = lane_max(v[u]);
+  bool clamp = false;
+  for (int q = first, i = tid; q < Q; q += step, i += NT) {
+    const bool whole = q >= whole0 && q < whole1;
+    const Piece<T> p = whole ? load_whole(x + ((long long)q * SPAN - off))
+                             : load_piece(x, V, q * SPAN - off, 0);
+    const float l = lane_max(p);
+    if (k > 0) {
+      most[i] = (unsigned short)(order_bits(l) >> 16);
       top = max_nan(top, l);
-      cm[u] = warp_max_nan(l);
-      g = max_nan(g, cm[u]);
     }
-    if (lane == 0 && k > 0)
-#pragma unroll
-      for (int u = 0; u < U; ++u) cmax[i + u] = cm[u];
+    const float g = warp_max_nan(l);
     if (!(g <= m)) {  // (NaN too: it stays in m)
       Sums a, b;
       a.m = b.m = m;
@@ -347,23 +359,19 @@ __global__ void __launch_bounds__(kThreads, 4)
       u2 = f2_pack(a.u, b.u);
       m = max_nan(m, g);
     }
-    if (m == -INFINITY) continue;
-    const unsigned long long m2 = f2_dup(m), c2 = f2_dup(c);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float x[8];
-      values(v[u], x);
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float y0, y1;
-        f2_split(f2_mul(f2_sub(f2_pack(x[e], x[e + 1]), m2), c2), y0, y1);
-        y0 = fmaxf(y0, kLowest);
-        y1 = fmaxf(y1, kLowest);
-        const unsigned long long p = f2_pack(exp2_fast(y0), exp2_fast(y1));
-        s2 = f2_add(s2, p);
-        u2 = f2_fma(f2_pack(y0, y1), p, u2);
+    if (whole && !clamp) {
+      unsigned long long s = s2, u = u2;
+      add_piece<false>(p, m, c, s, u);
+      float a, b;
+      f2_split(u, a, b);
+      clamp = __any_sync(kAll, isnan(a + b));
+      if (!clamp) {
+        s2 = s;
+        u2 = u;
+        continue;
       }
     }
+    if (m > -INFINITY) add_piece<true>(p, m, c, s2, u2);
   }
   {
     float a, b;
@@ -373,8 +381,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     const float u = warp_sum(a + b);
     if (lane == 0) wsum[warp] = {m, s, u};
   }
-  float tau = -INFINITY;
-  if (k > 0) tau = kth_bound(top, k);
+  (CS > 1 ? lanes : tops)[tid] = top;
   __syncthreads();
   if (CS > 1) {
     if (tid == 0) {
@@ -387,40 +394,46 @@ __global__ void __launch_bounds__(kThreads, 4)
       store_peer(peer(&csum[rank][1], 0), a.s);
       store_peer(peer(&csum[rank][2], 0), a.u);
     }
-    if (tid < CS) store_peer(peer(&ctau[rank], tid), tau);
+    // the blocks' lane maxima to all blocks, kTops / CS of each: of lanes with the same number
+    // in warps this far apart
+    const int mine = kTops / CS;
+    if (k > 0 && tid < mine) {
+      float t = -INFINITY;
+      for (int i = tid; i < NT; i += mine) t = max_nan(t, lanes[i]);
+      for (int b = 0; b < CS; ++b) store_peer(peer(&tops[rank * mine + tid], b), t);
+    }
     cluster_sync();
-    for (int b = 0; b < CS; ++b) tau = fmaxf(tau, ctau[b]);
   }
+  float zt = -INFINITY;
   if (k > 0) {
-    // the chunks that reach tau, read again
-    const float zt = __fmul_rn(tau, scale);
-    WarpBest best;
-    for (int i0 = 0; i0 < per_warp; i0 += 32) {
-      const float cm = i0 + lane < per_warp ? __fmul_rn(cmax[i0 + lane], scale) : -INFINITY;
-      unsigned hit = __ballot_sync(kAll, cm >= zt && cm > -INFINITY);
+    if (warp == 0) bound = kth_bound(tops, CS > 1 ? kTops : NT, k);
+    __syncthreads();
+    const unsigned reach = bound > kSlack ? bound - kSlack : 0u;
+    if (bound > order_bits(-INFINITY) >> 16) zt = __fmul_rn(from_order_bits(bound << 16), scale);
+    for (int q0 = first, i0 = tid; q0 < Q; q0 += 32 * step, i0 += 32 * NT) {
+      unsigned hit = 0u;  // this lane's parts of pieces that reach the bound
+      for (int b = 0, q = q0, i = i0; b < 32 && q < Q; ++b, q += step, i += NT)
+        hit |= (unsigned)(most[i] >= reach) << b;
       while (hit) {
-        const int ch = first + (i0 + __ffs(hit) - 1) * step;
+        const int at0 = (q0 + (__ffs(hit) - 1) * step) * SPAN - off;
         hit &= hit - 1;
-        if (ch >= C) continue;
-        const Chunk<T> v = r.load(ch);
-        float x[8];
-        values(v, x);
+        const Piece<T> p = load_piece(x, V, at0, 0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float z = __fmul_rn(x[e], scale);
-          const int j = ch * kChunk - r.off + Chunk<T>::index(e / Chunk<T>::E, e % Chunk<T>::E);
-          best.feed(z >= zt && z > -INFINITY, make_key(z, (unsigned)j), k, lane);
+        for (int j = 0; j < N; j += 2) {
+          float z[2];
+          pair(p, j / 2, z[0], z[1]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            z[e] = __fmul_rn(z[e], scale);
+            if (!(z[e] >= zt && z[e] > -INFINITY)) continue;
+            const int at = add_peer(peer(&nlist, 0), 1);
+            if (at < kList)
+              store_peer(peer(list, 0) + 8u * at,
+                         make_key(z[e], (unsigned)(at0 + Piece<T>::index(j + e))));
+            else hit = 0u, q0 = Q;
+          }
         }
       }
-    }
-    best.batch.flush(lane);
-    const unsigned have = __ballot_sync(kAll, lane < k && best.batch.top != 0ull);
-    if (have) {
-      int at = 0;
-      if (lane == 0) at = add_peer(peer(&nlist, 0), __popc(have));
-      at = __shfl_sync(kAll, at, 0) + lane;
-      if ((have >> lane & 1u) && BOUTE_INB(at, CS * W * 32))
-        store_peer(peer(list, 0) + 8u * at, best.batch.top);
     }
     if (CS > 1) cluster_sync();
     else __syncthreads();
@@ -438,18 +451,44 @@ __global__ void __launch_bounds__(kThreads, 4)
   bad |= M == INFINITY;
   const float ls = empty ? 0.f : logf(a.s);
   if (tid == 0) {
-    const long long t = targets[row];
     float lp = 0.f;
     if (t >= V || (bad && t >= 0)) lp = NAN;
-    else if (t >= 0 && BOUTE_INB(t, V))
-      lp = empty ? -INFINITY : __fmul_rn(to_float(r.x[t]), scale) - M - ls;
+    else if (t >= 0) lp = empty ? -INFINITY : __fmul_rn(xt, scale) - M - ls;
     lse[row] = bad ? NAN : M + ls;
     logprob[row] = lp;
     entropy[row] = bad ? NAN : empty ? 0.f : ls - kLn2 * (a.u / a.s);
   }
   if (k > 0) {
-    const int n = bad || empty ? 0 : nlist;
-    for (int i = tid; i < n; i += blockDim.x) {
+    int n = bad || empty ? 0 : nlist;
+    if (n > kList) {  // (many equal logits, or most of the largest in few lanes)
+      __syncthreads();
+      if (tid == 0) nlist = 0;
+      __syncthreads();
+      WarpBest best;
+      for (int q = warp; q < Q; q += W) {
+        const Piece<T> p = load_piece(x, V, q * SPAN - off, 0);
+        if (!__any_sync(kAll, __fmul_rn(lane_max(p), scale) >= zt)) continue;
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+          float z[2];
+          pair(p, j / 2, z[0], z[1]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            z[e] = __fmul_rn(z[e], scale);
+            best.feed(z[e] >= zt && z[e] > -INFINITY,
+                      make_key(z[e], (unsigned)(q * SPAN - off + Piece<T>::index(j + e))), k, lane);
+          }
+        }
+      }
+      best.batch.flush(lane);
+      if (lane < k && best.batch.top != 0ull) {
+        const int at = atomicAdd(&nlist, 1);
+        if (BOUTE_INB(at, kList)) list[at] = best.batch.top;
+      }
+      __syncthreads();
+      n = nlist;
+    }
+    for (int i = tid; i < n; i += NT) {
       const unsigned long long key = list[i];
       int place = 0;
       for (int j = 0; j < n; ++j) place += list[j] > key;
@@ -458,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         top_logprob[row * k + place] = from_order_bits((unsigned)(key >> 32)) - M - ls;
       }
     }
-    for (int i = n + tid; i < k; i += blockDim.x) {
+    for (int i = n + tid; i < k; i += NT) {
       top_idx[row * k + i] = -1;
       top_logprob[row * k + i] = bad ? NAN : -INFINITY;
     }
@@ -471,15 +510,15 @@ constexpr float kLargeLse = 1024.f;
 
 // With lp_j = z_j - lse and p_j = exp(lp_j):
 //   dlogits_j = p_j (A + B lp_j) + scale g [j = t],  A = -scale (g + gh H),  B = -scale gh.
-// A row per cluster of CS blocks; chunks as in the forward pass, but of the gradient's row (the
+// A row per cluster of CS blocks; pieces as in the forward pass, but of the gradient's row (the
 // logits' row may start elsewhere against a 16-byte boundary).
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4)
     token_logprobs_grad_kernel(const T *logits, int V, long long ld, const long long *targets,
                                float scale, const float *lse, const float *entropy,
                                const float *g_logprob, const float *g_entropy, T *dlogits,
-                               long long ldd, int CS, int per_warp) {
-  constexpr int U = sizeof(T) == 4 ? 2 : 4;
+                               long long ldd, int CS) {
+  constexpr int N = Piece<T>::N, SPAN = Piece<T>::SPAN;
   __shared__ Sums wsum[kThreads / 32];
   __shared__ float csum[kMaxCluster][3];
   const int W = blockDim.x / 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -488,34 +527,33 @@ __global__ void __launch_bounds__(kThreads, 4)
   const T *x = logits + row * ld;
   T *dx = dlogits + row * ldd;
   const int off = (int)((uintptr_t)dx % 16 / sizeof(T));
-  const int shift = (int)(((uintptr_t)x - off * sizeof(T)) % 16);  // of a chunk's first logit
-  const int C = Row<T>::chunks(off, V), step = CS * W, first = rank * W + warp;
+  const int shift = (int)(((uintptr_t)x - off * sizeof(T)) % 16);  // of a piece's first logit
+  const int Q = Piece<T>::count(off, V), step = CS * W, first = rank * W + warp;
+  const int whole0 = off ? 1 : 0, whole1 = (off + V) / SPAN;
+  auto load = [&](int q) {
+    return shift == 0 && q >= whole0 && q < whole1
+               ? load_whole(x + ((long long)q * SPAN - off))
+               : load_piece(x, V, q * SPAN - off, shift);
+  };
   const long long t = targets[row];
   const float l = lse[row];
-  float g = t < 0 ? 0.f : t >= V || isnan(l) ? NAN : g_logprob[row];
+  float g = t < 0 ? 0.f : t >= V ? NAN : g_logprob[row];
   float gh = g_entropy ? g_entropy[row] : 0.f, H = g_entropy ? entropy[row] : 0.f;
   if (l == -INFINITY && t < V) g = gh = H = 0.f;
   if (isnan(l)) g = NAN;
   float m = l == -INFINITY ? 0.f : l, ls = 0.f;  // lse = m + ls
-  auto load = [&](int ch) {
-    return shift ? load_shifted(x, V, ch * kChunk - off, shift) : [&] {
-      Row<T> r(x, V);
-      r.off = off;
-      return r.load(ch);
-    }();
-  };
   if (fabsf(l) > kLargeLse && isfinite(l)) {
     const float c = fminf(scale * kLog2e, FLT_MAX);
     Sums a = {-INFINITY, 0.f, 0.f};
-    for (int ch = first; ch < C; ch += step) {
-      const Chunk<T> v = load(ch);
-      float z[8];
-      values(v, z);
-      const float top = fmaxf(a.m, lane_max(v));
+    for (int q = first; q < Q; q += step) {
+      const Piece<T> p = load(q);
+      const float top = fmaxf(a.m, lane_max(p));
       a.move(top, c);
-      if (top > -INFINITY)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a.s += exp2_fast(fmaxf((z[e] - top) * c, kLowest));
+      unsigned long long s2 = 0ull, u2 = 0ull;
+      if (top > -INFINITY) add_piece<true>(p, top, c, s2, u2);
+      float s, t2;
+      f2_split(s2, s, t2);
+      a.s += s + t2;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -537,35 +575,30 @@ __global__ void __launch_bounds__(kThreads, 4)
     m = __fmul_rn(a.m, scale);
     ls = logf(a.s);
   }
-  const float A = -scale * (g + gh * H), B = -scale * gh, hit = scale * g;
+  const float A = -scale * (g + gh * H), B = -scale * gh, extra = scale * g;
   const unsigned long long A2 = f2_dup(A), B2 = f2_dup(B), c2 = f2_dup(scale), m2 = f2_dup(-m),
                            ls2 = f2_dup(ls), e2 = f2_dup(kLog2e);
-  for (int i = 0; i < per_warp; i += U) {
-    Chunk<T> v[U];
+  for (int q = first; q < Q; q += step) {
+    Piece<T> p = load(q);
+    const int at0 = q * SPAN - off;
+    const bool target = t >= at0 && t < at0 + SPAN;
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load(first + (i + u) * step);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int ch = first + (i + u) * step;
-      if (ch >= C) break;
-      float z[8];
-      values(v[u], z);
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float a, b;
-        f2_split(f2_sub(f2_fma(f2_pack(z[e], z[e + 1]), c2, m2), ls2), a, b);
-        const unsigned long long lp = f2_pack(fmaxf(a, kLowest), fmaxf(b, kLowest));
-        f2_split(f2_mul(lp, e2), a, b);
-        const unsigned long long p = f2_pack(exp2_fast(a), exp2_fast(b));
-        f2_split(f2_mul(p, f2_fma(B2, lp, A2)), z[e], z[e + 1]);
+    for (int j = 0; j < N / 2; ++j) {
+      float a, b;
+      pair(p, j, a, b);
+      f2_split(f2_sub(f2_fma(f2_pack(a, b), c2, m2), ls2), a, b);
+      const unsigned long long lp = f2_pack(fmaxf(a, kLowest), fmaxf(b, kLowest));
+      f2_split(f2_mul(lp, e2), a, b);
+      const unsigned long long e = f2_pack(exp2_fast(a), exp2_fast(b));
+      f2_split(f2_mul(e, f2_fma(B2, lp, A2)), a, b);
+      if (target) {
+        const int d = (int)(t - at0) - Piece<T>::index(2 * j);
+        a += d == 0 ? extra : 0.f;
+        b += d == 1 ? extra : 0.f;
       }
-      const long long at = t - ((long long)ch * kChunk - off);
-      if (at >= 0 && at < kChunk)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          z[e] += Chunk<T>::index(e / Chunk<T>::E, e % Chunk<T>::E) == at ? hit : 0.f;
-      store(dx, off, V, ch, chunk_of<T>(z));
+      set_pair(p, j, a, b);
     }
+    store_piece(dx, V, at0, p);
   }
 }
 
@@ -577,17 +610,19 @@ BOUTE_BOUNDS_READER(logprobs)
 
 using namespace boute;
 
-// How a row's chunks are spread: a warp per chunk, up to eight to a block, and the blocks of a
-// cluster while the rows alone leave the SMs without work and every warp gets a few chunks.
+// How a row's pieces are spread: a warp per piece, up to kWarps to a block, and the blocks of a
+// cluster while the rows alone leave the SMs without work and every warp gets a piece; with rows
+// so few that all their warps run at once, twice the warps.
 struct Spread {
   int W, CS, per_warp;
-  Spread(long long T, int V, size_t bytes) {
-    const int C = ((int)(16 / bytes) - 1 + V + kChunk - 1) / kChunk;
-    W = C < kThreads / 32 ? C : kThreads / 32;
+  template <class P>
+  Spread(long long T, int V, P) {
+    const int Q = P::count(P::E - 1, V), sms = num_sms();
+    W = Q < kWarps ? Q : kWarps;
     CS = 1;
-    const int sms = num_sms();
-    while (CS < kMaxCluster && 2 * CS * T <= 4 * sms && 4 * CS * W <= C) CS *= 2;
-    per_warp = round_up((C + CS * W - 1) / (CS * W), bytes == 4 ? 2 : 4);
+    while (CS < kMaxCluster && 2 * CS * T <= 8 * sms && 2 * CS * W <= Q) CS *= 2;
+    if (CS == kMaxCluster && 2 * W * CS * T <= 32 * sms && CS * W < Q) W *= 2;
+    per_warp = (Q + CS * W - 1) / (CS * W);
   }
 };
 
@@ -631,10 +666,14 @@ extern "C" int boute_token_logprobs(const void *logits, int dtype, long long T, 
   if (T == 0) return BOUTE_OK;
   return with_dtype(dtype, [&](auto tag) {
     using E = decltype(tag);
-    const Spread sp(T, V, sizeof(E));
-    const size_t smem = (size_t)sp.W * (sp.CS * 32 * 8 + sp.per_warp * 4);
+    const Spread sp(T, V, Piece<E>{});
+    const size_t smem = k > 0 ? (size_t)sp.W * 32 * sp.per_warp * 2 : 0;
+    if (smem > (40u << 10) &&
+        cudaFuncSetAttribute((const void *)token_logprobs_kernel<E>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+      return last_launch_status();
     return launch_rows(token_logprobs_kernel<E>, sp, T, smem, (cudaStream_t)stream,
-                       (const E *)logits, V, ld, targets, scale, k, sp.CS, sp.per_warp, logprob,
+                       (const E *)logits, V, ld, targets, scale, k, sp.CS, logprob,
                        entropy, lse, top_idx, top_logprob);
   });
 }
@@ -656,9 +695,9 @@ extern "C" int boute_token_logprobs_grad(const void *logits, int dtype, long lon
   if (T == 0) return BOUTE_OK;
   return with_dtype(dtype, [&](auto tag) {
     using E = decltype(tag);
-    const Spread sp(T, V, sizeof(E));
+    const Spread sp(T, V, Piece<E>{});
     return launch_rows(token_logprobs_grad_kernel<E>, sp, T, 0, (cudaStream_t)stream,
                        (const E *)logits, V, ld, targets, scale, lse, entropy, g_logprob,
-                       g_entropy, (E *)dlogits, ldd, sp.CS, sp.per_warp);
+                       g_entropy, (E *)dlogits, ldd, sp.CS);
   });
 }
