@@ -631,7 +631,8 @@ int boute_token_logprobs_grad(const void *logits, int dtype, long long T, int V,
  *   scores (Q x 4 fp32): mean logprob, lowest logprob, mean entropy, highest
  *   entropy; counts (Q int32): the positions counted. An answer without any
  *   has scores 0. NaN passes through to the mean and the extreme.
- * 0 <= T < 2^31, 0 <= Q < 2^31. */
+ * 0 <= T < 2^31, 0 <= Q <= BOUTE_MAX_ANSWERS. */
+#define BOUTE_MAX_ANSWERS (1 << 28)
 int boute_answer_scores(const float *logprob, const float *entropy, const long long *targets,
                         const long long *offsets, long long T, long long Q, float *scores,
                         int *counts, void *stream);
@@ -647,7 +648,9 @@ int boute_answer_scores_grad(const float *logprob, const float *entropy,
 
 /* Queries to experts (the models, or the replicas of their deployments), Sec.
  * 4.1 and App. C: for each of T queries with logits x over E experts,
- *   s = softmax(x) or 1 / (1 + exp(-x)) (mode; fp32: what underflows is 0), c = s + bias,
+ *   s = softmax(x) or 1 / (1 + exp(-x)) (mode; fp32: what underflows is 0), c = s + bias
+ *   (without a bias, but for the sums of two below, the logits are compared, which have
+ *   the scores' order without their rounding),
  * the experts in G groups of E / G neighbours (models with their replicas): a
  * group's score is the sum of its group_top (1 or 2) largest c, the keep groups
  * with the largest scores stay, and of their experts the k with the largest c

@@ -1,5 +1,5 @@
 // What the kernels over a model's answers share: the logits' element types,
-// and the checks of their C entry points.
+// the checks of their C entry points, and the shared memory of a cluster's blocks.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -45,5 +45,30 @@ inline bool array_ok(const void *p, size_t bytes) {
   return p != nullptr && (uintptr_t)p % bytes == 0;
 }
 inline bool optional_ok(const void *p, size_t bytes) { return p == nullptr || array_ok(p, bytes); }
+
+constexpr unsigned kAll = 0xffffffffu;
+
+// ---- clusters (a block launched alone is a cluster of one) ---------------------------
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+                   : "memory");
+}
+// Address of block r's copy of a shared variable.
+__device__ __forceinline__ uint32_t peer(const void *p, int r) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(r));
+  return a;
+}
+__device__ __forceinline__ void store_peer(uint32_t a, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
+}
+__device__ __forceinline__ void store_peer(uint32_t a, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+}
+__device__ __forceinline__ int add_peer(uint32_t a, int v) {
+  int old;
+  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
+  return old;
+}
 
 }  // namespace boute

@@ -17,7 +17,6 @@ namespace boute {
 
 namespace {
 
-constexpr unsigned kAll = 0xffffffffu;
 constexpr int kThreads = 256, kWarps = 4;  // a block's most; its warps when rows are many
 constexpr int kMaxCluster = 8;
 constexpr int kTops = 256;  // maxima from which the alternatives' bound is taken
@@ -50,29 +49,6 @@ __device__ __forceinline__ float exp2_fast(float y) {  // (2 ulp; what is below 
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
   return r;
-}
-
-// ---- clusters (a block launched alone is a cluster of one) ---------------------------
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
-                   : "memory");
-}
-// Address of block r's copy of a shared variable.
-__device__ __forceinline__ uint32_t peer(const void *p, int r) {
-  uint32_t a;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(r));
-  return a;
-}
-__device__ __forceinline__ void store_peer(uint32_t a, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
-}
-__device__ __forceinline__ void store_peer(uint32_t a, unsigned long long v) {
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
-}
-__device__ __forceinline__ int add_peer(uint32_t a, int v) {
-  int old;
-  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
-  return old;
 }
 
 // ---- a row in pieces -----------------------------------------------------------------
