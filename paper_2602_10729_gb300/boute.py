@@ -187,8 +187,18 @@ def _p(t, dtype=None, device=True):
 
 def _s(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return _current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+
+
+def _current_stream():
+    """The current stream's handle (torch.cuda.current_stream().cuda_stream builds a Stream
+    object first: 3 us a call)."""
+    return _raw_stream(torch.cuda.current_device())
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def boute_launch_count() -> int:
@@ -623,25 +633,32 @@ _DTYPES = {torch.float32: BOUTE_F32, torch.float16: BOUTE_F16, torch.bfloat16: B
 
 
 def _rows(t, like=None):
-    """(pointer, dtype code, pitch) of a 2-dimensional CUDA tensor whose rows are contiguous."""
+    """(pointer, dtype code, rows, row length, pitch) of a 2-dimensional CUDA tensor whose rows
+    are contiguous."""
     code = _DTYPES.get(t.dtype)
     if code is None or (like is not None and t.dtype != like.dtype):
         raise TypeError(f"unsupported or different dtype {t.dtype}")
-    if t.dim() != 2 or (like is not None and t.shape != like.shape):
+    shape = t.shape
+    if len(shape) != 2 or (like is not None and shape != like.shape):
         raise ValueError("expected a matrix" + ("" if like is None else " of the logits' shape"))
-    T, V = t.shape
-    if V > 1 and t.stride(1) != 1:
+    T, V = shape
+    pitch, one = t.stride()
+    if V > 1 and one != 1:
         raise ValueError("rows must be contiguous")
-    if T > 1 and t.stride(0) < V:
+    if T <= 1:
+        pitch = V
+    elif pitch < V:
         raise ValueError("rows must not overlap")
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    return t.data_ptr(), code, t.stride(0) if T > 1 else V
+    return t.data_ptr(), code, T, V, pitch
 
 
-def _pn(t, dtype, *shape):
+def _pn(t, dtype, shape):
     """Pointer of a contiguous CUDA tensor of this dtype and shape, or None."""
-    if t is not None and tuple(t.shape) != shape:
+    if t is None:
+        return None
+    if t.shape != shape:
         raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
     return _p(t, dtype)
 
@@ -652,13 +669,12 @@ def boute_token_logprobs(logits, targets, scale, logprob, entropy, lse, top_idx=
     (< 0: no token); logprob, entropy, lse: T fp32; top_idx: T x k int64 and
     top_logprob: T x k fp32, the k alternatives (both or neither)."""
     f32 = torch.float32
-    x, code, ld = _rows(logits)
-    T, V = logits.shape
+    x, code, T, V, ld = _rows(logits)
     k = 0 if top_idx is None else top_idx.shape[-1]
-    _check(load().boute_token_logprobs(x, code, T, V, ld, _pn(targets, torch.int64, T),
-                                       scale, k, _pn(logprob, f32, T), _pn(entropy, f32, T),
-                                       _pn(lse, f32, T), _pn(top_idx, torch.int64, T, k),
-                                       _pn(top_logprob, f32, T, k), _s(stream)),
+    _check(load().boute_token_logprobs(x, code, T, V, ld, _pn(targets, torch.int64, (T,)),
+                                       scale, k, _pn(logprob, f32, (T,)), _pn(entropy, f32, (T,)),
+                                       _pn(lse, f32, (T,)), _pn(top_idx, torch.int64, (T, k)),
+                                       _pn(top_logprob, f32, (T, k)), _s(stream)),
            "boute_token_logprobs")
 
 
@@ -666,12 +682,11 @@ def boute_token_logprobs_grad(logits, targets, scale, lse, entropy, g_logprob, g
                               stream=None):
     """entropy and g_entropy may be None; dlogits: T x V of the logits' dtype, may be logits."""
     f32 = torch.float32
-    x, code, ld = _rows(logits)
-    dx, _, ldd = _rows(dlogits, logits)
-    T, V = logits.shape
-    _check(load().boute_token_logprobs_grad(x, code, T, V, ld, _pn(targets, torch.int64, T),
-                                            scale, _pn(lse, f32, T), _pn(entropy, f32, T),
-                                            _pn(g_logprob, f32, T), _pn(g_entropy, f32, T), dx,
+    x, code, T, V, ld = _rows(logits)
+    dx, _, _, _, ldd = _rows(dlogits, logits)
+    _check(load().boute_token_logprobs_grad(x, code, T, V, ld, _pn(targets, torch.int64, (T,)),
+                                            scale, _pn(lse, f32, (T,)), _pn(entropy, f32, (T,)),
+                                            _pn(g_logprob, f32, (T,)), _pn(g_entropy, f32, (T,)), dx,
                                             ldd, _s(stream)), "boute_token_logprobs_grad")
 
 
@@ -680,9 +695,9 @@ def boute_answer_scores(logprob, entropy, targets, offsets, scores, counts, stre
     scores: Q x 4 fp32; counts: Q int32."""
     f32, i64 = torch.float32, torch.int64
     T, Q = logprob.shape[0], offsets.shape[0] - 1
-    _check(load().boute_answer_scores(_pn(logprob, f32, T), _pn(entropy, f32, T),
-                                      _pn(targets, i64, T), _pn(offsets, i64, Q + 1), T, Q,
-                                      _pn(scores, f32, Q, 4), _pn(counts, torch.int32, Q),
+    _check(load().boute_answer_scores(_pn(logprob, f32, (T,)), _pn(entropy, f32, (T,)),
+                                      _pn(targets, i64, (T,)), _pn(offsets, i64, (Q + 1,)), T, Q,
+                                      _pn(scores, f32, (Q, 4)), _pn(counts, torch.int32, (Q,)),
                                       _s(stream)), "boute_answer_scores")
 
 
@@ -691,10 +706,10 @@ def boute_answer_scores_grad(logprob, entropy, targets, offsets, g_scores, g_log
     """g_scores: Q x 4 fp32 in; g_logprob, g_entropy: T fp32 out."""
     f32, i64 = torch.float32, torch.int64
     T, Q = logprob.shape[0], offsets.shape[0] - 1
-    _check(load().boute_answer_scores_grad(_pn(logprob, f32, T), _pn(entropy, f32, T),
-                                           _pn(targets, i64, T), _pn(offsets, i64, Q + 1), T, Q,
-                                           _pn(g_scores, f32, Q, 4), _pn(g_logprob, f32, T),
-                                           _pn(g_entropy, f32, T), _s(stream)),
+    _check(load().boute_answer_scores_grad(_pn(logprob, f32, (T,)), _pn(entropy, f32, (T,)),
+                                           _pn(targets, i64, (T,)), _pn(offsets, i64, (Q + 1,)), T, Q,
+                                           _pn(g_scores, f32, (Q, 4)), _pn(g_logprob, f32, (T,)),
+                                           _pn(g_entropy, f32, (T,)), _s(stream)),
            "boute_answer_scores_grad")
 
 
@@ -702,23 +717,21 @@ def boute_route(logits, bias, mode, G, keep, group_top, renorm, factor, idx, wei
                 stream=None):
     """logits: T x E (fp32, fp16 or bf16, rows contiguous); bias: E fp32 or None;
     mode: BOUTE_ROUTE_*; idx: T x k int32; weight: T x k fp32; load_: E int32 or None."""
-    x, code, ld = _rows(logits)
-    T, E = logits.shape
+    x, code, T, E, ld = _rows(logits)
     k = idx.shape[-1]
-    _check(load().boute_route(x, code, T, E, ld, _pn(bias, torch.float32, E), mode, G, keep,
-                              group_top, k, bool(renorm), factor, _pn(idx, torch.int32, T, k),
-                              _pn(weight, torch.float32, T, k), _pn(load_, torch.int32, E),
+    _check(load().boute_route(x, code, T, E, ld, _pn(bias, torch.float32, (E,)), mode, G, keep,
+                              group_top, k, bool(renorm), factor, _pn(idx, torch.int32, (T, k)),
+                              _pn(weight, torch.float32, (T, k)), _pn(load_, torch.int32, (E,)),
                               _s(stream)), "boute_route")
 
 
 def boute_route_grad(logits, mode, renorm, factor, idx, g_weight, dlogits, stream=None):
     """idx: T x k int32 (-1: none); g_weight: T x k fp32; dlogits: T x E of the
     logits' dtype, may be logits."""
-    x, code, ld = _rows(logits)
-    dx, _, ldd = _rows(dlogits, logits)
-    T, E = logits.shape
+    x, code, T, E, ld = _rows(logits)
+    dx, _, _, _, ldd = _rows(dlogits, logits)
     k = idx.shape[-1]
     _check(load().boute_route_grad(x, code, T, E, ld, mode, k, bool(renorm), factor,
-                                   _pn(idx, torch.int32, T, k),
-                                   _pn(g_weight, torch.float32, T, k), dx, ldd, _s(stream)),
+                                   _pn(idx, torch.int32, (T, k)),
+                                   _pn(g_weight, torch.float32, (T, k)), dx, ldd, _s(stream)),
            "boute_route_grad")
