@@ -2,12 +2,12 @@
 // the weights and the load; and the gradient of the weights.
 //
 // A warp per query, lane l with the S experts l S .. l S + S - 1 (S a power of two,
-// 32 S >= E), so that the lowest lane has the lowest indices. Each lane sorts
-// its S values; k rounds then take the largest head of the 32 lists (one
-// reduction each). Without a bias the logits themselves are compared, which have
-// the order of the scores: only the chosen scores are computed then, and a softmax's
-// sum only where the weights are not renormalised. 16-bit logits carry their
-// expert's index in the key's lower half.
+// 32 S >= E), so that the lowest lane has the lowest indices. Each lane sorts the best
+// of its values; k rounds then take the largest head of the 32 lists (one reduction
+// each). Without a bias the logits themselves are compared, which have the order of the
+// scores: only the chosen scores are computed then, and a softmax's sum only where the
+// weights are not renormalised. 16-bit logits are compared as keys of their order bits
+// with the expert's index below.
 #include <math.h>
 
 #include <algorithm>
@@ -45,8 +45,10 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 __device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_sync(kAll, v); }
 
-__device__ __forceinline__ float logistic(float x) {  // (0 where exp(-x) overflows, as in fp32)
-  return __fdividef(1.f, 1.f + fminf(exp2_fast(-x * kLog2e), 3e38f));
+__device__ __forceinline__ float logistic(float x) {  // (0 where exp(-x) overflows)
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_fast(-x * kLog2e)));
+  return r;
 }
 
 // ---- a query's logits -----------------------------------------------------------------
@@ -101,143 +103,182 @@ struct Raw {
 __device__ __forceinline__ float key_none(float) { return -INFINITY; }
 __device__ __forceinline__ unsigned key_none(unsigned) { return 0u; }
 
-// v in descending order (Batcher's odd-even merge sort).
-template <int S, class K>
-__device__ __forceinline__ void sort_desc(K (&v)[S]) {
+// Two values, and four or more by Batcher's odd-even merge sort, in descending order.
+template <int L, class K>
+__device__ __forceinline__ void sort_desc(K *v) {
 #pragma unroll
-  for (int p = 1; p < S; p *= 2)
+  for (int p = 1; p < L; p *= 2)
 #pragma unroll
     for (int q = p; q > 0; q /= 2)
 #pragma unroll
-      for (int j = q % p; j + q < S; j += 2 * q)
+      for (int j = q % p; j + q < L; j += 2 * q)
 #pragma unroll
         for (int i = 0; i < q; ++i)
-          if (i + j + q < S && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+          if (i + j + q < L && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
             const K a = v[i + j], b = v[i + j + q];
             v[i + j] = max(a, b);
             v[i + j + q] = min(a, b);
           }
 }
+// The L largest of c's S in descending order: runs of L are sorted, then joined two by two (the
+// larger of each and the other's reverse form a bitonic run).
+template <int S, int L, class K>
+__device__ __forceinline__ void best_of(const K (&c)[S], K (&best)[L]) {
+  K v[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) v[s] = c[s];
+#pragma unroll
+  for (int s = 0; s < S; s += L) sort_desc<L>(v + s);
+#pragma unroll
+  for (int o = L; o < S; o *= 2)
+#pragma unroll
+    for (int s = 0; s < S; s += 2 * o) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) v[s + i] = max(v[s + i], v[s + o + L - 1 - i]);
+#pragma unroll
+      for (int q = L / 2; q > 0; q /= 2)
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+          if (!(i & q)) {
+            const K a = v[s + i], b = v[s + i + q];
+            v[s + i] = max(a, b);
+            v[s + i + q] = min(a, b);
+          }
+    }
+#pragma unroll
+  for (int i = 0; i < L; ++i) best[i] = v[i];
+}
 
 // The k largest of the lanes' values, lane r with the r-th: its value and its expert (-1: none).
-// Keys are unique and carry the expert; equal floats go to the lowest expert: of several lanes
-// the lowest, of one lane's the occurrences in order.
-template <int S>
-__device__ __forceinline__ void choose(const unsigned (&c)[S], int k, unsigned &mine, int &expert) {
+// v: each lane's L largest in descending order, L >= min(k, S). Keys (unsigned) are unique and
+// carry the expert; equal floats go to the lowest expert: of several lanes the lowest, of one
+// lane's the occurrences in order.
+template <int S, int L, class K>
+__device__ __forceinline__ void choose(const K (&c)[S], K (&v)[L], int k, K &mine, int &expert) {
+  constexpr bool kKeys = std::is_same<K, unsigned>::value;
   const int lane = threadIdx.x & 31;
-  unsigned v[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) v[s] = c[s];
-  sort_desc(v);
-  mine = 0u;
-  for (int r = 0; r < k; ++r) {
-    const unsigned b = warp_max(v[0]);
-    if (lane == r) mine = b;
-    if (v[0] == b) {
-#pragma unroll
-      for (int s = 0; s + 1 < S; ++s) v[s] = v[s + 1];
-      v[S - 1] = 0u;
-    }
-  }
-  expert = mine ? (int)(0xffffu - (mine & 0xffffu)) : -1;
-}
-template <int S>
-__device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, int &expert) {
-  const int lane = threadIdx.x & 31;
-  float v[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) v[s] = c[s];
-  sort_desc(v);
-  mine = -INFINITY;
+  mine = key_none(K{});
   int owner = 0;
-  for (int r = 0; r < k; ++r) {
-    const float b = warp_max(v[0]);
-    if (b == -INFINITY) break;
-    const int from = __ffs(__ballot_sync(kAll, v[0] == b)) - 1;
-    if (lane == r) {
-      mine = b;
-      owner = from;
+#pragma unroll (L <= 4 ? L : 1)
+  for (int r = 0; r < (L <= 4 && L < S ? L : k); ++r) {  // (picks beyond k are not used)
+    const K best = warp_max(v[0]);
+    bool own = v[0] == best;
+    if constexpr (!kKeys) {
+      const int from = __ffs(__ballot_sync(kAll, own)) - 1;
+      owner = lane == r ? from : owner;
+      own = lane == from;
     }
-    if (lane == from) {
+    mine = lane == r ? best : mine;
 #pragma unroll
-      for (int s = 0; s + 1 < S; ++s) v[s] = v[s + 1];
-      v[S - 1] = -INFINITY;
-    }
+    for (int i = 0; i + 1 < L; ++i) v[i] = own ? v[i + 1] : v[i];
+    v[L - 1] = own ? key_none(K{}) : v[L - 1];
   }
-  const float before = __shfl_up_sync(kAll, mine, 1);
-  const int by = __shfl_up_sync(kAll, owner, 1);
-  const bool again = lane > 0 && mine == before && owner == by && mine > -INFINITY;
-  const unsigned repeats = __ballot_sync(kAll, again);
-  int nth = 0;  // which of its lane's equal values this one is
-  if (repeats)
-    for (int r = lane; repeats >> r & 1u; --r) ++nth;
-  expert = -1;
+  if constexpr (kKeys) {
+    expert = mine ? (int)(0xffffu - (mine & 0xffffu)) : -1;
+  } else {
+    const float before = __shfl_up_sync(kAll, mine, 1);
+    const int by = __shfl_up_sync(kAll, owner, 1);
+    const bool again = lane > 0 && mine == before && owner == by && mine > -INFINITY;
+    const unsigned repeats = __ballot_sync(kAll, again);
+    int nth = 0;  // which of its lane's equal values this one is
+    if (repeats)
+      for (int r = lane; repeats >> r & 1u; --r) ++nth;
+    expert = -1;
 #pragma unroll
-  for (int s = 0; s < S; ++s)
-    if (__shfl_sync(kAll, c[s], owner) == mine && nth-- == 0) expert = owner * S + s;
-  if (mine == -INFINITY) expert = -1;
+    for (int s = 0; s < S; ++s)
+      if (__shfl_sync(kAll, c[s], owner) == mine && nth-- == 0) expert = owner * S + s;
+    if (mine == -INFINITY) expert = -1;
+  }
 }
 
-// Bits of the `keep` groups with the largest scores, from the queries' c in shared memory; 2^q
-// lanes to a group.
-__device__ __forceinline__ unsigned keep_groups(const float *c, int G, int per, int keep,
+// The two largest of two pairs a >= b.
+__device__ __forceinline__ void join_two(float &a, float &b, float a2, float b2) {
+  b = fmaxf(fminf(a, a2), fmaxf(b, b2));
+  a = fmaxf(a, a2);
+}
+
+// ---- groups ----------------------------------------------------------------------------
+// Whether the lane's groups stay: a bit for each lane number g * width of a kept group g, 2^q =
+// width lanes to a group. a, b: the two largest c of this lane's share of its group.
+__device__ __forceinline__ unsigned keep_groups(float a, float b, int width, int keep,
                                                 int group_top) {
+  for (int o = 1; o < width; o *= 2)
+    join_two(a, b, __shfl_xor_sync(kAll, a, o), __shfl_xor_sync(kAll, b, o));
+  float score = group_top == 2 && b > -INFINITY ? a + b : a;
   const int lane = threadIdx.x & 31;
-  int width = 32;
-  while (width * G > 32) width /= 2;
-  const int g = lane / width;
-  float a = -INFINITY, b = -INFINITY;  // the two largest
-  if (g < G)
-    for (int i = lane % width; i < per; i += width) {
-      const float v = c[g * per + i];
-      b = fmaxf(b, fminf(a, v));
-      a = fmaxf(a, v);
-    }
-  for (int o = 1; o < width; o *= 2) {
-    const float a2 = __shfl_xor_sync(kAll, a, o), b2 = __shfl_xor_sync(kAll, b, o);
-    b = fmaxf(fminf(a, a2), fmaxf(b, b2));
-    a = fmaxf(a, a2);
-  }
-  const float mine = group_top == 2 && b > -INFINITY ? a + b : a;
-  int rank = 0;
-  for (int h = 0; h < G; ++h) {
-    const float other = __shfl_sync(kAll, mine, h * width);
-    rank += other > mine || (other == mine && h < g);
-  }
-  const unsigned in = __ballot_sync(kAll, g < G && rank < keep && mine > -INFINITY);
   unsigned kept = 0u;
-  for (int h = 0; h < G; ++h) kept |= (in >> (h * width) & 1u) << h;
+  for (int r = 0; r < keep; ++r) {
+    const float best = warp_max(score);
+    if (best == -INFINITY) break;
+    const int at = __ffs(__ballot_sync(kAll, score == best)) - 1;  // its group's first lane
+    kept |= 1u << at;
+    if ((lane ^ at) < width) score = -INFINITY;
+  }
   return kept;
+}
+
+// Over teams of lanes (a power of two).
+__device__ __forceinline__ float team_sum(float v, int team) {
+  for (int o = team / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+
+// Pairs of 16-bit logits with -0 as +0 (and NaNs as one).
+__device__ __forceinline__ uint32_t plus_zero(uint32_t w, __half) {
+  uint32_t r;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
+  return r;
+}
+__device__ __forceinline__ uint32_t plus_zero(uint32_t w, __nv_bfloat16) {
+  uint32_t r;
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
+  return r;
 }
 
 struct RouteArgs {
   long long rows, ld;
   const float *bias;
   int E, mode, G, keep, group_top, k, renorm, by_logits, vec;
+  int team;   // lanes that hold the choices, a power of two
+  int width;  // lanes to a group when its score is formed
+  int whole;  // a lane's experts are of one group
   float factor;
   int *idx, *load;
   float *weight;
 };
 
 // K: unsigned for 16-bit logits compared as they are, float else (by_logits: the logits, else the
-// scores with their bias).
-template <class T, int S, class K>
-__global__ void __launch_bounds__(kThreads) route_kernel(const T *logits, RouteArgs A) {
+// scores with their bias). L: the lanes' lists.
+template <int S, class K>
+constexpr int kBlocks = S > 8 ? 1 : std::is_same<K, unsigned>::value ? 6 : 5;  // an SM's, at least
+template <class T, int S, class K, int L>
+__global__ void __launch_bounds__(kThreads, kBlocks<S, K>)
+    route_kernel(const T *logits, RouteArgs A) {
   extern __shared__ int hist[];  // the block's load; then, with groups, c of each warp's query
+  __shared__ float2 lanes_two[kWarps][32];
   constexpr bool kKeys = std::is_same<K, unsigned>::value;
-  const bool by_logits = kKeys || A.by_logits, groups = A.keep < A.G;
+  const bool groups = A.keep < A.G;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, k = A.k;
   const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
   float *shared_c = (float *)(hist + E) + warp * E;
+  float2 *pairs = lanes_two[warp];
   if (A.load) {
     for (int e = threadIdx.x; e < E; e += kThreads) hist[e] = 0;
     __syncthreads();
   }
   float bias[kKeys ? 1 : S];
-  if constexpr (!kKeys)
+  unsigned below[kKeys ? S / 2 : 1];  // pairs of the experts' complements
+  if constexpr (kKeys) {
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i)
+      below[i] = (0xffffu - (lane * S + 2 * i)) | (0xffffu - (lane * S + 2 * i + 1)) << 16;
+  } else {
 #pragma unroll
     for (int s = 0; s < S; ++s)
-      bias[s] = A.bias && lane * S + s < E ? A.bias[lane * S + s] : 0.f;
+      bias[s] = A.bias && lane * S + s < E ? fmaxf(A.bias[lane * S + s], -INFINITY) : 0.f;  // (NaN)
+  }
+  // the group whose share this lane takes, its first position there, its experts' (first) group
+  const int per = E / A.G, g = lane / A.width, i0 = lane % A.width, of0 = lane * S / per;
   const long long step = (long long)gridDim.x * kWarps;
   long long row = (long long)blockIdx.x * kWarps + warp;
   Raw<T, S> next;
@@ -245,80 +286,134 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const T *logits, RouteA
   for (; row < A.rows; row += step) {
     const Raw<T, S> raw = next;
     if (row + step < A.rows) next.load(logits + (row + step) * A.ld, E, A.vec);
-    float x[S], m = -INFINITY;
+    K c[S], v[L], mine;
+    float m = -INFINITY, inv_sum = 1.f;  // of the softmax
+    bool bad;
+    int e;
+    if constexpr (kKeys) {
+      // order bits of pairs of logits, each over its expert's complement; a NaN is largest, +inf
+      // next, -inf (and what is beyond E) smallest
+      constexpr unsigned kInf = std::is_same<T, __half>::value ? 0xfc00u : 0xff80u;
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      x[s] = to_float(raw.at(s));
-      m = max_nan(m, x[s]);
-    }
-    m = warp_max(m);
-    const bool bad = isnan(m) || (soft && m == INFINITY);
-    float inv_sum = 0.f;  // of the softmax
-    if (soft && (!by_logits || !A.renorm)) {
-      float sum = 0.f;
-#pragma unroll
-      for (int s = 0; s < S; ++s) sum += exp2_fast((x[s] - m) * kLog2e);
-      inv_sum = __fdividef(1.f, warp_sum(sum));
-    }
-    K c[S];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      if constexpr (kKeys) {  // upper half of order bits, expert
-        unsigned u = __float_as_uint(x[s] == 0.f ? 0.f : x[s]);
-        if constexpr (std::is_same<T, __half>::value) {  // (fp16 as its own bits)
-          const __half h = x[s] == 0.f ? __float2half_rn(0.f) : raw.at(s);
-          unsigned short q;
-          memcpy(&q, &h, 2);
-          u = (unsigned)q << 16;
-        }
-        u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-        c[s] = x[s] > -INFINITY && !bad ? (u & 0xffff0000u) | (0xffffu - (lane * S + s)) : 0u;
-      } else if (by_logits) {
-        c[s] = bad ? -INFINITY : x[s];
-      } else {
-        const float v = soft ? exp2_fast((x[s] - m) * kLog2e) * inv_sum : logistic(x[s]);
-        // (fmaxf: no NaN of the bias)
-        c[s] = x[s] > -INFINITY && !bad ? fmaxf(v + bias[s], -INFINITY) : -INFINITY;
+      for (int i = 0; i < S / 2; ++i) {
+        const uint32_t w = plus_zero(raw.w[i], T{});
+        const uint32_t o = w ^ (((w >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
+        c[2 * i] = __byte_perm(o, below[i], 0x1054);
+        c[2 * i + 1] = __byte_perm(o, below[i], 0x3276);
       }
-    }
-    if (groups) {
-      const int per = E / A.G;
+      best_of(c, v);
+      if (soft && !A.renorm) {
+        float x[S];
 #pragma unroll
-      for (int s = 0; s < S; ++s)
-        if (lane * S + s < E) {
-          if constexpr (kKeys) shared_c[lane * S + s] = bad ? -INFINITY : x[s];
-          else shared_c[lane * S + s] = c[s];
-        }
-      __syncwarp();
-      const unsigned kept = keep_groups(shared_c, A.G, per, A.keep, A.group_top);
-      __syncwarp();
-      // (the lane's experts are neighbours: one division, then steps)
-      int g = lane * S / per, left = (g + 1) * per - lane * S;
+        for (int s = 0; s < S; ++s) m = max_nan(m, x[s] = to_float(raw.at(s)));
+        m = warp_max(m);
+        inv_sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s) inv_sum += exp2_fast((x[s] - m) * kLog2e);
+        inv_sum = __fdividef(1.f, warp_sum(inv_sum));
+      }
+      choose(c, v, k, mine, e);
+      const unsigned top = __shfl_sync(kAll, mine, 0) >> 16;
+      bad = top > kInf || (soft && top == kInf);
+      if (bad || mine >> 16 <= (0xffffu ^ kInf)) e = -1;
+    } else {
+      float x[S];
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        if (left-- == 0) {
-          ++g;
-          left = per - 1;
-        }
-        if (!(kept >> (g & 31) & 1u)) c[s] = key_none(K{});
+        x[s] = to_float(raw.at(s));
+        m = max_nan(m, x[s]);
       }
+      m = warp_max(m);
+      bad = isnan(m) || (soft && m == INFINITY);
+      if (soft && (!A.by_logits || !A.renorm)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s) sum += exp2_fast((x[s] - m) * kLog2e);
+        inv_sum = __fdividef(1.f, warp_sum(sum));
+      }
+      if (A.by_logits) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) c[s] = x[s];
+      } else if (soft) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) c[s] = exp2_fast((x[s] - m) * kLog2e) * inv_sum + bias[s];
+      } else {
+#pragma unroll
+        for (int s = 0; s < S; ++s) c[s] = logistic(x[s]) + bias[s];
+      }
+#pragma unroll
+      for (int s = 0; s < S; ++s) c[s] = x[s] > -INFINITY && !bad ? c[s] : -INFINITY;
+      if (groups) {
+        float a = -INFINITY, b = -INFINITY;
+        if (A.whole) {  // a lane's experts are of one group: the lanes' two largest will do
+          float first = c[0], second = -INFINITY;
+#pragma unroll
+          for (int s = 1; s < S; ++s) join_two(first, second, c[s], -INFINITY);
+          pairs[lane] = make_float2(first, second);
+          __syncwarp();
+          if (g < A.G)
+            for (int i = i0; i < per / S; i += A.width) {
+              const float2 v = pairs[g * per / S + i];
+              join_two(a, b, v.x, v.y);
+            }
+        } else {
+#pragma unroll
+          for (int s = 0; s < S; ++s)
+            if (lane * S + s < E) shared_c[lane * S + s] = c[s];
+          __syncwarp();
+          if (g < A.G)
+            for (int i = i0; i < per; i += A.width)
+              join_two(a, b, shared_c[g * per + i], -INFINITY);
+        }
+        const unsigned kept = keep_groups(a, b, A.width, A.keep, A.group_top);
+        __syncwarp();
+        if (A.whole) {
+          const bool in = of0 < A.G && (kept >> (of0 * A.width) & 1u);
+#pragma unroll
+          for (int s = 0; s < S; ++s) c[s] = in ? c[s] : -INFINITY;
+        } else {
+          // (the lane's experts are neighbours: one division, then steps)
+          int of = of0, left = (of + 1) * per - lane * S;
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            if (left-- == 0) {
+              ++of;
+              left = per - 1;
+            }
+            if (of >= A.G || !(kept >> (of * A.width) & 1u)) c[s] = -INFINITY;
+          }
+        }
+      }
+      best_of(c, v);
+      choose(c, v, k, mine, e);
     }
-    K mine;
-    int e;
-    choose(c, k, mine, e);
+    if (lane >= k) e = -1;
     // the chosen scores
-    float v = 0.f;
-    if (e >= 0) {
-      const float xe = to_float(logits[row * A.ld + e]);
-      v = !soft ? logistic(xe) : exp2_fast((xe - m) * kLog2e) * (inv_sum > 0.f ? inv_sum : 1.f);
+    float w = 0.f;
+    if (kKeys || A.by_logits) {
+      float x;
+      if constexpr (kKeys) {
+        const unsigned o = mine >> 16, u = o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu;
+        const unsigned short h = (unsigned short)u;
+        T t;
+        memcpy(&t, &h, 2);
+        x = to_float(t);
+      } else {
+        x = mine;
+      }
+      if (soft && A.renorm) m = __shfl_sync(kAll, x, 0);
+      if (e >= 0) w = !soft ? logistic(x) : exp2_fast((x - m) * kLog2e) * inv_sum;
+    } else if (e >= 0) {
+      const float x = to_float(logits[row * A.ld + e]);
+      w = !soft ? logistic(x) : exp2_fast((x - m) * kLog2e) * inv_sum;
     }
     if (A.renorm) {
-      const float sum = warp_sum(v);
-      v = sum > 0.f ? v / sum : 0.f;
+      const float sum = team_sum(w, A.team);
+      w = sum > 0.f ? __fdividef(w, sum) : 0.f;
     }
     if (lane < k) {
       A.idx[row * k + lane] = e;
-      A.weight[row * k + lane] = bad ? NAN : A.factor * v;
+      A.weight[row * k + lane] = bad ? NAN : A.factor * w;
       if (A.load && e >= 0 && BOUTE_INB(e, E)) atomicAdd(hist + e, 1);
     }
   }
@@ -344,13 +439,6 @@ struct RouteGradArgs {
   const int *idx;
   const float *g_weight;
 };
-
-// ds for this lane's choice of its query, in teams of `team` lanes (a power of two >= k) with a
-// query each: v the chosen score (or anything proportional to it, with renorm), g its gradient.
-__device__ __forceinline__ float team_sum(float v, int team) {
-  for (int o = team / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
-}
 
 // The gradient where it is 0 but for the chosen experts: logistic scores, and a renormalised
 // softmax, of which only the chosen logits count:
@@ -487,6 +575,11 @@ static int with_slots(int E, Go go) {
   if (E <= 512) return go(std::integral_constant<int, 16>{});
   return go(std::integral_constant<int, 32>{});
 }
+static int power_of_two(int k) {  // at least k
+  int p = 1;
+  while (p < k) p *= 2;
+  return p;
+}
 // Whether a lane's S logits are vectors of up to 16 bytes on their boundaries in every row.
 static bool vectors(const void *p, long long ld, int E, int S, size_t bytes) {
   const size_t b = std::min<size_t>(16, S * bytes);
@@ -526,23 +619,31 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   const bool groups = keep < G;
   // (the sum of two scores has no counterpart among the logits)
   const bool by_logits = !bias && !(groups && group_top == 2);
-  RouteArgs A = {T,         ld, bias,   E,   mode, G,   keep, group_top, k, renorm,
-                 by_logits, 0,  factor, idx, load, weight};
+  RouteArgs A = {};
+  A.rows = T, A.ld = ld, A.bias = bias, A.E = E, A.mode = mode, A.G = G, A.keep = keep;
+  A.group_top = group_top, A.k = k, A.renorm = renorm, A.by_logits = by_logits;
+  A.factor = factor, A.idx = idx, A.load = load, A.weight = weight;
+  A.team = power_of_two(k);
+  A.width = 32 / power_of_two(G);
   return with_dtype(dtype, [&](auto tag) {
     using X = decltype(tag);
     return with_slots(E, [&](auto slots) {
       constexpr int S = decltype(slots)::value;
       A.vec = vectors(logits, ld, E, S, sizeof(X));
-      const size_t smem = (size_t)E * 4 * (groups ? 1 + kWarps : 1);
+      A.whole = E / G % S == 0;
+      const size_t smem = (size_t)E * 4 * (groups && !A.whole ? 1 + kWarps : 1);
       const long long all = (T + kWarps - 1) / kWarps;
-      // a few queries: one block, which writes the load itself
-      const unsigned grid = all <= 4 ? 1u : (unsigned)std::min<long long>(all, 4ll * num_sms());
-      if (load && grid > 1) {
-        clear_load_kernel<<<1, 256, 0, s>>>(load, E);
-        count_launch();
-      }
-      auto go = [&](auto key) {
-        auto kernel = route_kernel<X, S, decltype(key)>;
+      auto go = [&](auto key, auto list) {
+        using K = decltype(key);
+        // a few queries whose load is wanted: one block, which writes it itself
+        const unsigned grid =
+            load && all <= 4 ? 1u : (unsigned)std::min<long long>(all, (S > 8 ? 4ll : kBlocks<S, K>) *
+                                                                           num_sms());
+        if (load && grid > 1) {
+          clear_load_kernel<<<1, 256, 0, s>>>(load, E);
+          count_launch();
+        }
+        auto kernel = route_kernel<X, S, K, decltype(list)::value>;
         if (load && grid > 1)
           launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, s, (const X *)logits, A);
         else
@@ -550,9 +651,14 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
         count_launch();
         return last_launch_status();
       };
+      // (lists of the k best at least; shorter ones take fewer steps)
+      constexpr int kShort = S < 4 ? S : 4;
       if constexpr (sizeof(X) == 2 && S <= 8)
-        if (A.by_logits) return go(0u);
-      return go(0.f);
+        if (by_logits && !groups)
+          return k <= kShort ? go(0u, std::integral_constant<int, kShort>{})
+                             : go(0u, std::integral_constant<int, S>{});
+      return k <= kShort ? go(0.f, std::integral_constant<int, kShort>{})
+                         : go(0.f, std::integral_constant<int, S>{});
     });
   });
 }
@@ -574,8 +680,7 @@ extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int 
   return with_dtype(dtype, [&](auto tag) {
     using X = decltype(tag);
     if (mode == BOUTE_ROUTE_SIGMOID || renorm) {
-      int team = 1;
-      while (team < k) team *= 2;
+      const int team = power_of_two(k);
       A.vec = (uintptr_t)dlogits % 16 == 0 && (size_t)E * sizeof(X) % 16 == 0;
       const long long all = (T + kWarps * (32 / team) - 1) / (kWarps * (32 / team));
       const unsigned grid = (unsigned)std::min<long long>(all, 8ll * num_sms());

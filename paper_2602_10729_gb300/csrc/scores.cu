@@ -1,6 +1,13 @@
 // The scores of answers (mean and lowest log-probability, mean and highest
 // entropy of the positions that hold a token) and their gradient.
+//
+// A block's teams (8 or 32 lanes, or all of it, by the mean length) take an answer each.
+// Lengths are ragged: what is too long for a team is taken by its block afterwards, and
+// where answers are long in the mean, by the eight blocks of a cluster. Latency bounds it:
+// the offsets, then the positions, are one trip to memory each.
 #include <math.h>
+
+#include <algorithm>
 
 #include "answers.cuh"
 
@@ -8,9 +15,9 @@ namespace boute {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kCluster = 8;
-constexpr int kTeamLane = 32;  // positions a lane of a team takes at most
-constexpr int kUnroll = 4;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
+constexpr int kMost = 32;  // positions a lane of a team of 8 or 32 lanes, or of a block, takes
+constexpr int kUnroll = 4;  // positions on their way to a lane
 
 // Order-preserving bits of a float, -0 as +0, a NaN above every number.
 __device__ __forceinline__ unsigned order_bits(float v) {
@@ -40,32 +47,30 @@ struct Answers {
   const float *logprob, *entropy;
   const long long *targets, *offsets;
   long long T, Q;
+  int cluster;  // blocks of a cluster, 1 or kMaxCluster
+  int per;      // answers of a block, or 0: one of a cluster
 
-  // an answer's positions within [0, T]
-  __device__ __forceinline__ void range(long long q, long long &a, long long &b) const {
-    a = offsets[q];
-    b = offsets[q + 1];
-    a = a < 0 ? 0 : a > T ? T : a;
-    b = b < a ? a : b > T ? T : b;
-  }
-  // Thread i of `by` over the positions [a, b) (2^31 at most).
-  __device__ __forceinline__ Part part(long long a, long long b, int i, int by) const {
+  // Thread i of `by` over the positions [a, b) (2^31 at most); on: which of its first 64 count.
+  __device__ __forceinline__ Part part(long long a, long long b, int i, int by,
+                                       unsigned long long &on) const {
     Part p = {0ull, 0ull, 0.f, 0.f, 0, 0};
-    for (long long t0 = a + i; t0 < b; t0 += kUnroll * by) {
+    on = 0ull;
+    int first = 0;  // of this round's positions, in the thread's order
+    for (long long t0 = a + i; t0 < b; t0 += kUnroll * by, first += kUnroll) {
       float l[kUnroll], h[kUnroll];
-      bool on[kUnroll];
+      unsigned in = 0u;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const long long t = t0 + u * by;
-        on[u] = t < b;
-        if (!on[u]) continue;
+        if (t >= b) continue;
         l[u] = logprob[t];
         h[u] = entropy[t];
-        if (targets) on[u] = targets[t] >= 0;
+        in |= (unsigned)(targets ? targets[t] >= 0 : true) << u;
       }
+      if (first < 64) on |= (unsigned long long)in << first;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        if (!on[u]) continue;
+        if (!(in >> u & 1u)) continue;
         const unsigned at = 0xffffffffu - (unsigned)(t0 + u * by - a);
         p.lp += l[u];
         p.ent += h[u];
@@ -78,30 +83,38 @@ struct Answers {
   }
 };
 
-__device__ __forceinline__ long long position(unsigned long long key, long long a) {
+// The float whose order_bits a key has (-0 as +0), and the position, of an answer from a on.
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const unsigned o = (unsigned)(key >> 32);
+  return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ long long key_position(unsigned long long key, long long a) {
   return a + (long long)(0xffffffffu - (unsigned)key);
 }
 
-__device__ __forceinline__ Part warp_join(Part p) {
+// Of `lanes` neighbouring lanes, in each of them.
+__device__ __forceinline__ Part lanes_join(Part p, int lanes) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
-    add(p, {shfl_xor64(p.lo, o), shfl_xor64(p.hi, o), __shfl_xor_sync(kAll, p.lp, o),
-            __shfl_xor_sync(kAll, p.ent, o), __shfl_xor_sync(kAll, p.n, o), 0});
+    if (o < lanes)
+      add(p, {shfl_xor64(p.lo, o), shfl_xor64(p.hi, o), __shfl_xor_sync(kAll, p.lp, o),
+              __shfl_xor_sync(kAll, p.ent, o), __shfl_xor_sync(kAll, p.n, o), 0});
   return p;
 }
 // Of the whole block, in every thread; red (kWarps Parts) may be used again after a barrier.
 __device__ __forceinline__ Part block_join(Part p, Part *red) {
-  p = warp_join(p);
+  p = lanes_join(p, 32);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = p;
   __syncthreads();
   p = red[0];
   for (int w = 1; w < kWarps; ++w) add(p, red[w]);
   return p;
 }
-// Of the whole cluster, in every thread; a cluster barrier before the next call.
-__device__ __forceinline__ Part cluster_join(Part p, int rank, Part *red, Part *parts) {
+// Of the whole cluster, in every thread; a cluster barrier before a block may end.
+__device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part *red,
+                                             Part *parts) {
   p = block_join(p, red);
-  if (threadIdx.x < kCluster) {
+  if (threadIdx.x < cluster) {
     const uint32_t to = peer(&parts[rank], threadIdx.x);
     store_peer(to, p.lo);
     store_peer(to + 8, p.hi);
@@ -111,91 +124,92 @@ __device__ __forceinline__ Part cluster_join(Part p, int rank, Part *red, Part *
   }
   cluster_sync();
   p = parts[0];
-  for (int r = 1; r < kCluster; ++r) add(p, parts[r]);
+  for (int r = 1; r < cluster; ++r) add(p, parts[r]);
   return p;
 }
 
-// A cluster of 8 blocks takes `per` answers: one by all its threads (per = 1), one a block (8), or
-// one a warp (64); answers too long for such a team (ragged lengths) by the whole cluster
-// afterwards. emit(q, a, b, p, i, by): thread i of `by` writes its share of answer q's results.
+// emit(q, a, b, p, on, i, by): thread i of `by` writes its share of answer q's results.
 template <class Emit>
-__device__ __forceinline__ void for_answers(const Answers &A, int per, Emit emit) {
-  __shared__ Part red[kWarps], parts[kCluster];
-  const int rank = blockIdx.x % kCluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long q0 = (long long)(blockIdx.x / kCluster) * per;
-  const long long most = (long long)kTeamLane * (per == 64 ? 32 : kThreads);
+__device__ __forceinline__ void for_answers(const Answers &A, Emit emit) {
+  __shared__ Part red[kWarps], parts[kMaxCluster];
+  const int tid = threadIdx.x;
   long long a, b;
-  if (per == 64) {
-    const long long q = q0 + rank * kWarps + warp;
-    if (q < A.Q) {
-      A.range(q, a, b);
-      if (b - a <= most) emit(q, a, b, warp_join(A.part(a, b, lane, 32)), lane, 32);
-    }
-  } else if (per == kCluster) {
-    const long long q = q0 + rank;
-    if (q < A.Q) {
-      A.range(q, a, b);
-      if (b - a <= most) {
-        const Part p = block_join(A.part(a, b, threadIdx.x, kThreads), red);
-        emit(q, a, b, p, (int)threadIdx.x, kThreads);
-      }
-    }
+  unsigned long long on;
+  auto range = [&](long long q) {  // within [0, T]
+    a = min(max(A.offsets[q], 0ll), A.T);
+    b = max(min(A.offsets[q + 1], A.T), a);
+  };
+  if (A.per == 0) {
+    const int rank = blockIdx.x % A.cluster, i = rank * kThreads + tid, by = A.cluster * kThreads;
+    const long long q = blockIdx.x / A.cluster;
+    range(q);
+    Part p = A.part(a, b, i, by, on);
+    if (A.cluster > 1) p = cluster_join(p, rank, A.cluster, red, parts);
+    else p = block_join(p, red);
+    emit(q, a, b, p, on, i, by);
+    if (A.cluster > 1) cluster_sync();
+    return;
   }
-  __syncthreads();
-  for (int j0 = 0; j0 < per; j0 += 32) {
-    long long n = 0;
-    if (j0 + lane < per && q0 + j0 + lane < A.Q) {
-      A.range(q0 + j0 + lane, a, b);
-      n = b - a;
-    }
-    // (the same in all of the cluster's warps)
-    unsigned left = __ballot_sync(kAll, per == 1 ? lane == 0 : n > most);
-    while (left) {
-      const long long q = q0 + j0 + __ffs(left) - 1;
-      left &= left - 1;
-      A.range(q, a, b);
-      const int i = rank * kThreads + threadIdx.x, by = kCluster * kThreads;
-      emit(q, a, b, cluster_join(A.part(a, b, i, by), rank, red, parts), i, by);
-      cluster_sync();
-    }
+  const int team = kThreads / A.per, i = tid % team;
+  const long long q = (long long)blockIdx.x * A.per + tid / team;
+  if (q < A.Q) range(q);
+  else a = b = 0;
+  const bool more = b - a > kMost * team;
+  const Part p = lanes_join(A.part(a, more ? a : b, i, team, on), team);
+  if (!more && q < A.Q) emit(q, a, b, p, on, i, team);
+  // the long ones, one after another by the whole block
+  __shared__ unsigned char longer[kThreads / 8];
+  if (i == 0) longer[tid / team] = more;
+  if (!__syncthreads_or(more)) return;
+  for (int j = 0; j < A.per; ++j) {
+    if (!longer[j]) continue;
+    range((long long)blockIdx.x * A.per + j);
+    const Part whole = block_join(A.part(a, b, tid, kThreads, on), red);
+    emit((long long)blockIdx.x * A.per + j, a, b, whole, on, tid, kThreads);
+    __syncthreads();
   }
 }
 
-__global__ void __launch_bounds__(kThreads)
-    answer_scores_kernel(Answers A, int per, float *scores, int *counts) {
-  for_answers(A, per, [&](long long q, long long a, long long b, const Part &p, int i, int by) {
+__global__ void __launch_bounds__(kThreads, 5)
+    answer_scores_kernel(Answers A, float *scores, int *counts) {
+  for_answers(A, [&](long long q, long long a, long long b, const Part &p, unsigned long long on,
+                     int i, int by) {
     if (i != 0) return;
-    counts[q] = p.n;
     const float n = (float)p.n;
+    counts[q] = p.n;
     scores[4 * q] = p.n ? p.lp / n : 0.f;
-    scores[4 * q + 1] = p.n ? A.logprob[position(p.lo, a)] : 0.f;
+    scores[4 * q + 1] = p.n ? 0.f - key_value(p.lo) : 0.f;  // (0 - v: +0 for -0)
     scores[4 * q + 2] = p.n ? p.ent / n : 0.f;
-    scores[4 * q + 3] = p.n ? A.entropy[position(p.hi, a)] : 0.f;
+    scores[4 * q + 3] = p.n ? key_value(p.hi) : 0.f;
   });
 }
 
-__global__ void __launch_bounds__(kThreads)
-    answer_scores_grad_kernel(Answers A, int per, const float *g_scores, float *g_logprob,
+__global__ void __launch_bounds__(kThreads, 5)
+    answer_scores_grad_kernel(Answers A, const float *g_scores, float *g_logprob,
                               float *g_entropy) {
-  for_answers(A, per, [&](long long q, long long a, long long b, const Part &p, int i, int by) {
+  for_answers(A, [&](long long q, long long a, long long b, const Part &p, unsigned long long on,
+                     int i, int by) {
     const float n = p.n ? (float)p.n : 1.f;
     const float *g = g_scores + 4 * q;
     const float g0 = g[0] / n, g1 = g[1], g2 = g[2] / n, g3 = g[3];
-    const long long lo = position(p.lo, a), hi = position(p.hi, a);
+    const long long lo = key_position(p.lo, a), hi = key_position(p.hi, a);
+    int nth = 0;
 #pragma unroll 4
-    for (long long t = a + i; t < b; t += by) {
-      const bool on = !A.targets || A.targets[t] >= 0;
-      g_logprob[t] = on ? g0 + (t == lo ? g1 : 0.f) : 0.f;
-      g_entropy[t] = on ? g2 + (t == hi ? g3 : 0.f) : 0.f;
+    for (long long t = a + i; t < b; t += by, ++nth) {
+      const bool in = nth < 64 ? on >> nth & 1ull : !A.targets || A.targets[t] >= 0;
+      g_logprob[t] = in ? g0 + (t == lo ? g1 : 0.f) : 0.f;
+      g_entropy[t] = in ? g2 + (t == hi ? g3 : 0.f) : 0.f;
     }
   });
   // positions before the first answer and after the last
-  const long long before = min(max(A.offsets[0], 0ll), A.T);
-  const long long after = min(max(A.offsets[A.Q], 0ll), A.T);
-  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-  const long long by = (long long)gridDim.x * kThreads;
-  for (long long t = i; t < before; t += by) g_logprob[t] = g_entropy[t] = 0.f;
-  for (long long t = after + i; t < A.T; t += by) g_logprob[t] = g_entropy[t] = 0.f;
+  if (blockIdx.x == 0) {
+    const long long end = min(max(A.offsets[0], 0ll), A.T);
+    for (long long t = threadIdx.x; t < end; t += kThreads) g_logprob[t] = g_entropy[t] = 0.f;
+  }
+  if (blockIdx.x == gridDim.x - 1) {
+    const long long from = min(max(A.offsets[A.Q], 0ll), A.T);
+    for (long long t = from + threadIdx.x; t < A.T; t += kThreads) g_logprob[t] = g_entropy[t] = 0.f;
+  }
 }
 
 }  // namespace
@@ -214,27 +228,29 @@ static int sizes_ok(long long T, long long Q, const float *logprob, const float 
   return T >= (1ll << 31) || Q > BOUTE_MAX_ANSWERS ? BOUTE_ERR_UNSUPPORTED : device_ok();
 }
 
-// Answers of a cluster: as many at a time as leave a lane 16 positions of the mean answer or
-// fewer, while there are clusters enough for two blocks an SM.
+// Teams by the mean length: 8 lanes up to 48 positions, 32 up to 512, else a block; and up to the
+// eight blocks of a cluster for answers over 1024 positions a block that are too few to fill the SMs.
+// (13665 answers of 31: 9.8 us with 8 lanes, 14 with 32; 4096 of 200: 10.5 with 32, 15.6 with a
+// block; 96 of 16384: 13 with eight blocks, 18 with four.)
 template <class... KArgs, class... Args>
-static int launch_answers(void (*kernel)(Answers, int, KArgs...), const Answers &A,
-                          cudaStream_t s, Args... args) {
-  const int sms = num_sms();
-  int per = kCluster * kWarps;
-  while (per > 1 && (A.T / A.Q > 16 * kCluster * kThreads / per ||
-                     A.Q * kCluster < 2ll * sms * per))
-    per /= 8;
+static int launch_answers(void (*kernel)(Answers, KArgs...), Answers A, cudaStream_t s,
+                          Args... args) {
+  const long long mean = A.T / A.Q, at_once = 8ll * num_sms();
+  A.per = mean <= 48 ? 32 : mean <= 512 ? 8 : 0;
+  while (A.cluster < kMaxCluster && A.per == 0 && mean > 1024 * A.cluster &&
+         2 * A.cluster * A.Q <= at_once)
+    A.cluster *= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((A.Q + per - 1) / per * kCluster));
+  cfg.gridDim = dim3((unsigned)(A.per ? (A.Q + A.per - 1) / A.per : A.Q * A.cluster));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kCluster;
+  attr[0].val.clusterDim.x = A.cluster;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  cudaLaunchKernelEx(&cfg, kernel, A, per, static_cast<KArgs>(args)...);
+  cfg.numAttrs = A.cluster > 1;
+  cudaLaunchKernelEx(&cfg, kernel, A, static_cast<KArgs>(args)...);
   count_launch();
   return last_launch_status();
 }
@@ -247,7 +263,7 @@ extern "C" int boute_answer_scores(const float *logprob, const float *entropy,
   if (Q > 0 && (!array_ok(scores, 4) || !array_ok(counts, 4))) return BOUTE_ERR_INVALID_ARG;
   if (int r = sizes_ok(T, Q, logprob, entropy, targets, offsets)) return r;
   if (Q == 0) return BOUTE_OK;
-  return launch_answers(answer_scores_kernel, {logprob, entropy, targets, offsets, T, Q},
+  return launch_answers(answer_scores_kernel, {logprob, entropy, targets, offsets, T, Q, 1, 0},
                         (cudaStream_t)stream, scores, counts);
 }
 
@@ -267,6 +283,6 @@ extern "C" int boute_answer_scores_grad(const float *logprob, const float *entro
       return last_launch_status();
     return BOUTE_OK;
   }
-  return launch_answers(answer_scores_grad_kernel, {logprob, entropy, targets, offsets, T, Q},
+  return launch_answers(answer_scores_grad_kernel, {logprob, entropy, targets, offsets, T, Q, 1, 0},
                         (cudaStream_t)stream, g_scores, g_logprob, g_entropy);
 }
