@@ -76,4 +76,27 @@ __device__ __forceinline__ int add_peer(uint32_t a, int v) {
   return old;
 }
 
+// Launches blocks of `threads` in clusters of `cluster` (1: none). As with launch_pdl, the kernel
+// may be set up while the previous one on the stream ends, and begins with pdl_wait.
+template <class... KArgs, class... Args>
+inline int launch_cluster(void (*kernel)(KArgs...), long long blocks, int threads, int cluster,
+                          size_t smem, cudaStream_t s, Args &&...args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+  count_launch();
+  return last_launch_status();
+}
+
 }  // namespace boute

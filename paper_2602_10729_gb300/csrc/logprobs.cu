@@ -295,6 +295,8 @@ __global__ void __launch_bounds__(kThreads, 4)
   __shared__ float csum[kMaxCluster][3];
   __shared__ unsigned bound;
   __shared__ int nlist;
+  pdl_wait();
+  pdl_trigger();
   const int NT = blockDim.x, W = NT / 32, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = CS > 1 ? blockIdx.x % CS : 0;
   const long long row = blockIdx.x / CS;
@@ -497,6 +499,8 @@ __global__ void __launch_bounds__(kThreads, 4)
   constexpr int N = Piece<T>::N, SPAN = Piece<T>::SPAN;
   __shared__ Sums wsum[kThreads / 32];
   __shared__ float csum[kMaxCluster][3];
+  pdl_wait();
+  pdl_trigger();
   const int W = blockDim.x / 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rank = CS > 1 ? blockIdx.x % CS : 0;
   const long long row = blockIdx.x / CS;
@@ -602,25 +606,6 @@ struct Spread {
   }
 };
 
-template <class... KArgs, class... Args>
-static int launch_rows(void (*kernel)(KArgs...), const Spread &sp, long long T, size_t smem,
-                       cudaStream_t s, Args &&...args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(T * sp.CS));
-  cfg.blockDim = dim3(32 * sp.W);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = sp.CS;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = sp.CS > 1;
-  cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-  count_launch();
-  return last_launch_status();
-}
-
 static bool logits_ok(const void *logits, int dtype, long long T, int V, long long ld,
                       const long long *targets, float scale) {
   return dtype_known(dtype) && T >= 0 && V >= 1 && ld >= V && scale > 0.f && isfinite(scale) &&
@@ -648,8 +633,8 @@ extern "C" int boute_token_logprobs(const void *logits, int dtype, long long T, 
         cudaFuncSetAttribute((const void *)token_logprobs_kernel<E>,
                              cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
       return last_launch_status();
-    return launch_rows(token_logprobs_kernel<E>, sp, T, smem, (cudaStream_t)stream,
-                       (const E *)logits, V, ld, targets, scale, k, sp.CS, logprob,
+    return launch_cluster(token_logprobs_kernel<E>, T * sp.CS, 32 * sp.W, sp.CS, smem,
+                          (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, k, sp.CS, logprob,
                        entropy, lse, top_idx, top_logprob);
   });
 }
@@ -672,8 +657,8 @@ extern "C" int boute_token_logprobs_grad(const void *logits, int dtype, long lon
   return with_dtype(dtype, [&](auto tag) {
     using E = decltype(tag);
     const Spread sp(T, V, Piece<E>{});
-    return launch_rows(token_logprobs_grad_kernel<E>, sp, T, 0, (cudaStream_t)stream,
-                       (const E *)logits, V, ld, targets, scale, lse, entropy, g_logprob,
+    return launch_cluster(token_logprobs_grad_kernel<E>, T * sp.CS, 32 * sp.W, sp.CS, 0,
+                          (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, lse, entropy, g_logprob,
                        g_entropy, (E *)dlogits, ldd, sp.CS);
   });
 }

@@ -262,6 +262,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks<S, K>)
   const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
   float *shared_c = (float *)(hist + E) + warp * E;
   float2 *pairs = lanes_two[warp];
+  // (behind clear_load_kernel, which has waited for what came before, only the load waits)
+  if (!A.load || gridDim.x == 1) pdl_wait();
+  pdl_trigger();
   if (A.load) {
     for (int e = threadIdx.x; e < E; e += kThreads) hist[e] = 0;
     __syncthreads();
@@ -427,6 +430,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks<S, K>)
 }
 
 __global__ void clear_load_kernel(int *load, int E) {
+  pdl_wait();
   pdl_trigger();
   for (int e = threadIdx.x; e < E; e += blockDim.x) load[e] = 0;
 }
@@ -448,6 +452,8 @@ struct RouteGradArgs {
 template <class T>
 __global__ void __launch_bounds__(kThreads)
     route_grad_chosen_kernel(const T *logits, RouteGradArgs A, T *dlogits, int team) {
+  pdl_wait();
+  pdl_trigger();
   const int lane = threadIdx.x & 31, r = lane % team, per = 32 / team;
   const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
   const long long step = (long long)gridDim.x * kWarps * per;
@@ -501,6 +507,8 @@ __global__ void __launch_bounds__(kThreads)
 template <class T, int S>
 __global__ void __launch_bounds__(kThreads)
     route_grad_softmax_kernel(const T *logits, RouteGradArgs A, T *dlogits) {
+  pdl_wait();
+  pdl_trigger();
   const int lane = threadIdx.x & 31, E = A.E, k = A.k;
   const long long step = (long long)gridDim.x * kWarps;
   for (long long row = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); row < A.rows;
@@ -640,16 +648,10 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
             load && all <= 4 ? 1u : (unsigned)std::min<long long>(all, (S > 8 ? 4ll : kBlocks<S, K>) *
                                                                            num_sms());
         if (load && grid > 1) {
-          clear_load_kernel<<<1, 256, 0, s>>>(load, E);
-          count_launch();
+          if (int r = launch_cluster(clear_load_kernel, 1, 256, 1, 0, s, load, E)) return r;
         }
         auto kernel = route_kernel<X, S, K, decltype(list)::value>;
-        if (load && grid > 1)
-          launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, s, (const X *)logits, A);
-        else
-          kernel<<<grid, kThreads, smem, s>>>((const X *)logits, A);
-        count_launch();
-        return last_launch_status();
+        return launch_cluster(kernel, grid, kThreads, 1, smem, s, (const X *)logits, A);
       };
       // (lists of the k best at least; shorter ones take fewer steps)
       constexpr int kShort = S < 4 ? S : 4;
@@ -684,19 +686,15 @@ extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int 
       A.vec = (uintptr_t)dlogits % 16 == 0 && (size_t)E * sizeof(X) % 16 == 0;
       const long long all = (T + kWarps * (32 / team) - 1) / (kWarps * (32 / team));
       const unsigned grid = (unsigned)std::min<long long>(all, 8ll * num_sms());
-      route_grad_chosen_kernel<X><<<grid, kThreads, 0, s>>>((const X *)logits, A, (X *)dlogits,
-                                                            team);
-      count_launch();
-      return last_launch_status();
+      return launch_cluster(route_grad_chosen_kernel<X>, grid, kThreads, 1, 0, s, (const X *)logits, A,
+                            (X *)dlogits, team);
     }
     return with_slots(E, [&](auto slots) {
       constexpr int S = decltype(slots)::value;
       A.vec = vectors(logits, ld, E, S, sizeof(X)) && vectors(dlogits, ldd, E, S, sizeof(X));
       const unsigned grid = (unsigned)std::min<long long>((T + kWarps - 1) / kWarps, 8ll * num_sms());
-      route_grad_softmax_kernel<X, S><<<grid, kThreads, 0, s>>>((const X *)logits, A,
-                                                                (X *)dlogits);
-      count_launch();
-      return last_launch_status();
+      return launch_cluster(route_grad_softmax_kernel<X, S>, grid, kThreads, 1, 0, s,
+                            (const X *)logits, A, (X *)dlogits);
     });
   });
 }

@@ -131,6 +131,8 @@ __device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part
 // emit(q, a, b, p, on, i, by): thread i of `by` writes its share of answer q's results.
 template <class Emit>
 __device__ __forceinline__ void for_answers(const Answers &A, Emit emit) {
+  pdl_wait();
+  pdl_trigger();
   __shared__ Part red[kWarps], parts[kMaxCluster];
   const int tid = threadIdx.x;
   long long a, b;
@@ -240,19 +242,8 @@ static int launch_answers(void (*kernel)(Answers, KArgs...), Answers A, cudaStre
   while (A.cluster < kMaxCluster && A.per == 0 && mean > 1024 * A.cluster &&
          2 * A.cluster * A.Q <= at_once)
     A.cluster *= 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(A.per ? (A.Q + A.per - 1) / A.per : A.Q * A.cluster));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = A.cluster;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = A.cluster > 1;
-  cudaLaunchKernelEx(&cfg, kernel, A, static_cast<KArgs>(args)...);
-  count_launch();
-  return last_launch_status();
+  return launch_cluster(kernel, A.per ? (A.Q + A.per - 1) / A.per : A.Q * A.cluster, kThreads,
+                        A.cluster, 0, s, A, args...);
 }
 
 extern "C" int boute_answer_scores(const float *logprob, const float *entropy,
