@@ -4,10 +4,13 @@
 // With z = scale x, m = max z, s = sum exp(z - m) and u = sum (z - m) exp(z - m):
 //   lse = m + ln s,  logprob = z_t - m - ln s,  entropy = ln s - u / s.
 // One pass over a row: each warp keeps a running maximum and s and u relative to
-// it, and every lane leaves the maximum of each 64 bytes of logits it saw. The k-th
-// largest of the lanes' own maxima is reached by k logits at least, and by few others;
-// only the 64 bytes whose maximum reaches it are read again, and what reaches it there
-// is ranked. A row is a block's, or a cluster's when there are few rows.
+// it, and every lane notes the two of the 64-byte parts of the row it saw whose maxima
+// are largest. The k-th largest of the lanes' own maxima is reached by k logits at least,
+// and by few others; the noted parts that reach it are read again, and what reaches it
+// there is ranked. (A lane with a third such part reads all of its parts again.) A row is
+// a block's, or a cluster's when there are few rows. Shared memory is left to the L1
+// cache, through which the loads in flight pass: with 16 KB a block for the parts
+// themselves, reads were 10 % slower.
 #include <float.h>
 #include <math.h>
 
@@ -60,30 +63,35 @@ struct Piece {
   static constexpr int E = 16 / sizeof(T), N = 4 * E, SPAN = 32 * N;
   uint4 v[4];
   // of a lane's j-th logit, within the piece
-  static __device__ __forceinline__ int index(int j) {
-    return (j / E * 32 + (threadIdx.x & 31)) * E + j % E;
+  static __device__ __forceinline__ int index(int j, int lane = threadIdx.x & 31) {
+    return (j / E * 32 + lane) * E + j % E;
   }
   static __host__ __device__ int count(int off, int V) { return (off + V + SPAN - 1) / SPAN; }
 };
 
-// A whole piece; at: its first logit.
+// A whole piece, read once (its lines need not stay in L1); at: its first logit.
 template <class T>
 __device__ __forceinline__ Piece<T> load_whole(const T *at) {
   Piece<T> r;
   const uint4 *p = (const uint4 *)at + (threadIdx.x & 31);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r.v[i] = p[32 * i];
+  for (int i = 0; i < 4; ++i)
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w)
+                 : "l"(p + 32 * i)
+                 : "memory");
   return r;
 }
 // The piece of a row y of V logits from its logit `first` on, `shift` bytes after a 16-byte
-// boundary: -inf outside the row, of which nothing is read.
+// boundary: -inf outside the row, of which nothing is read. (lane: whose part)
 template <class T>
-__device__ __forceinline__ Piece<T> load_piece(const T *y, int V, int first, int shift) {
+__device__ __forceinline__ Piece<T> load_piece(const T *y, int V, int first, int shift,
+                                               int lane = threadIdx.x & 31) {
   constexpr int E = Piece<T>::E;
   Piece<T> r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int j0 = first + Piece<T>::index(i * E);
+    const int j0 = first + Piece<T>::index(i * E, lane);
     if (shift == 0 && j0 >= 0 && j0 + E <= V) {
       r.v[i] = *(const uint4 *)(y + j0);
     } else if (j0 >= E && j0 + 2 * E <= V) {  // two vectors, of which these 16 bytes
@@ -244,24 +252,28 @@ __device__ __forceinline__ float from_order_bits(unsigned o) {
 }
 
 // An upper half of order bits that k of n floats reach (n a multiple of 32, at most kTops), close
-// to the largest such one: built bit by bit until exactly k reach it; by one warp. That of -inf
-// where fewer than k are above it.
+// to the largest such one: built two bits at a time until exactly k reach it; by one warp. That
+// of -inf where fewer than k are above it.
 __device__ __forceinline__ unsigned kth_bound(const float *v, int n, int k) {
   const int lane = threadIdx.x & 31;
   unsigned o[kTops / 32], t = 0u;
 #pragma unroll
   for (int i = 0; i < kTops / 32; ++i) o[i] = 32 * i < n ? order_bits(v[32 * i + lane]) >> 16 : 0u;
-  for (unsigned bit = 1u << 15; bit; bit >>= 1) {
-    int c = 0;
+  for (int b = 14; b >= 0; b -= 2) {
+    unsigned c = 0u;  // the counts at or above three trials, ten bits each
 #pragma unroll
-    for (int i = 0; i < kTops / 32; ++i) c += o[i] >= (t | bit);
+    for (int i = 0; i < kTops / 32; ++i) {
+      c += o[i] >= (t | 1u << b) ? 1u : 0u;
+      c += o[i] >= (t | 2u << b) ? 1u << 10 : 0u;
+      c += o[i] >= (t | 3u << b) ? 1u << 20 : 0u;
+    }
     c = __reduce_add_sync(kAll, c);
-    if (c >= k) t |= bit;
-    if (c == k) break;
+    const int c1 = c & 1023u, c2 = c >> 10 & 1023u, c3 = c >> 20;
+    t |= (c3 >= k ? 3u : c2 >= k ? 2u : c1 >= k ? 1u : 0u) << b;
+    if (c3 == k || c2 == k || c1 == k) break;
   }
   return max(t, order_bits(-INFINITY) >> 16);
 }
-
 // A warp's best 32 keys, fed with those above a bound that rises with the k-th of them.
 struct WarpBest {
   WarpTopBatch batch;
@@ -285,10 +297,6 @@ __global__ void __launch_bounds__(kThreads, 4)
                           float scale, int k, int CS, float *logprob, float *entropy, float *lse,
                           long long *top_idx, float *top_logprob) {
   constexpr int N = Piece<T>::N, SPAN = Piece<T>::SPAN;
-  // a bound this much lower lets no logit slip that the scale rounds onto the bound (16-bit
-  // logits are too far apart for that)
-  constexpr unsigned kSlack = sizeof(T) == 4 ? 1 : 0;
-  extern __shared__ unsigned short most[];  // upper order bits of each piece's lanes' maxima
   __shared__ unsigned long long list[kList];  // (the leader's) candidates' keys
   __shared__ float tops[kTops], lanes[kThreads];
   __shared__ Sums wsum[kThreads / 32];
@@ -313,17 +321,23 @@ __global__ void __launch_bounds__(kThreads, 4)
 
   const int Q = Piece<T>::count(off, V), step = CS * W, first = rank * W + warp;
   const int whole0 = off ? 1 : 0, whole1 = (off + V) / SPAN;  // pieces within the row
-  float m = -INFINITY, top = -INFINITY;
+  float m = -INFINITY;
   unsigned long long s2 = 0ull, u2 = 0ull;  // pairs of partial sums
   bool clamp = false;
-  for (int q = first, i = tid; q < Q; q += step, i += NT) {
+  // the three largest maxima of this lane's parts, and the pieces of the first two
+  float top = -INFINITY, second = -INFINITY, third = -INFINITY;
+  int q1 = -1, q2 = -1;
+  for (int q = first; q < Q; q += step) {
     const bool whole = q >= whole0 && q < whole1;
     const Piece<T> p = whole ? load_whole(x + ((long long)q * SPAN - off))
                              : load_piece(x, V, q * SPAN - off, 0);
     const float l = lane_max(p);
     if (k > 0) {
-      most[i] = (unsigned short)(order_bits(l) >> 16);
-      top = max_nan(top, l);
+      q2 = l > top ? q1 : l > second ? q : q2;
+      q1 = l > top ? q : q1;
+      third = fmaxf(third, fminf(second, l));
+      second = fmaxf(second, fminf(top, l));
+      top = fmaxf(top, l);
     }
     const float g = warp_max_nan(l);
     if (!(g <= m)) {  // (NaN too: it stays in m)
@@ -384,33 +398,50 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
   float zt = -INFINITY;
   if (k > 0) {
+    // a bound that k lanes reach
     if (warp == 0) bound = kth_bound(tops, CS > 1 ? kTops : NT, k);
     __syncthreads();
-    const unsigned reach = bound > kSlack ? bound - kSlack : 0u;
     if (bound > order_bits(-INFINITY) >> 16) zt = __fmul_rn(from_order_bits(bound << 16), scale);
-    for (int q0 = first, i0 = tid; q0 < Q; q0 += 32 * step, i0 += 32 * NT) {
-      unsigned hit = 0u;  // this lane's parts of pieces that reach the bound
-      for (int b = 0, q = q0, i = i0; b < 32 && q < Q; ++b, q += step, i += NT)
-        hit |= (unsigned)(most[i] >= reach) << b;
+    bool full = false;
+    // a part's logits that reach the bound, into the list
+    auto take_from = [&](const Piece<T> &p, int q, int of) {
+      unsigned hit = 0u;
+#pragma unroll
+      for (int j = 0; j < N; j += 2) {
+        float a, b;
+        pair(p, j / 2, a, b);
+        hit |= (__fmul_rn(a, scale) >= zt ? 1u : 0u) << j;
+        hit |= (__fmul_rn(b, scale) >= zt ? 1u : 0u) << (j + 1);
+      }
       while (hit) {
-        const int at0 = (q0 + (__ffs(hit) - 1) * step) * SPAN - off;
+        const int j = __ffs(hit) - 1;
         hit &= hit - 1;
-        const Piece<T> p = load_piece(x, V, at0, 0);
-#pragma unroll
-        for (int j = 0; j < N; j += 2) {
-          float z[2];
-          pair(p, j / 2, z[0], z[1]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            z[e] = __fmul_rn(z[e], scale);
-            if (!(z[e] >= zt && z[e] > -INFINITY)) continue;
-            const int at = add_peer(peer(&nlist, 0), 1);
-            if (at < kList)
-              store_peer(peer(list, 0) + 8u * at,
-                         make_key(z[e], (unsigned)(at0 + Piece<T>::index(j + e))));
-            else hit = 0u, q0 = Q;
-          }
-        }
+        const int index = q * SPAN - off + Piece<T>::index(j, of);
+        if (index < 0 || index >= V) continue;  // (-inf beyond the row, with a bound of -inf)
+        const float z = __fmul_rn(to_float(x[index]), scale);
+        if (z == -INFINITY) continue;
+        const int to = add_peer(peer(&nlist, 0), 1);
+        if (to < kList) store_peer(peer(list, 0) + 8u * to, make_key(z, (unsigned)index));
+        else full = true, hit = 0u;
+      }
+    };
+    auto reaches = [&](float v) { return v > -INFINITY && __fmul_rn(v, scale) >= zt; };
+    const bool r1 = reaches(top), r2 = reaches(second);
+    Piece<T> p1, p2;
+    if (r1) p1 = load_piece(x, V, q1 * SPAN - off, 0);
+    if (r2) p2 = load_piece(x, V, q2 * SPAN - off, 0);
+    if (r1) take_from(p1, q1, lane);
+    if (r2) take_from(p2, q2, lane);
+    // a lane with a third: its other parts, a piece to each lane
+    unsigned more = __ballot_sync(kAll, reaches(third));
+    while (more) {
+      const int of = __ffs(more) - 1;
+      more &= more - 1;
+      const int skip1 = __shfl_sync(kAll, q1, of), skip2 = __shfl_sync(kAll, q2, of);
+      for (int q = first + lane * step; q < Q && !full; q += 32 * step) {
+        if (q == skip1 || q == skip2) continue;
+        const Piece<T> p = load_piece(x, V, q * SPAN - off, 0, of);
+        if (reaches(lane_max(p))) take_from(p, q, of);
       }
     }
     if (CS > 1) cluster_sync();
@@ -594,7 +625,7 @@ using namespace boute;
 // cluster while the rows alone leave the SMs without work and every warp gets a piece; with rows
 // so few that all their warps run at once, twice the warps.
 struct Spread {
-  int W, CS, per_warp;
+  int W, CS;
   template <class P>
   Spread(long long T, int V, P) {
     const int Q = P::count(P::E - 1, V), sms = num_sms();
@@ -602,7 +633,6 @@ struct Spread {
     CS = 1;
     while (CS < kMaxCluster && 2 * CS * T <= 8 * sms && 2 * CS * W <= Q) CS *= 2;
     if (CS == kMaxCluster && 2 * W * CS * T <= 32 * sms && CS * W < Q) W *= 2;
-    per_warp = (Q + CS * W - 1) / (CS * W);
   }
 };
 
@@ -628,12 +658,7 @@ extern "C" int boute_token_logprobs(const void *logits, int dtype, long long T, 
   return with_dtype(dtype, [&](auto tag) {
     using E = decltype(tag);
     const Spread sp(T, V, Piece<E>{});
-    const size_t smem = k > 0 ? (size_t)sp.W * 32 * sp.per_warp * 2 : 0;
-    if (smem > (40u << 10) &&
-        cudaFuncSetAttribute((const void *)token_logprobs_kernel<E>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-      return last_launch_status();
-    return launch_cluster(token_logprobs_kernel<E>, T * sp.CS, 32 * sp.W, sp.CS, smem,
+    return launch_cluster(token_logprobs_kernel<E>, T * sp.CS, 32 * sp.W, sp.CS, 0,
                           (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, k, sp.CS, logprob,
                        entropy, lse, top_idx, top_logprob);
   });
