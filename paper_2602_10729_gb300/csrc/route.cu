@@ -1,13 +1,17 @@
 // Routing of queries to experts: scores, the choice within the best groups,
 // the weights and the load; and the gradient of the weights.
 //
-// A warp per query, lane l with the S experts l S .. l S + S - 1 (S a power of two,
-// 32 S >= E), so that the lowest lane has the lowest indices. Each lane sorts the best
-// of its values; k rounds then take the largest head of the 32 lists (one reduction
-// each). Without a bias the logits themselves are compared, which have the order of the
-// scores: only the chosen scores are computed then, and a softmax's sum only where the
-// weights are not renormalised. 16-bit logits are compared as keys of their order bits
-// with the expert's index below.
+// A team of L lanes per query (8 up to 256 experts, so four queries to a warp), lane l
+// with the S experts l S .. l S + S - 1. Experts are compared as 32-bit keys: the upper
+// bits of the order bits of c, and the expert's complement below, so that equal values
+// go to the lowest index. Each lane sorts its K largest keys in registers; the lanes' lists
+// join two by two, of which log2 L steps leave the query's K best in every lane. 16-bit
+// logits that are compared as they are (no bias) fit a key whole. Of other values a key
+// holds 22 to 24 bits: K > k candidates are ranked by their exact values, and a query
+// whose last candidate shares the k-th's upper bits (one in a thousand or fewer) is
+// chosen again by exact values alone. Without a bias the logits themselves are compared,
+// which have the order of the scores: only the chosen scores are computed then, and a
+// softmax's sum only where the weights are not renormalised.
 #include <math.h>
 
 #include <algorithm>
@@ -37,18 +41,542 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// The warp's maximum in one instruction (a NaN wins; keys: unsigned).
-__device__ __forceinline__ float warp_max(float v) {
+__device__ __forceinline__ float warp_max(float v) {  // (a NaN wins)
   float r;
   asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-__device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_sync(kAll, v); }
-
 __device__ __forceinline__ float logistic(float x) {  // (0 where exp(-x) overflows)
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_fast(-x * kLog2e)));
   return r;
+}
+// Over teams of lanes (a power of two).
+template <int L>
+__device__ __forceinline__ float team_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+__device__ __forceinline__ float team_sum(float v, int team) {
+  for (int o = team / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+
+// ---- choosing --------------------------------------------------------------------------
+struct RouteArgs {
+  const void *logits;
+  long long rows, ld;
+  const float *bias;
+  int dtype, E, mode, G, keep, group_top, k, renorm;
+  int by_logits;  // the logits are compared
+  int whole;      // and fit a key whole (16-bit logits, no groups)
+  int vec;        // rows on 16-byte boundaries, E a multiple of a vector's logits
+  int index_bits; // of a key that holds a part of a value
+  float factor;
+  int *idx, *load;
+  float *weight;
+};
+
+__device__ __forceinline__ float logit_at(const RouteArgs &A, long long row, int e) {
+  const long long i = row * A.ld + e;
+  if (A.dtype == BOUTE_F32) return ((const float *)A.logits)[i];
+  if (A.dtype == BOUTE_F16) return __half2float(((const __half *)A.logits)[i]);
+  return __bfloat162float(((const __nv_bfloat16 *)A.logits)[i]);
+}
+// The words of the N 16-byte-aligned words of 4-byte (PER = 1) or pairs of 2-byte logits from e0
+// on; `none` beyond E.
+template <int N, int PER>
+__device__ __forceinline__ void load_words(uint32_t *w, const void *row, int e0, int E, bool vec,
+                                           uint32_t none) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      uint4 v = {none, none, none, none};
+      if (e0 + 4 * PER * i < E) v = *(const uint4 *)((const uint32_t *)row + e0 / PER + 4 * i);
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
+  } else if constexpr (PER == 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = e0 + i < E ? ((const uint32_t *)row)[e0 + i] : none;
+  } else {
+    const unsigned short *h = (const unsigned short *)row;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = e0 + 2 * i;
+      w[i] = (e < E ? (uint32_t)h[e] : none & 0xffffu) |
+             (e + 1 < E ? (uint32_t)h[e + 1] << 16 : none & 0xffff0000u);
+    }
+  }
+}
+// Pairs of 16-bit logits with -0 as +0 (and NaNs as one).
+__device__ __forceinline__ uint32_t plus_zero(uint32_t w, int dtype) {
+  uint32_t r;
+  if (dtype == BOUTE_F16) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
+  else asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
+  return r;
+}
+__device__ __forceinline__ unsigned order_bits(float v) {
+  const unsigned u = __float_as_uint(v);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+
+// L values in descending order (Batcher's odd-even merge sort).
+template <int L, class V>
+__device__ __forceinline__ void sort_desc(V *v) {
+#pragma unroll
+  for (int p = 1; p < L; p *= 2)
+#pragma unroll
+    for (int q = p; q > 0; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < L; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < L && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+            const V a = v[i + j], b = v[i + j + q];
+            v[i + j] = max(a, b);
+            v[i + j + q] = min(a, b);
+          }
+}
+// v: a bitonic run of L, into descending order.
+template <int L, class V>
+__device__ __forceinline__ void merge_desc(V *v) {
+#pragma unroll
+  for (int q = L / 2; q > 0; q /= 2)
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (!(i & q)) {
+        const V a = v[i], b = v[i + q];
+        v[i] = max(a, b);
+        v[i + q] = min(a, b);
+      }
+}
+// The K largest of a lane's S values in descending order, in c[0 .. K): runs of K are sorted, then
+// joined two by two (the larger of each and the other's reverse form a bitonic run).
+template <int S, int K, class V>
+__device__ __forceinline__ void best_in_lane(V (&c)[S]) {
+#pragma unroll
+  for (int s = 0; s < S; s += K) sort_desc<K>(c + s);
+#pragma unroll
+  for (int o = K; o < S; o *= 2)
+#pragma unroll
+    for (int s = 0; s < S; s += 2 * o) {
+#pragma unroll
+      for (int i = 0; i < K; ++i) c[s + i] = max(c[s + i], c[s + o + K - 1 - i]);
+      merge_desc<K>(c + s);
+    }
+}
+// The K <= S largest of the team's keys (S in each of its L lanes), in every lane: the lanes' lists
+// joined in the same way.
+template <int S, int L, int K>
+__device__ __forceinline__ void best_of(unsigned (&c)[S], unsigned (&best)[K]) {
+  best_in_lane<S, K>(c);
+#pragma unroll
+  for (int i = 0; i < K; ++i) best[i] = c[i];
+#pragma unroll
+  for (int o = 1; o < L; o *= 2) {
+    unsigned other[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) other[i] = __shfl_xor_sync(kAll, best[K - 1 - i], o);
+#pragma unroll
+    for (int i = 0; i < K; ++i) best[i] = max(best[i], other[i]);
+    merge_desc<K>(best);
+  }
+}
+
+// The two largest of two pairs a >= b.
+__device__ __forceinline__ void join_two(float &a, float &b, float a2, float b2) {
+  b = fmaxf(fminf(a, a2), fmaxf(b, b2));
+  a = fmaxf(a, a2);
+}
+// Bits of the groups that stay, from a query's c in shared memory; lane l of the team's L. Several
+// lanes to a group where there are enough, else groups in turn.
+template <int L>
+__device__ __forceinline__ unsigned keep_groups(const float *c, float *scores, const RouteArgs &A,
+                                                int per, int l) {
+  int width = 1;
+  while (2 * width * A.G <= L) width *= 2;
+  for (int g0 = 0; g0 < A.G; g0 += L / width) {
+    const int g = g0 + l / width;
+    float a = -INFINITY, b = -INFINITY;
+    if (g < A.G)
+#pragma unroll 4
+      for (int i = l % width; i < per; i += width) join_two(a, b, c[g * per + i], -INFINITY);
+    for (int o = 1; o < width; o *= 2)
+      join_two(a, b, __shfl_xor_sync(kAll, a, o), __shfl_xor_sync(kAll, b, o));
+    if (g < A.G && l % width == 0) scores[g] = A.group_top == 2 && b > -INFINITY ? a + b : a;
+  }
+  __syncwarp();
+  unsigned kept = 0u;
+  for (int g = l; g < A.G; g += L) {
+    const float mine = scores[g];
+    int rank = 0;
+    for (int h = 0; h < A.G; ++h) rank += scores[h] > mine || (scores[h] == mine && h < g);
+    kept |= rank < A.keep && mine > -INFINITY ? 1u << g : 0u;
+  }
+#pragma unroll
+  for (int o = 1; o < L; o *= 2) kept |= __shfl_xor_sync(kAll, kept, o);
+  return kept;
+}
+// -inf for the lane's S experts from e0 on that are in no kept group.
+template <int S>
+__device__ __forceinline__ void drop_groups(float (&c)[S], unsigned kept, int e0, int per) {
+  int g = e0 / per, left = (g + 1) * per - e0;  // (neighbours: one division, then steps)
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    if (left-- == 0) {
+      ++g;
+      left = per - 1;
+    }
+    if (!(kept >> (g & 31) & 1u)) c[s] = -INFINITY;
+  }
+}
+
+// Floats of a query's c and groups' scores (teams' rows begin in different banks).
+__host__ __device__ inline int shared_stride(int E) {
+  return round_up(E + BOUTE_MAX_GROUPS, 32) + 2;
+}
+
+// What a query's choice among its experts is made of, for a team of L lanes.
+struct Query {
+  float m, inv_sum;  // of the softmax
+  bool bad;          // no distribution
+  // c of expert e with logit x: the same sums for every lane and in every place
+  __device__ __forceinline__ float value(const RouteArgs &A, float x, int e) const {
+    float v = x;
+    if (!A.by_logits) {
+      v = score(A, x);
+      if (A.bias) v = __fadd_rn(v, fmaxf(A.bias[e], -INFINITY));  // (no NaN)
+    }
+    return x > -INFINITY && !bad ? v : -INFINITY;
+  }
+  __device__ __forceinline__ float score(const RouteArgs &A, float x) const {
+    return A.mode == BOUTE_ROUTE_SOFTMAX ? exp2_fast((x - m) * kLog2e) * inv_sum : logistic(x);
+  }
+};
+// c of the lane's S experts from e0 on (-inf: not to be chosen).
+template <int S>
+__device__ __forceinline__ void load_bias(const RouteArgs &A, int e0, float (&bias)[S]) {
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+    bias[s] = A.bias && e0 + s < A.E ? fmaxf(A.bias[e0 + s], -INFINITY) : 0.f;  // (no NaN)
+}
+template <int S, int L>
+__device__ __forceinline__ Query load_query(const RouteArgs &A, long long row, int e0,
+                                            const float (&bias)[S], float (&c)[S]) {
+  const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
+  if (A.dtype == BOUTE_F32) {
+    uint32_t w[S];
+    load_words<S, 1>(w, (const float *)A.logits + row * A.ld, e0, A.E, A.vec, 0xff800000u);
+#pragma unroll
+    for (int s = 0; s < S; ++s) c[s] = __uint_as_float(w[s]);
+  } else {
+    uint32_t w[S / 2];
+    load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, A.E, A.vec,
+                         A.dtype == BOUTE_F16 ? 0xfc00fc00u : 0xff80ff80u);
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i)
+      if (A.dtype == BOUTE_F16) {
+        unpack_f16x2(w[i], c[2 * i], c[2 * i + 1]);
+      } else {
+        c[2 * i] = __uint_as_float(w[i] << 16);
+        c[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+  }
+  Query q = {-INFINITY, 1.f, false};
+#pragma unroll
+  for (int s = 0; s < S; ++s) q.m = max_nan(q.m, c[s]);
+  if constexpr (L == 32) {
+    q.m = warp_max(q.m);
+  } else {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) q.m = max_nan(q.m, __shfl_xor_sync(kAll, q.m, o));
+  }
+  q.bad = isnan(q.m) || (soft && q.m == INFINITY);
+  if (soft && (!A.by_logits || !A.renorm)) {
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) sum += exp2_fast((c[s] - q.m) * kLog2e);
+    q.inv_sum = __fdividef(1.f, team_sum<L>(sum));
+  }
+  if (A.by_logits) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) c[s] = q.bad ? -INFINITY : c[s];
+  } else {
+    // (the mode asked once, not for every expert)
+    if (soft)
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+        c[s] = c[s] > -INFINITY && !q.bad
+                   ? __fadd_rn(exp2_fast((c[s] - q.m) * kLog2e) * q.inv_sum, bias[s])
+                   : -INFINITY;
+    else
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+        c[s] = c[s] > -INFINITY && !q.bad ? __fadd_rn(logistic(c[s]), bias[s]) : -INFINITY;
+  }
+  return q;
+}
+// Writes the chosen of a query: this lane's N candidates e (-1: none) of logits x in their places.
+template <int N, int L>
+__device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q, long long row,
+                                             bool live, const int (&e)[N], const int (&place)[N],
+                                             const float (&x)[N], int *hist) {
+  float w[N], sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    w[j] = e[j] >= 0 && place[j] < A.k ? q.score(A, x[j]) : 0.f;
+    sum += w[j];
+  }
+  float f = A.factor;
+  if (A.renorm) {
+    sum = team_sum<L>(sum);
+    f = sum > 0.f ? __fdividef(f, sum) : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if (!live || place[j] >= A.k) continue;
+    A.idx[row * A.k + place[j]] = e[j];
+    A.weight[row * A.k + place[j]] = q.bad ? NAN : f * w[j];
+    if (A.load && e[j] >= 0 && BOUTE_INB(e[j], A.E)) atomicAdd(hist + e[j], 1);
+  }
+}
+// The block's load: cleared, and added to the whole one. (Behind clear_load_kernel, which has
+// waited for what came before, only the second waits.)
+__device__ __forceinline__ void begin_load(const RouteArgs &A, int *hist) {
+  if (!A.load || gridDim.x == 1) pdl_wait();
+  pdl_trigger();
+  if (!A.load) return;
+  for (int e = threadIdx.x; e < A.E; e += kThreads) hist[e] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ void end_load(const RouteArgs &A, const int *hist) {
+  if (!A.load) return;
+  __syncthreads();
+  pdl_wait();
+  for (int e = threadIdx.x; e < A.E; e += kThreads)
+    if (gridDim.x == 1) A.load[e] = hist[e];
+    else if (hist[e]) atomicAdd(A.load + e, hist[e]);
+}
+
+// WHOLE: keys hold the values whole (16-bit logits compared as they are, no groups).
+template <int S, int L, int K, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
+    route_team_kernel(RouteArgs A) {
+  constexpr int kTeams = 32 / L, kOwn = (K + L - 1) / L;  // queries of a warp; a lane's candidates
+  extern __shared__ int hist[];  // the block's load; then, with groups, c and the groups' scores
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, l = lane % L, e0 = l * S;
+  const int per = E / A.G;
+  const bool groups = A.keep < A.G;
+  float *shared_c = (float *)(hist + E) + (warp * kTeams + lane / L) * shared_stride(E);
+  begin_load(A, hist);
+  const long long step = (long long)gridDim.x * kWarps * kTeams;
+  for (long long row0 = ((long long)blockIdx.x * kWarps + warp) * kTeams; row0 < A.rows;
+       row0 += step) {
+    // (a team beyond the last query repeats the last, and writes nothing)
+    const bool live = row0 + lane / L < A.rows;
+    const long long row = min(row0 + lane / L, A.rows - 1);
+    unsigned best[K], c[S];
+    int e[kOwn], place[kOwn];  // candidates l, l + L .., and their ranks
+    float x[kOwn];             // their logits
+    Query q = {-INFINITY, 1.f, false};
+    if constexpr (WHOLE) {
+      // order bits of pairs of logits, each over its expert's complement; a NaN is largest, +inf
+      // next, -inf (and what is beyond E) smallest
+      const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX, half = A.dtype == BOUTE_F16;
+      const unsigned inf = half ? 0xfc00u : 0xff80u;
+      uint32_t w[S / 2];
+      load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, E, A.vec,
+                           half ? 0xfc00fc00u : 0xff80ff80u);
+      const unsigned below = (0xffffu - e0) | (0xffffu - e0 - 1u) << 16;
+#pragma unroll
+      for (int i = 0; i < S / 2; ++i) {
+        const uint32_t v = plus_zero(w[i], A.dtype);
+        const uint32_t o = v ^ (((v >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
+        c[2 * i] = __byte_perm(o, below - 0x00020002u * i, 0x1054);
+        c[2 * i + 1] = __byte_perm(o, below - 0x00020002u * i, 0x3276);
+      }
+      best_of<S, L, K>(c, best);
+      auto value = [&](unsigned key) {
+        const unsigned o = key >> 16, u = o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu;
+        return half ? __half2float(__ushort_as_half((unsigned short)u)) : __uint_as_float(u << 16);
+      };
+      q.bad = best[0] >> 16 > inf || (soft && best[0] >> 16 == inf);
+      q.m = value(best[0]);
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) {
+        unsigned mine = 0u;
+#pragma unroll
+        for (int i = j * L; i < K && i < (j + 1) * L; ++i) mine = l == i - j * L ? best[i] : mine;
+        place[j] = l + j * L;
+        e[j] = !q.bad && mine >> 16 > (0xffffu ^ inf) ? (int)(0xffffu - (mine & 0xffffu)) : -1;
+        x[j] = value(mine);
+      }
+      if (soft && !A.renorm) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < S / 2; ++i) {
+          float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
+          if (half) unpack_f16x2(w[i], a, b);
+          sum += exp2_fast((a - q.m) * kLog2e) + exp2_fast((b - q.m) * kLog2e);
+        }
+        q.inv_sum = __fdividef(1.f, team_sum<L>(sum));
+      }
+    } else {
+      unsigned kept = kAll;
+      {
+        float v[S], b[S];
+        load_bias(A, e0, b);
+        q = load_query<S, L>(A, row, e0, b, v);
+        if (groups) {
+#pragma unroll
+          for (int s = 0; s < S; ++s)
+            if (e0 + s < E) shared_c[e0 + s] = v[s];
+          __syncwarp();
+          kept = keep_groups<L>(shared_c, shared_c + E, A, per, l);
+          __syncwarp();
+          drop_groups(v, kept, e0, per);
+        }
+        const unsigned low = (1u << A.index_bits) - 1u;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          const float u = v[s] == 0.f ? 0.f : v[s];
+          c[s] = u > -INFINITY ? (order_bits(u) & ~low) | (low - (unsigned)(e0 + s)) : 0u;
+        }
+      }
+      const unsigned low = (1u << A.index_bits) - 1u;
+      best_of<S, L, K>(c, best);
+      // the candidates' exact values, and their ranks (the list has equal ones in order)
+      float v[kOwn];
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) {
+        unsigned mine = 0u;
+#pragma unroll
+        for (int i = j * L; i < K && i < (j + 1) * L; ++i) mine = l == i - j * L ? best[i] : mine;
+        e[j] = mine ? (int)(low - (mine & low)) : -1;
+        x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
+        v[j] = e[j] >= 0 ? q.value(A, x[j], e[j]) : -INFINITY;
+        place[j] = 0;
+      }
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const float o = __shfl_sync(kAll, v[i / L], i % L, L);
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) place[j] += o > v[j] || (o == v[j] && i < l + j * L);
+      }
+      // a candidate may be missing where the last shares the k-th's bits: then by exact values
+      bool doubt = false;
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j)
+        doubt |= place[j] == A.k - 1 && e[j] >= 0 && best[K - 1] != 0u &&
+                 ((order_bits(v[j] == 0.f ? 0.f : v[j]) ^ best[K - 1]) & ~low) == 0u;
+      doubt = __ballot_sync(kAll, doubt) >> (lane - l) & (kAll >> (32 - L));
+      if (__any_sync(kAll, doubt)) {
+        unsigned long long last = ~0ull;
+        for (int r = 0; r < A.k; ++r) {
+          unsigned long long top = 0ull;
+          for (int s = 0; s < S; ++s) {
+            const int at = e0 + s;
+            if (at >= E || (groups && !(kept >> (at / per) & 1u))) continue;
+            const float u = q.value(A, logit_at(A, row, at), at);
+            const unsigned long long t = make_key(u, (unsigned)at);
+            if (u > -INFINITY && t < last && t > top) top = t;
+          }
+#pragma unroll
+          for (int o = L / 2; o > 0; o >>= 1) {
+            const unsigned long long t = shfl_xor64(top, o);
+            top = t > top ? t : top;
+          }
+          last = top;  // (0: nothing is left)
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j)
+            if (doubt && r == l + j * L) {
+              e[j] = top ? (int)key_index(top) : -1;
+              x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j)
+          if (doubt) place[j] = l + j * L;
+      }
+    }
+    write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist);
+  }
+  end_load(A, hist);
+}
+
+// ---- a warp to a query -------------------------------------------------------------------
+// The k largest of the lanes' values, lane r with the r-th: its value and its expert (-1: none).
+// Each lane sorts its K >= min(k, S) best; k rounds take the largest head of the 32 lists. Equal values go to
+// the lowest expert: of several lanes the lowest, of one lane's the occurrences in order.
+template <int S, int K>
+__device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, int &expert) {
+  const int lane = threadIdx.x & 31;
+  float v[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) v[s] = c[s];
+  best_in_lane<S, K>(v);
+  mine = -INFINITY;
+  int owner = 0;
+#pragma unroll (K <= 4 ? K : 1)
+  for (int r = 0; r < (K <= 4 ? K : k); ++r) {  // (picks beyond k are not used)
+    const float best = warp_max(v[0]);
+    const int from = __ffs(__ballot_sync(kAll, v[0] == best)) - 1;
+    owner = lane == r ? from : owner;
+    mine = lane == r ? best : mine;
+    const bool own = lane == from;
+#pragma unroll
+    for (int i = 0; i + 1 < K; ++i) v[i] = own ? v[i + 1] : v[i];
+    v[K - 1] = own ? -INFINITY : v[K - 1];
+  }
+  const float before = __shfl_up_sync(kAll, mine, 1);
+  const int by = __shfl_up_sync(kAll, owner, 1);
+  const bool again = lane > 0 && mine == before && owner == by && mine > -INFINITY;
+  const unsigned repeats = __ballot_sync(kAll, again);
+  int nth = 0;  // which of its lane's equal values this one is
+  if (repeats)
+    for (int r = lane; repeats >> r & 1u; --r) ++nth;
+  expert = -1;
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+    if (__shfl_sync(kAll, c[s], owner) == mine && nth-- == 0) expert = owner * S + s;
+  if (mine == -INFINITY) expert = -1;
+}
+
+template <int S, int K>
+__global__ void __launch_bounds__(kThreads, S > 8 ? 1 : 5) route_warp_kernel(RouteArgs A) {
+  extern __shared__ int hist[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e0 = lane * S, per = A.E / A.G;
+  float *shared_c = (float *)(hist + A.E) + warp * shared_stride(A.E);
+  begin_load(A, hist);
+  float bias[S];
+  load_bias(A, e0, bias);
+  for (long long row = (long long)blockIdx.x * kWarps + warp; row < A.rows;
+       row += (long long)gridDim.x * kWarps) {
+    float c[S], mine;
+    const Query q = load_query<S, 32>(A, row, e0, bias, c);
+    if (A.keep < A.G) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+        if (e0 + s < A.E) shared_c[e0 + s] = c[s];
+      __syncwarp();
+      const unsigned kept = keep_groups<32>(shared_c, shared_c + A.E, A, per, lane);
+      __syncwarp();
+      drop_groups(c, kept, e0, per);
+    }
+    int e[1], place[1] = {lane};
+    choose<S, K>(c, A.k, mine, e[0]);
+    if (lane >= A.k) e[0] = -1;
+    const float x[1] = {e[0] < 0 ? -INFINITY : A.by_logits ? mine : logit_at(A, row, e[0])};
+    write_chosen<1, 32>(A, q, row, true, e, place, x, hist);
+  }
+  end_load(A, hist);
+}
+
+__global__ void clear_load_kernel(int *load, int E) {
+  pdl_wait();
+  pdl_trigger();
+  for (int e = threadIdx.x; e < E; e += blockDim.x) load[e] = 0;
 }
 
 // ---- a query's logits -----------------------------------------------------------------
@@ -98,342 +626,6 @@ struct Raw {
     return v;
   }
 };
-
-// ---- choosing --------------------------------------------------------------------------
-__device__ __forceinline__ float key_none(float) { return -INFINITY; }
-__device__ __forceinline__ unsigned key_none(unsigned) { return 0u; }
-
-// Two values, and four or more by Batcher's odd-even merge sort, in descending order.
-template <int L, class K>
-__device__ __forceinline__ void sort_desc(K *v) {
-#pragma unroll
-  for (int p = 1; p < L; p *= 2)
-#pragma unroll
-    for (int q = p; q > 0; q /= 2)
-#pragma unroll
-      for (int j = q % p; j + q < L; j += 2 * q)
-#pragma unroll
-        for (int i = 0; i < q; ++i)
-          if (i + j + q < L && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
-            const K a = v[i + j], b = v[i + j + q];
-            v[i + j] = max(a, b);
-            v[i + j + q] = min(a, b);
-          }
-}
-// The L largest of c's S in descending order: runs of L are sorted, then joined two by two (the
-// larger of each and the other's reverse form a bitonic run).
-template <int S, int L, class K>
-__device__ __forceinline__ void best_of(const K (&c)[S], K (&best)[L]) {
-  K v[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) v[s] = c[s];
-#pragma unroll
-  for (int s = 0; s < S; s += L) sort_desc<L>(v + s);
-#pragma unroll
-  for (int o = L; o < S; o *= 2)
-#pragma unroll
-    for (int s = 0; s < S; s += 2 * o) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) v[s + i] = max(v[s + i], v[s + o + L - 1 - i]);
-#pragma unroll
-      for (int q = L / 2; q > 0; q /= 2)
-#pragma unroll
-        for (int i = 0; i < L; ++i)
-          if (!(i & q)) {
-            const K a = v[s + i], b = v[s + i + q];
-            v[s + i] = max(a, b);
-            v[s + i + q] = min(a, b);
-          }
-    }
-#pragma unroll
-  for (int i = 0; i < L; ++i) best[i] = v[i];
-}
-
-// The k largest of the lanes' values, lane r with the r-th: its value and its expert (-1: none).
-// v: each lane's L largest in descending order, L >= min(k, S). Keys (unsigned) are unique and
-// carry the expert; equal floats go to the lowest expert: of several lanes the lowest, of one
-// lane's the occurrences in order.
-template <int S, int L, class K>
-__device__ __forceinline__ void choose(const K (&c)[S], K (&v)[L], int k, K &mine, int &expert) {
-  constexpr bool kKeys = std::is_same<K, unsigned>::value;
-  const int lane = threadIdx.x & 31;
-  mine = key_none(K{});
-  int owner = 0;
-#pragma unroll (L <= 4 ? L : 1)
-  for (int r = 0; r < (L <= 4 && L < S ? L : k); ++r) {  // (picks beyond k are not used)
-    const K best = warp_max(v[0]);
-    bool own = v[0] == best;
-    if constexpr (!kKeys) {
-      const int from = __ffs(__ballot_sync(kAll, own)) - 1;
-      owner = lane == r ? from : owner;
-      own = lane == from;
-    }
-    mine = lane == r ? best : mine;
-#pragma unroll
-    for (int i = 0; i + 1 < L; ++i) v[i] = own ? v[i + 1] : v[i];
-    v[L - 1] = own ? key_none(K{}) : v[L - 1];
-  }
-  if constexpr (kKeys) {
-    expert = mine ? (int)(0xffffu - (mine & 0xffffu)) : -1;
-  } else {
-    const float before = __shfl_up_sync(kAll, mine, 1);
-    const int by = __shfl_up_sync(kAll, owner, 1);
-    const bool again = lane > 0 && mine == before && owner == by && mine > -INFINITY;
-    const unsigned repeats = __ballot_sync(kAll, again);
-    int nth = 0;  // which of its lane's equal values this one is
-    if (repeats)
-      for (int r = lane; repeats >> r & 1u; --r) ++nth;
-    expert = -1;
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (__shfl_sync(kAll, c[s], owner) == mine && nth-- == 0) expert = owner * S + s;
-    if (mine == -INFINITY) expert = -1;
-  }
-}
-
-// The two largest of two pairs a >= b.
-__device__ __forceinline__ void join_two(float &a, float &b, float a2, float b2) {
-  b = fmaxf(fminf(a, a2), fmaxf(b, b2));
-  a = fmaxf(a, a2);
-}
-
-// ---- groups ----------------------------------------------------------------------------
-// Whether the lane's groups stay: a bit for each lane number g * width of a kept group g, 2^q =
-// width lanes to a group. a, b: the two largest c of this lane's share of its group.
-__device__ __forceinline__ unsigned keep_groups(float a, float b, int width, int keep,
-                                                int group_top) {
-  for (int o = 1; o < width; o *= 2)
-    join_two(a, b, __shfl_xor_sync(kAll, a, o), __shfl_xor_sync(kAll, b, o));
-  float score = group_top == 2 && b > -INFINITY ? a + b : a;
-  const int lane = threadIdx.x & 31;
-  unsigned kept = 0u;
-  for (int r = 0; r < keep; ++r) {
-    const float best = warp_max(score);
-    if (best == -INFINITY) break;
-    const int at = __ffs(__ballot_sync(kAll, score == best)) - 1;  // its group's first lane
-    kept |= 1u << at;
-    if ((lane ^ at) < width) score = -INFINITY;
-  }
-  return kept;
-}
-
-// Over teams of lanes (a power of two).
-__device__ __forceinline__ float team_sum(float v, int team) {
-  for (int o = team / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
-}
-
-// Pairs of 16-bit logits with -0 as +0 (and NaNs as one).
-__device__ __forceinline__ uint32_t plus_zero(uint32_t w, __half) {
-  uint32_t r;
-  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
-  return r;
-}
-__device__ __forceinline__ uint32_t plus_zero(uint32_t w, __nv_bfloat16) {
-  uint32_t r;
-  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
-  return r;
-}
-
-struct RouteArgs {
-  long long rows, ld;
-  const float *bias;
-  int E, mode, G, keep, group_top, k, renorm, by_logits, vec;
-  int team;   // lanes that hold the choices, a power of two
-  int width;  // lanes to a group when its score is formed
-  int whole;  // a lane's experts are of one group
-  float factor;
-  int *idx, *load;
-  float *weight;
-};
-
-// K: unsigned for 16-bit logits compared as they are, float else (by_logits: the logits, else the
-// scores with their bias). L: the lanes' lists.
-template <int S, class K>
-constexpr int kBlocks = S > 8 ? 1 : std::is_same<K, unsigned>::value ? 6 : 5;  // an SM's, at least
-template <class T, int S, class K, int L>
-__global__ void __launch_bounds__(kThreads, kBlocks<S, K>)
-    route_kernel(const T *logits, RouteArgs A) {
-  extern __shared__ int hist[];  // the block's load; then, with groups, c of each warp's query
-  __shared__ float2 lanes_two[kWarps][32];
-  constexpr bool kKeys = std::is_same<K, unsigned>::value;
-  const bool groups = A.keep < A.G;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, k = A.k;
-  const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
-  float *shared_c = (float *)(hist + E) + warp * E;
-  float2 *pairs = lanes_two[warp];
-  // (behind clear_load_kernel, which has waited for what came before, only the load waits)
-  if (!A.load || gridDim.x == 1) pdl_wait();
-  pdl_trigger();
-  if (A.load) {
-    for (int e = threadIdx.x; e < E; e += kThreads) hist[e] = 0;
-    __syncthreads();
-  }
-  float bias[kKeys ? 1 : S];
-  unsigned below[kKeys ? S / 2 : 1];  // pairs of the experts' complements
-  if constexpr (kKeys) {
-#pragma unroll
-    for (int i = 0; i < S / 2; ++i)
-      below[i] = (0xffffu - (lane * S + 2 * i)) | (0xffffu - (lane * S + 2 * i + 1)) << 16;
-  } else {
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-      bias[s] = A.bias && lane * S + s < E ? fmaxf(A.bias[lane * S + s], -INFINITY) : 0.f;  // (NaN)
-  }
-  // the group whose share this lane takes, its first position there, its experts' (first) group
-  const int per = E / A.G, g = lane / A.width, i0 = lane % A.width, of0 = lane * S / per;
-  const long long step = (long long)gridDim.x * kWarps;
-  long long row = (long long)blockIdx.x * kWarps + warp;
-  Raw<T, S> next;
-  if (row < A.rows) next.load(logits + row * A.ld, E, A.vec);
-  for (; row < A.rows; row += step) {
-    const Raw<T, S> raw = next;
-    if (row + step < A.rows) next.load(logits + (row + step) * A.ld, E, A.vec);
-    K c[S], v[L], mine;
-    float m = -INFINITY, inv_sum = 1.f;  // of the softmax
-    bool bad;
-    int e;
-    if constexpr (kKeys) {
-      // order bits of pairs of logits, each over its expert's complement; a NaN is largest, +inf
-      // next, -inf (and what is beyond E) smallest
-      constexpr unsigned kInf = std::is_same<T, __half>::value ? 0xfc00u : 0xff80u;
-#pragma unroll
-      for (int i = 0; i < S / 2; ++i) {
-        const uint32_t w = plus_zero(raw.w[i], T{});
-        const uint32_t o = w ^ (((w >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
-        c[2 * i] = __byte_perm(o, below[i], 0x1054);
-        c[2 * i + 1] = __byte_perm(o, below[i], 0x3276);
-      }
-      best_of(c, v);
-      if (soft && !A.renorm) {
-        float x[S];
-#pragma unroll
-        for (int s = 0; s < S; ++s) m = max_nan(m, x[s] = to_float(raw.at(s)));
-        m = warp_max(m);
-        inv_sum = 0.f;
-#pragma unroll
-        for (int s = 0; s < S; ++s) inv_sum += exp2_fast((x[s] - m) * kLog2e);
-        inv_sum = __fdividef(1.f, warp_sum(inv_sum));
-      }
-      choose(c, v, k, mine, e);
-      const unsigned top = __shfl_sync(kAll, mine, 0) >> 16;
-      bad = top > kInf || (soft && top == kInf);
-      if (bad || mine >> 16 <= (0xffffu ^ kInf)) e = -1;
-    } else {
-      float x[S];
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        x[s] = to_float(raw.at(s));
-        m = max_nan(m, x[s]);
-      }
-      m = warp_max(m);
-      bad = isnan(m) || (soft && m == INFINITY);
-      if (soft && (!A.by_logits || !A.renorm)) {
-        float sum = 0.f;
-#pragma unroll
-        for (int s = 0; s < S; ++s) sum += exp2_fast((x[s] - m) * kLog2e);
-        inv_sum = __fdividef(1.f, warp_sum(sum));
-      }
-      if (A.by_logits) {
-#pragma unroll
-        for (int s = 0; s < S; ++s) c[s] = x[s];
-      } else if (soft) {
-#pragma unroll
-        for (int s = 0; s < S; ++s) c[s] = exp2_fast((x[s] - m) * kLog2e) * inv_sum + bias[s];
-      } else {
-#pragma unroll
-        for (int s = 0; s < S; ++s) c[s] = logistic(x[s]) + bias[s];
-      }
-#pragma unroll
-      for (int s = 0; s < S; ++s) c[s] = x[s] > -INFINITY && !bad ? c[s] : -INFINITY;
-      if (groups) {
-        float a = -INFINITY, b = -INFINITY;
-        if (A.whole) {  // a lane's experts are of one group: the lanes' two largest will do
-          float first = c[0], second = -INFINITY;
-#pragma unroll
-          for (int s = 1; s < S; ++s) join_two(first, second, c[s], -INFINITY);
-          pairs[lane] = make_float2(first, second);
-          __syncwarp();
-          if (g < A.G)
-            for (int i = i0; i < per / S; i += A.width) {
-              const float2 v = pairs[g * per / S + i];
-              join_two(a, b, v.x, v.y);
-            }
-        } else {
-#pragma unroll
-          for (int s = 0; s < S; ++s)
-            if (lane * S + s < E) shared_c[lane * S + s] = c[s];
-          __syncwarp();
-          if (g < A.G)
-            for (int i = i0; i < per; i += A.width)
-              join_two(a, b, shared_c[g * per + i], -INFINITY);
-        }
-        const unsigned kept = keep_groups(a, b, A.width, A.keep, A.group_top);
-        __syncwarp();
-        if (A.whole) {
-          const bool in = of0 < A.G && (kept >> (of0 * A.width) & 1u);
-#pragma unroll
-          for (int s = 0; s < S; ++s) c[s] = in ? c[s] : -INFINITY;
-        } else {
-          // (the lane's experts are neighbours: one division, then steps)
-          int of = of0, left = (of + 1) * per - lane * S;
-#pragma unroll
-          for (int s = 0; s < S; ++s) {
-            if (left-- == 0) {
-              ++of;
-              left = per - 1;
-            }
-            if (of >= A.G || !(kept >> (of * A.width) & 1u)) c[s] = -INFINITY;
-          }
-        }
-      }
-      best_of(c, v);
-      choose(c, v, k, mine, e);
-    }
-    if (lane >= k) e = -1;
-    // the chosen scores
-    float w = 0.f;
-    if (kKeys || A.by_logits) {
-      float x;
-      if constexpr (kKeys) {
-        const unsigned o = mine >> 16, u = o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu;
-        const unsigned short h = (unsigned short)u;
-        T t;
-        memcpy(&t, &h, 2);
-        x = to_float(t);
-      } else {
-        x = mine;
-      }
-      if (soft && A.renorm) m = __shfl_sync(kAll, x, 0);
-      if (e >= 0) w = !soft ? logistic(x) : exp2_fast((x - m) * kLog2e) * inv_sum;
-    } else if (e >= 0) {
-      const float x = to_float(logits[row * A.ld + e]);
-      w = !soft ? logistic(x) : exp2_fast((x - m) * kLog2e) * inv_sum;
-    }
-    if (A.renorm) {
-      const float sum = team_sum(w, A.team);
-      w = sum > 0.f ? __fdividef(w, sum) : 0.f;
-    }
-    if (lane < k) {
-      A.idx[row * k + lane] = e;
-      A.weight[row * k + lane] = bad ? NAN : A.factor * w;
-      if (A.load && e >= 0 && BOUTE_INB(e, E)) atomicAdd(hist + e, 1);
-    }
-  }
-  if (A.load) {
-    __syncthreads();
-    pdl_wait();  // (until the load has been cleared)
-    for (int e = threadIdx.x; e < E; e += kThreads)
-      if (gridDim.x == 1) A.load[e] = hist[e];
-      else if (hist[e]) atomicAdd(A.load + e, hist[e]);
-  }
-}
-
-__global__ void clear_load_kernel(int *load, int E) {
-  pdl_wait();
-  pdl_trigger();
-  for (int e = threadIdx.x; e < E; e += blockDim.x) load[e] = 0;
-}
 
 // ---- gradient ----------------------------------------------------------------------------
 struct RouteGradArgs {
@@ -624,45 +816,51 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
       return last_launch_status();
     return BOUTE_OK;
   }
+  RouteArgs A = {};
+  A.logits = logits, A.dtype = dtype, A.rows = T, A.ld = ld, A.bias = bias, A.E = E, A.mode = mode;
+  A.G = G, A.keep = keep, A.group_top = group_top, A.k = k, A.renorm = renorm;
+  A.factor = factor, A.idx = idx, A.load = load, A.weight = weight;
   const bool groups = keep < G;
   // (the sum of two scores has no counterpart among the logits)
-  const bool by_logits = !bias && !(groups && group_top == 2);
-  RouteArgs A = {};
-  A.rows = T, A.ld = ld, A.bias = bias, A.E = E, A.mode = mode, A.G = G, A.keep = keep;
-  A.group_top = group_top, A.k = k, A.renorm = renorm, A.by_logits = by_logits;
-  A.factor = factor, A.idx = idx, A.load = load, A.weight = weight;
-  A.team = power_of_two(k);
-  A.width = 32 / power_of_two(G);
-  return with_dtype(dtype, [&](auto tag) {
-    using X = decltype(tag);
-    return with_slots(E, [&](auto slots) {
-      constexpr int S = decltype(slots)::value;
-      A.vec = vectors(logits, ld, E, S, sizeof(X));
-      A.whole = E / G % S == 0;
-      const size_t smem = (size_t)E * 4 * (groups && !A.whole ? 1 + kWarps : 1);
-      const long long all = (T + kWarps - 1) / kWarps;
-      auto go = [&](auto key, auto list) {
-        using K = decltype(key);
-        // a few queries whose load is wanted: one block, which writes it itself
-        const unsigned grid =
-            load && all <= 4 ? 1u : (unsigned)std::min<long long>(all, (S > 8 ? 4ll : kBlocks<S, K>) *
-                                                                           num_sms());
-        if (load && grid > 1) {
-          if (int r = launch_cluster(clear_load_kernel, 1, 256, 1, 0, s, load, E)) return r;
-        }
-        auto kernel = route_kernel<X, S, K, decltype(list)::value>;
-        return launch_cluster(kernel, grid, kThreads, 1, smem, s, (const X *)logits, A);
-      };
-      // (lists of the k best at least; shorter ones take fewer steps)
-      constexpr int kShort = S < 4 ? S : 4;
-      if constexpr (sizeof(X) == 2 && S <= 8)
-        if (by_logits && !groups)
-          return k <= kShort ? go(0u, std::integral_constant<int, kShort>{})
-                             : go(0u, std::integral_constant<int, S>{});
-      return k <= kShort ? go(0.f, std::integral_constant<int, kShort>{})
-                         : go(0.f, std::integral_constant<int, S>{});
-    });
-  });
+  A.by_logits = !bias && !(groups && group_top == 2);
+  A.whole = A.by_logits && !groups && dtype != BOUTE_F32;
+  const size_t bytes = dtype_bytes(dtype);
+  A.vec = (uintptr_t)logits % 16 == 0 && ld * bytes % 16 == 0 && E * bytes % 16 == 0;
+  A.index_bits = E <= 256 ? 8 : 10;
+  // A team of lanes per query where its lists are short (candidates: more than choices where keys do
+  // not hold the values whole) and its values few or whole in their keys; else a warp.
+  const int need = A.whole ? k : k + 1;
+  auto run = [&](auto kernel, int queries, int blocks) {  // of a warp; of an SM
+    const size_t smem =
+        (size_t)E * 4 + (groups ? (size_t)kWarps * queries * shared_stride(E) * 4 : 0);
+    const long long all = (T + kWarps * queries - 1) / (kWarps * queries);
+    // a few queries whose load is wanted: one block, which writes it itself
+    const unsigned grid =
+        load && all <= 2 ? 1u : (unsigned)std::min<long long>(all, (long long)blocks * num_sms());
+    if (load && grid > 1)
+      if (int r = launch_cluster(clear_load_kernel, 1, 256, 1, 0, s, load, E)) return r;
+    if (smem > (48u << 10) &&
+        cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)smem) != cudaSuccess)
+      return last_launch_status();
+    return launch_cluster(kernel, grid, kThreads, 1, smem, s, A);
+  };
+  auto team = [&](auto list) {
+    constexpr int K = decltype(list)::value;
+    if (A.whole) {
+      if (E <= 64) return run(route_team_kernel<8, 8, K, true>, 4, 4);
+      if (E <= 128) return run(route_team_kernel<16, 8, K, true>, 4, 4);
+      return run(route_team_kernel<32, 8, K, true>, 4, 4);
+    }
+    if (E <= 64) return run(route_team_kernel<8, 8, K, false>, 4, 4);
+    if (E <= 128) return run(route_team_kernel<16, 8, K, false>, 4, 4);
+    return run(route_team_kernel<16, 16, K, false>, 2, 4);
+  };
+  if (E <= (A.whole ? 256 : 128) && need <= 8)
+    return need <= 4 ? team(std::integral_constant<int, 4>{}) : team(std::integral_constant<int, 8>{});
+  if (E <= 256) return k <= 4 ? run(route_warp_kernel<8, 4>, 1, 5) : run(route_warp_kernel<8, 8>, 1, 5);
+  if (E <= 512) return run(route_warp_kernel<16, 16>, 1, 4);
+  return run(route_warp_kernel<32, 32>, 1, 4);
 }
 
 extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int E, long long ld,
