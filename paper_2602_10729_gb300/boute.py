@@ -660,7 +660,9 @@ def _pn(t, dtype, shape):
         return None
     if t.shape != shape:
         raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
-    return _p(t, dtype)
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        return _p(t, dtype)  # raises
+    return t.data_ptr()
 
 
 def boute_token_logprobs(logits, targets, scale, logprob, entropy, lse, top_idx=None,

@@ -85,12 +85,13 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-inline int num_sms() {
-  int dev = 0, sms = 152;
-  cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  return sms;
-}
+// What the library asks of a device on every call, asked of the runtime once (abi.cu).
+struct DeviceInfo {
+  int ok;   // BOUTE_OK for sm_103a
+  int sms;  // multiprocessors
+};
+DeviceInfo device_info();  // of the current device; ok != BOUTE_OK without one
+inline int num_sms() { return device_info().sms; }
 
 void count_launch(int k = 1);
 unsigned long long launch_count();
