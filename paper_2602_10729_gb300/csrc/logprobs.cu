@@ -301,6 +301,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   __shared__ float tops[kTops], lanes[kThreads];
   __shared__ Sums wsum[kThreads / 32];
   __shared__ float csum[kMaxCluster][3];
+  __shared__ float stat[2];  // m (NaN: no distribution) and ln s
   __shared__ unsigned bound;
   __shared__ int nlist;
   pdl_wait();
@@ -313,9 +314,9 @@ __global__ void __launch_bounds__(kThreads, 4)
   const float c = fminf(scale * kLog2e, FLT_MAX);
   long long t = -1;
   float xt = 0.f;
-  if (tid == 0) {
-    nlist = 0;
-    if (rank == 0) t = targets[row];
+  if (tid == 0) nlist = 0;
+  if (tid == NT - 32 && rank == 0) {  // (of the warp that writes the row's statistics)
+    t = targets[row];
     if (t >= 0 && t < V) xt = to_float(x[t]);
   }
 
@@ -396,6 +397,30 @@ __global__ void __launch_bounds__(kThreads, 4)
     }
     cluster_sync();
   }
+  if (rank == 0 && warp == W - 1) {  // (the bound is another warp's)
+    const int n = CS > 1 ? CS : W;
+    Sums a = {-INFINITY, 0.f, 0.f};
+    if (lane < n) a = CS > 1 ? Sums{csum[lane][0], csum[lane][1], csum[lane][2]} : wsum[lane];
+    bool bad = __any_sync(kAll, isnan(a.m));
+#pragma unroll
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1)
+      a = join(a, {__shfl_xor_sync(kAll, a.m, o), __shfl_xor_sync(kAll, a.s, o),
+                   __shfl_xor_sync(kAll, a.u, o)}, c);
+    const float M = __fmul_rn(a.m, scale);
+    const bool empty = M == -INFINITY;  // (scaled values that underflow the type are masked too)
+    bad |= M == INFINITY;
+    const float ls = empty ? 0.f : logf(a.s);
+    if (lane == 0) {
+      float lp = 0.f;
+      if (t >= V || (bad && t >= 0)) lp = NAN;
+      else if (t >= 0) lp = empty ? -INFINITY : __fmul_rn(xt, scale) - M - ls;
+      lse[row] = bad ? NAN : M + ls;
+      logprob[row] = lp;
+      entropy[row] = bad ? NAN : empty ? 0.f : ls - kLn2 * (a.u / a.s);
+      stat[0] = bad ? NAN : M;
+      stat[1] = ls;
+    }
+  }
   float zt = -INFINITY;
   if (k > 0) {
     // a bound that k lanes reach
@@ -448,26 +473,9 @@ __global__ void __launch_bounds__(kThreads, 4)
     else __syncthreads();
   }
   if (rank != 0) return;
-  Sums a = CS > 1 ? Sums{csum[0][0], csum[0][1], csum[0][2]} : wsum[0];
-  bool bad = isnan(a.m);
-  for (int w = 1; w < (CS > 1 ? CS : W); ++w) {
-    const Sums b = CS > 1 ? Sums{csum[w][0], csum[w][1], csum[w][2]} : wsum[w];
-    bad |= isnan(b.m);
-    a = join(a, b, c);
-  }
-  const float M = __fmul_rn(a.m, scale);
-  const bool empty = M == -INFINITY;  // (scaled values that underflow the type are masked too)
-  bad |= M == INFINITY;
-  const float ls = empty ? 0.f : logf(a.s);
-  if (tid == 0) {
-    float lp = 0.f;
-    if (t >= V || (bad && t >= 0)) lp = NAN;
-    else if (t >= 0) lp = empty ? -INFINITY : __fmul_rn(xt, scale) - M - ls;
-    lse[row] = bad ? NAN : M + ls;
-    logprob[row] = lp;
-    entropy[row] = bad ? NAN : empty ? 0.f : ls - kLn2 * (a.u / a.s);
-  }
   if (k > 0) {
+    const float M = stat[0], ls = stat[1];
+    const bool bad = isnan(M), empty = M == -INFINITY;
     int n = bad || empty ? 0 : nlist;
     if (n > kList) {  // (many equal logits, or most of the largest in few lanes)
       __syncthreads();
