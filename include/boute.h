@@ -631,7 +631,8 @@ int boute_token_logprobs_grad(const void *logits, int dtype, long long T, int V,
  *   scores (Q x 4 fp32): mean logprob, lowest logprob, mean entropy, highest
  *   entropy; counts (Q int32): the positions counted. An answer without any
  *   has scores 0. NaN passes through to the mean and the extreme.
- * 0 <= T < 2^31, 0 <= Q <= BOUTE_MAX_ANSWERS. */
+ * 0 <= T <= BOUTE_MAX_POSITIONS, 0 <= Q <= BOUTE_MAX_ANSWERS. */
+#define BOUTE_MAX_POSITIONS 0x7fff0000
 #define BOUTE_MAX_ANSWERS (1 << 28)
 int boute_answer_scores(const float *logprob, const float *entropy, const long long *targets,
                         const long long *offsets, long long T, long long Q, float *scores,

@@ -65,11 +65,6 @@ __device__ __forceinline__ void store_peer(uint32_t a, float v) {
 __device__ __forceinline__ void store_peer(uint32_t a, unsigned long long v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
-__device__ __forceinline__ unsigned long long load_peer64(uint32_t a) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-  return v;
-}
 __device__ __forceinline__ int add_peer(uint32_t a, int v) {
   int old;
   asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");

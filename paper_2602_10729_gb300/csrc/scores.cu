@@ -3,11 +3,15 @@
 //
 // A block's teams (8 or 32 lanes, or all of it, by the mean length) take an answer each.
 // Lengths are ragged: what is too long for a team is taken by its block afterwards, and
-// where answers are long in the mean, by the eight blocks of a cluster. Latency bounds it:
-// the offsets, then the positions, are one trip to memory each.
+// where answers are long in the mean, by up to eight blocks of a cluster. Latency bounds
+// it: the offsets, then the positions, are one trip to memory each, and the longest
+// answer's rounds another each. 4096 answers of 200 positions in the mean: 7.6 us (13 MB,
+// a floor of 2), their gradient 9.4; 96 of 16384: 9 to 11 and 12 to 18, as the longest
+// has it (floors of 3.7 and 5.6). Blocks of 512 or 1024 threads: 12.5 and 23 to 30.
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "answers.cuh"
 
@@ -47,49 +51,79 @@ struct Answers {
   const float *logprob, *entropy;
   const long long *targets, *offsets;
   long long T, Q;
-  int cluster;  // blocks of a cluster, 1 or kMaxCluster
-  int per;      // answers of a block, or 0: one of a cluster
+  int cluster;  // blocks that share an answer
 
-  // Thread i of `by` over the positions [a, b) (2^31 at most); on: which of its first 64 count.
-  __device__ __forceinline__ Part part(long long a, long long b, int i, int by,
+  __device__ __forceinline__ bool counts(long long t) const { return !targets || targets[t] >= 0; }
+  // Thread i of BY over the positions [a, b) of an answer from `from` on (2^31 at most); on: which
+  // of its first 64 count. The extremes are compared as floats (3 instructions a position; keys of
+  // their order bits took 13, which bounded long answers) unless a NaN or an infinity throughout
+  // asks for the keys.
+  template <int BY>
+  __device__ __forceinline__ Part part(long long from, long long a, long long b, int i,
                                        unsigned long long &on) const {
     Part p = {0ull, 0ull, 0.f, 0.f, 0, 0};
     on = 0ull;
-    int first = 0;  // of this round's positions, in the thread's order
-    for (long long t0 = a + i; t0 < b; t0 += kUnroll * by, first += kUnroll) {
+    float lo = INFINITY, hi = -INFINITY;
+    int lo_at = -1, hi_at = -1, first = 0;  // of this round, in the thread's order
+    for (long long t0 = a + i; t0 < b; t0 += kUnroll * BY, first += kUnroll) {
+      const float *pl = logprob + t0, *ph = entropy + t0;
+      const long long *pt = targets + t0;
+      const int at0 = (int)(t0 - from);
       float l[kUnroll], h[kUnroll];
-      unsigned in = 0u;
+      bool in[kUnroll];
+      if (t0 + (kUnroll - 1) * BY < b) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const long long t = t0 + u * by;
-        if (t >= b) continue;
-        l[u] = logprob[t];
-        h[u] = entropy[t];
-        in |= (unsigned)(targets ? targets[t] >= 0 : true) << u;
+        for (int u = 0; u < kUnroll; ++u) {
+          l[u] = pl[u * BY];
+          h[u] = ph[u * BY];
+          in[u] = targets ? pt[u * BY] >= 0 : true;
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          in[u] = t0 + u * BY < b;
+          if (!in[u]) continue;
+          l[u] = pl[u * BY];
+          h[u] = ph[u * BY];
+          if (targets) in[u] = pt[u * BY] >= 0;
+        }
       }
-      if (first < 64) on |= (unsigned long long)in << first;
+      unsigned bits = 0u;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        if (!(in >> u & 1u)) continue;
-        const unsigned at = 0xffffffffu - (unsigned)(t0 + u * by - a);
+        if (!in[u]) continue;
+        bits |= 1u << u;
         p.lp += l[u];
         p.ent += h[u];
-        p.n += 1;
-        p.lo = max(p.lo, ((unsigned long long)order_bits(-l[u]) << 32) | at);
-        p.hi = max(p.hi, ((unsigned long long)order_bits(h[u]) << 32) | at);
+        if (l[u] < lo) lo = l[u], lo_at = at0 + u * BY;
+        if (h[u] > hi) hi = h[u], hi_at = at0 + u * BY;
       }
+      p.n += __popc(bits);
+      if (first < 64) on |= (unsigned long long)bits << first;
+    }
+    if (p.n == 0) return p;
+    if (lo_at >= 0 && hi_at >= 0 && !isnan(p.lp) && !isnan(p.ent)) {
+      p.lo = ((unsigned long long)order_bits(-lo) << 32) | (0xffffffffu - (unsigned)lo_at);
+      p.hi = ((unsigned long long)order_bits(hi) << 32) | (0xffffffffu - (unsigned)hi_at);
+      return p;
+    }
+    for (long long t = a + i; t < b; t += BY) {
+      if (!counts(t)) continue;
+      const unsigned at = 0xffffffffu - (unsigned)(t - from);
+      p.lo = max(p.lo, ((unsigned long long)order_bits(-logprob[t]) << 32) | at);
+      p.hi = max(p.hi, ((unsigned long long)order_bits(entropy[t]) << 32) | at);
     }
     return p;
   }
 };
 
-// The float whose order_bits a key has (-0 as +0), and the position, of an answer from a on.
+// The float whose order_bits a key has (-0 as +0), and the position; -1 without one.
 __device__ __forceinline__ float key_value(unsigned long long key) {
   const unsigned o = (unsigned)(key >> 32);
   return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
-__device__ __forceinline__ long long key_position(unsigned long long key, long long a) {
-  return a + (long long)(0xffffffffu - (unsigned)key);
+__device__ __forceinline__ int key_position(unsigned long long key) {
+  return key ? (int)(0xffffffffu - (unsigned)key) : -1;
 }
 
 // Of `lanes` neighbouring lanes, in each of them.
@@ -128,12 +162,13 @@ __device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part
   return p;
 }
 
-// emit(q, a, b, p, on, i, by): thread i of `by` writes its share of answer q's results.
-template <class Emit>
+// emit(q, from, p, a, b, on, i, by): thread i of `by` writes what positions [a, b) of answer q take,
+// which begins at `from` and has the Part p.
+template <int TEAM, class Emit>
 __device__ __forceinline__ void for_answers(const Answers &A, Emit emit) {
+  __shared__ Part red[kWarps], parts[kMaxCluster];
   pdl_wait();
   pdl_trigger();
-  __shared__ Part red[kWarps], parts[kMaxCluster];
   const int tid = threadIdx.x;
   long long a, b;
   unsigned long long on;
@@ -141,42 +176,47 @@ __device__ __forceinline__ void for_answers(const Answers &A, Emit emit) {
     a = min(max(A.offsets[q], 0ll), A.T);
     b = max(min(A.offsets[q + 1], A.T), a);
   };
-  if (A.per == 0) {
-    const int rank = blockIdx.x % A.cluster, i = rank * kThreads + tid, by = A.cluster * kThreads;
+  if constexpr (TEAM == kThreads) {
+    // a stretch of the answer to each of the cluster's blocks
+    const int rank = A.cluster > 1 ? blockIdx.x % A.cluster : 0;
     const long long q = blockIdx.x / A.cluster;
     range(q);
-    Part p = A.part(a, b, i, by, on);
+    const long long stretch = (b - a + A.cluster - 1) / A.cluster;
+    const long long a1 = min(a + rank * stretch, b), b1 = min(a1 + stretch, b);
+    Part p = A.part<kThreads>(a, a1, b1, tid, on);
     if (A.cluster > 1) p = cluster_join(p, rank, A.cluster, red, parts);
     else p = block_join(p, red);
-    emit(q, a, b, p, on, i, by);
+    emit(q, a, p, a1, b1, on, tid, std::integral_constant<int, kThreads>{});
     if (A.cluster > 1) cluster_sync();
-    return;
-  }
-  const int team = kThreads / A.per, i = tid % team;
-  const long long q = (long long)blockIdx.x * A.per + tid / team;
-  if (q < A.Q) range(q);
-  else a = b = 0;
-  const bool more = b - a > kMost * team;
-  const Part p = lanes_join(A.part(a, more ? a : b, i, team, on), team);
-  if (!more && q < A.Q) emit(q, a, b, p, on, i, team);
-  // the long ones, one after another by the whole block
-  __shared__ unsigned char longer[kThreads / 8];
-  if (i == 0) longer[tid / team] = more;
-  if (!__syncthreads_or(more)) return;
-  for (int j = 0; j < A.per; ++j) {
-    if (!longer[j]) continue;
-    range((long long)blockIdx.x * A.per + j);
-    const Part whole = block_join(A.part(a, b, tid, kThreads, on), red);
-    emit((long long)blockIdx.x * A.per + j, a, b, whole, on, tid, kThreads);
-    __syncthreads();
+  } else {
+    constexpr int kPer = kThreads / TEAM;
+    const int i = tid % TEAM;
+    const long long q0 = (long long)blockIdx.x * kPer, q = q0 + tid / TEAM;
+    if (q < A.Q) range(q);
+    else a = b = 0;
+    const bool more = b - a > kMost * TEAM;
+    const Part p = lanes_join(A.part<TEAM>(a, a, more ? a : b, i, on), TEAM);
+    if (!more && q < A.Q) emit(q, a, p, a, b, on, i, std::integral_constant<int, TEAM>{});
+    // the long ones, one after another by the whole block
+    __shared__ unsigned char longer[kPer];
+    if (i == 0) longer[tid / TEAM] = more;
+    if (!__syncthreads_or(more)) return;
+    for (int j = 0; j < kPer; ++j) {
+      if (!longer[j]) continue;
+      range(q0 + j);
+      const Part whole = block_join(A.part<kThreads>(a, a, b, tid, on), red);
+      emit(q0 + j, a, whole, a, b, on, tid, std::integral_constant<int, kThreads>{});
+      __syncthreads();
+    }
   }
 }
 
+template <int TEAM>
 __global__ void __launch_bounds__(kThreads, 5)
     answer_scores_kernel(Answers A, float *scores, int *counts) {
-  for_answers(A, [&](long long q, long long a, long long b, const Part &p, unsigned long long on,
-                     int i, int by) {
-    if (i != 0) return;
+  for_answers<TEAM>(A, [&](long long q, long long from, const Part &p, long long a, long long b,
+                           unsigned long long on, int i, auto by) {
+    if (i != 0 || a != from) return;
     const float n = (float)p.n;
     counts[q] = p.n;
     scores[4 * q] = p.n ? p.lp / n : 0.f;
@@ -186,21 +226,35 @@ __global__ void __launch_bounds__(kThreads, 5)
   });
 }
 
+template <int TEAM>
 __global__ void __launch_bounds__(kThreads, 5)
     answer_scores_grad_kernel(Answers A, const float *g_scores, float *g_logprob,
                               float *g_entropy) {
-  for_answers(A, [&](long long q, long long a, long long b, const Part &p, unsigned long long on,
-                     int i, int by) {
+  for_answers<TEAM>(A, [&](long long q, long long from, const Part &p, long long a, long long b,
+                           unsigned long long on, int i, auto by) {
+    constexpr int BY = decltype(by)::value;
     const float n = p.n ? (float)p.n : 1.f;
     const float *g = g_scores + 4 * q;
     const float g0 = g[0] / n, g1 = g[1], g2 = g[2] / n, g3 = g[3];
-    const long long lo = key_position(p.lo, a), hi = key_position(p.hi, a);
-    int nth = 0;
-#pragma unroll 4
-    for (long long t = a + i; t < b; t += by, ++nth) {
-      const bool in = nth < 64 ? on >> nth & 1ull : !A.targets || A.targets[t] >= 0;
-      g_logprob[t] = in ? g0 + (t == lo ? g1 : 0.f) : 0.f;
-      g_entropy[t] = in ? g2 + (t == hi ? g3 : 0.f) : 0.f;
+    const int lo = key_position(p.lo), hi = key_position(p.hi);  // from `from` on
+    int first = 0;
+    for (long long t0 = a + i; t0 < b; t0 += kUnroll * BY, first += kUnroll) {
+      float *pl = g_logprob + t0, *ph = g_entropy + t0;
+      const int at0 = (int)(t0 - from), left = (int)min(b - t0, (long long)kUnroll * BY);
+      unsigned bits = (unsigned)(on >> first);
+      if (first >= 64) {
+        bits = 0u;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (u * BY < left) bits |= (unsigned)A.counts(t0 + u * BY) << u;
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (u * BY >= left) break;
+        const bool in = bits >> u & 1u;
+        pl[u * BY] = in ? g0 + (at0 + u * BY == lo ? g1 : 0.f) : 0.f;
+        ph[u * BY] = in ? g2 + (at0 + u * BY == hi ? g3 : 0.f) : 0.f;
+      }
     }
   });
   // positions before the first answer and after the last
@@ -227,23 +281,21 @@ static int sizes_ok(long long T, long long Q, const float *logprob, const float 
   if (T < 0 || Q < 0 || (Q > 0 && !array_ok(offsets, 8)) ||
       (T > 0 && (!array_ok(logprob, 4) || !array_ok(entropy, 4))) || !optional_ok(targets, 8))
     return BOUTE_ERR_INVALID_ARG;
-  return T >= (1ll << 31) || Q > BOUTE_MAX_ANSWERS ? BOUTE_ERR_UNSUPPORTED : device_ok();
+  return T > BOUTE_MAX_POSITIONS || Q > BOUTE_MAX_ANSWERS ? BOUTE_ERR_UNSUPPORTED : device_ok();
 }
 
-// Teams by the mean length: 8 lanes up to 48 positions, 32 up to 512, else a block; and up to the
+// Teams by the mean length: 8 lanes up to 24 positions, 32 up to 512, else a block; and up to the
 // eight blocks of a cluster for answers over 1024 positions a block that are too few to fill the SMs.
-// (13665 answers of 31: 9.8 us with 8 lanes, 14 with 32; 4096 of 200: 10.5 with 32, 15.6 with a
-// block; 96 of 16384: 13 with eight blocks, 18 with four.)
-template <class... KArgs, class... Args>
-static int launch_answers(void (*kernel)(Answers, KArgs...), Answers A, cudaStream_t s,
-                          Args... args) {
-  const long long mean = A.T / A.Q, at_once = 8ll * num_sms();
-  A.per = mean <= 48 ? 32 : mean <= 512 ? 8 : 0;
-  while (A.cluster < kMaxCluster && A.per == 0 && mean > 1024 * A.cluster &&
-         2 * A.cluster * A.Q <= at_once)
-    A.cluster *= 2;
-  return launch_cluster(kernel, A.per ? (A.Q + A.per - 1) / A.per : A.Q * A.cluster, kThreads,
-                        A.cluster, 0, s, A, args...);
+// (13665 answers of 31: 6.4 us with 32 lanes, 8.3 with 8; 10010 of 16: 5.4 with 8, 8.6 with 32; 2245
+// of 682: 10.5 with a block, 15.4 with 32 lanes; 96 of 16384: 10.8 with eight blocks, 18 with four.)
+template <class Go>
+static int with_team(long long T, long long Q, Go go) {
+  const long long mean = T / Q, at_once = 8ll * num_sms();
+  if (mean <= 24) return go(std::integral_constant<int, 8>{}, (Q + 31) / 32, 1);
+  if (mean <= 512) return go(std::integral_constant<int, 32>{}, (Q + 7) / 8, 1);
+  int cluster = 1;
+  while (cluster < kMaxCluster && mean > 1024 * cluster && 2 * cluster * Q <= at_once) cluster *= 2;
+  return go(std::integral_constant<int, kThreads>{}, Q * cluster, cluster);
 }
 
 extern "C" int boute_answer_scores(const float *logprob, const float *entropy,
@@ -254,8 +306,11 @@ extern "C" int boute_answer_scores(const float *logprob, const float *entropy,
   if (Q > 0 && (!array_ok(scores, 4) || !array_ok(counts, 4))) return BOUTE_ERR_INVALID_ARG;
   if (int r = sizes_ok(T, Q, logprob, entropy, targets, offsets)) return r;
   if (Q == 0) return BOUTE_OK;
-  return launch_answers(answer_scores_kernel, {logprob, entropy, targets, offsets, T, Q, 1, 0},
-                        (cudaStream_t)stream, scores, counts);
+  return with_team(T, Q, [&](auto team, long long blocks, int cluster) {
+    return launch_cluster(answer_scores_kernel<decltype(team)::value>, blocks, kThreads, cluster, 0,
+                          (cudaStream_t)stream,
+                          Answers{logprob, entropy, targets, offsets, T, Q, cluster}, scores, counts);
+  });
 }
 
 extern "C" int boute_answer_scores_grad(const float *logprob, const float *entropy,
@@ -274,6 +329,10 @@ extern "C" int boute_answer_scores_grad(const float *logprob, const float *entro
       return last_launch_status();
     return BOUTE_OK;
   }
-  return launch_answers(answer_scores_grad_kernel, {logprob, entropy, targets, offsets, T, Q, 1, 0},
-                        (cudaStream_t)stream, g_scores, g_logprob, g_entropy);
+  return with_team(T, Q, [&](auto team, long long blocks, int cluster) {
+    return launch_cluster(answer_scores_grad_kernel<decltype(team)::value>, blocks, kThreads, cluster,
+                          0, (cudaStream_t)stream,
+                          Answers{logprob, entropy, targets, offsets, T, Q, cluster}, g_scores,
+                          g_logprob, g_entropy);
+  });
 }
