@@ -1,17 +1,24 @@
 // Routing of queries to experts: scores, the choice within the best groups,
 // the weights and the load; and the gradient of the weights.
 //
-// A team of L lanes per query (8 up to 256 experts, so four queries to a warp), lane l
-// with the S experts l S .. l S + S - 1. Experts are compared as 32-bit keys: the upper
-// bits of the order bits of c, and the expert's complement below, so that equal values
-// go to the lowest index. Each lane sorts its K largest keys in registers; the lanes' lists
-// join two by two, of which log2 L steps leave the query's K best in every lane. 16-bit
-// logits that are compared as they are (no bias) fit a key whole. Of other values a key
-// holds 22 to 24 bits: K > k candidates are ranked by their exact values, and a query
-// whose last candidate shares the k-th's upper bits (one in a thousand or fewer) is
-// chosen again by exact values alone. Without a bias the logits themselves are compared,
-// which have the order of the scores: only the chosen scores are computed then, and a
-// softmax's sum only where the weights are not renormalised.
+// Arithmetic bounds it: a query's logits are one or two lines, its choice some hundred
+// instructions. So as little as possible is compared, and in one word where it fits:
+//  - Teams of 8 lanes to a query, four queries to a warp, lane l with the S experts l S ..
+//    l S + S - 1. Experts are compared as 32-bit keys: the upper bits of the order bits of
+//    c, and the expert's complement below, so that equal values go to the lowest index. Each
+//    lane sorts its K largest keys in registers; the lanes' lists join two by two, of which
+//    three steps leave the query's K best in every lane. 16-bit logits that are compared as
+//    they are (no bias, no groups) fit a key whole. Of other values a key holds 24 bits:
+//    K > k candidates are ranked by their exact values, and a query whose last candidate
+//    shares the k-th's upper bits (one in thousands, or equal values) is chosen again by
+//    exact values alone.
+//  - A warp to a query for longer lists and more experts: each lane sorts its own, and k
+//    rounds take the largest of the 32 heads.
+// Without a bias the logits themselves are compared, which have the order of the scores:
+// only the chosen scores are computed then, and a softmax's sum only where the weights are
+// not renormalised. 262144 queries of 256 bf16 logits, k = 4: 48 us (2.9 TB/s; a floor of 21;
+// the arithmetic units are 79 % busy); 131072 of 192, logistic with bias, 8 groups, k = 6: 99.
+// The gradient moves bytes: 26.3 us where they take 25.7 (262144 x 256 bf16 cleared).
 #include <math.h>
 
 #include <algorithm>
@@ -73,6 +80,7 @@ struct RouteArgs {
   int whole;      // and fit a key whole (16-bit logits, no groups)
   int vec;        // rows on 16-byte boundaries, E a multiple of a vector's logits
   int index_bits; // of a key that holds a part of a value
+  int group_lanes; // lanes that hold a group, where each holds experts of one; else 0
   float factor;
   int *idx, *load;
   float *weight;
@@ -84,12 +92,19 @@ __device__ __forceinline__ float logit_at(const RouteArgs &A, long long row, int
   if (A.dtype == BOUTE_F16) return __half2float(((const __half *)A.logits)[i]);
   return __bfloat162float(((const __nv_bfloat16 *)A.logits)[i]);
 }
-// The words of the N 16-byte-aligned words of 4-byte (PER = 1) or pairs of 2-byte logits from e0
-// on; `none` beyond E.
+// N words of 4-byte (PER = 1) or pairs of 2-byte logits from e0 on, by vectors of up to 16 bytes where
+// rows allow (`vec`); `none` beyond E.
 template <int N, int PER>
 __device__ __forceinline__ void load_words(uint32_t *w, const void *row, int e0, int E, bool vec,
                                            uint32_t none) {
-  if (vec) {
+  static_assert(N == 1 || N == 2 || N % 4 == 0, "whole vectors");
+  if (vec && N == 1) {
+    w[0] = e0 < E ? *((const uint32_t *)row + e0 / PER) : none;
+  } else if (vec && N == 2) {
+    uint2 v = {none, none};
+    if (e0 < E) v = *(const uint2 *)((const uint32_t *)row + e0 / PER);
+    w[0] = v.x, w[N - 1] = v.y;
+  } else if (vec) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
       uint4 v = {none, none, none, none};
@@ -188,6 +203,31 @@ __device__ __forceinline__ void best_of(unsigned (&c)[S], unsigned (&best)[K]) {
 __device__ __forceinline__ void join_two(float &a, float &b, float a2, float b2) {
   b = fmaxf(fminf(a, a2), fmaxf(b, b2));
   a = fmaxf(a, a2);
+}
+// Whether the lane's experts, all of them of one group, are in one that stays; lane l of the team's
+// L. (A group's lanes join theirs in its first, in any number of lanes.)
+template <int S, int L>
+__device__ __forceinline__ bool keeps_lane(const float (&c)[S], const RouteArgs &A, int l) {
+  const int n = A.group_lanes, g = l / n, i = l - g * n;
+  float a = c[0], b = -INFINITY;
+#pragma unroll
+  for (int s = 1; s < S; ++s) {
+    b = fmaxf(b, fminf(a, c[s]));
+    a = fmaxf(a, c[s]);
+  }
+  for (int o = L / 2; o > 0; o >>= 1) {
+    if (o >= n) continue;
+    const float a2 = __shfl_down_sync(kAll, a, o, L), b2 = __shfl_down_sync(kAll, b, o, L);
+    if (i < o && i + o < n) join_two(a, b, a2, b2);
+  }
+  const float score = A.group_top == 2 && b > -INFINITY ? a + b : a;
+  const float mine = __shfl_sync(kAll, score, l - i, L);
+  int rank = 0;
+  for (int h = 0; h < A.G; ++h) {
+    const float other = __shfl_sync(kAll, score, h * n, L);
+    rank += other > mine || (other == mine && h < g);
+  }
+  return rank < A.keep && mine > -INFINITY;
 }
 // Bits of the groups that stay, from a query's c in shared memory; lane l of the team's L. Several
 // lanes to a group where there are enough, else groups in turn.
@@ -428,7 +468,11 @@ __global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
         float v[S], b[S];
         load_bias(A, e0, b);
         q = load_query<S, L>(A, row, e0, b, v);
-        if (groups) {
+        if (groups && A.group_lanes) {
+          kept = keeps_lane<S, L>(v, A, l) ? kAll : 0u;
+#pragma unroll
+          for (int s = 0; s < S; ++s) v[s] = kept ? v[s] : -INFINITY;
+        } else if (groups) {
 #pragma unroll
           for (int s = 0; s < S; ++s)
             if (e0 + s < E) shared_c[e0 + s] = v[s];
@@ -507,8 +551,8 @@ __global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
 
 // ---- a warp to a query -------------------------------------------------------------------
 // The k largest of the lanes' values, lane r with the r-th: its value and its expert (-1: none).
-// Each lane sorts its K >= min(k, S) best; k rounds take the largest head of the 32 lists. Equal values go to
-// the lowest expert: of several lanes the lowest, of one lane's the occurrences in order.
+// Each lane sorts its K >= min(k, S) best; k rounds take the largest head of the 32 lists. Equal
+// values go to the lowest expert: of several lanes the lowest, of one lane's the occurrences in order.
 template <int S, int K>
 __device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, int &expert) {
   const int lane = threadIdx.x & 31;
@@ -518,8 +562,10 @@ __device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, 
   best_in_lane<S, K>(v);
   mine = -INFINITY;
   int owner = 0;
-#pragma unroll (K <= 4 ? K : 1)
-  for (int r = 0; r < (K <= 4 ? K : k); ++r) {  // (picks beyond k are not used)
+  constexpr bool kShort = K < S;  // lists of K >= k: picks beyond k are not used
+  constexpr int kTimes = kShort ? K : 4;
+#pragma unroll (kTimes)
+  for (int r = 0; r < (kShort ? K : k); ++r) {
     const float best = warp_max(v[0]);
     const int from = __ffs(__ballot_sync(kAll, v[0] == best)) - 1;
     owner = lane == r ? from : owner;
@@ -555,7 +601,11 @@ __global__ void __launch_bounds__(kThreads, S > 8 ? 1 : 5) route_warp_kernel(Rou
        row += (long long)gridDim.x * kWarps) {
     float c[S], mine;
     const Query q = load_query<S, 32>(A, row, e0, bias, c);
-    if (A.keep < A.G) {
+    if (A.keep < A.G && A.group_lanes) {
+      const bool kept = keeps_lane<S, 32>(c, A, lane);
+#pragma unroll
+      for (int s = 0; s < S; ++s) c[s] = kept ? c[s] : -INFINITY;
+    } else if (A.keep < A.G) {
 #pragma unroll
       for (int s = 0; s < S; ++s)
         if (e0 + s < A.E) shared_c[e0 + s] = c[s];
@@ -828,11 +878,14 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   A.vec = (uintptr_t)logits % 16 == 0 && ld * bytes % 16 == 0 && E * bytes % 16 == 0;
   A.index_bits = E <= 256 ? 8 : 10;
   // A team of lanes per query where its lists are short (candidates: more than choices where keys do
-  // not hold the values whole) and its values few or whole in their keys; else a warp.
+  // not hold the values whole) and its values few or whole in their keys; else a warp. (us by team
+  // and by warp: 262144 x 256 bf16, k = 4: 48, 107, k = 8: 64, 155; 131072 queries: 128 bf16 with
+  // bias, k = 6: 42, 57; 64 fp32, k = 2: 21, 34; 128 fp32, k = 4: 38, 45.)
   const int need = A.whole ? k : k + 1;
-  auto run = [&](auto kernel, int queries, int blocks) {  // of a warp; of an SM
+  auto run = [&](auto kernel, int queries, int blocks, int S) {  // of a warp; of an SM; of a lane
+    A.group_lanes = E / G % S == 0 ? E / G / S : 0;
     const size_t smem =
-        (size_t)E * 4 + (groups ? (size_t)kWarps * queries * shared_stride(E) * 4 : 0);
+        (size_t)E * 4 + (groups && !A.group_lanes ? (size_t)kWarps * queries * shared_stride(E) * 4 : 0);
     const long long all = (T + kWarps * queries - 1) / (kWarps * queries);
     // a few queries whose load is wanted: one block, which writes it itself
     const unsigned grid =
@@ -848,19 +901,20 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   auto team = [&](auto list) {
     constexpr int K = decltype(list)::value;
     if (A.whole) {
-      if (E <= 64) return run(route_team_kernel<8, 8, K, true>, 4, 4);
-      if (E <= 128) return run(route_team_kernel<16, 8, K, true>, 4, 4);
-      return run(route_team_kernel<32, 8, K, true>, 4, 4);
+      if (E <= 64) return run(route_team_kernel<8, 8, K, true>, 4, 4, 8);
+      if (E <= 128) return run(route_team_kernel<16, 8, K, true>, 4, 4, 16);
+      return run(route_team_kernel<32, 8, K, true>, 4, 4, 32);
     }
-    if (E <= 64) return run(route_team_kernel<8, 8, K, false>, 4, 4);
-    if (E <= 128) return run(route_team_kernel<16, 8, K, false>, 4, 4);
-    return run(route_team_kernel<16, 16, K, false>, 2, 4);
+    if (E <= 64) return run(route_team_kernel<8, 8, K, false>, 4, 4, 8);
+    return run(route_team_kernel<16, 8, K, false>, 4, 4, 16);
   };
   if (E <= (A.whole ? 256 : 128) && need <= 8)
     return need <= 4 ? team(std::integral_constant<int, 4>{}) : team(std::integral_constant<int, 8>{});
-  if (E <= 256) return k <= 4 ? run(route_warp_kernel<8, 4>, 1, 5) : run(route_warp_kernel<8, 8>, 1, 5);
-  if (E <= 512) return run(route_warp_kernel<16, 16>, 1, 4);
-  return run(route_warp_kernel<32, 32>, 1, 4);
+  if (E <= 64) return run(route_warp_kernel<2, 2>, 1, 5, 2);
+  if (E <= 128) return run(route_warp_kernel<4, 4>, 1, 5, 4);
+  if (E <= 256) return k <= 4 ? run(route_warp_kernel<8, 4>, 1, 5, 8) : run(route_warp_kernel<8, 8>, 1, 5, 8);
+  if (E <= 512) return run(route_warp_kernel<16, 16>, 1, 4, 16);
+  return run(route_warp_kernel<32, 32>, 1, 4, 32);
 }
 
 extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int E, long long ld,

@@ -116,6 +116,23 @@ def test_ties_go_to_the_lowest_index():
                 check(x.to(DT[dtype]), *a, routed(x.to(DT[dtype]).cuda(), *a))
 
 
+@pytest.mark.parametrize("mode", [SOFT, SIG])
+@pytest.mark.parametrize("T,E,G,keep,gtop,k", [  # lists as long as a lane's values, and groups that
+    (300, 64, 1, 1, 1, 8), (300, 50, 1, 1, 1, 32), (300, 128, 1, 1, 1, 12),  # 1 to 16 lanes hold
+    (300, 100, 1, 1, 1, 20), (300, 60, 6, 3, 1, 8), (300, 64, 8, 3, 2, 4), (300, 128, 8, 4, 2, 6),
+    (300, 240, 5, 2, 2, 9), (300, 256, 2, 1, 1, 30), (300, 160, 20, 3, 2, 20),
+    (40, 480, 3, 2, 2, 32), (40, 1024, 32, 2, 1, 32), (300, 168, 8, 5, 2, 9)])
+def test_long_choices_and_groups_of_lanes(mode, T, E, G, keep, gtop, k):
+    g = torch.Generator().manual_seed(E + k)
+    bias = torch.randint(-100, 100, (E,), generator=g).float() * 1e-3
+    x = queries(E, T, E, "bf16")
+    x[::7, ::3] = float("-inf")
+    ties = torch.randint(0, 3, (T, E), generator=g).float()
+    for v, b in ((x, None), (x, bias), (ties, None)):
+        a = (None if b is None else b.cuda(), mode, G, keep, gtop, k, True, 1.0)
+        check(v, *a, routed(v.cuda(), *a))
+
+
 def test_load_is_written_and_optional():
     x = queries(2, 100, 16, "bf16").cuda()
     a = (None, SOFT, 1, 1, 1, 3, True, 1.0)
