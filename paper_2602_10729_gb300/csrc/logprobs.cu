@@ -632,6 +632,9 @@ using namespace boute;
 // How a row's pieces are spread: a warp per piece, up to kWarps to a block, and the blocks of a
 // cluster while the rows alone leave the SMs without work and every warp gets a piece; with rows
 // so few that all their warps run at once, twice the warps.
+// (us by the most blocks an SM that clusters may make of rows, 4, 8 or 16: 600 x 131072 bf16, k = 8:
+// 36, 31, 41; 256 x 131072, k = 20: 23, 19, 24. Warps to a block, 2, 4 or 8: 2039 x 50021 fp16, k = 8:
+// 44, 43, 46; 2500 x 32000 bf16, k = 5: 42, 38, 41.)
 struct Spread {
   int W, CS;
   template <class P>
@@ -641,6 +644,15 @@ struct Spread {
     CS = 1;
     while (CS < kMaxCluster && 2 * CS * T <= 8 * sms && 2 * CS * W <= Q) CS *= 2;
     if (CS == kMaxCluster && 2 * W * CS * T <= 32 * sms && CS * W < Q) W *= 2;
+  }
+  // Many short rows: what follows a row's loads takes as long as they do, and rows of one warp (of
+  // two, where many alternatives are ranked) have more of it going on at once. (us by 1, 2 and 4
+  // warps: 9000 x 8000 bf16, k = 4: 40, 44, 54, k = 20: 62, 58, 64, k = 0: 28, 29, 30; 20000 x 32000,
+  // k = 4: 220, 218, 235, k = 0: 200, 194, 193; 5000 x 13000, k = 20: 57, 47, 46.)
+  template <class P>
+  void for_alternatives(long long T, int V, int k, P) {
+    const int Q = P::count(P::E - 1, V), few = k <= 8 ? 1 : 2;
+    if (T >= 48ll * num_sms() && Q <= (k ? 32 : 8)) W = W < few ? W : few;
   }
 };
 
@@ -665,10 +677,11 @@ extern "C" int boute_token_logprobs(const void *logits, int dtype, long long T, 
   if (T == 0) return BOUTE_OK;
   return with_dtype(dtype, [&](auto tag) {
     using E = decltype(tag);
-    const Spread sp(T, V, Piece<E>{});
+    Spread sp(T, V, Piece<E>{});
+    sp.for_alternatives(T, V, k, Piece<E>{});
     return launch_cluster(token_logprobs_kernel<E>, T * sp.CS, 32 * sp.W, sp.CS, 0,
-                          (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, k, sp.CS, logprob,
-                       entropy, lse, top_idx, top_logprob);
+                          (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, k, sp.CS,
+                          logprob, entropy, lse, top_idx, top_logprob);
   });
 }
 
@@ -691,7 +704,7 @@ extern "C" int boute_token_logprobs_grad(const void *logits, int dtype, long lon
     using E = decltype(tag);
     const Spread sp(T, V, Piece<E>{});
     return launch_cluster(token_logprobs_grad_kernel<E>, T * sp.CS, 32 * sp.W, sp.CS, 0,
-                          (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, lse, entropy, g_logprob,
-                       g_entropy, (E *)dlogits, ldd, sp.CS);
+                          (cudaStream_t)stream, (const E *)logits, V, ld, targets, scale, lse,
+                          entropy, g_logprob, g_entropy, (E *)dlogits, ldd, sp.CS);
   });
 }

@@ -99,6 +99,24 @@ def test_forward_sizes_types_and_places(dtype, T, V, k, scale, pitch, shift):
     check_forward(x, t, scale, k, out)
 
 
+@pytest.mark.parametrize("dtype,V,k", [
+    ("f32", 900, 0), ("bf16", 700, 4), ("f16", 7001, 8), ("bf16", 7001, 20), ("f32", 5003, 32),
+    ("bf16", 2049, 1), ("f32", 513, 0)])
+def test_forward_many_short_rows(dtype, V, k):
+    T = 16001
+    x, t = logits(V, 97, V, dtype)
+    x[5, ::2] = -float("inf")
+    x[7] = -float("inf")
+    x[11, V // 3] = float("nan")
+    x[13] = 0.5
+    t[17] = -1
+    rows = torch.arange(T) % 97
+    out = forward(placed(x[rows], 1, 3), t[rows].cuda(), 1.25, k)
+    some = torch.cat([torch.arange(97), T - 1 - torch.arange(97)])
+    check_forward(x[rows[some]], t[rows[some]], 1.25, k,
+                  tuple(None if v is None else v[some.cuda()] for v in out))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("V", [5, 300, 9001, 131071])
 def test_forward_masks_and_rows_without_a_token(dtype, V):
