@@ -99,7 +99,7 @@ def errors(router, answers, idx):
 
 
 def train(router, answers, steps=60, lr=0.5):
-    """Gradient descent on the expected error plus the expected time, weights over k = 4 replicas."""
+    """Gradient descent on the expected error plus the expected time, k = 4 replicas a query."""
     scores = answers.scores()
     feats = router.features(scores)
     cost = 0.05 * torch.tensor(COST, device="cuda")

@@ -47,6 +47,42 @@ inline bool array_ok(const void *p, size_t bytes) {
 inline bool optional_ok(const void *p, size_t bytes) { return p == nullptr || array_ok(p, bytes); }
 
 constexpr unsigned kAll = 0xffffffffu;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+// The warp's maximum in one instruction; a NaN anywhere wins.
+__device__ __forceinline__ float warp_max_nan(float v) {
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float y) {  // (2 ulp; what is below 2^-126 is 0)
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+  return r;
+}
+// Order-preserving bits of a float, and back.
+__device__ __forceinline__ unsigned order_bits(float v) {
+  const unsigned u = __float_as_uint(v);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_order_bits(unsigned o) {
+  return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+}
 
 // ---- clusters (a block launched alone is a cluster of one) ---------------------------
 __device__ __forceinline__ void cluster_sync() {
@@ -67,7 +103,10 @@ __device__ __forceinline__ void store_peer(uint32_t a, unsigned long long v) {
 }
 __device__ __forceinline__ int add_peer(uint32_t a, int v) {
   int old;
-  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
+  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;"
+               : "=r"(old)
+               : "r"(a), "r"(v)
+               : "memory");
   return old;
 }
 

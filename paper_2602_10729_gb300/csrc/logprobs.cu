@@ -11,6 +11,13 @@
 // a block's, or a cluster's when there are few rows. Shared memory is left to the L1
 // cache, through which the loads in flight pass: with 16 KB a block for the parts
 // themselves, reads were 10 % slower.
+//
+// Memory bounds the large calls: 8192 rows of 131072 bf16 logits, k = 20: 335 us
+// (6.4 TB/s, 0.95 of the copy rate; k = 0: 305 us, 1.04); their gradient, which writes
+// as much as it reads, 640 us (0.99). Rows that do not fill whole waves of blocks pay for
+// the last one: 2039 rows of 50021 fp16, k = 8: 43 us (0.70). What follows a row's loads
+// (joining, the bound, the second look, the ranks) is 4 us of latency, which bounds the
+// small calls: one row of 50021, k = 5: 5.2 us; 64 of 131072 fp32, k = 20: 10.8.
 #include <float.h>
 #include <math.h>
 
@@ -25,34 +32,7 @@ constexpr int kMaxCluster = 8;
 constexpr int kTops = 256;  // maxima from which the alternatives' bound is taken
 constexpr int kList = 256;  // candidates ranked at once, 32 a warp at least
 constexpr float kLowest = -200.f;  // exp(kLowest) = 2^kLowest = 0 in fp32
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
-}
-// The warp's maximum in one instruction; a NaN anywhere wins.
-__device__ __forceinline__ float warp_max_nan(float v) {
-  float r;
-  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b, float c) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ float exp2_fast(float y) {  // (2 ulp; what is below 2^-126 is 0)
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-  return r;
-}
+constexpr float kLn2 = 0.6931471805599453f;
 
 // ---- a row in pieces -----------------------------------------------------------------
 // A piece is 2 KB of a row, of which a lane holds four 16-byte vectors 512 bytes apart. Piece q
@@ -242,18 +222,9 @@ __device__ __forceinline__ void add_piece(const Piece<T> &p, float m, float c,
 }
 
 // ---- alternatives --------------------------------------------------------------------
-// Order-preserving bits of a float, and their upper half, which stands for a lower bound of it.
-__device__ __forceinline__ unsigned order_bits(float v) {
-  const unsigned u = __float_as_uint(v);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float from_order_bits(unsigned o) {
-  return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
-}
-
-// An upper half of order bits that k of n floats reach (n a multiple of 32, at most kTops), close
-// to the largest such one: built two bits at a time until exactly k reach it; by one warp. That
-// of -inf where fewer than k are above it.
+// An upper half of order bits, which stands for a lower bound, that k of n floats reach (n a
+// multiple of 32, at most kTops), close to the largest such one: built two bits at a time until
+// exactly k reach it; by one warp. That of -inf where fewer than k are above it.
 __device__ __forceinline__ unsigned kth_bound(const float *v, int n, int k) {
   const int lane = threadIdx.x & 31;
   unsigned o[kTops / 32], t = 0u;
@@ -632,9 +603,9 @@ using namespace boute;
 // How a row's pieces are spread: a warp per piece, up to kWarps to a block, and the blocks of a
 // cluster while the rows alone leave the SMs without work and every warp gets a piece; with rows
 // so few that all their warps run at once, twice the warps.
-// (us by the most blocks an SM that clusters may make of rows, 4, 8 or 16: 600 x 131072 bf16, k = 8:
-// 36, 31, 41; 256 x 131072, k = 20: 23, 19, 24. Warps to a block, 2, 4 or 8: 2039 x 50021 fp16, k = 8:
-// 44, 43, 46; 2500 x 32000 bf16, k = 5: 42, 38, 41.)
+// (us by the most blocks an SM that clusters may make of rows, 4, 8 or 16: 600 x 131072 bf16,
+// k = 8: 36, 31, 41; 256 x 131072, k = 20: 23, 19, 24. Warps to a block, 2, 4 or 8: 2039 x 50021
+// fp16, k = 8: 44, 43, 46; 2500 x 32000 bf16, k = 5: 42, 38, 41.)
 struct Spread {
   int W, CS;
   template <class P>
@@ -647,8 +618,8 @@ struct Spread {
   }
   // Many short rows: what follows a row's loads takes as long as they do, and rows of one warp (of
   // two, where many alternatives are ranked) have more of it going on at once. (us by 1, 2 and 4
-  // warps: 9000 x 8000 bf16, k = 4: 40, 44, 54, k = 20: 62, 58, 64, k = 0: 28, 29, 30; 20000 x 32000,
-  // k = 4: 220, 218, 235, k = 0: 200, 194, 193; 5000 x 13000, k = 20: 57, 47, 46.)
+  // warps: 9000 x 8000 bf16, k = 4: 40, 44, 54, k = 20: 62, 58, 64, k = 0: 28, 29, 30; 20000 x
+  // 32000, k = 4: 220, 218, 235, k = 0: 200, 194, 193; 5000 x 13000, k = 20: 57, 47, 46.)
   template <class P>
   void for_alternatives(long long T, int V, int k, P) {
     const int Q = P::count(P::E - 1, V), few = k <= 8 ? 1 : 2;

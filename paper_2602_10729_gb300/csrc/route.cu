@@ -8,7 +8,7 @@
 //    c, and the expert's complement below, so that equal values go to the lowest index. Each
 //    lane sorts its K largest keys in registers; the lanes' lists join two by two, of which
 //    three steps leave the query's K best in every lane. 16-bit logits that are compared as
-//    they are (no bias, no groups) fit a key whole. Of other values a key holds 24 bits:
+//    they are (no bias, no groups) fit a key whole. Of other values a key holds 25 bits:
 //    K > k candidates are ranked by their exact values, and a query whose last candidate
 //    shares the k-th's upper bits (one in thousands, or equal values) is chosen again by
 //    exact values alone.
@@ -31,28 +31,7 @@ namespace boute {
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
-}
-__device__ __forceinline__ float exp2_fast(float y) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-  return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float warp_max(float v) {  // (a NaN wins)
-  float r;
-  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
 __device__ __forceinline__ float logistic(float x) {  // (0 where exp(-x) overflows)
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_fast(-x * kLog2e)));
@@ -79,7 +58,6 @@ struct RouteArgs {
   int by_logits;  // the logits are compared
   int whole;      // and fit a key whole (16-bit logits, no groups)
   int vec;        // rows on 16-byte boundaries, E a multiple of a vector's logits
-  int index_bits; // of a key that holds a part of a value
   int group_lanes; // lanes that hold a group, where each holds experts of one; else 0
   float factor;
   int *idx, *load;
@@ -92,8 +70,8 @@ __device__ __forceinline__ float logit_at(const RouteArgs &A, long long row, int
   if (A.dtype == BOUTE_F16) return __half2float(((const __half *)A.logits)[i]);
   return __bfloat162float(((const __nv_bfloat16 *)A.logits)[i]);
 }
-// N words of 4-byte (PER = 1) or pairs of 2-byte logits from e0 on, by vectors of up to 16 bytes where
-// rows allow (`vec`); `none` beyond E.
+// N words of 4-byte (PER = 1) or pairs of 2-byte logits from e0 on, by vectors of up to 16 bytes
+// where rows allow (`vec`); `none` beyond E.
 template <int N, int PER>
 __device__ __forceinline__ void load_words(uint32_t *w, const void *row, int e0, int E, bool vec,
                                            uint32_t none) {
@@ -130,10 +108,6 @@ __device__ __forceinline__ uint32_t plus_zero(uint32_t w, int dtype) {
   if (dtype == BOUTE_F16) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
   else asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
   return r;
-}
-__device__ __forceinline__ unsigned order_bits(float v) {
-  const unsigned u = __float_as_uint(v);
-  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 
 // L values in descending order (Batcher's odd-even merge sort).
@@ -327,7 +301,7 @@ __device__ __forceinline__ Query load_query(const RouteArgs &A, long long row, i
 #pragma unroll
   for (int s = 0; s < S; ++s) q.m = max_nan(q.m, c[s]);
   if constexpr (L == 32) {
-    q.m = warp_max(q.m);
+    q.m = warp_max_nan(q.m);
   } else {
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) q.m = max_nan(q.m, __shfl_xor_sync(kAll, q.m, o));
@@ -401,8 +375,10 @@ __device__ __forceinline__ void end_load(const RouteArgs &A, const int *hist) {
 
 // WHOLE: keys hold the values whole (16-bit logits compared as they are, no groups).
 template <int S, int L, int K, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
+__global__ void __launch_bounds__(kThreads, 4)
     route_team_kernel(RouteArgs A) {
+  constexpr unsigned kLow = 127u;  // the experts' bits of a key that holds a part of a value
+  static_assert(WHOLE || S * L <= 128, "experts of such keys");
   constexpr int kTeams = 32 / L, kOwn = (K + L - 1) / L;  // queries of a warp; a lane's candidates
   extern __shared__ int hist[];  // the block's load; then, with groups, c and the groups' scores
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, l = lane % L, e0 = l * S;
@@ -481,14 +457,12 @@ __global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
           __syncwarp();
           drop_groups(v, kept, e0, per);
         }
-        const unsigned low = (1u << A.index_bits) - 1u;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
           const float u = v[s] == 0.f ? 0.f : v[s];
-          c[s] = u > -INFINITY ? (order_bits(u) & ~low) | (low - (unsigned)(e0 + s)) : 0u;
+          c[s] = u > -INFINITY ? (order_bits(u) & ~kLow) | (kLow - (unsigned)(e0 + s)) : 0u;
         }
       }
-      const unsigned low = (1u << A.index_bits) - 1u;
       best_of<S, L, K>(c, best);
       // the candidates' exact values, and their ranks (the list has equal ones in order)
       float v[kOwn];
@@ -497,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
         unsigned mine = 0u;
 #pragma unroll
         for (int i = j * L; i < K && i < (j + 1) * L; ++i) mine = l == i - j * L ? best[i] : mine;
-        e[j] = mine ? (int)(low - (mine & low)) : -1;
+        e[j] = mine ? (int)(kLow - (mine & kLow)) : -1;
         x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
         v[j] = e[j] >= 0 ? q.value(A, x[j], e[j]) : -INFINITY;
         place[j] = 0;
@@ -513,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, WHOLE ? 4 : S > 16 ? 2 : 4)
 #pragma unroll
       for (int j = 0; j < kOwn; ++j)
         doubt |= place[j] == A.k - 1 && e[j] >= 0 && best[K - 1] != 0u &&
-                 ((order_bits(v[j] == 0.f ? 0.f : v[j]) ^ best[K - 1]) & ~low) == 0u;
+                 ((order_bits(v[j] == 0.f ? 0.f : v[j]) ^ best[K - 1]) & ~kLow) == 0u;
       doubt = __ballot_sync(kAll, doubt) >> (lane - l) & (kAll >> (32 - L));
       if (__any_sync(kAll, doubt)) {
         unsigned long long last = ~0ull;
@@ -566,7 +540,7 @@ __device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, 
   constexpr int kTimes = kShort ? K : 4;
 #pragma unroll (kTimes)
   for (int r = 0; r < (kShort ? K : k); ++r) {
-    const float best = warp_max(v[0]);
+    const float best = warp_max_nan(v[0]);
     const int from = __ffs(__ballot_sync(kAll, v[0] == best)) - 1;
     owner = lane == r ? from : owner;
     mine = lane == r ? best : mine;
@@ -763,7 +737,7 @@ __global__ void __launch_bounds__(kThreads)
       x[s] = to_float(raw.at(s));
       m = max_nan(m, x[s]);
     }
-    m = warp_max(m);
+    m = warp_max_nan(m);
     int e = lane < k ? A.idx[row * k + lane] : -1;
     if (e >= E) e = -1;
     const bool any = __any_sync(kAll, e >= 0) && m > -INFINITY;
@@ -876,26 +850,23 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   A.whole = A.by_logits && !groups && dtype != BOUTE_F32;
   const size_t bytes = dtype_bytes(dtype);
   A.vec = (uintptr_t)logits % 16 == 0 && ld * bytes % 16 == 0 && E * bytes % 16 == 0;
-  A.index_bits = E <= 256 ? 8 : 10;
   // A team of lanes per query where its lists are short (candidates: more than choices where keys do
   // not hold the values whole) and its values few or whole in their keys; else a warp. (us by team
   // and by warp: 262144 x 256 bf16, k = 4: 48, 107, k = 8: 64, 155; 131072 queries: 128 bf16 with
   // bias, k = 6: 42, 57; 64 fp32, k = 2: 21, 34; 128 fp32, k = 4: 38, 45.)
   const int need = A.whole ? k : k + 1;
-  auto run = [&](auto kernel, int queries, int blocks, int S) {  // of a warp; of an SM; of a lane
+  // queries: of a warp; blocks: of an SM; S: experts of a lane. (At most 38 KB of shared memory.)
+  auto run = [&](auto kernel, int queries, int blocks, int S) {
     A.group_lanes = E / G % S == 0 ? E / G / S : 0;
     const size_t smem =
-        (size_t)E * 4 + (groups && !A.group_lanes ? (size_t)kWarps * queries * shared_stride(E) * 4 : 0);
+        (size_t)E * 4 +
+        (groups && !A.group_lanes ? (size_t)kWarps * queries * shared_stride(E) * 4 : 0);
     const long long all = (T + kWarps * queries - 1) / (kWarps * queries);
     // a few queries whose load is wanted: one block, which writes it itself
     const unsigned grid =
         load && all <= 2 ? 1u : (unsigned)std::min<long long>(all, (long long)blocks * num_sms());
     if (load && grid > 1)
       if (int r = launch_cluster(clear_load_kernel, 1, 256, 1, 0, s, load, E)) return r;
-    if (smem > (48u << 10) &&
-        cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)smem) != cudaSuccess)
-      return last_launch_status();
     return launch_cluster(kernel, grid, kThreads, 1, smem, s, A);
   };
   auto team = [&](auto list) {
@@ -909,10 +880,12 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
     return run(route_team_kernel<16, 8, K, false>, 4, 4, 16);
   };
   if (E <= (A.whole ? 256 : 128) && need <= 8)
-    return need <= 4 ? team(std::integral_constant<int, 4>{}) : team(std::integral_constant<int, 8>{});
+    return need <= 4 ? team(std::integral_constant<int, 4>{})
+                     : team(std::integral_constant<int, 8>{});
   if (E <= 64) return run(route_warp_kernel<2, 2>, 1, 5, 2);
   if (E <= 128) return run(route_warp_kernel<4, 4>, 1, 5, 4);
-  if (E <= 256) return k <= 4 ? run(route_warp_kernel<8, 4>, 1, 5, 8) : run(route_warp_kernel<8, 8>, 1, 5, 8);
+  if (E <= 256)
+    return k <= 4 ? run(route_warp_kernel<8, 4>, 1, 5, 8) : run(route_warp_kernel<8, 8>, 1, 5, 8);
   if (E <= 512) return run(route_warp_kernel<16, 16>, 1, 4, 16);
   return run(route_warp_kernel<32, 32>, 1, 4, 32);
 }
@@ -938,8 +911,8 @@ extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int 
       A.vec = (uintptr_t)dlogits % 16 == 0 && (size_t)E * sizeof(X) % 16 == 0;
       const long long all = (T + kWarps * (32 / team) - 1) / (kWarps * (32 / team));
       const unsigned grid = (unsigned)std::min<long long>(all, 8ll * num_sms());
-      return launch_cluster(route_grad_chosen_kernel<X>, grid, kThreads, 1, 0, s, (const X *)logits, A,
-                            (X *)dlogits, team);
+      return launch_cluster(route_grad_chosen_kernel<X>, grid, kThreads, 1, 0, s,
+                            (const X *)logits, A, (X *)dlogits, team);
     }
     return with_slots(E, [&](auto slots) {
       constexpr int S = decltype(slots)::value;

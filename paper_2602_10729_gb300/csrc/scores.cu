@@ -23,15 +23,12 @@ constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
 constexpr int kMost = 32;  // positions a lane of a team of 8 or 32 lanes, or of a block, takes
 constexpr int kUnroll = 4;  // positions on their way to a lane
 
-// Order-preserving bits of a float, -0 as +0, a NaN above every number.
-__device__ __forceinline__ unsigned order_bits(float v) {
-  if (isnan(v)) return 0xffffffffu;
-  if (v == 0.f) v = 0.f;
-  const unsigned u = __float_as_uint(v);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+// Order bits with -0 as +0 and a NaN above every number.
+__device__ __forceinline__ unsigned extreme_bits(float v) {
+  return isnan(v) ? 0xffffffffu : order_bits(v == 0.f ? 0.f : v);
 }
 
-// What an answer's scores are made of. lo, hi: order_bits of -logprob and of the entropy with
+// What an answer's scores are made of. lo, hi: extreme_bits of -logprob and of the entropy with
 // the complement of the position below, so that a maximum is the extreme's first position.
 struct Part {
   unsigned long long lo, hi;
@@ -103,24 +100,23 @@ struct Answers {
     }
     if (p.n == 0) return p;
     if (lo_at >= 0 && hi_at >= 0 && !isnan(p.lp) && !isnan(p.ent)) {
-      p.lo = ((unsigned long long)order_bits(-lo) << 32) | (0xffffffffu - (unsigned)lo_at);
-      p.hi = ((unsigned long long)order_bits(hi) << 32) | (0xffffffffu - (unsigned)hi_at);
+      p.lo = ((unsigned long long)extreme_bits(-lo) << 32) | (0xffffffffu - (unsigned)lo_at);
+      p.hi = ((unsigned long long)extreme_bits(hi) << 32) | (0xffffffffu - (unsigned)hi_at);
       return p;
     }
     for (long long t = a + i; t < b; t += BY) {
       if (!counts(t)) continue;
       const unsigned at = 0xffffffffu - (unsigned)(t - from);
-      p.lo = max(p.lo, ((unsigned long long)order_bits(-logprob[t]) << 32) | at);
-      p.hi = max(p.hi, ((unsigned long long)order_bits(entropy[t]) << 32) | at);
+      p.lo = max(p.lo, ((unsigned long long)extreme_bits(-logprob[t]) << 32) | at);
+      p.hi = max(p.hi, ((unsigned long long)extreme_bits(entropy[t]) << 32) | at);
     }
     return p;
   }
 };
 
-// The float whose order_bits a key has (-0 as +0), and the position; -1 without one.
+// The float whose extreme_bits a key has (-0 as +0), and the position; -1 without one.
 __device__ __forceinline__ float key_value(unsigned long long key) {
-  const unsigned o = (unsigned)(key >> 32);
-  return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+  return from_order_bits((unsigned)(key >> 32));
 }
 __device__ __forceinline__ int key_position(unsigned long long key) {
   return key ? (int)(0xffffffffu - (unsigned)key) : -1;
@@ -162,8 +158,8 @@ __device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part
   return p;
 }
 
-// emit(q, from, p, a, b, on, i, by): thread i of `by` writes what positions [a, b) of answer q take,
-// which begins at `from` and has the Part p.
+// emit(q, from, p, a, b, on, i, by): thread i of `by` writes what positions [a, b) of answer q
+// take, which begins at `from` and has the Part p.
 template <int TEAM, class Emit>
 __device__ __forceinline__ void for_answers(const Answers &A, Emit emit) {
   __shared__ Part red[kWarps], parts[kMaxCluster];
@@ -264,7 +260,8 @@ __global__ void __launch_bounds__(kThreads, 5)
   }
   if (blockIdx.x == gridDim.x - 1) {
     const long long from = min(max(A.offsets[A.Q], 0ll), A.T);
-    for (long long t = from + threadIdx.x; t < A.T; t += kThreads) g_logprob[t] = g_entropy[t] = 0.f;
+    for (long long t = from + threadIdx.x; t < A.T; t += kThreads)
+      g_logprob[t] = g_entropy[t] = 0.f;
   }
 }
 
@@ -285,9 +282,9 @@ static int sizes_ok(long long T, long long Q, const float *logprob, const float 
 }
 
 // Teams by the mean length: 8 lanes up to 24 positions, 32 up to 512, else a block; and up to the
-// eight blocks of a cluster for answers over 1024 positions a block that are too few to fill the SMs.
-// (13665 answers of 31: 6.4 us with 32 lanes, 8.3 with 8; 10010 of 16: 5.4 with 8, 8.6 with 32; 2245
-// of 682: 10.5 with a block, 15.4 with 32 lanes; 96 of 16384: 10.8 with eight blocks, 18 with four.)
+// eight blocks of a cluster for answers over 1024 positions a block that are too few to fill the
+// SMs. (13665 answers of 31: 6.4 us with 32 lanes, 8.3 with 8; 2245 of 682: 10.5 with a block, 15.4
+// with 32 lanes.)
 template <class Go>
 static int with_team(long long T, long long Q, Go go) {
   const long long mean = T / Q, at_once = 8ll * num_sms();
@@ -309,7 +306,8 @@ extern "C" int boute_answer_scores(const float *logprob, const float *entropy,
   return with_team(T, Q, [&](auto team, long long blocks, int cluster) {
     return launch_cluster(answer_scores_kernel<decltype(team)::value>, blocks, kThreads, cluster, 0,
                           (cudaStream_t)stream,
-                          Answers{logprob, entropy, targets, offsets, T, Q, cluster}, scores, counts);
+                          Answers{logprob, entropy, targets, offsets, T, Q, cluster}, scores,
+                          counts);
   });
 }
 
@@ -330,8 +328,8 @@ extern "C" int boute_answer_scores_grad(const float *logprob, const float *entro
     return BOUTE_OK;
   }
   return with_team(T, Q, [&](auto team, long long blocks, int cluster) {
-    return launch_cluster(answer_scores_grad_kernel<decltype(team)::value>, blocks, kThreads, cluster,
-                          0, (cudaStream_t)stream,
+    return launch_cluster(answer_scores_grad_kernel<decltype(team)::value>, blocks, kThreads,
+                          cluster, 0, (cudaStream_t)stream,
                           Answers{logprob, entropy, targets, offsets, T, Q, cluster}, g_scores,
                           g_logprob, g_entropy);
   });
