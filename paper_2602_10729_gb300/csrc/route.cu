@@ -102,11 +102,54 @@ __device__ __forceinline__ void load_words(uint32_t *w, const void *row, int e0,
     }
   }
 }
-// Pairs of 16-bit logits with -0 as +0 (and NaNs as one).
-__device__ __forceinline__ uint32_t plus_zero(uint32_t w, int dtype) {
-  uint32_t r;
-  if (dtype == BOUTE_F16) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
-  else asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0u));
+// Pairs of 16-bit logits: f16 or bf16 by HALF.
+template <bool HALF>
+struct Pair {
+  uint32_t w;
+  static constexpr unsigned kInf = HALF ? 0x7c00u : 0x7f80u;
+  __device__ __forceinline__ Pair swapped() const { return {__byte_perm(w, 0u, 0x1032)}; }
+  // with -0 as +0 (and NaNs as one)
+  __device__ __forceinline__ Pair plus_zero() const {
+    Pair r;
+    if (HALF) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r.w) : "r"(w), "r"(0u));
+    else asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r.w) : "r"(w), "r"(0u));
+    return r;
+  }
+  // 0xffff where it is at least o
+  __device__ __forceinline__ uint32_t reaches(Pair o) const {
+    uint32_t r;
+    if (HALF) {
+      __half2 a, b;
+      memcpy(&a, &w, 4);
+      memcpy(&b, &o.w, 4);
+      r = __hge2_mask(a, b);
+    } else {
+      __nv_bfloat162 a, b;
+      memcpy(&a, &w, 4);
+      memcpy(&b, &o.w, 4);
+      r = __hge2_mask(a, b);
+    }
+    return r;
+  }
+  static __device__ __forceinline__ float value(unsigned u) {
+    return HALF ? __half2float(__ushort_as_half((unsigned short)u)) : __uint_as_float(u << 16);
+  }
+};
+using ::max;
+using ::min;
+// (a NaN wins in max, and is left behind by min)
+template <bool HALF>
+__device__ __forceinline__ Pair<HALF> max(Pair<HALF> a, Pair<HALF> b) {
+  Pair<HALF> r;
+  if (HALF) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r.w) : "r"(a.w), "r"(b.w));
+  else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r.w) : "r"(a.w), "r"(b.w));
+  return r;
+}
+template <bool HALF>
+__device__ __forceinline__ Pair<HALF> min(Pair<HALF> a, Pair<HALF> b) {
+  Pair<HALF> r;
+  if (HALF) asm("min.f16x2 %0, %1, %2;" : "=r"(r.w) : "r"(a.w), "r"(b.w));
+  else asm("min.bf16x2 %0, %1, %2;" : "=r"(r.w) : "r"(a.w), "r"(b.w));
   return r;
 }
 
@@ -171,6 +214,44 @@ __device__ __forceinline__ void best_of(unsigned (&c)[S], unsigned (&best)[K]) {
     for (int i = 0; i < K; ++i) best[i] = max(best[i], other[i]);
     merge_desc<K>(best);
   }
+}
+
+// A value that K of a query's logits reach, and few others, and its largest one, each in both halves;
+// of the team of 8 lanes with N pairs each. It is the K-th largest of 4 K parts' maxima, K / 2 parts
+// to a lane, whose lists join lane by lane (two lists of halves at once).
+template <int N, int K, bool HALF>
+__device__ __forceinline__ Pair<HALF> bound_of(const Pair<HALF> (&w)[N], Pair<HALF> &top) {
+  constexpr int kParts = K / 4;
+  Pair<HALF> a[K], other[K];
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    a[i] = w[i];
+#pragma unroll
+    for (int s = i + kParts; s < N; s += kParts) a[i] = max(a[i], w[s]);
+  }
+  sort_desc<kParts>(a);
+#pragma unroll
+  for (int o = 1, n = kParts; o < 8; o *= 2) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) other[i].w = __shfl_xor_sync(kAll, a[n - 1 - i].w, o);
+    if (n < K) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) a[n + i] = other[i];
+      n *= 2;
+      if (n == 2) merge_desc<2>(a);
+      if (n == 4) merge_desc<4>(a);
+      if (n == 8) merge_desc<8>(a);
+    } else {
+#pragma unroll
+      for (int i = 0; i < K; ++i) a[i] = max(a[i], other[i]);
+      merge_desc<K>(a);
+    }
+  }
+  top = max(a[0], a[0].swapped());
+  Pair<HALF> bound = max(a[0], a[K - 1].swapped());
+#pragma unroll
+  for (int i = 1; i < K; ++i) bound = min(bound, max(a[i], a[K - 1 - i].swapped()));
+  return bound;
 }
 
 // The two largest of two pairs a >= b.
@@ -373,13 +454,21 @@ __device__ __forceinline__ void end_load(const RouteArgs &A, const int *hist) {
     else if (hist[e]) atomicAdd(A.load + e, hist[e]);
 }
 
-// WHOLE: keys hold the values whole (16-bit logits compared as they are, no groups).
-template <int S, int L, int K, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, 4)
-    route_team_kernel(RouteArgs A) {
+// What a team's keys hold: parts of fp32 values, or 16-bit logits whole (no bias, no groups).
+enum Keys { kParts, kHalf, kBfloat };
+
+template <int S, int L, int K, Keys KEYS>
+__global__ void __launch_bounds__(kThreads, 4) route_team_kernel(RouteArgs A) {
+  constexpr bool WHOLE = KEYS != kParts;
+  // Where a lane's logits are many against its list, those that reach a bound are ranked alone (two
+  // comparisons to an instruction; 262144 queries of 256, k = 4: 35 us, all as keys 48, k = 8: 51
+  // and 64; but 131072 of 64, k = 8: 23 and 17). All as keys also where more than two lists reach
+  // it (many equal ones).
+  constexpr bool BOUND = WHOLE && S >= 4 * K;
   constexpr unsigned kLow = 127u;  // the experts' bits of a key that holds a part of a value
   static_assert(WHOLE || S * L <= 128, "experts of such keys");
-  constexpr int kTeams = 32 / L, kOwn = (K + L - 1) / L;  // queries of a warp; a lane's candidates
+  // queries of a warp; a lane's candidates
+  constexpr int kTeams = 32 / L, kOwn = BOUND ? K / 4 : (K + L - 1) / L;
   extern __shared__ int hist[];  // the block's load; then, with groups, c and the groups' scores
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, l = lane % L, e0 = l * S;
   const int per = E / A.G;
@@ -392,54 +481,106 @@ __global__ void __launch_bounds__(kThreads, 4)
     // (a team beyond the last query repeats the last, and writes nothing)
     const bool live = row0 + lane / L < A.rows;
     const long long row = min(row0 + lane / L, A.rows - 1);
-    unsigned best[K], c[S];
     int e[kOwn], place[kOwn];  // candidates l, l + L .., and their ranks
     float x[kOwn];             // their logits
     Query q = {-INFINITY, 1.f, false};
     if constexpr (WHOLE) {
-      // order bits of pairs of logits, each over its expert's complement; a NaN is largest, +inf
-      // next, -inf (and what is beyond E) smallest
-      const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX, half = A.dtype == BOUTE_F16;
-      const unsigned inf = half ? 0xfc00u : 0xff80u;
-      uint32_t w[S / 2];
-      load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, E, A.vec,
-                           half ? 0xfc00fc00u : 0xff80ff80u);
-      const unsigned below = (0xffffu - e0) | (0xffffu - e0 - 1u) << 16;
-#pragma unroll
-      for (int i = 0; i < S / 2; ++i) {
-        const uint32_t v = plus_zero(w[i], A.dtype);
-        const uint32_t o = v ^ (((v >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
-        c[2 * i] = __byte_perm(o, below - 0x00020002u * i, 0x1054);
-        c[2 * i + 1] = __byte_perm(o, below - 0x00020002u * i, 0x3276);
-      }
-      best_of<S, L, K>(c, best);
-      auto value = [&](unsigned key) {
-        const unsigned o = key >> 16, u = o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu;
-        return half ? __half2float(__ushort_as_half((unsigned short)u)) : __uint_as_float(u << 16);
+      constexpr bool HALF = KEYS == kHalf;
+      using P = Pair<HALF>;
+      constexpr unsigned inf = P::kInf, kSlots = L * kOwn;
+      auto value = [](unsigned key) {
+        const unsigned o = key >> 16;
+        return P::value(o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu);
       };
-      q.bad = best[0] >> 16 > inf || (soft && best[0] >> 16 == inf);
-      q.m = value(best[0]);
+      __shared__ unsigned keys[kWarps * kTeams][kSlots];
+      const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
+      const unsigned short *logits = (const unsigned short *)A.logits + row * A.ld;
+      P w[S / 2], top;
+      {
+        uint32_t v[S / 2];
+        load_words<S / 2, 2>(v, logits, e0, E, A.vec, (inf | 0x8000u) * 0x10001u);
+#pragma unroll
+        for (int i = 0; i < S / 2; ++i) w[i].w = v[i];
+      }
+      // keys: order bits (-0 as +0) over the expert's complement: equal values go to the lowest index
+      unsigned hit = 0u, key[kOwn];
+      int n = kSlots + 1, mine = 0, upto = 0;
+      if constexpr (BOUND) {
+        // a bound that K reach, of finite values: which of this lane's logits do (of its pair i
+        // bits i and 16 + i)
+        const P lowest = {((inf | 0x8000u) - 1u) * 0x10001u};
+        const P bound = max(bound_of<S / 2, K>(w, top), lowest);
+        q.m = P::value(top.w & 0xffffu);
+#pragma unroll
+        for (int i = 0; i < S / 2; ++i) hit |= w[i].reaches(bound) & 0x00010001u << i;
+        upto = mine = __popc(hit);
+#pragma unroll
+        for (int o = 1; o < L; o *= 2) {
+          const int v = __shfl_up_sync(kAll, upto, o, L);
+          upto += l >= o ? v : 0;
+        }
+        n = __shfl_sync(kAll, upto, L - 1, L);
+      }
+      if (BOUND && !__any_sync(kAll, n > (int)kSlots)) {
+        unsigned *to = keys[warp * kTeams + lane / L];
+        for (int at = upto - mine; hit; ++at) {
+          const int b = __ffs(hit) - 1, index = e0 + 2 * (b & 15) + (b >> 4);
+          hit &= hit - 1u;
+          unsigned u = logits[index];
+          if (u == 0x8000u) u = 0u;
+          u ^= u & 0x8000u ? 0xffffu : 0x8000u;
+          to[at] = u << 16 | (0xffffu - (unsigned)index);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) key[j] = l + j * L < n ? to[l + j * L] : 0u;
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) place[j] = key[j] ? 0 : l + j * L;
+#pragma unroll
+        for (int i = 0; i < (int)kSlots; ++i) {
+          const unsigned o = __shfl_sync(kAll, key[i / L], i % L, L);
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j) place[j] += key[j] != 0u && o > key[j];
+        }
+      } else {  // all as keys; a NaN is largest, +inf next, -inf smallest
+        unsigned c[S], best[K];
+        const unsigned below = (0xffffu - e0) | (0xffffu - e0 - 1u) << 16;
+#pragma unroll
+        for (int i = 0; i < S / 2; ++i) {
+          const uint32_t v = w[i].plus_zero().w;
+          const uint32_t o = v ^ (((v >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
+          c[2 * i] = __byte_perm(o, below - 0x00020002u * i, 0x1054);
+          c[2 * i + 1] = __byte_perm(o, below - 0x00020002u * i, 0x3276);
+        }
+        best_of<S, L, K>(c, best);
+        if (!BOUND) q.m = value(best[0]);
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+          key[j] = 0u;
+#pragma unroll
+          for (int i = j * L; i < K && i < (j + 1) * L; ++i)
+            key[j] = l == i - j * L ? best[i] : key[j];
+          if (key[j] >> 16 <= (0x7fffu ^ inf)) key[j] = 0u;  // -inf
+          place[j] = l + j * L;
+        }
+      }
+      q.bad = isnan(q.m) || (soft && q.m == INFINITY);
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) {
-        unsigned mine = 0u;
-#pragma unroll
-        for (int i = j * L; i < K && i < (j + 1) * L; ++i) mine = l == i - j * L ? best[i] : mine;
-        place[j] = l + j * L;
-        e[j] = !q.bad && mine >> 16 > (0xffffu ^ inf) ? (int)(0xffffu - (mine & 0xffffu)) : -1;
-        x[j] = value(mine);
+        e[j] = key[j] && !q.bad ? (int)(0xffffu - (key[j] & 0xffffu)) : -1;
+        x[j] = value(key[j]);
       }
       if (soft && !A.renorm) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < S / 2; ++i) {
-          float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
-          if (half) unpack_f16x2(w[i], a, b);
-          sum += exp2_fast((a - q.m) * kLog2e) + exp2_fast((b - q.m) * kLog2e);
-        }
+        for (int i = 0; i < S / 2; ++i)
+          sum += exp2_fast((P::value(w[i].w & 0xffffu) - q.m) * kLog2e) +
+                 exp2_fast((P::value(w[i].w >> 16) - q.m) * kLog2e);
         q.inv_sum = __fdividef(1.f, team_sum<L>(sum));
       }
     } else {
-      unsigned kept = kAll;
+      unsigned best[K], c[S], kept = kAll;
       {
         float v[S], b[S];
         load_bias(A, e0, b);
@@ -871,13 +1012,17 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   };
   auto team = [&](auto list) {
     constexpr int K = decltype(list)::value;
-    if (A.whole) {
-      if (E <= 64) return run(route_team_kernel<8, 8, K, true>, 4, 4, 8);
-      if (E <= 128) return run(route_team_kernel<16, 8, K, true>, 4, 4, 16);
-      return run(route_team_kernel<32, 8, K, true>, 4, 4, 32);
-    }
-    if (E <= 64) return run(route_team_kernel<8, 8, K, false>, 4, 4, 8);
-    return run(route_team_kernel<16, 8, K, false>, 4, 4, 16);
+    auto whole = [&](auto keys) {
+      constexpr Keys KEYS = decltype(keys)::value;
+      if (E <= 64) return run(route_team_kernel<8, 8, K, KEYS>, 4, 4, 8);
+      if (E <= 128) return run(route_team_kernel<16, 8, K, KEYS>, 4, 4, 16);
+      return run(route_team_kernel<32, 8, K, KEYS>, 4, 4, 32);
+    };
+    if (A.whole)
+      return dtype == BOUTE_F16 ? whole(std::integral_constant<Keys, kHalf>{})
+                                : whole(std::integral_constant<Keys, kBfloat>{});
+    if (E <= 64) return run(route_team_kernel<8, 8, K, kParts>, 4, 4, 8);
+    return run(route_team_kernel<16, 8, K, kParts>, 4, 4, 16);
   };
   if (E <= (A.whole ? 256 : 128) && need <= 8)
     return need <= 4 ? team(std::integral_constant<int, 4>{})
