@@ -2,23 +2,22 @@
 // the weights and the load; and the gradient of the weights.
 //
 // Arithmetic bounds it: a query's logits are one or two lines, its choice some hundred
-// instructions. So as little as possible is compared, and in one word where it fits:
-//  - Teams of 8 lanes to a query, four queries to a warp, lane l with the S experts l S ..
-//    l S + S - 1. Experts are compared as 32-bit keys: the upper bits of the order bits of
-//    c, and the expert's complement below, so that equal values go to the lowest index. Each
-//    lane sorts its K largest keys in registers; the lanes' lists join two by two, of which
-//    three steps leave the query's K best in every lane. 16-bit logits that are compared as
-//    they are (no bias, no groups) fit a key whole. Of other values a key holds 25 bits:
-//    K > k candidates are ranked by their exact values, and a query whose last candidate
-//    shares the k-th's upper bits (one in thousands, or equal values) is chosen again by
-//    exact values alone.
-//  - A warp to a query for longer lists and more experts: each lane sorts its own, and k
-//    rounds take the largest of the 32 heads.
+// instructions. So as little as possible is compared:
+//  - Teams of 8 lanes to a query, four queries to a warp, take up to 8 of up to 256 experts.
+//    Each lane's values are parts, 4 K in all, whose maxima's K-th largest is a bound that K
+//    values reach, and few others; those alone become keys (order bits over the expert's
+//    complement, so that equal values go to the lowest index) and are ranked. 16-bit logits
+//    that are compared as they are (no bias, no groups) stay as pairs, two to an instruction;
+//    where they are few to a lane, all of them become keys, whole in 32 bits, of which each
+//    lane sorts its K largest and the lanes' lists join two by two.
+//  - A warp to a query for more choices, more experts, and too few queries to fill the SMs:
+//    each lane sorts its own, and k rounds take the largest of the 32 heads.
 // Without a bias the logits themselves are compared, which have the order of the scores:
 // only the chosen scores are computed then, and a softmax's sum only where the weights are
-// not renormalised. 262144 queries of 256 bf16 logits, k = 4: 48 us (2.9 TB/s; a floor of 21;
-// the arithmetic units are 79 % busy); 131072 of 192, logistic with bias, 8 groups, k = 6: 99.
+// not renormalised. 262144 queries of 256 bf16 logits, k = 4: 35 us (4.1 TB/s; a floor of
+// 21); 131072 of 256, logistic with bias, k = 4: 37, in 8 groups with k = 8: 63.
 // The gradient moves bytes: 131072 queries of 160 fp32, k = 6: 26.3 us where they take 25.7.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -56,8 +55,8 @@ struct RouteArgs {
   const float *bias;
   int dtype, E, mode, G, keep, group_top, k, renorm;
   int by_logits;  // the logits are compared
-  int whole;      // and fit a key whole (16-bit logits, no groups)
   int vec;        // rows on 16-byte boundaries, E a multiple of a vector's logits
+  int own;  // experts of a lane (route_bound_kernel)
   int group_lanes; // lanes that hold a group, where each holds experts of one; else 0
   float factor;
   int *idx, *load;
@@ -216,24 +215,19 @@ __device__ __forceinline__ void best_of(unsigned (&c)[S], unsigned (&best)[K]) {
   }
 }
 
-// A value that K of a query's logits reach, and few others, and its largest one, each in both halves;
-// of the team of 8 lanes with N pairs each. It is the K-th largest of 4 K parts' maxima, K / 2 parts
-// to a lane, whose lists join lane by lane (two lists of halves at once).
-template <int N, int K, bool HALF>
-__device__ __forceinline__ Pair<HALF> bound_of(const Pair<HALF> (&w)[N], Pair<HALF> &top) {
-  constexpr int kParts = K / 4;
-  Pair<HALF> a[K], other[K];
+template <bool HALF>
+__device__ __forceinline__ Pair<HALF> other_lane(Pair<HALF> v, int o) {
+  return {__shfl_xor_sync(kAll, v.w, o)};
+}
+__device__ __forceinline__ float other_lane(float v, int o) { return __shfl_xor_sync(kAll, v, o); }
+// The K largest in order of 8 lanes' lists of FROM in order, in every lane.
+template <int FROM, int K, class V>
+__device__ __forceinline__ void join_lanes(V (&a)[K]) {
+  V other[K];
 #pragma unroll
-  for (int i = 0; i < kParts; ++i) {
-    a[i] = w[i];
+  for (int o = 1, n = FROM; o < 8; o *= 2) {
 #pragma unroll
-    for (int s = i + kParts; s < N; s += kParts) a[i] = max(a[i], w[s]);
-  }
-  sort_desc<kParts>(a);
-#pragma unroll
-  for (int o = 1, n = kParts; o < 8; o *= 2) {
-#pragma unroll
-    for (int i = 0; i < n; ++i) other[i].w = __shfl_xor_sync(kAll, a[n - 1 - i].w, o);
+    for (int i = 0; i < n; ++i) other[i] = other_lane(a[n - 1 - i], o);
     if (n < K) {
 #pragma unroll
       for (int i = 0; i < n; ++i) a[n + i] = other[i];
@@ -247,11 +241,52 @@ __device__ __forceinline__ Pair<HALF> bound_of(const Pair<HALF> (&w)[N], Pair<HA
       merge_desc<K>(a);
     }
   }
+}
+// A value that K of the team's values reach, N in each of its 8 lanes, and few others: the K-th
+// largest of 4 K parts' maxima, K / 2 parts to a lane.
+template <int K, int N>
+__device__ __forceinline__ float bound_of(const float (&v)[N]) {
+  constexpr int kOf = K / 2;
+  float a[K];
+#pragma unroll
+  for (int i = 0; i < kOf; ++i) {
+    a[i] = v[i];
+#pragma unroll
+    for (int s = i + kOf; s < N; s += kOf) a[i] = fmaxf(a[i], v[s]);
+  }
+  sort_desc<kOf>(a);
+  join_lanes<kOf>(a);
+  return a[K - 1];
+}
+// The same of pairs, two lists of halves at once; the bound and the largest value in both halves.
+template <int K, int N, bool HALF>
+__device__ __forceinline__ Pair<HALF> bound_of(const Pair<HALF> (&w)[N], Pair<HALF> &top) {
+  constexpr int kOf = K / 4;
+  Pair<HALF> a[K];
+#pragma unroll
+  for (int i = 0; i < kOf; ++i) {
+    a[i] = w[i];
+#pragma unroll
+    for (int s = i + kOf; s < N; s += kOf) a[i] = max(a[i], w[s]);
+  }
+  sort_desc<kOf>(a);
+  join_lanes<kOf>(a);
   top = max(a[0], a[0].swapped());
   Pair<HALF> bound = max(a[0], a[K - 1].swapped());
 #pragma unroll
   for (int i = 1; i < K; ++i) bound = min(bound, max(a[i], a[K - 1 - i].swapped()));
   return bound;
+}
+// Of the team's 8 lanes, how many of their hits precede lane l's (which has `mine`), and all of them.
+__device__ __forceinline__ int hits_before(int mine, int l, int &all) {
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 8; o *= 2) {
+    const int v = __shfl_up_sync(kAll, upto, o, 8);
+    upto += l >= o ? v : 0;
+  }
+  all = __shfl_sync(kAll, upto, 7, 8);
+  return upto - mine;
 }
 
 // The two largest of two pairs a >= b.
@@ -332,6 +367,27 @@ __host__ __device__ inline int shared_stride(int E) {
   return round_up(E + BOUTE_MAX_GROUPS, 32) + 2;
 }
 
+// -inf for the lane's experts [e0, end) in groups that do not stay; shared: a query's
+// shared_stride(E) floats where lanes hold experts of several groups.
+template <int S, int L>
+__device__ __forceinline__ void apply_groups(const RouteArgs &A, float (&c)[S], float *shared,
+                                             int e0, int end, int l) {
+  if (A.keep == A.G) return;
+  if (A.group_lanes) {
+    const bool kept = keeps_lane<S, L>(c, A, l);
+#pragma unroll
+    for (int s = 0; s < S; ++s) c[s] = kept ? c[s] : -INFINITY;
+    return;
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+    if (e0 + s < end) shared[e0 + s] = c[s];
+  __syncwarp();
+  const unsigned kept = keep_groups<L>(shared, shared + A.E, A, A.E / A.G, l);
+  __syncwarp();
+  drop_groups(c, kept, e0, A.E / A.G);
+}
+
 // What a query's choice among its experts is made of, for a team of L lanes.
 struct Query {
   float m, inv_sum;  // of the softmax
@@ -356,18 +412,18 @@ __device__ __forceinline__ void load_bias(const RouteArgs &A, int e0, float (&bi
   for (int s = 0; s < S; ++s)
     bias[s] = A.bias && e0 + s < A.E ? fmaxf(A.bias[e0 + s], -INFINITY) : 0.f;  // (no NaN)
 }
-template <int S, int L>
-__device__ __forceinline__ Query load_query(const RouteArgs &A, long long row, int e0,
-                                            const float (&bias)[S], float (&c)[S]) {
-  const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
+// The lane's logits from e0 on, -inf from `end` on.
+template <int S>
+__device__ __forceinline__ void load_logits(const RouteArgs &A, long long row, int e0, int end,
+                                            float (&c)[S]) {
   if (A.dtype == BOUTE_F32) {
     uint32_t w[S];
-    load_words<S, 1>(w, (const float *)A.logits + row * A.ld, e0, A.E, A.vec, 0xff800000u);
+    load_words<S, 1>(w, (const float *)A.logits + row * A.ld, e0, end, A.vec, 0xff800000u);
 #pragma unroll
     for (int s = 0; s < S; ++s) c[s] = __uint_as_float(w[s]);
   } else {
     uint32_t w[S / 2];
-    load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, A.E, A.vec,
+    load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, end, A.vec,
                          A.dtype == BOUTE_F16 ? 0xfc00fc00u : 0xff80ff80u);
 #pragma unroll
     for (int i = 0; i < S / 2; ++i)
@@ -378,6 +434,11 @@ __device__ __forceinline__ Query load_query(const RouteArgs &A, long long row, i
         c[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
       }
   }
+}
+// A query's statistics, and c of the lane's S logits in their place; bias(s): of the s-th.
+template <int S, int L, class Bias>
+__device__ __forceinline__ Query score_query(const RouteArgs &A, Bias bias, float (&c)[S]) {
+  const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
   Query q = {-INFINITY, 1.f, false};
 #pragma unroll
   for (int s = 0; s < S; ++s) q.m = max_nan(q.m, c[s]);
@@ -403,12 +464,12 @@ __device__ __forceinline__ Query load_query(const RouteArgs &A, long long row, i
 #pragma unroll
       for (int s = 0; s < S; ++s)
         c[s] = c[s] > -INFINITY && !q.bad
-                   ? __fadd_rn(exp2_fast((c[s] - q.m) * kLog2e) * q.inv_sum, bias[s])
+                   ? __fadd_rn(exp2_fast((c[s] - q.m) * kLog2e) * q.inv_sum, bias(s))
                    : -INFINITY;
     else
 #pragma unroll
       for (int s = 0; s < S; ++s)
-        c[s] = c[s] > -INFINITY && !q.bad ? __fadd_rn(logistic(c[s]), bias[s]) : -INFINITY;
+        c[s] = c[s] > -INFINITY && !q.bad ? __fadd_rn(logistic(c[s]), bias(s)) : -INFINITY;
   }
   return q;
 }
@@ -454,26 +515,46 @@ __device__ __forceinline__ void end_load(const RouteArgs &A, const int *hist) {
     else if (hist[e]) atomicAdd(A.load + e, hist[e]);
 }
 
-// What a team's keys hold: parts of fp32 values, or 16-bit logits whole (no bias, no groups).
-enum Keys { kParts, kHalf, kBfloat };
+// A team's n <= 8 OWN keys (all different, in its part of shared memory, any order) in order: lane l
+// has those of places l, l + 8 .. (0: none), whatever the warp's other teams do.
+template <int OWN, class Key>
+__device__ __forceinline__ void in_order(Key *to, int n, int l, Key (&key)[OWN],
+                                         int (&place)[OWN]) {
+  __syncwarp();
+  int rank[OWN];
+#pragma unroll
+  for (int j = 0; j < OWN; ++j) {
+    place[j] = l + j * 8;
+    key[j] = place[j] < n ? to[place[j]] : Key(0);
+    rank[j] = 0;
+  }
+#pragma unroll
+  for (int i = 0; i < 8 * OWN; ++i) {
+    const Key o = __shfl_sync(kAll, key[i / 8], i % 8, 8);
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) rank[j] += o > key[j];
+  }
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < OWN; ++j)
+    if (place[j] < n) to[rank[j]] = key[j];
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < OWN; ++j) key[j] = place[j] < n ? to[place[j]] : Key(0);
+  __syncwarp();
+}
 
-template <int S, int L, int K, Keys KEYS>
-__global__ void __launch_bounds__(kThreads, 4) route_team_kernel(RouteArgs A) {
-  constexpr bool WHOLE = KEYS != kParts;
-  // Where a lane's logits are many against its list, those that reach a bound are ranked alone (two
-  // comparisons to an instruction; 262144 queries of 256, k = 4: 35 us, all as keys 48, k = 8: 51
-  // and 64; but 131072 of 64, k = 8: 23 and 17). All as keys also where more than two lists reach
-  // it (many equal ones).
-  constexpr bool BOUND = WHOLE && S >= 4 * K;
-  constexpr unsigned kLow = 127u;  // the experts' bits of a key that holds a part of a value
-  static_assert(WHOLE || S * L <= 128, "experts of such keys");
+// 16-bit logits, compared as they are.
+template <int S, int K, bool HALF>
+__global__ void __launch_bounds__(kThreads, 4) route_pairs_kernel(RouteArgs A) {
+  // Where a lane's logits are many against its list, those that reach a bound are ranked alone
+  // (262144 queries of 256, k = 4: 35 us, all as keys 48, k = 8: 51 and 64; but 131072 of 64,
+  // k = 8: 23 and 17). All as keys also where more than two lists reach it (many equal ones).
+  constexpr bool BOUND = S >= 4 * K;
   // queries of a warp; a lane's candidates
-  constexpr int kTeams = 32 / L, kOwn = BOUND ? K / 4 : (K + L - 1) / L;
-  extern __shared__ int hist[];  // the block's load; then, with groups, c and the groups' scores
+  constexpr int L = 8, kTeams = 32 / L, kOwn = BOUND ? K / 4 : (K + L - 1) / L;
+  extern __shared__ int hist[];  // the block's load
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, l = lane % L, e0 = l * S;
-  const int per = E / A.G;
-  const bool groups = A.keep < A.G;
-  float *shared_c = (float *)(hist + E) + (warp * kTeams + lane / L) * shared_stride(E);
   begin_load(A, hist);
   const long long step = (long long)gridDim.x * kWarps * kTeams;
   for (long long row0 = ((long long)blockIdx.x * kWarps + warp) * kTeams; row0 < A.rows;
@@ -484,180 +565,161 @@ __global__ void __launch_bounds__(kThreads, 4) route_team_kernel(RouteArgs A) {
     int e[kOwn], place[kOwn];  // candidates l, l + L .., and their ranks
     float x[kOwn];             // their logits
     Query q = {-INFINITY, 1.f, false};
-    if constexpr (WHOLE) {
-      constexpr bool HALF = KEYS == kHalf;
-      using P = Pair<HALF>;
-      constexpr unsigned inf = P::kInf, kSlots = L * kOwn;
-      auto value = [](unsigned key) {
-        const unsigned o = key >> 16;
-        return P::value(o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu);
-      };
-      __shared__ unsigned keys[kWarps * kTeams][kSlots];
-      const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
-      const unsigned short *logits = (const unsigned short *)A.logits + row * A.ld;
-      P w[S / 2], top;
-      {
-        uint32_t v[S / 2];
-        load_words<S / 2, 2>(v, logits, e0, E, A.vec, (inf | 0x8000u) * 0x10001u);
+    using P = Pair<HALF>;
+    constexpr unsigned inf = P::kInf, kSlots = L * kOwn;
+    auto value = [](unsigned key) {
+      const unsigned o = key >> 16;
+      return P::value(o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu);
+    };
+    __shared__ unsigned keys[kWarps * kTeams][kSlots];
+    const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
+    const unsigned short *logits = (const unsigned short *)A.logits + row * A.ld;
+    P w[S / 2], top;
+    {
+      uint32_t v[S / 2];
+      load_words<S / 2, 2>(v, logits, e0, E, A.vec, (inf | 0x8000u) * 0x10001u);
 #pragma unroll
-        for (int i = 0; i < S / 2; ++i) w[i].w = v[i];
+      for (int i = 0; i < S / 2; ++i) w[i].w = v[i];
+    }
+    // keys: order bits (-0 as +0) over the expert's complement: equal values go to the lowest index
+    unsigned hit = 0u, key[kOwn];
+    int n = kSlots + 1, first = 0;
+    if constexpr (BOUND) {
+      // a bound that K reach, of finite values: which of this lane's logits do (of its pair i
+      // bits i and 16 + i)
+      const P lowest = {((inf | 0x8000u) - 1u) * 0x10001u};
+      const P bound = max(bound_of<K>(w, top), lowest);
+      q.m = P::value(top.w & 0xffffu);
+#pragma unroll
+      for (int i = 0; i < S / 2; ++i) hit |= w[i].reaches(bound) & 0x00010001u << i;
+      first = hits_before(__popc(hit), l, n);
+    }
+    if (BOUND && !__any_sync(kAll, n > (int)kSlots)) {
+      unsigned *to = keys[warp * kTeams + lane / L];
+      for (int at = first; hit; ++at) {
+        const int b = __ffs(hit) - 1, index = e0 + 2 * (b & 15) + (b >> 4);
+        hit &= hit - 1u;
+        unsigned u = logits[index];
+        if (u == 0x8000u) u = 0u;
+        u ^= u & 0x8000u ? 0xffffu : 0x8000u;
+        to[at] = u << 16 | (0xffffu - (unsigned)index);
       }
-      // keys: order bits (-0 as +0) over the expert's complement: equal values go to the lowest index
-      unsigned hit = 0u, key[kOwn];
-      int n = kSlots + 1, mine = 0, upto = 0;
-      if constexpr (BOUND) {
-        // a bound that K reach, of finite values: which of this lane's logits do (of its pair i
-        // bits i and 16 + i)
-        const P lowest = {((inf | 0x8000u) - 1u) * 0x10001u};
-        const P bound = max(bound_of<S / 2, K>(w, top), lowest);
-        q.m = P::value(top.w & 0xffffu);
+      in_order<kOwn>(to, n, l, key, place);
+    } else {  // all as keys; a NaN is largest, +inf next, -inf smallest
+      unsigned c[S], best[K];
+      const unsigned below = (0xffffu - e0) | (0xffffu - e0 - 1u) << 16;
 #pragma unroll
-        for (int i = 0; i < S / 2; ++i) hit |= w[i].reaches(bound) & 0x00010001u << i;
-        upto = mine = __popc(hit);
-#pragma unroll
-        for (int o = 1; o < L; o *= 2) {
-          const int v = __shfl_up_sync(kAll, upto, o, L);
-          upto += l >= o ? v : 0;
-        }
-        n = __shfl_sync(kAll, upto, L - 1, L);
-      }
-      if (BOUND && !__any_sync(kAll, n > (int)kSlots)) {
-        unsigned *to = keys[warp * kTeams + lane / L];
-        for (int at = upto - mine; hit; ++at) {
-          const int b = __ffs(hit) - 1, index = e0 + 2 * (b & 15) + (b >> 4);
-          hit &= hit - 1u;
-          unsigned u = logits[index];
-          if (u == 0x8000u) u = 0u;
-          u ^= u & 0x8000u ? 0xffffu : 0x8000u;
-          to[at] = u << 16 | (0xffffu - (unsigned)index);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < kOwn; ++j) key[j] = l + j * L < n ? to[l + j * L] : 0u;
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < kOwn; ++j) place[j] = key[j] ? 0 : l + j * L;
-#pragma unroll
-        for (int i = 0; i < (int)kSlots; ++i) {
-          const unsigned o = __shfl_sync(kAll, key[i / L], i % L, L);
-#pragma unroll
-          for (int j = 0; j < kOwn; ++j) place[j] += key[j] != 0u && o > key[j];
-        }
-      } else {  // all as keys; a NaN is largest, +inf next, -inf smallest
-        unsigned c[S], best[K];
-        const unsigned below = (0xffffu - e0) | (0xffffu - e0 - 1u) << 16;
-#pragma unroll
-        for (int i = 0; i < S / 2; ++i) {
-          const uint32_t v = w[i].plus_zero().w;
-          const uint32_t o = v ^ (((v >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
-          c[2 * i] = __byte_perm(o, below - 0x00020002u * i, 0x1054);
-          c[2 * i + 1] = __byte_perm(o, below - 0x00020002u * i, 0x3276);
-        }
-        best_of<S, L, K>(c, best);
-        if (!BOUND) q.m = value(best[0]);
-#pragma unroll
-        for (int j = 0; j < kOwn; ++j) {
-          key[j] = 0u;
-#pragma unroll
-          for (int i = j * L; i < K && i < (j + 1) * L; ++i)
-            key[j] = l == i - j * L ? best[i] : key[j];
-          if (key[j] >> 16 <= (0x7fffu ^ inf)) key[j] = 0u;  // -inf
-          place[j] = l + j * L;
-        }
-      }
-      q.bad = isnan(q.m) || (soft && q.m == INFINITY);
-#pragma unroll
-      for (int j = 0; j < kOwn; ++j) {
-        e[j] = key[j] && !q.bad ? (int)(0xffffu - (key[j] & 0xffffu)) : -1;
-        x[j] = value(key[j]);
-      }
-      if (soft && !A.renorm) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < S / 2; ++i)
-          sum += exp2_fast((P::value(w[i].w & 0xffffu) - q.m) * kLog2e) +
-                 exp2_fast((P::value(w[i].w >> 16) - q.m) * kLog2e);
-        q.inv_sum = __fdividef(1.f, team_sum<L>(sum));
-      }
-    } else {
-      unsigned best[K], c[S], kept = kAll;
-      {
-        float v[S], b[S];
-        load_bias(A, e0, b);
-        q = load_query<S, L>(A, row, e0, b, v);
-        if (groups && A.group_lanes) {
-          kept = keeps_lane<S, L>(v, A, l) ? kAll : 0u;
-#pragma unroll
-          for (int s = 0; s < S; ++s) v[s] = kept ? v[s] : -INFINITY;
-        } else if (groups) {
-#pragma unroll
-          for (int s = 0; s < S; ++s)
-            if (e0 + s < E) shared_c[e0 + s] = v[s];
-          __syncwarp();
-          kept = keep_groups<L>(shared_c, shared_c + E, A, per, l);
-          __syncwarp();
-          drop_groups(v, kept, e0, per);
-        }
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-          const float u = v[s] == 0.f ? 0.f : v[s];
-          c[s] = u > -INFINITY ? (order_bits(u) & ~kLow) | (kLow - (unsigned)(e0 + s)) : 0u;
-        }
+      for (int i = 0; i < S / 2; ++i) {
+        const uint32_t v = w[i].plus_zero().w;
+        const uint32_t o = v ^ (((v >> 15 & 0x00010001u) * 0x7fffu) | 0x80008000u);
+        c[2 * i] = __byte_perm(o, below - 0x00020002u * i, 0x1054);
+        c[2 * i + 1] = __byte_perm(o, below - 0x00020002u * i, 0x3276);
       }
       best_of<S, L, K>(c, best);
-      // the candidates' exact values, and their ranks (the list has equal ones in order)
-      float v[kOwn];
+      if (!BOUND) q.m = value(best[0]);
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) {
-        unsigned mine = 0u;
+        key[j] = 0u;
 #pragma unroll
-        for (int i = j * L; i < K && i < (j + 1) * L; ++i) mine = l == i - j * L ? best[i] : mine;
-        e[j] = mine ? (int)(kLow - (mine & kLow)) : -1;
-        x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
-        v[j] = e[j] >= 0 ? q.value(A, x[j], e[j]) : -INFINITY;
-        place[j] = 0;
+        for (int i = j * L; i < K && i < (j + 1) * L; ++i)
+          key[j] = l == i - j * L ? best[i] : key[j];
+        if (key[j] >> 16 <= (0x7fffu ^ inf)) key[j] = 0u;  // -inf
+        place[j] = l + j * L;
       }
+    }
+    q.bad = isnan(q.m) || (soft && q.m == INFINITY);
 #pragma unroll
-      for (int i = 0; i < K; ++i) {
-        const float o = __shfl_sync(kAll, v[i / L], i % L, L);
+    for (int j = 0; j < kOwn; ++j) {
+      e[j] = key[j] && !q.bad ? (int)(0xffffu - (key[j] & 0xffffu)) : -1;
+      x[j] = value(key[j]);
+    }
+    if (soft && !A.renorm) {
+      float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) place[j] += o > v[j] || (o == v[j] && i < l + j * L);
+      for (int i = 0; i < S / 2; ++i)
+        sum += exp2_fast((P::value(w[i].w & 0xffffu) - q.m) * kLog2e) +
+               exp2_fast((P::value(w[i].w >> 16) - q.m) * kLog2e);
+      q.inv_sum = __fdividef(1.f, team_sum<L>(sum));
+    }
+    write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist);
+  }
+  end_load(A, hist);
+}
+
+// Teams of 8 lanes with S exact values each, of which those that reach a bound are ranked alone.
+// Lane l has the A.own <= S experts from l own on.
+template <int S, int K>
+__global__ void __launch_bounds__(kThreads, S > 16 ? 4 : 5) route_bound_kernel(RouteArgs A) {
+  constexpr int L = 8, kTeams = 32 / L, kOwn = K / 4, kSlots = L * kOwn;
+  extern __shared__ int hist[];  // the block's load; then, with groups, c and the groups' scores
+  __shared__ unsigned long long keys[kWarps * kTeams][kSlots];
+  __shared__ alignas(16) float bias[L * (S + 4)];  // (lanes' parts begin in different banks)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, l = lane % L;
+  const int e0 = l * A.own, end = min(e0 + A.own, E);
+  float *shared_c = (float *)(hist + E) + (warp * kTeams + lane / L) * shared_stride(E);
+  unsigned long long *to = keys[warp * kTeams + lane / L];
+  begin_load(A, hist);
+  for (int i = threadIdx.x; i < L * S; i += kThreads) {
+    const int at = i % S, e = i / S * A.own + at;
+    bias[i / S * (S + 4) + at] = A.bias && at < A.own && e < E ? fmaxf(A.bias[e], -INFINITY) : 0.f;
+  }  // (no NaN)
+  __syncthreads();
+  const float4 *mine = (const float4 *)(bias + l * (S + 4));
+  const long long step = (long long)gridDim.x * kWarps * kTeams;
+  for (long long row0 = ((long long)blockIdx.x * kWarps + warp) * kTeams; row0 < A.rows;
+       row0 += step) {
+    // (a team beyond the last query repeats the last, and writes nothing)
+    const bool live = row0 + lane / L < A.rows;
+    const long long row = min(row0 + lane / L, A.rows - 1);
+    float c[S];
+    load_logits(A, row, e0, end, c);
+    const Query q = score_query<S, L>(A, [&](int s) {
+      const float4 b = mine[s / 4];
+      return s % 4 == 0 ? b.x : s % 4 == 1 ? b.y : s % 4 == 2 ? b.z : b.w;
+    }, c);
+    apply_groups<S, L>(A, c, shared_c, e0, end, l);
+    const float bound = fmaxf(bound_of<K>(c), -FLT_MAX);
+    unsigned hit = 0u;
+#pragma unroll
+    for (int s = 0; s < S; ++s) hit |= c[s] >= bound ? 1u << s : 0u;
+    int n, e[kOwn], place[kOwn];
+    float x[kOwn];
+    unsigned long long key[kOwn];
+    const int first = hits_before(__popc(hit), l, n);
+    if (!__any_sync(kAll, n > kSlots)) {
+      for (int at = first; hit; ++at) {
+        const int i = e0 + __ffs(hit) - 1;
+        hit &= hit - 1u;
+        to[at] = make_key(q.value(A, logit_at(A, row, i), i), (unsigned)i);
       }
-      // a candidate may be missing where the last shares the k-th's bits: then by exact values
-      bool doubt = false;
+      in_order<kOwn>(to, n, l, key, place);
+    } else {  // many equal ones: the largest, k times
 #pragma unroll
-      for (int j = 0; j < kOwn; ++j)
-        doubt |= place[j] == A.k - 1 && e[j] >= 0 && best[K - 1] != 0u &&
-                 ((order_bits(v[j] == 0.f ? 0.f : v[j]) ^ best[K - 1]) & ~kLow) == 0u;
-      doubt = __ballot_sync(kAll, doubt) >> (lane - l) & (kAll >> (32 - L));
-      if (__any_sync(kAll, doubt)) {
-        unsigned long long last = ~0ull;
-        for (int r = 0; r < A.k; ++r) {
-          unsigned long long top = 0ull;
-          for (int s = 0; s < S; ++s) {
-            const int at = e0 + s;
-            if (at >= E || (groups && !(kept >> (at / per) & 1u))) continue;
-            const float u = q.value(A, logit_at(A, row, at), at);
-            const unsigned long long t = make_key(u, (unsigned)at);
-            if (u > -INFINITY && t < last && t > top) top = t;
-          }
+      for (int j = 0; j < kOwn; ++j) key[j] = 0ull, place[j] = l + j * L;
+      for (int r = 0; r < A.k; ++r) {
+        float top = c[0];
 #pragma unroll
-          for (int o = L / 2; o > 0; o >>= 1) {
-            const unsigned long long t = shfl_xor64(top, o);
-            top = t > top ? t : top;
-          }
-          last = top;  // (0: nothing is left)
+        for (int s = 1; s < S; ++s) top = fmaxf(top, c[s]);
 #pragma unroll
-          for (int j = 0; j < kOwn; ++j)
-            if (doubt && r == l + j * L) {
-              e[j] = top ? (int)key_index(top) : -1;
-              x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
-            }
-        }
+        for (int o = 1; o < L; o *= 2) top = fmaxf(top, other_lane(top, o));
+        int at = S;
+#pragma unroll
+        for (int s = S - 1; s >= 0; --s) at = c[s] == top ? s : at;
+        int from = at < S && top > -INFINITY ? l : L;
+#pragma unroll
+        for (int o = 1; o < L; o *= 2) from = min(from, __shfl_xor_sync(kAll, from, o));
+        const int i = __shfl_sync(kAll, e0 + at, from % L, L);
+#pragma unroll
+        for (int s = 0; s < S; ++s) c[s] = l == from && s == at ? -INFINITY : c[s];
 #pragma unroll
         for (int j = 0; j < kOwn; ++j)
-          if (doubt) place[j] = l + j * L;
+          if (r == l + j * L && from < L) key[j] = make_key(top, (unsigned)i);
       }
+    }
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      e[j] = key[j] ? (int)key_index(key[j]) : -1;
+      x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
     }
     write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist);
   }
@@ -707,7 +769,7 @@ __device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, 
 template <int S, int K>
 __global__ void __launch_bounds__(kThreads, S > 8 ? 1 : 5) route_warp_kernel(RouteArgs A) {
   extern __shared__ int hist[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e0 = lane * S, per = A.E / A.G;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e0 = lane * S;
   float *shared_c = (float *)(hist + A.E) + warp * shared_stride(A.E);
   begin_load(A, hist);
   float bias[S];
@@ -715,20 +777,9 @@ __global__ void __launch_bounds__(kThreads, S > 8 ? 1 : 5) route_warp_kernel(Rou
   for (long long row = (long long)blockIdx.x * kWarps + warp; row < A.rows;
        row += (long long)gridDim.x * kWarps) {
     float c[S], mine;
-    const Query q = load_query<S, 32>(A, row, e0, bias, c);
-    if (A.keep < A.G && A.group_lanes) {
-      const bool kept = keeps_lane<S, 32>(c, A, lane);
-#pragma unroll
-      for (int s = 0; s < S; ++s) c[s] = kept ? c[s] : -INFINITY;
-    } else if (A.keep < A.G) {
-#pragma unroll
-      for (int s = 0; s < S; ++s)
-        if (e0 + s < A.E) shared_c[e0 + s] = c[s];
-      __syncwarp();
-      const unsigned kept = keep_groups<32>(shared_c, shared_c + A.E, A, per, lane);
-      __syncwarp();
-      drop_groups(c, kept, e0, per);
-    }
+    load_logits(A, row, e0, A.E, c);
+    const Query q = score_query<S, 32>(A, [&](int s) { return bias[s]; }, c);
+    apply_groups<S, 32>(A, c, shared_c, e0, A.E, lane);
     int e[1], place[1] = {lane};
     choose<S, K>(c, A.k, mine, e[0]);
     if (lane >= A.k) e[0] = -1;
@@ -988,14 +1039,8 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   const bool groups = keep < G;
   // (the sum of two scores has no counterpart among the logits)
   A.by_logits = !bias && !(groups && group_top == 2);
-  A.whole = A.by_logits && !groups && dtype != BOUTE_F32;
   const size_t bytes = dtype_bytes(dtype);
   A.vec = (uintptr_t)logits % 16 == 0 && ld * bytes % 16 == 0 && E * bytes % 16 == 0;
-  // A team of lanes per query where its lists are short (candidates: more than choices where keys do
-  // not hold the values whole) and its values few or whole in their keys; else a warp. (us by team
-  // and by warp: 262144 x 256 bf16, k = 4: 48, 107, k = 8: 64, 155; 131072 queries: 128 bf16 with
-  // bias, k = 6: 42, 57; 64 fp32, k = 2: 21, 34; 128 fp32, k = 4: 38, 45.)
-  const int need = A.whole ? k : k + 1;
   // queries: of a warp; blocks: of an SM; S: experts of a lane. (At most 38 KB of shared memory.)
   auto run = [&](auto kernel, int queries, int blocks, int S) {
     A.group_lanes = E / G % S == 0 ? E / G / S : 0;
@@ -1010,23 +1055,33 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
       if (int r = launch_cluster(clear_load_kernel, 1, 256, 1, 0, s, load, E)) return r;
     return launch_cluster(kernel, grid, kThreads, 1, smem, s, A);
   };
-  auto team = [&](auto list) {
-    constexpr int K = decltype(list)::value;
-    auto whole = [&](auto keys) {
-      constexpr Keys KEYS = decltype(keys)::value;
-      if (E <= 64) return run(route_team_kernel<8, 8, K, KEYS>, 4, 4, 8);
-      if (E <= 128) return run(route_team_kernel<16, 8, K, KEYS>, 4, 4, 16);
-      return run(route_team_kernel<32, 8, K, KEYS>, 4, 4, 32);
+  // Teams for pairs, and for other values where the queries give most SMs a block or two. (us by
+  // team and by warp: 131072 x 256 bf16 with bias, k = 4: 37, 60, in 8 groups, k = 8: 63, 107; 131072
+  // x 64, 8 groups, k = 4: 29, 66; 256 experts, 8 groups, k = 8, of 300, 2000, 4099 and 10000
+  // queries: 7.2, 4.1; 7.3, 5.7; 7.4, 8.4; 10.6, 13.9; 64 experts, k = 4, of 300, 2000 and 4099: 3.8,
+  // 3.0; 3.9, 3.9; 4.0, 5.2.)
+  using std::integral_constant;
+  const bool pairs = A.by_logits && !groups && dtype != BOUTE_F32;
+  auto team = [&](auto experts) {
+    constexpr int S = decltype(experts)::value;
+    auto teams = [&](auto list) {
+      constexpr int K = decltype(list)::value;
+      if (pairs)
+        return dtype == BOUTE_F16 ? run(route_pairs_kernel<S, K, true>, 4, 4, S)
+                                  : run(route_pairs_kernel<S, K, false>, 4, 4, S);
+      // the lanes' shares of E: equal ones where they are whole vectors, unless only shares of S
+      // leave each with experts of one group
+      const int equal = E % (8 * (16 / (int)bytes)) == 0 ? E / 8 : S, per = E / G;
+      A.own = groups && per % equal != 0 && per % S == 0 ? S : equal;
+      return run(route_bound_kernel<S, K>, 4, S > 16 ? 4 : 5, A.own);
     };
-    if (A.whole)
-      return dtype == BOUTE_F16 ? whole(std::integral_constant<Keys, kHalf>{})
-                                : whole(std::integral_constant<Keys, kBfloat>{});
-    if (E <= 64) return run(route_team_kernel<8, 8, K, kParts>, 4, 4, 8);
-    return run(route_team_kernel<16, 8, K, kParts>, 4, 4, 16);
+    return k <= 4 ? teams(integral_constant<int, 4>{}) : teams(integral_constant<int, 8>{});
   };
-  if (E <= (A.whole ? 256 : 128) && need <= 8)
-    return need <= 4 ? team(std::integral_constant<int, 4>{})
-                     : team(std::integral_constant<int, 8>{});
+  if (E <= 256 && k <= 8 && (pairs || T >= (E <= 128 ? 16ll : 24ll) * num_sms())) {
+    if (E <= 64) return team(integral_constant<int, 8>{});
+    if (E <= 128) return team(integral_constant<int, 16>{});
+    return team(integral_constant<int, 32>{});
+  }
   if (E <= 64) return run(route_warp_kernel<2, 2>, 1, 5, 2);
   if (E <= 128) return run(route_warp_kernel<4, 4>, 1, 5, 4);
   if (E <= 256)

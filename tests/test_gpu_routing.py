@@ -133,6 +133,66 @@ def test_long_choices_and_groups_of_lanes(mode, T, E, G, keep, gtop, k):
         check(v, *a, routed(v.cuda(), *a))
 
 
+def check_many(x, *a, T=4999, pitch=0, shift=0):
+    """The queries over and over, enough to fill the device: equal ones are treated alike."""
+    rows = torch.arange(T) % len(x)
+    i, w, ld = routed(placed(x[rows], pitch, shift), *a)
+    rows = rows.cuda()
+    assert torch.equal(i, i[:len(x)][rows])
+    assert torch.equal(w.view(torch.int32), w[:len(x)][rows].view(torch.int32))
+    assert ld.tolist() == torch.bincount(i[i >= 0].long(), minlength=x.shape[1]).tolist()
+    check(x, *a, (i[:len(x)], w[:len(x)], None))
+
+
+@pytest.mark.parametrize("mode", [SOFT, SIG])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,E,G,keep,gtop,k", SHAPES + [
+    (61, 256, 1, 1, 1, 4), (61, 256, 8, 4, 2, 8), (61, 192, 8, 4, 2, 6), (61, 190, 10, 4, 2, 6),
+    (61, 160, 5, 2, 2, 6), (61, 160, 10, 3, 1, 3), (61, 128, 8, 2, 2, 8), (61, 64, 8, 3, 1, 8),
+    (61, 61, 1, 1, 1, 8), (61, 254, 2, 1, 1, 5), (61, 8, 1, 1, 1, 8), (61, 129, 3, 1, 2, 1)])
+def test_many_queries(mode, dtype, T, E, G, keep, gtop, k):
+    x = queries(T * 5 + E, min(T, 19), E, dtype, 0.7)
+    x[::9, ::2] = float("-inf")
+    g = torch.Generator().manual_seed(E)
+    bias = (torch.randint(-100, 100, (E,), generator=g).float() * 1e-3).cuda()
+    for b, renorm in ((None, True), (bias, E % 2 == 0), (None, False)):
+        check_many(x, b, mode, G, keep, gtop, k, renorm, 2.5, pitch=E % 3, shift=k % 2)
+    ties = torch.randint(0, 3, x.shape, generator=g).to(DT[dtype])
+    check_many(ties, None, mode, G, keep, gtop, k, True, 1.0)
+
+
+@pytest.mark.parametrize("mode", [SOFT, SIG])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("E,k", [(48, 6), (100, 3), (256, 4), (256, 8), (200, 7)])
+def test_many_queries_broken_rows(mode, dtype, E, k):
+    x = queries(E, 18, E, dtype)
+    inf, low = float("inf"), torch.finfo(DT[dtype]).min
+    x[0] = -inf                      # nobody in service
+    x[1, 2:] = -inf                  # fewer than k
+    x[2, 12:36] = -inf
+    x[3, 7] = float("nan")
+    x[4, 9] = inf
+    x[5] = 0.25                      # all equal: the lowest indices
+    x[6] = low
+    x[7, 1:] = low
+    x[8] = -200.0
+    x[9, ::2] = -inf
+    x[10] = float("nan")
+    x[11] = 0.0
+    x[11, ::2] = -0.0                # one value
+    x[12] = torch.arange(E).to(DT[dtype]) / 64
+    x[13] = -torch.arange(E).to(DT[dtype]) / 64
+    x[14] = 1.0                      # all of the largest in one lane
+    x[14, 16:24] = 2.0
+    x[15, :40] = -inf
+    x[16, 40:] = -inf
+    off = torch.where(torch.arange(E) % 3 == 0, -inf, 0.125)
+    for b in (None, torch.zeros(E), off):
+        for G, keep, renorm in ((1, 1, True), (1, 1, False), (4, 2, True)):
+            if k <= keep * (E // G):
+                check_many(x, None if b is None else b.cuda(), mode, G, keep, 2, k, renorm, 1.0)
+
+
 def test_load_is_written_and_optional():
     x = queries(2, 100, 16, "bf16").cuda()
     a = (None, SOFT, 1, 1, 1, 3, True, 1.0)
