@@ -197,29 +197,14 @@ __device__ __forceinline__ void best_in_lane(V (&c)[S]) {
       merge_desc<K>(c + s);
     }
 }
-// The K <= S largest of the team's keys (S in each of its L lanes), in every lane: the lanes' lists
-// joined in the same way.
-template <int S, int L, int K>
-__device__ __forceinline__ void best_of(unsigned (&c)[S], unsigned (&best)[K]) {
-  best_in_lane<S, K>(c);
-#pragma unroll
-  for (int i = 0; i < K; ++i) best[i] = c[i];
-#pragma unroll
-  for (int o = 1; o < L; o *= 2) {
-    unsigned other[K];
-#pragma unroll
-    for (int i = 0; i < K; ++i) other[i] = __shfl_xor_sync(kAll, best[K - 1 - i], o);
-#pragma unroll
-    for (int i = 0; i < K; ++i) best[i] = max(best[i], other[i]);
-    merge_desc<K>(best);
-  }
-}
-
 template <bool HALF>
 __device__ __forceinline__ Pair<HALF> other_lane(Pair<HALF> v, int o) {
   return {__shfl_xor_sync(kAll, v.w, o)};
 }
-__device__ __forceinline__ float other_lane(float v, int o) { return __shfl_xor_sync(kAll, v, o); }
+template <class V>
+__device__ __forceinline__ V other_lane(V v, int o) {
+  return __shfl_xor_sync(kAll, v, o);
+}
 // The K largest in order of 8 lanes' lists of FROM in order, in every lane.
 template <int FROM, int K, class V>
 __device__ __forceinline__ void join_lanes(V (&a)[K]) {
@@ -241,6 +226,14 @@ __device__ __forceinline__ void join_lanes(V (&a)[K]) {
       merge_desc<K>(a);
     }
   }
+}
+// The K <= S largest of the team's keys, S in each of its 8 lanes, in every lane.
+template <int S, int K>
+__device__ __forceinline__ void best_of(unsigned (&c)[S], unsigned (&best)[K]) {
+  best_in_lane<S, K>(c);
+#pragma unroll
+  for (int i = 0; i < K; ++i) best[i] = c[i];
+  join_lanes<K>(best);
 }
 // A value that K of the team's values reach, N in each of its 8 lanes, and few others: the K-th
 // largest of 4 K parts' maxima, K / 2 parts to a lane.
@@ -277,7 +270,7 @@ __device__ __forceinline__ Pair<HALF> bound_of(const Pair<HALF> (&w)[N], Pair<HA
   for (int i = 1; i < K; ++i) bound = min(bound, max(a[i], a[K - 1 - i].swapped()));
   return bound;
 }
-// Of the team's 8 lanes, how many of their hits precede lane l's (which has `mine`), and all of them.
+// Of the hits of the team's 8 lanes, how many precede lane l's (which has `mine`), and all of them.
 __device__ __forceinline__ int hits_before(int mine, int l, int &all) {
   int upto = mine;
 #pragma unroll
@@ -515,8 +508,9 @@ __device__ __forceinline__ void end_load(const RouteArgs &A, const int *hist) {
     else if (hist[e]) atomicAdd(A.load + e, hist[e]);
 }
 
-// A team's n <= 8 OWN keys (all different, in its part of shared memory, any order) in order: lane l
-// has those of places l, l + 8 .. (0: none), whatever the warp's other teams do.
+// A team's n <= 8 OWN keys (all different, in its part of shared memory, any order) in order: lane
+// l has those of places l, l + 8 .. (0: none). Sums in this order do not depend on how a query's
+// team found them.
 template <int OWN, class Key>
 __device__ __forceinline__ void in_order(Key *to, int n, int l, Key (&key)[OWN],
                                          int (&place)[OWN]) {
@@ -615,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 4) route_pairs_kernel(RouteArgs A) {
         c[2 * i] = __byte_perm(o, below - 0x00020002u * i, 0x1054);
         c[2 * i + 1] = __byte_perm(o, below - 0x00020002u * i, 0x3276);
       }
-      best_of<S, L, K>(c, best);
+      best_of<S, K>(c, best);
       if (!BOUND) q.m = value(best[0]);
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) {
@@ -729,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, S > 16 ? 4 : 5) route_bound_kernel(R
 // ---- a warp to a query -------------------------------------------------------------------
 // The k largest of the lanes' values, lane r with the r-th: its value and its expert (-1: none).
 // Each lane sorts its K >= min(k, S) best; k rounds take the largest head of the 32 lists. Equal
-// values go to the lowest expert: of several lanes the lowest, of one lane's the occurrences in order.
+// values go to the lowest expert: of several lanes the lowest, of a lane's the occurrences in order.
 template <int S, int K>
 __device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, int &expert) {
   const int lane = threadIdx.x & 31;
@@ -1117,7 +1111,8 @@ extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int 
     return with_slots(E, [&](auto slots) {
       constexpr int S = decltype(slots)::value;
       A.vec = vectors(logits, ld, E, S, sizeof(X)) && vectors(dlogits, ldd, E, S, sizeof(X));
-      const unsigned grid = (unsigned)std::min<long long>((T + kWarps - 1) / kWarps, 8ll * num_sms());
+      const unsigned grid =
+          (unsigned)std::min<long long>((T + kWarps - 1) / kWarps, 8ll * num_sms());
       return launch_cluster(route_grad_softmax_kernel<X, S>, grid, kThreads, 1, 0, s,
                             (const X *)logits, A, (X *)dlogits);
     });
