@@ -1049,7 +1049,9 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
       if (int r = launch_cluster(clear_load_kernel, 1, 256, 1, 0, s, load, E)) return r;
     return launch_cluster(kernel, grid, kThreads, 1, smem, s, A);
   };
-  // Teams for pairs, and for other values where the queries give most SMs a block or two. (us by
+  // Teams for pairs, and for other values where the queries give most SMs a block or two; and where
+  // one block of them takes all queries, which then needs no launch to clear the load (32 queries
+  // of 64 fp32: 2.2 and one launch, 2.5 and two). (us by
   // team and by warp: 131072 x 256 bf16 with bias, k = 4: 37, 60, in 8 groups, k = 8: 63, 107; 131072
   // x 64, 8 groups, k = 4: 29, 66; 256 experts, 8 groups, k = 8, of 300, 2000, 4099 and 10000
   // queries: 7.2, 4.1; 7.3, 5.7; 7.4, 8.4; 10.6, 13.9; 64 experts, k = 4, of 300, 2000 and 4099: 3.8,
@@ -1071,7 +1073,9 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
     };
     return k <= 4 ? teams(integral_constant<int, 4>{}) : teams(integral_constant<int, 8>{});
   };
-  if (E <= 256 && k <= 8 && (pairs || T >= (E <= 128 ? 16ll : 24ll) * num_sms())) {
+  const bool one_block = load && T <= 2 * 4 * kWarps;
+  if (E <= 256 && k <= 8 &&
+      (pairs || one_block || T >= (E <= 128 ? 16ll : 24ll) * num_sms())) {
     if (E <= 64) return team(integral_constant<int, 8>{});
     if (E <= 128) return team(integral_constant<int, 16>{});
     return team(integral_constant<int, 32>{});
