@@ -846,6 +846,17 @@ struct RouteGradArgs {
   const float *g_weight;
 };
 
+// A warp's: n elements from p on are 0, by 16-byte vectors between the ends.
+template <class T>
+__device__ __forceinline__ void clear_run(T *p, int n, int lane) {
+  constexpr int kOf = 16 / sizeof(T);
+  const int head = min(n, (int)((16 - (uintptr_t)p % 16) % 16 / sizeof(T)));
+  const int whole = (n - head) / kOf, tail = head + whole * kOf;
+  uint4 *v = (uint4 *)(p + head);
+  for (int i = lane; i < whole; i += 32) v[i] = make_uint4(0u, 0u, 0u, 0u);
+  if (lane < head) p[lane] = from_float<T>(0.f);
+  if (tail + lane < n) p[tail + lane] = from_float<T>(0.f);
+}
 // The gradient where it is 0 but for the chosen experts: logistic scores, and a renormalised
 // softmax, of which only the chosen logits count:
 //   w_i = factor s_i / S:  dx_i = factor s_i / S (g_i - sum_j g_j s_j / S) [ (1 - s_i): logistic ].
@@ -890,10 +901,14 @@ __global__ void __launch_bounds__(kThreads)
       d = g * q / ((1.f + q) * (1.f + q));
     }
     __syncwarp();  // (in place: every chosen logit has been read)
+    // (131072 rows of 160 fp32 with a pitch: element by element 29 us, looking for each row's ends
+    // 31; of 61 bf16 without one: 13.2 element by element, 6.7 looking for the run's ends)
     if (A.vec && A.ldd == A.E) {  // the rows are one run of 16-byte vectors
       uint4 *p = (uint4 *)(dlogits + row0 * A.E);
       const int vectors = n * A.E / (16 / (int)sizeof(T));
       for (int i = lane; i < vectors; i += 32) p[i] = make_uint4(0u, 0u, 0u, 0u);
+    } else if (A.ldd == A.E) {
+      clear_run(dlogits + row0 * A.E, n * A.E, lane);
     } else {
       for (int i = 0; i < n; ++i)
         for (int j = lane; j < A.E; j += 32)
@@ -1084,8 +1099,12 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
   if (E <= 128) return run(route_warp_kernel<4, 4>, 1, 5, 4);
   if (E <= 256)
     return k <= 4 ? run(route_warp_kernel<8, 4>, 1, 5, 8) : run(route_warp_kernel<8, 8>, 1, 5, 8);
-  if (E <= 512) return run(route_warp_kernel<16, 16>, 1, 4, 16);
-  return run(route_warp_kernel<32, 32>, 1, 4, 32);
+  // (lists as short as the choice allows: 131072 x 512 bf16, k = 4: 95 us, whole lists 218)
+  if (E <= 512)
+    return k <= 4   ? run(route_warp_kernel<16, 4>, 1, 4, 16)
+           : k <= 8 ? run(route_warp_kernel<16, 8>, 1, 4, 16)
+                    : run(route_warp_kernel<16, 16>, 1, 4, 16);
+  return k <= 8 ? run(route_warp_kernel<32, 8>, 1, 4, 32) : run(route_warp_kernel<32, 32>, 1, 4, 32);
 }
 
 extern "C" int boute_route_grad(const void *logits, int dtype, long long T, int E, long long ld,
