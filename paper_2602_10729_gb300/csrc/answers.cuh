@@ -89,6 +89,15 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
                    : "memory");
 }
+// A block's shared memory may be written by others once it runs. Every thread arrives at
+// cluster_begin (at the kernel's start, before its loads) and waits at cluster_runs before the
+// first store to a peer; by then the others have long begun.
+__device__ __forceinline__ void cluster_begin() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_runs() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // Address of block r's copy of a shared variable.
 __device__ __forceinline__ uint32_t peer(const void *p, int r) {
   uint32_t a;

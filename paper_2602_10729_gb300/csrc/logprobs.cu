@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   __shared__ float stat[2];  // m (NaN: no distribution) and ln s
   __shared__ unsigned bound;
   __shared__ int nlist;
+  if (CS > 1) cluster_begin();
   pdl_wait();
   pdl_trigger();
   const int NT = blockDim.x, W = NT / 32, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -348,6 +349,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   (CS > 1 ? lanes : tops)[tid] = top;
   __syncthreads();
   if (CS > 1) {
+    cluster_runs();
     if (tid == 0) {
       Sums a = wsum[0];
       for (int w = 1; w < W; ++w) {
@@ -533,6 +535,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   if (isnan(l)) g = NAN;
   float m = l == -INFINITY ? 0.f : l, ls = 0.f;  // lse = m + ls
   if (fabsf(l) > kLargeLse && isfinite(l)) {
+    if (CS > 1) cluster_begin();  // (l is the row's: all of its blocks are here, or none)
     const float c = fminf(scale * kLog2e, FLT_MAX);
     Sums a = {-INFINITY, 0.f, 0.f};
     for (int q = first; q < Q; q += step) {
@@ -554,6 +557,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     for (int w = 1; w < W; ++w) a = join(a, wsum[w], c);
     if (CS > 1) {
       // (every block has read its part of the row before any writes: in place)
+      cluster_runs();
       if (threadIdx.x < CS) {
         store_peer(peer(&csum[rank][0], threadIdx.x), a.m);
         store_peer(peer(&csum[rank][1], threadIdx.x), a.s);

@@ -140,10 +140,12 @@ __device__ __forceinline__ Part block_join(Part p, Part *red) {
   for (int w = 1; w < kWarps; ++w) add(p, red[w]);
   return p;
 }
-// Of the whole cluster, in every thread; a cluster barrier before a block may end.
+// Of the whole cluster, in every thread, which have been at cluster_begin; a cluster barrier before
+// a block may end.
 __device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part *red,
                                              Part *parts) {
   p = block_join(p, red);
+  cluster_runs();
   if (threadIdx.x < cluster) {
     const uint32_t to = peer(&parts[rank], threadIdx.x);
     store_peer(to, p.lo);
@@ -163,6 +165,7 @@ __device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part
 template <int TEAM, class Emit>
 __device__ __forceinline__ void for_answers(const Answers &A, Emit emit) {
   __shared__ Part red[kWarps], parts[kMaxCluster];
+  if (TEAM == kThreads && A.cluster > 1) cluster_begin();
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x;
