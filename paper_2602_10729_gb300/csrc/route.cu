@@ -490,10 +490,11 @@ __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q,
     if (A.load && e[j] >= 0 && BOUTE_INB(e[j], A.E)) atomicAdd(hist + e[j], 1);
   }
 }
-// The block's load: cleared, and added to the whole one. (Behind clear_load_kernel, which has
-// waited for what came before, only the second waits.)
+// The block's load: cleared, and added to the whole one. (Behind clear_load_kernel too the wait
+// comes before any read or write of the call's arrays: that kernel has waited for what came before
+// it, but only a grid's own wait makes that visible to it.)
 __device__ __forceinline__ void begin_load(const RouteArgs &A, int *hist) {
-  if (!A.load || gridDim.x == 1) pdl_wait();
+  pdl_wait();
   pdl_trigger();
   if (!A.load) return;
   for (int e = threadIdx.x; e < A.E; e += kThreads) hist[e] = 0;
@@ -502,7 +503,6 @@ __device__ __forceinline__ void begin_load(const RouteArgs &A, int *hist) {
 __device__ __forceinline__ void end_load(const RouteArgs &A, const int *hist) {
   if (!A.load) return;
   __syncthreads();
-  pdl_wait();
   for (int e = threadIdx.x; e < A.E; e += kThreads)
     if (gridDim.x == 1) A.load[e] = hist[e];
     else if (hist[e]) atomicAdd(A.load + e, hist[e]);

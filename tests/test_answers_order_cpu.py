@@ -1,6 +1,7 @@
 """The order that the kernels over a model's answers keep on the device, read from their sources
 (what goes wrong without it may be rare, or a fault): a block writes into another's shared memory
-only after every block of the cluster has begun."""
+only after every block of the cluster has begun, and a kernel that may begin while the one before
+it ends waits before it reads or writes."""
 import os
 import re
 
@@ -36,3 +37,23 @@ def test_peers_are_written_once_their_blocks_run(name, of):
         begin = bodies[n] if n != "cluster_join" else bodies["for_answers"]
         at = begin.index("cluster_begin();")
         assert at < begin.index("cluster_runs();" if n != "cluster_join" else "cluster_join("), n
+
+
+@pytest.mark.parametrize("name", ["logprobs.cu", "scores.cu", "route.cu"])
+def test_kernels_wait_before_they_read_or_write(name):
+    """The wait is unconditional and comes before any access to an argument's array."""
+    bodies = dict(functions(name))
+    waiting = {n for n, b in bodies.items() if "pdl_wait();" in b}
+    for n in waiting:
+        assert bodies[n].count("pdl_wait();") == 1, n
+        before = bodies[n][:bodies[n].index("pdl_wait();")]
+        assert not re.search(r"\w\[|if \([^)]*\)\s*$|for \(", re.sub(r"__shared__[^;]*;", "", before)), n
+    kernels = [n for n in bodies if n.endswith("_kernel")]
+    assert len(kernels) >= 2
+    for n in kernels:
+        if n in waiting:
+            continue
+        first = re.search(r"\b(%s)(<\w+>)?\(" % "|".join(waiting), bodies[n])
+        assert first, n
+        assert not re.search(r"load_\w+\(|logit_at\(|A\.bias\[",
+                             bodies[n][:first.start()].replace("begin_load(", "")), n
