@@ -495,7 +495,9 @@ __global__ void __launch_bounds__(kThreads, 4)
 }
 
 // Beyond this |lse| its rounding (2^-24 of it) would show in p: rows whose mask is the type's
-// lowest value throughout have an lse that has lost ln s, and take m and ln s from the row.
+// lowest value throughout have an lse that has lost ln s, and take the largest logit and ln s from
+// the row. The product of that logit and the scale has a rounding of the same size, so lp is then
+// (x - max x) scale - ln s: the difference comes first, as in the sums.
 constexpr float kLargeLse = 1024.f;
 
 // With lp_j = z_j - lse and p_j = exp(lp_j):
@@ -533,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   float gh = g_entropy ? g_entropy[row] : 0.f, H = g_entropy ? entropy[row] : 0.f;
   if (l == -INFINITY && t < V) g = gh = H = 0.f;
   if (isnan(l)) g = NAN;
-  float m = l == -INFINITY ? 0.f : l, ls = 0.f;  // lse = m + ls
+  float m = 0.f, ls = l == -INFINITY ? 0.f : l;  // lp = (x - m) scale - ls
   if (fabsf(l) > kLargeLse && isfinite(l)) {
     if (CS > 1) cluster_begin();  // (l is the row's: all of its blocks are here, or none)
     const float c = fminf(scale * kLog2e, FLT_MAX);
@@ -566,12 +568,12 @@ __global__ void __launch_bounds__(kThreads, 4)
       a = {csum[0][0], csum[0][1], 0.f};
       for (int b = 1; b < CS; ++b) a = join(a, {csum[b][0], csum[b][1], 0.f}, c);
     }
-    m = __fmul_rn(a.m, scale);
+    m = a.m;
     ls = logf(a.s);
   }
   const float A = -scale * (g + gh * H), B = -scale * gh, extra = scale * g;
-  const unsigned long long A2 = f2_dup(A), B2 = f2_dup(B), c2 = f2_dup(scale), m2 = f2_dup(-m),
-                           ls2 = f2_dup(ls), e2 = f2_dup(kLog2e);
+  const unsigned long long A2 = f2_dup(A), B2 = f2_dup(B), c2 = f2_dup(scale), m2 = f2_dup(m),
+                           ls2 = f2_dup(-ls), e2 = f2_dup(kLog2e);
   for (int q = first; q < Q; q += step) {
     Piece<T> p = load(q);
     const int at0 = q * SPAN - off;
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     for (int j = 0; j < N / 2; ++j) {
       float a, b;
       pair(p, j, a, b);
-      f2_split(f2_sub(f2_fma(f2_pack(a, b), c2, m2), ls2), a, b);
+      f2_split(f2_fma(f2_sub(f2_pack(a, b), m2), c2, ls2), a, b);
       const unsigned long long lp = f2_pack(fmaxf(a, kLowest), fmaxf(b, kLowest));
       f2_split(f2_mul(lp, e2), a, b);
       const unsigned long long e = f2_pack(exp2_fast(a), exp2_fast(b));

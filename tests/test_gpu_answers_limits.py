@@ -4,9 +4,9 @@ import numpy as np
 import pytest
 import torch
 
-from _answers import U, answer_grad, answer_rows
+from _answers import U, answer_grad, answer_rows, token_grad_row
 from paper_2602_10729_gb300 import boute as bt
-from test_gpu_answers import answers, check_forward, close, forward, logits, scored
+from test_gpu_answers import DT, EPS, answers, check_forward, close, forward, logits, scored
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +47,50 @@ def test_clusters_on_streams_at_once():
     for out in outs:
         assert all(torch.equal(a, b) for a, b in zip(want, out))
     check_forward(x, t, 1.0, 9, want)
+
+
+# ---------------------------------------------------------------- logits far from 0
+# With |lse| over 1024 the gradient takes p from the row: x - max is exact where p is not 0, its
+# product with the scale has one rounding of |z - m| <= 200, ln s a few of 2 + ln V. So
+#   |dx_j - want| <= scale (|g| + |gh| 2 (2 + ln V + d)) exp(-d) U (8 (2 + 200) + 4 sqrt(V))
+# holds whatever the size of the logits (d = m - z_j); with the entropy given as the forward call
+# had it (its own tolerance above enters through g_entropy p H: another 8 U (2 + 200) (2 + ln V)).
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("scale", [0.7, 1 / 0.7, 1.0])
+@pytest.mark.parametrize("T,V", [(5, 11), (5, 5003), (4, 70001), (1300, 2049)])  # one block and more
+@pytest.mark.parametrize("ent", [True, False])
+def test_gradient_of_logits_far_from_zero(dtype, scale, T, V, ent):
+    base, t = logits(V, T, V, "f32", spread=1.0)
+    x = base.to(DT[dtype])
+    low = torch.finfo(DT[dtype]).min
+    far = {"f32": -1e9, "f16": -6e4, "bf16": -1e9}[dtype]
+    x[0] = low                                        # uniform
+    x[1] = far
+    x[2] = (base[2] * 3 + {"f32": 1e6, "f16": 3e4, "bf16": 1e4}[dtype]).to(DT[dtype])
+    x[3] = low
+    x[3, :3] = far / 4                                # three tokens left
+    if scale > 1:                                     # (a scaled lowest value is -inf: masked)
+        x[0] = far / 2
+    t[:4] = torch.tensor([0, -1, V - 1, 2])
+    gen = torch.Generator().manual_seed(V)
+    g, gh = torch.randn(T, generator=gen), torch.randn(T, generator=gen) if ent else None
+    xs, ts = x.cuda(), t.cuda()
+    lp, H, lse, _, _ = forward(xs, ts, scale, 0)
+    dx = torch.full_like(xs, 5.0)
+    bt.boute_token_logprobs_grad(xs, ts, scale, lse, H if ent else None, g.cuda(),
+                                 gh.cuda() if ent else None, dx)
+    tiny = {"f32": 1e-38, "f16": 2.0 ** -25, "bf16": 1e-38}[dtype]
+    got = dx[:5].float().cpu().numpy()
+    for r in range(len(got)):
+        row = x[r].float().numpy()
+        gr, hr = float(g[r]), float(gh[r]) if ent else 0.0
+        want = token_grad_row(row, scale, int(t[r]), gr, hr)
+        z = row.astype(np.float64) * float(np.float32(scale))
+        d = np.minimum(z.max() - z, 200.0)
+        rel = U * (8 * (2 + 200.0) + 4 * np.sqrt(V))
+        part = abs(gr) * (t[r] >= 0).item() + abs(hr) * 4 * (2 + np.log(V) + d)
+        tol = scale * rel * part * np.exp(-d) + np.abs(want) * (EPS[dtype] + 8 * U) + tiny
+        close(got[r], want, tol)
+    bt.boute_token_logprobs_grad(xs, ts, scale, lse, H if ent else None, g.cuda(),
+                                 gh.cuda() if ent else None, xs)  # in place
+    assert torch.equal(xs, dx)
