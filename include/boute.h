@@ -649,7 +649,7 @@ int boute_answer_scores_grad(const float *logprob, const float *entropy,
 
 /* Queries to experts (the models, or the replicas of their deployments), Sec.
  * 4.1 and App. C: for each of T queries with logits x over E experts,
- *   s = softmax(x) or 1 / (1 + exp(-x)) (mode; fp32: what underflows is 0), c = s + bias
+ *   s = softmax(x) or 1 / (1 + exp(-x)) (mode; what is below 2^-149 is 0), c = s + bias
  *   (without a bias, but for the sums of two below, the logits are compared, which have
  *   the scores' order without their rounding),
  * the experts in G groups of E / G neighbours (models with their replicas): a

@@ -75,6 +75,11 @@ __device__ __forceinline__ float exp2_fast(float y) {  // (2 ulp; what is below 
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
   return r;
 }
+__device__ __forceinline__ float exp2_gradual(float y) {  // (2 ulp; down to 2^-149)
+  float r;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(y));
+  return r;
+}
 // Order-preserving bits of a float, and back.
 __device__ __forceinline__ unsigned order_bits(float v) {
   const unsigned u = __float_as_uint(v);

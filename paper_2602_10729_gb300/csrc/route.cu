@@ -31,7 +31,14 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 
-__device__ __forceinline__ float logistic(float x) {  // (0 where exp(-x) overflows)
+// A score may be as small as fp32 holds, 2^-149; below it is 0. Choices are made with approximate
+// instructions (exponential 2 ulp, reciprocal 1), as they are some hundred to a query.
+constexpr float kLeastLog2 = -149.f;
+// Scores that a sum of small ones is made of are taken relative to the largest of them where fewer
+// bits of them are left than fp32 has; beside a sum of 1/8 what is below 2^-126 is below 2^-123.
+constexpr float kFewBits = 0x1p-100f, kSmallSum = 0.125f;
+
+__device__ __forceinline__ float logistic(float x) {  // (0 below 2^-126)
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_fast(-x * kLog2e)));
   return r;
@@ -41,6 +48,12 @@ template <int L>
 __device__ __forceinline__ float team_sum(float v) {
 #pragma unroll
   for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float team_max(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
   return v;
 }
 __device__ __forceinline__ float team_sum(float v, int team) {
@@ -397,6 +410,19 @@ struct Query {
   __device__ __forceinline__ float score(const RouteArgs &A, float x) const {
     return A.mode == BOUTE_ROUTE_SOFTMAX ? exp2_fast((x - m) * kLog2e) * inv_sum : logistic(x);
   }
+  // the same with all the bits that fp32 has for it, for a weight
+  __device__ __forceinline__ float whole_score(const RouteArgs &A, float x) const {
+    if (A.mode == BOUTE_ROUTE_SOFTMAX) return exp2_gradual((x - m) * kLog2e) * inv_sum;
+    return x < -64.f ? exp2_gradual(x * kLog2e) : logistic(x);  // (1 + exp(x) is 1)
+  }
+  // a score over that of a logit `of` >= x, both below 1/8; 0 where the score is
+  __device__ __forceinline__ float score_over(const RouteArgs &A, float x, float of) const {
+    const bool soft = A.mode == BOUTE_ROUTE_SOFTMAX;
+    const float least = soft ? (x - m) * kLog2e + __log2f(inv_sum) : x * kLog2e;
+    if (!(least >= kLeastLog2)) return 0.f;
+    const float e = exp2_fast((x - of) * kLog2e);
+    return soft ? e : __fdividef(e, 1.f + exp2_fast(x * kLog2e));  // (but for 1 + exp(of))
+  }
 };
 // c of the lane's S experts from e0 on (-inf: not to be chosen).
 template <int S>
@@ -472,21 +498,46 @@ __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q,
                                              bool live, const int (&e)[N], const int (&place)[N],
                                              const float (&x)[N], int *hist) {
   float w[N], sum = 0.f;
+  bool few = false;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    w[j] = e[j] >= 0 && place[j] < A.k ? q.score(A, x[j]) : 0.f;
+    const bool in = e[j] >= 0 && place[j] < A.k;
+    w[j] = in ? q.score(A, x[j]) : 0.f;
     sum += w[j];
+    few |= in && w[j] < kFewBits;
   }
-  float f = A.factor;
+  if (A.renorm) sum = team_sum<L>(sum);
+  const unsigned teams = __ballot_sync(kAll, few);
+  if (teams) {  // (a team's, whatever the warp's other queries)
+    float top = -INFINITY, over[N], all = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = e[j] >= 0 && place[j] < A.k ? fmaxf(top, x[j]) : top;
+    top = team_max<L>(top);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const bool in = e[j] >= 0 && place[j] < A.k;
+      over[j] = !in ? 0.f
+                : A.renorm && sum < kSmallSum ? q.score_over(A, x[j], top)
+                                              : q.whole_score(A, x[j]);
+      all += over[j];
+    }
+    all = team_sum<L>(all);
+    if (L == 32 || teams >> (threadIdx.x & 31) / L * L & ((1ull << L) - 1)) {
+      sum = all;
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = over[j];
+    }
+  }
   if (A.renorm) {
-    sum = team_sum<L>(sum);
-    f = sum > 0.f ? __fdividef(f, sum) : 0.f;
+    const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) w[j] *= inv;
   }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     if (!live || place[j] >= A.k) continue;
     A.idx[row * A.k + place[j]] = e[j];
-    A.weight[row * A.k + place[j]] = q.bad ? NAN : f * w[j];
+    A.weight[row * A.k + place[j]] = q.bad ? NAN : A.factor * w[j];
     if (A.load && e[j] >= 0 && BOUTE_INB(e[j], A.E)) atomicAdd(hist + e[j], 1);
   }
 }

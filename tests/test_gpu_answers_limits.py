@@ -4,9 +4,10 @@ import numpy as np
 import pytest
 import torch
 
-from _answers import U, answer_grad, answer_rows, token_grad_row
+from _answers import U, answer_grad, answer_rows, route_row, token_grad_row
 from paper_2602_10729_gb300 import boute as bt
 from test_gpu_answers import DT, EPS, answers, check_forward, close, forward, logits, scored
+from test_gpu_routing import SIG, SOFT, rel_tol, routed
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +95,67 @@ def test_gradient_of_logits_far_from_zero(dtype, scale, T, V, ent):
     bt.boute_token_logprobs_grad(xs, ts, scale, lse, H if ent else None, g.cuda(),
                                  gh.cuda() if ent else None, xs)  # in place
     assert torch.equal(xs, dx)
+
+
+# ---------------------------------------------------------------- scores that fp32 hardly holds
+# A score is at least 2^-149 or 0. Of a weight that is not renormalised |got - want| is at most a
+# score's relative error (that of the other tests) and two units of 2^-149, times the factor. A
+# renormalised weight has the relative error alone, whatever the size of its sum: it is a quotient,
+# of which only parts below 2^-123 may be lost.
+def tiny_queries(E, dtype):
+    """Logits whose scores lie between 2^-148 and 2^-60 beside one of 0 (softmax) or without."""
+    x = torch.full((9, E), -1e4)
+    x[:, 0] = 0.0
+    some = torch.linspace(-102.0, -84.0, 6)
+    x[0, 2:8] = some
+    x[1, 2:8] = some.flip(0) + 2.0
+    x[2, 2:8] = -88.0
+    x[3, 2:8] = -100.0
+    x[4, 2:8] = torch.tensor([-42.0, -90.0, -60.0, -95.0, -41.0, -87.0])
+    x[5, 2:8] = torch.tensor([-2.5, -90.0, -60.0, -95.0, -89.0, -87.0])
+    x[6, 2:8] = -150.0                 # none of them held: weights 0
+    x[7, 2:8] = torch.tensor([-150.0, -99.0, -150.0, -101.0, -150.0, -96.0])
+    x[8, 2:8] = torch.tensor([1.0, -99.0, -2.0, -101.0, 0.5, -96.0])
+    return x.to(DT[dtype])
+
+
+def tiny_weights(x, bias, mode, k, renorm, factor, T=None, load=True):
+    rows = torch.arange(T or len(x)) % len(x)
+    idx, w, _ = routed(x[rows].cuda(), bias, mode, 1, 1, 1, k, renorm, factor, load=load)
+    xs, b = x.float().numpy(), None if bias is None else bias.cpu().numpy()
+    idx, w = idx.cpu().numpy(), w.cpu().numpy()
+    for r in range(len(x)):
+        wi, ww, _ = route_row(xs[r], b, mode, 1, 1, 1, k, renorm, factor)
+        assert idx[r].tolist() == wi, r
+        lost = 2.0 ** -123 if renorm else 2.0 ** -148
+        close(w[r], ww, 2 * rel_tol(xs[r]) * np.abs(ww) + factor * lost)
+    again = torch.as_tensor(w[:len(x)])[rows].numpy()
+    assert np.array_equal(w.view(np.int32), again.view(np.int32))
+
+
+@pytest.mark.parametrize("mode", [SOFT, SIG])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("factor", [2.5, 8.0, 1e30])
+@pytest.mark.parametrize("E,T,load", [(12, None, True), (12, None, False), (12, 9000, True),
+                                      (100, 9000, True), (250, 9000, True), (300, None, True),
+                                      (600, None, True)])
+def test_weights_of_scores_that_fp32_hardly_holds(mode, renorm, factor, E, T, load):
+    """The bias chooses: six experts of tiny scores, in an order of its own."""
+    bias = torch.zeros(E)
+    bias[0] = -10.0
+    bias[2:8] = torch.tensor([3.0, 8.0, 4.0, 7.0, 5.0, 6.0])
+    for dtype in ("f32", "bf16"):
+        for k in (2, 6):
+            tiny_weights(tiny_queries(E, dtype), bias.cuda(), mode, k, renorm, factor, T, load)
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("E,T", [(12, None), (12, 9000), (64, 9000), (250, 9000), (300, None)])
+def test_logistic_weights_far_below_zero(renorm, E, T):
+    """Without a bias, 16-bit and 32-bit logits: all scores of a query are tiny."""
+    x = tiny_queries(E, "f32")[[0, 1, 2, 3, 4, 5, 8]]  # (scores of 0 are compared as logits)
+    x[:, 0] = -1e4
+    x[:, 2:8] += torch.arange(6) * 0.5  # (no ties by bf16's rounding)
+    for dtype in ("f32", "f16", "bf16"):
+        for k in (1, 4, 6):
+            tiny_weights(x.to(DT[dtype]), None, SIG, k, renorm, 8.0, T)
