@@ -31,8 +31,8 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 
-// A score may be as small as fp32 holds, 2^-149; below it is 0. Choices are made with approximate
-// instructions (exponential 2 ulp, reciprocal 1), as they are some hundred to a query.
+// A score may be as small as fp32 holds, 2^-149; below it is 0. Scores are made with approximate
+// instructions (exponential 2 ulp, reciprocal 1), as there are some hundred to a query.
 constexpr float kLeastLog2 = -149.f;
 // Scores that a sum of small ones is made of are taken relative to the largest of them where fewer
 // bits of them are left than fp32 has; beside a sum of 1/8 what is below 2^-126 is below 2^-123.
@@ -49,6 +49,11 @@ __device__ __forceinline__ float team_sum(float v) {
 #pragma unroll
   for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
   return v;
+}
+// Whether a ballot has a bit of this lane's team.
+template <int L>
+__device__ __forceinline__ bool of_team(unsigned ballot) {
+  return (ballot >> (threadIdx.x & 31) / L * L & (unsigned)((1ull << L) - 1)) != 0u;
 }
 template <int L>
 __device__ __forceinline__ float team_max(float v) {
@@ -492,11 +497,16 @@ __device__ __forceinline__ Query score_query(const RouteArgs &A, Bias bias, floa
   }
   return q;
 }
+// In place of the first choice of a query whose choice hangs on tiny values, of which those
+// compared have too few bits: it is made after the main loop, straight from the definition. (Rare:
+// making every value with all its bits took 4 to 8 % longer.)
+constexpr int kLater = -2;
 // Writes the chosen of a query: this lane's N candidates e (-1: none) of logits x in their places.
+// later (if any): the warp's note that a query has been left for later.
 template <int N, int L>
 __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q, long long row,
                                              bool live, const int (&e)[N], const int (&place)[N],
-                                             const float (&x)[N], int *hist) {
+                                             const float (&x)[N], int *hist, int *later) {
   float w[N], sum = 0.f;
   bool few = false;
 #pragma unroll
@@ -509,6 +519,18 @@ __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q,
   if (A.renorm) sum = team_sum<L>(sum);
   const unsigned teams = __ballot_sync(kAll, few);
   if (teams) {  // (a team's, whatever the warp's other queries)
+    if (later && !A.by_logits) {
+      bool tiny = false;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        tiny |= e[j] >= 0 && place[j] < A.k && fabsf(q.value(A, x[j], e[j])) < kFewBits;
+      if (of_team<L>(__ballot_sync(kAll, tiny))) {
+        if (live && (threadIdx.x & 31) % L == 0) A.idx[row * A.k] = kLater;
+        live = false;
+        *later = 1;
+      }
+      __syncwarp();
+    }
     float top = -INFINITY, over[N], all = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) top = e[j] >= 0 && place[j] < A.k ? fmaxf(top, x[j]) : top;
@@ -522,7 +544,7 @@ __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q,
       all += over[j];
     }
     all = team_sum<L>(all);
-    if (L == 32 || teams >> (threadIdx.x & 31) / L * L & ((1ull << L) - 1)) {
+    if (of_team<L>(teams)) {
       sum = all;
 #pragma unroll
       for (int j = 0; j < N; ++j) w[j] = over[j];
@@ -540,6 +562,69 @@ __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q,
     A.weight[row * A.k + place[j]] = q.bad ? NAN : A.factor * w[j];
     if (A.load && e[j] >= 0 && BOUTE_INB(e[j], A.E)) atomicAdd(hist + e[j], 1);
   }
+}
+// c of an expert, with the bits that fp32 has for its score where it is tiny.
+__device__ __forceinline__ float value_refined(const RouteArgs &A, const Query &q, long long row,
+                                               int e) {
+  const float x = logit_at(A, row, e), v = q.value(A, x, e);
+  if (!(fabsf(v) < kFewBits)) return v;
+  return __fadd_rn(q.whole_score(A, x), A.bias ? A.bias[e] : 0.f);
+}
+// A query by such values, by a whole warp.
+__device__ __forceinline__ void route_refined(const RouteArgs &A, long long row, int *hist) {
+  const int lane = threadIdx.x & 31, per = A.E / A.G;
+  Query q = {-INFINITY, 1.f, false};  // (a query without a distribution is not marked)
+  for (int i = lane; i < A.E; i += 32) q.m = fmaxf(q.m, logit_at(A, row, i));
+  q.m = team_max<32>(q.m);
+  if (A.mode == BOUTE_ROUTE_SOFTMAX) {
+    float sum = 0.f;
+    for (int i = lane; i < A.E; i += 32) sum += exp2_fast((logit_at(A, row, i) - q.m) * kLog2e);
+    q.inv_sum = __fdividef(1.f, team_sum<32>(sum));
+  }
+  float score = -INFINITY;  // of group `lane`
+  for (int g = 0; g < A.G; ++g) {
+    float a = -INFINITY, b = -INFINITY;
+    for (int i = lane; i < per; i += 32)
+      join_two(a, b, value_refined(A, q, row, g * per + i), -INFINITY);
+    for (int o = 16; o > 0; o >>= 1)
+      join_two(a, b, __shfl_xor_sync(kAll, a, o), __shfl_xor_sync(kAll, b, o));
+    if (lane == g) score = A.group_top == 2 && b > -INFINITY ? a + b : a;
+  }
+  int rank = 0, e[1] = {-1}, place[1] = {lane};
+  for (int h = 0; h < A.G; ++h) {
+    const float other = __shfl_sync(kAll, score, h);
+    rank += other > score || (other == score && h < lane);
+  }
+  const unsigned kept =
+      __ballot_sync(kAll, A.keep == A.G || (rank < A.keep && score > -INFINITY));
+  unsigned long long last = ~0ull;
+  for (int r = 0; r < A.k; ++r) {
+    unsigned long long best = 0ull;
+    for (int i = lane; i < A.E; i += 32) {
+      const float v = kept >> (i / per) & 1u ? value_refined(A, q, row, i) : -INFINITY;
+      const unsigned long long key = v > -INFINITY ? make_key(v, (unsigned)i) : 0ull;
+      if (key < last) best = max(best, key);
+    }
+    for (int o = 16; o > 0; o >>= 1) best = max(best, shfl_xor64(best, o));
+    if (lane == r && best) e[0] = (int)key_index(best);
+    last = best;
+  }
+  const float x[1] = {e[0] >= 0 ? logit_at(A, row, e[0]) : -INFINITY};
+  write_chosen<1, 32>(A, q, row, true, e, place, x, hist, nullptr);
+}
+// A warp's marked queries, of the groups of `of` neighbours that it took.
+__device__ __forceinline__ void route_later(const RouteArgs &A, const int *later, int of,
+                                            int *hist) {
+  __syncwarp();
+  if (*later == 0) return;
+  const long long step = (long long)gridDim.x * kWarps * of;
+  for (long long row0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * of; row0 < A.rows;
+       row0 += step)
+    for (long long row = row0; row < min(row0 + of, A.rows); ++row)
+      if (A.idx[row * A.k] == kLater) {
+        __syncwarp();
+        route_refined(A, row, hist);
+      }
 }
 // The block's load: cleared, and added to the whole one. (Behind clear_load_kernel too the wait
 // comes before any read or write of the call's arrays: that kernel has waited for what came before
@@ -686,7 +771,7 @@ __global__ void __launch_bounds__(kThreads, 4) route_pairs_kernel(RouteArgs A) {
                exp2_fast((P::value(w[i].w >> 16) - q.m) * kLog2e);
       q.inv_sum = __fdividef(1.f, team_sum<L>(sum));
     }
-    write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist);
+    write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist, nullptr);
   }
   end_load(A, hist);
 }
@@ -698,11 +783,13 @@ __global__ void __launch_bounds__(kThreads, S > 16 ? 4 : 5) route_bound_kernel(R
   constexpr int L = 8, kTeams = 32 / L, kOwn = K / 4, kSlots = L * kOwn;
   extern __shared__ int hist[];  // the block's load; then, with groups, c and the groups' scores
   __shared__ unsigned long long keys[kWarps * kTeams][kSlots];
+  __shared__ int later[kWarps];
   __shared__ alignas(16) float bias[L * (S + 4)];  // (lanes' parts begin in different banks)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = A.E, l = lane % L;
   const int e0 = l * A.own, end = min(e0 + A.own, E);
   float *shared_c = (float *)(hist + E) + (warp * kTeams + lane / L) * shared_stride(E);
   unsigned long long *to = keys[warp * kTeams + lane / L];
+  if (lane == 0) later[warp] = 0;
   begin_load(A, hist);
   for (int i = threadIdx.x; i < L * S; i += kThreads) {
     const int at = i % S, e = i / S * A.own + at;
@@ -766,8 +853,9 @@ __global__ void __launch_bounds__(kThreads, S > 16 ? 4 : 5) route_bound_kernel(R
       e[j] = key[j] ? (int)key_index(key[j]) : -1;
       x[j] = e[j] >= 0 ? logit_at(A, row, e[j]) : -INFINITY;
     }
-    write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist);
+    write_chosen<kOwn, L>(A, q, row, live, e, place, x, hist, later + warp);
   }
+  route_later(A, later + warp, kTeams, hist);
   end_load(A, hist);
 }
 
@@ -814,8 +902,11 @@ __device__ __forceinline__ void choose(const float (&c)[S], int k, float &mine, 
 template <int S, int K>
 __global__ void __launch_bounds__(kThreads, S > 8 ? 1 : 5) route_warp_kernel(RouteArgs A) {
   extern __shared__ int hist[];
+  __shared__ int later[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e0 = lane * S;
   float *shared_c = (float *)(hist + A.E) + warp * shared_stride(A.E);
+  if (lane == 0) later[warp] = 0;
+  __syncwarp();
   begin_load(A, hist);
   float bias[S];
   load_bias(A, e0, bias);
@@ -829,8 +920,9 @@ __global__ void __launch_bounds__(kThreads, S > 8 ? 1 : 5) route_warp_kernel(Rou
     choose<S, K>(c, A.k, mine, e[0]);
     if (lane >= A.k) e[0] = -1;
     const float x[1] = {e[0] < 0 ? -INFINITY : A.by_logits ? mine : logit_at(A, row, e[0])};
-    write_chosen<1, 32>(A, q, row, true, e, place, x, hist);
+    write_chosen<1, 32>(A, q, row, true, e, place, x, hist, later + warp);
   }
+  route_later(A, later + warp, 1, hist);
   end_load(A, hist);
 }
 

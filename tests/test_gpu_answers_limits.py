@@ -159,3 +159,29 @@ def test_logistic_weights_far_below_zero(renorm, E, T):
     for dtype in ("f32", "f16", "bf16"):
         for k in (1, 4, 6):
             tiny_weights(x.to(DT[dtype]), None, SIG, k, renorm, 8.0, T)
+
+
+@pytest.mark.parametrize("mode", [SOFT, SIG])
+@pytest.mark.parametrize("groups", [False, True])
+@pytest.mark.parametrize("E,T,load", [(12, None, True), (12, None, False), (12, 9000, True),
+                                      (100, 9000, True), (250, 9000, True), (300, None, True),
+                                      (1000, None, True)])
+def test_choice_among_scores_that_fp32_hardly_holds(mode, groups, E, T, load):
+    """Tiny scores decide: beside a bias of 0 whose best expert is out of service, and as groups'
+    sums of two. (They are some units of 2^-149 apart, or 0 and equal.)"""
+    for dtype in ("f32", "bf16"):
+        x = tiny_queries(E, dtype)
+        if groups:
+            bias, a = None, (E // (4 if E < 200 else 10 if E < 300 else 12 if E == 300 else 40), 1, 2, 4)
+            if mode == SIG:
+                x[:, 0] = -1e4
+        else:
+            bias, a = torch.zeros(E), (1, 1, 1, 6)
+            bias[0] = -float("inf")
+        rows = torch.arange(T or len(x)) % len(x)
+        idx, _, _ = routed(x[rows].cuda(), None if bias is None else bias.cuda(), mode, *a, True, 1.0,
+                           load=load)
+        xs = x.float().numpy()
+        want = [route_row(r, None if bias is None else bias.numpy(), mode, *a, True, 1.0)[0] for r in xs]
+        assert idx[:len(x)].tolist() == want
+        assert torch.equal(idx, idx[:len(x)][rows.cuda()])
