@@ -61,6 +61,10 @@ __device__ __forceinline__ float team_max(float v) {
   for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
   return v;
 }
+__device__ __forceinline__ float team_max(float v, int team) {
+  for (int o = team / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+  return v;
+}
 __device__ __forceinline__ float team_sum(float v, int team) {
   for (int o = team / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
   return v;
@@ -1035,12 +1039,21 @@ __global__ void __launch_bounds__(kThreads)
       const float S = team_sum(v, team), w = S > 0.f ? v / S : 0.f;
       d = w * (g - team_sum(w * g, team));
     } else if (A.renorm) {
-      const float v = e >= 0 ? logistic(x) : 0.f, S = team_sum(v, team);
+      float v = e >= 0 ? logistic(x) : 0.f, S = team_sum(v, team);
+      if (__any_sync(kAll, e >= 0 && v < kFewBits)) {  // tiny scores, as in write_chosen
+        const float tiny = team_max(e >= 0 && v < kFewBits ? 1.f : 0.f, team);
+        const float top = team_max(e >= 0 ? x : -INFINITY, team);
+        const float over = e >= 0 && x * kLog2e >= kLeastLog2
+                               ? exp2_fast((x - top) * kLog2e) / (1.f + exp2_fast(x * kLog2e))
+                               : 0.f;
+        const float all = team_sum(over, team);
+        if (tiny > 0.f && S < kSmallSum) v = over, S = all;
+      }
       const float w = S > 0.f ? v / S : 0.f;
       const float q = exp2_fast(-fabsf(x) * kLog2e);  // 1 - s without the difference
       d = w * (g - team_sum(w * g, team)) * (x >= 0.f ? q : 1.f) / (1.f + q);
     } else if (e >= 0) {
-      const float q = exp2_fast(-fabsf(x) * kLog2e);
+      const float q = exp2_gradual(-fabsf(x) * kLog2e);
       d = g * q / ((1.f + q) * (1.f + q));
     }
     __syncwarp();  // (in place: every chosen logit has been read)

@@ -4,9 +4,11 @@ import numpy as np
 import pytest
 import torch
 
-from _answers import U, answer_grad, answer_rows, route_row, token_grad_row
+from _answers import (U, answer_grad, answer_rows, route_grad_row, route_row, scores,
+                      token_grad_row)
 from paper_2602_10729_gb300 import boute as bt
-from test_gpu_answers import DT, EPS, answers, check_forward, close, forward, logits, scored
+from test_gpu_answers import (DT, EPS, answers, check_forward, close, forward, logits, placed,
+                              scored)
 from test_gpu_routing import SIG, SOFT, rel_tol, routed
 
 pytestmark = pytest.mark.gpu
@@ -185,3 +187,47 @@ def test_choice_among_scores_that_fp32_hardly_holds(mode, groups, E, T, load):
         want = [route_row(r, None if bias is None else bias.numpy(), mode, *a, True, 1.0)[0] for r in xs]
         assert idx[:len(x)].tolist() == want
         assert torch.equal(idx, idx[:len(x)][rows.cuda()])
+
+
+# Of a gradient the error is that of the other tests: of the scores' relative error times the terms
+# that they scale, which for weights with a sum are w (|g| + sum w |g|), whatever the sum's size.
+def tiny_gradient(x, mode, idx, renorm, factor, seed, pitch=0, shift=0):
+    T, k = idx.shape
+    g = torch.randn((T, k), generator=torch.Generator().manual_seed(seed))
+    xs = placed(x, pitch, shift)
+    dx = torch.full(x.shape, 9.0, dtype=x.dtype, device="cuda")
+    bt.boute_route_grad(xs, mode, renorm, factor, idx.cuda(), g.cuda(), dx)
+    got, xf = dx.float().cpu().numpy(), x.float().numpy()
+    name = {v: n for n, v in DT.items()}[x.dtype]
+    for r in range(T):
+        i = idx[r].tolist()
+        want = route_grad_row(xf[r], mode, i, g[r].tolist(), renorm, factor)
+        s = scores(xf[r], mode)
+        on = [e for e in i if e >= 0]
+        gm = float(g[r].abs().max()) * factor
+        terms = np.zeros(len(xf[r]))
+        terms[on] = 2 * gm * (s[on] / s[on].sum() if renorm and s[on].sum() > 0 else s[on])
+        if mode == SOFT and not renorm:
+            terms = gm * (terms > 0) * s + gm * s * s[on].sum()
+        tiny = 2.0 ** -25 if name == "f16" else factor * 2.0 ** -122
+        close(got[r], want, 4 * rel_tol(xf[r]) * terms + np.abs(want) * EPS[name] * 1.01 + tiny)
+    bt.boute_route_grad(xs, mode, renorm, factor, idx.cuda(), g.cuda(), xs)  # in place
+    assert torch.equal(xs, dx)
+
+
+def tiny_choices(T, k):
+    """The experts of tiny scores in turn, one row without a choice, one with a choice missing."""
+    idx = torch.stack([(torch.arange(k) + r) % 6 + 2 for r in range(T)]).to(torch.int32)
+    idx[2] = -1
+    idx[3, 0] = -1
+    return idx
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("E,k,pitch,shift", [(12, 1, 0, 0), (12, 6, 3, 1), (100, 4, 0, 0), (61, 5, 0, 1),
+                                             (1000, 6, 8, 0)])
+def test_gradient_of_logistic_scores_that_fp32_hardly_holds(renorm, E, k, pitch, shift):
+    for dtype in ("f32", "bf16"):
+        for factor in (1.0, 64.0):
+            x = tiny_queries(E, dtype)
+            tiny_gradient(x, SIG, tiny_choices(len(x), k), renorm, factor, E, pitch, shift)
