@@ -204,6 +204,11 @@ def tiny_gradient(x, mode, idx, renorm, factor, seed, pitch=0, shift=0):
         want = route_grad_row(xf[r], mode, i, g[r].tolist(), renorm, factor)
         s = scores(xf[r], mode)
         on = [e for e in i if e >= 0]
+        if mode == SOFT and renorm:  # the same with w = s / S, in which what 64 bits leave of S - S is 0
+            w = s[on] / s[on].sum() if s[on].sum() > 0 else 0.0 * s[on]
+            gs = factor * np.array([g[r, j] for j in range(k) if i[j] >= 0], np.float64)
+            want = np.zeros(len(want))
+            want[on] = w * (gs - (w * gs).sum())
         gm = float(g[r].abs().max()) * factor
         terms = np.zeros(len(xf[r]))
         terms[on] = 2 * gm * (s[on] / s[on].sum() if renorm and s[on].sum() > 0 else s[on])
@@ -231,3 +236,27 @@ def test_gradient_of_logistic_scores_that_fp32_hardly_holds(renorm, E, k, pitch,
         for factor in (1.0, 64.0):
             x = tiny_queries(E, dtype)
             tiny_gradient(x, SIG, tiny_choices(len(x), k), renorm, factor, E, pitch, shift)
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("E,k,pitch,shift", [(12, 1, 0, 0), (12, 6, 3, 1), (100, 4, 0, 0), (61, 5, 0, 1),
+                                             (61, 2, 0, 3), (1000, 6, 8, 0), (333, 3, 1, 5)])
+def test_gradient_of_softmax_scores_that_fp32_hardly_holds(renorm, dtype, E, k, pitch, shift):
+    """A bias (or groups) has chosen experts far below the row's largest logit: weights that are 0
+    have gradient 0."""
+    for factor in (1.0, 64.0):
+        x = tiny_queries(E, dtype)
+        x[5, E - 1] = 3.0 if E > 12 else x[5, E - 1]   # the largest logit at the row's end
+        x[6, -2:] = 1.5
+        tiny_gradient(x, SOFT, tiny_choices(len(x), k), renorm, factor, E, pitch, shift)
+
+
+def test_weights_and_gradient_agree_where_a_softmax_underflows():
+    x = torch.tensor([[200.0, 0.0, 0.0, -1.0]]).cuda()
+    bias = torch.tensor([-10.0, 0.0, 0.0, 0.0]).cuda()
+    idx, w, _ = routed(x, bias, SOFT, 1, 1, 1, 2, True, 1.0, load=False)
+    assert idx.tolist() == [[1, 2]] and w.tolist() == [[0.0, 0.0]]
+    dx = torch.full_like(x, 9.0)
+    bt.boute_route_grad(x, SOFT, True, 1.0, idx, torch.tensor([[1.0, -2.0]]).cuda(), dx)
+    assert (dx == 0).all()
