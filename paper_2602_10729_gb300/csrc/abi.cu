@@ -28,27 +28,9 @@ int last_launch_status() {
   return BOUTE_ERR_CUDA;
 }
 
-// The kernels are built for sm_103a only: refuse other devices up front (a
-// failed device query leaves no error behind for later calls to report).
-// A device's answer does not change; asking took 0.7 us a call.
 DeviceInfo device_info() {
-  constexpr int kMax = 64;
-  static std::atomic<int> known[kMax];  // 0, or sms * 2 + (ok: 1)
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) {
-    cudaGetLastError();
-    return {BOUTE_ERR_UNSUPPORTED, 152};
-  }
-  int v = dev < kMax ? known[dev].load(std::memory_order_relaxed) : 0;
-  if (v == 0) {
-    int major = 0, minor = 0, sms = 152;
-    cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-    cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
-    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    v = sms * 2 + (major == 10 && minor == 3);
-    if (dev < kMax) known[dev].store(v, std::memory_order_relaxed);
-  }
-  return {v & 1 ? BOUTE_OK : BOUTE_ERR_UNSUPPORTED, v / 2};
+  static std::atomic<int> known[kKnownDevices];
+  return ask_device(known);
 }
 int device_ok() { return device_info().ok; }
 

@@ -5,6 +5,7 @@
 
 #include "bounds.cuh"
 #include "common.cuh"
+#include "device_info.h"
 
 #include <nvtx3/nvToolsExt.h>
 
@@ -85,11 +86,6 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// What the library asks of a device on every call, asked of the runtime once (abi.cu).
-struct DeviceInfo {
-  int ok;   // BOUTE_OK for sm_103a
-  int sms;  // multiprocessors
-};
 DeviceInfo device_info();  // of the current device; ok != BOUTE_OK without one
 inline int num_sms() { return device_info().sms; }
 
