@@ -632,9 +632,9 @@ def boute_engine_free(e: Engine):
 _DTYPES = {torch.float32: BOUTE_F32, torch.float16: BOUTE_F16, torch.bfloat16: BOUTE_BF16}
 
 
-def _rows(t, like=None):
-    """(pointer, dtype code, rows, row length, pitch) of a 2-dimensional CUDA tensor whose rows
-    are contiguous."""
+def _rows(t, dev=None, like=None):
+    """(pointer, device, dtype code, rows, row length, pitch) of a 2-dimensional CUDA tensor (on
+    device dev, if given) whose rows are contiguous."""
     code = _DTYPES.get(t.dtype)
     if code is None or (like is not None and t.dtype != like.dtype):
         raise TypeError(f"unsupported or different dtype {t.dtype}")
@@ -649,20 +649,41 @@ def _rows(t, like=None):
         pitch = V
     elif pitch < V:
         raise ValueError("rows must not overlap")
-    if not t.is_cuda:
+    on = t.get_device()
+    if on < 0:
         raise ValueError("expected a CUDA tensor")
-    return t.data_ptr(), code, T, V, pitch
+    if dev is not None and on != dev:
+        raise ValueError(f"tensors on devices {dev} and {on}")
+    return t.data_ptr(), on, code, T, V, pitch
 
 
-def _pn(t, dtype, shape):
-    """Pointer of a contiguous CUDA tensor of this dtype and shape, or None."""
+def _pn(t, dtype, shape, dev):
+    """Pointer of a contiguous CUDA tensor of this dtype and shape on device dev, or None."""
     if t is None:
         return None
     if t.shape != shape:
         raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_contiguous():
         return _p(t, dtype)  # raises
+    on = t.get_device()
+    if on != dev or on < 0:
+        raise ValueError("expected a CUDA tensor" if on < 0 else
+                         f"tensors on devices {dev} and {on}")
     return t.data_ptr()
+
+
+def _s_on(stream, dev):
+    """The stream's handle for a launch with tensors of device dev, which has to be the current
+    one."""
+    cur = torch.cuda.current_device()
+    if dev != cur:
+        raise ValueError(f"tensors on device {dev}, but device {cur} is the current one")
+    if stream is None:
+        return _raw_stream(cur)
+    if getattr(stream, "device_index", cur) != cur:
+        raise ValueError(f"a stream of device {stream.device_index}, but device {cur} is the "
+                         "current one")
+    return _s(stream)
 
 
 def boute_token_logprobs(logits, targets, scale, logprob, entropy, lse, top_idx=None,
@@ -671,12 +692,13 @@ def boute_token_logprobs(logits, targets, scale, logprob, entropy, lse, top_idx=
     (< 0: no token); logprob, entropy, lse: T fp32; top_idx: T x k int64 and
     top_logprob: T x k fp32, the k alternatives (both or neither)."""
     f32 = torch.float32
-    x, code, T, V, ld = _rows(logits)
+    x, dev, code, T, V, ld = _rows(logits)
     k = 0 if top_idx is None else top_idx.shape[-1]
-    _check(load().boute_token_logprobs(x, code, T, V, ld, _pn(targets, torch.int64, (T,)),
-                                       scale, k, _pn(logprob, f32, (T,)), _pn(entropy, f32, (T,)),
-                                       _pn(lse, f32, (T,)), _pn(top_idx, torch.int64, (T, k)),
-                                       _pn(top_logprob, f32, (T, k)), _s(stream)),
+    _check(load().boute_token_logprobs(x, code, T, V, ld, _pn(targets, torch.int64, (T,), dev),
+                                       scale, k, _pn(logprob, f32, (T,), dev),
+                                       _pn(entropy, f32, (T,), dev), _pn(lse, f32, (T,), dev),
+                                       _pn(top_idx, torch.int64, (T, k), dev),
+                                       _pn(top_logprob, f32, (T, k), dev), _s_on(stream, dev)),
            "boute_token_logprobs")
 
 
@@ -684,34 +706,41 @@ def boute_token_logprobs_grad(logits, targets, scale, lse, entropy, g_logprob, g
                               stream=None):
     """entropy and g_entropy may be None; dlogits: T x V of the logits' dtype, may be logits."""
     f32 = torch.float32
-    x, code, T, V, ld = _rows(logits)
-    dx, _, _, _, ldd = _rows(dlogits, logits)
-    _check(load().boute_token_logprobs_grad(x, code, T, V, ld, _pn(targets, torch.int64, (T,)),
-                                            scale, _pn(lse, f32, (T,)), _pn(entropy, f32, (T,)),
-                                            _pn(g_logprob, f32, (T,)), _pn(g_entropy, f32, (T,)), dx,
-                                            ldd, _s(stream)), "boute_token_logprobs_grad")
+    x, dev, code, T, V, ld = _rows(logits)
+    dx, _, _, _, _, ldd = _rows(dlogits, dev, logits)
+    _check(load().boute_token_logprobs_grad(x, code, T, V, ld, _pn(targets, torch.int64, (T,), dev),
+                                            scale, _pn(lse, f32, (T,), dev),
+                                            _pn(entropy, f32, (T,), dev),
+                                            _pn(g_logprob, f32, (T,), dev),
+                                            _pn(g_entropy, f32, (T,), dev), dx, ldd,
+                                            _s_on(stream, dev)), "boute_token_logprobs_grad")
 
 
 def boute_answer_scores(logprob, entropy, targets, offsets, scores, counts, stream=None):
     """logprob, entropy: T fp32; targets: T int64 or None; offsets: Q + 1 int64;
     scores: Q x 4 fp32; counts: Q int32."""
     f32, i64 = torch.float32, torch.int64
-    T, Q = logprob.shape[0], offsets.shape[0] - 1
-    _check(load().boute_answer_scores(_pn(logprob, f32, (T,)), _pn(entropy, f32, (T,)),
-                                      _pn(targets, i64, (T,)), _pn(offsets, i64, (Q + 1,)), T, Q,
-                                      _pn(scores, f32, (Q, 4)), _pn(counts, torch.int32, (Q,)),
-                                      _s(stream)), "boute_answer_scores")
+    T, Q, dev = logprob.shape[0], offsets.shape[0] - 1, logprob.get_device()
+    _check(load().boute_answer_scores(_pn(logprob, f32, (T,), dev), _pn(entropy, f32, (T,), dev),
+                                      _pn(targets, i64, (T,), dev),
+                                      _pn(offsets, i64, (Q + 1,), dev), T, Q,
+                                      _pn(scores, f32, (Q, 4), dev),
+                                      _pn(counts, torch.int32, (Q,), dev),
+                                      _s_on(stream, dev)), "boute_answer_scores")
 
 
 def boute_answer_scores_grad(logprob, entropy, targets, offsets, g_scores, g_logprob, g_entropy,
                              stream=None):
     """g_scores: Q x 4 fp32 in; g_logprob, g_entropy: T fp32 out."""
     f32, i64 = torch.float32, torch.int64
-    T, Q = logprob.shape[0], offsets.shape[0] - 1
-    _check(load().boute_answer_scores_grad(_pn(logprob, f32, (T,)), _pn(entropy, f32, (T,)),
-                                           _pn(targets, i64, (T,)), _pn(offsets, i64, (Q + 1,)), T, Q,
-                                           _pn(g_scores, f32, (Q, 4)), _pn(g_logprob, f32, (T,)),
-                                           _pn(g_entropy, f32, (T,)), _s(stream)),
+    T, Q, dev = logprob.shape[0], offsets.shape[0] - 1, logprob.get_device()
+    _check(load().boute_answer_scores_grad(_pn(logprob, f32, (T,), dev),
+                                           _pn(entropy, f32, (T,), dev),
+                                           _pn(targets, i64, (T,), dev),
+                                           _pn(offsets, i64, (Q + 1,), dev), T, Q,
+                                           _pn(g_scores, f32, (Q, 4), dev),
+                                           _pn(g_logprob, f32, (T,), dev),
+                                           _pn(g_entropy, f32, (T,), dev), _s_on(stream, dev)),
            "boute_answer_scores_grad")
 
 
@@ -719,21 +748,24 @@ def boute_route(logits, bias, mode, G, keep, group_top, renorm, factor, idx, wei
                 stream=None):
     """logits: T x E (fp32, fp16 or bf16, rows contiguous); bias: E fp32 or None;
     mode: BOUTE_ROUTE_*; idx: T x k int32; weight: T x k fp32; load_: E int32 or None."""
-    x, code, T, E, ld = _rows(logits)
+    x, dev, code, T, E, ld = _rows(logits)
     k = idx.shape[-1]
-    _check(load().boute_route(x, code, T, E, ld, _pn(bias, torch.float32, (E,)), mode, G, keep,
-                              group_top, k, bool(renorm), factor, _pn(idx, torch.int32, (T, k)),
-                              _pn(weight, torch.float32, (T, k)), _pn(load_, torch.int32, (E,)),
-                              _s(stream)), "boute_route")
+    _check(load().boute_route(x, code, T, E, ld, _pn(bias, torch.float32, (E,), dev), mode, G, keep,
+                              group_top, k, bool(renorm), factor,
+                              _pn(idx, torch.int32, (T, k), dev),
+                              _pn(weight, torch.float32, (T, k), dev),
+                              _pn(load_, torch.int32, (E,), dev),
+                              _s_on(stream, dev)), "boute_route")
 
 
 def boute_route_grad(logits, mode, renorm, factor, idx, g_weight, dlogits, stream=None):
     """idx: T x k int32 (-1: none); g_weight: T x k fp32; dlogits: T x E of the
     logits' dtype, may be logits."""
-    x, code, T, E, ld = _rows(logits)
-    dx, _, _, _, ldd = _rows(dlogits, logits)
+    x, dev, code, T, E, ld = _rows(logits)
+    dx, _, _, _, _, ldd = _rows(dlogits, dev, logits)
     k = idx.shape[-1]
     _check(load().boute_route_grad(x, code, T, E, ld, mode, k, bool(renorm), factor,
-                                   _pn(idx, torch.int32, (T, k)),
-                                   _pn(g_weight, torch.float32, (T, k)), dx, ldd, _s(stream)),
+                                   _pn(idx, torch.int32, (T, k), dev),
+                                   _pn(g_weight, torch.float32, (T, k), dev), dx, ldd,
+                                   _s_on(stream, dev)),
            "boute_route_grad")
