@@ -49,11 +49,16 @@ struct Piece {
   static __host__ __device__ int count(int off, int V) { return (off + V + SPAN - 1) / SPAN; }
 };
 
-// A whole piece, read once (its lines need not stay in L1); at: its first logit.
+// A whole piece of a row y of V logits from its logit `first` on, read once (its lines need not stay
+// in L1).
 template <class T>
-__device__ __forceinline__ Piece<T> load_whole(const T *at) {
+__device__ __forceinline__ Piece<T> load_whole(const T *y, int V, long long first) {
   Piece<T> r;
-  const uint4 *p = (const uint4 *)at + (threadIdx.x & 31);
+  if (!BOUTE_INB(first, V) || !BOUTE_INB(first + Piece<T>::SPAN - 1, V)) {
+    memset(r.v, 0, sizeof(r.v));
+    return r;
+  }
+  const uint4 *p = (const uint4 *)(y + first) + (threadIdx.x & 31);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
@@ -102,6 +107,7 @@ template <class T>
 __device__ __forceinline__ void store_piece(T *y, int V, int first, const Piece<T> &r) {
   constexpr int E = Piece<T>::E;
   if (first >= 0 && first + Piece<T>::SPAN <= V) {
+    if (!BOUTE_INB((uintptr_t)(y + first) % 16, 1)) return;  // (a boundary)
     uint4 *p = (uint4 *)(y + first) + (threadIdx.x & 31);
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[32 * i] = r.v[i];
@@ -302,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   int q1 = -1, q2 = -1;
   for (int q = first; q < Q; q += step) {
     const bool whole = q >= whole0 && q < whole1;
-    const Piece<T> p = whole ? load_whole(x + ((long long)q * SPAN - off))
+    const Piece<T> p = whole ? load_whole(x, V, (long long)q * SPAN - off)
                              : load_piece(x, V, q * SPAN - off, 0);
     const float l = lane_max(p);
     if (k > 0) {
@@ -350,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   __syncthreads();
   if (CS > 1) {
     cluster_runs();
-    if (tid == 0) {
+    if (tid == 0 && BOUTE_INB(rank, kMaxCluster)) {
       Sums a = wsum[0];
       for (int w = 1; w < W; ++w) {
         if (isnan(wsum[w].m)) a.m = NAN;
@@ -366,7 +372,8 @@ __global__ void __launch_bounds__(kThreads, 4)
     if (k > 0 && tid < mine) {
       float t = -INFINITY;
       for (int i = tid; i < NT; i += mine) t = max_nan(t, lanes[i]);
-      for (int b = 0; b < CS; ++b) store_peer(peer(&tops[rank * mine + tid], b), t);
+      for (int b = 0; b < CS; ++b)
+        if (BOUTE_INB(rank * mine + tid, kTops)) store_peer(peer(&tops[rank * mine + tid], b), t);
     }
     cluster_sync();
   }
@@ -416,6 +423,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         hit &= hit - 1;
         const int index = q * SPAN - off + Piece<T>::index(j, of);
         if (index < 0 || index >= V) continue;  // (-inf beyond the row, with a bound of -inf)
+        if (!BOUTE_INB(q, Q)) continue;  // (a piece of this row)
         const float z = __fmul_rn(to_float(x[index]), scale);
         if (z == -INFINITY) continue;
         const int to = add_peer(peer(&nlist, 0), 1);
@@ -482,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 4)
       const unsigned long long key = list[i];
       int place = 0;
       for (int j = 0; j < n; ++j) place += list[j] > key;
-      if (place < k) {
+      if (place < k && BOUTE_INB(key_index(key), V)) {
         top_idx[row * k + place] = (long long)key_index(key);
         top_logprob[row * k + place] = from_order_bits((unsigned)(key >> 32)) - M - ls;
       }
@@ -526,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   const int whole0 = off ? 1 : 0, whole1 = (off + V) / SPAN;
   auto load = [&](int q) {
     return shift == 0 && q >= whole0 && q < whole1
-               ? load_whole(x + ((long long)q * SPAN - off))
+               ? load_whole(x, V, (long long)q * SPAN - off)
                : load_piece(x, V, q * SPAN - off, shift);
   };
   const long long t = targets[row];
@@ -560,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     if (CS > 1) {
       // (every block has read its part of the row before any writes: in place)
       cluster_runs();
-      if (threadIdx.x < CS) {
+      if (threadIdx.x < CS && BOUTE_INB(rank, kMaxCluster)) {
         store_peer(peer(&csum[rank][0], threadIdx.x), a.m);
         store_peer(peer(&csum[rank][1], threadIdx.x), a.s);
       }

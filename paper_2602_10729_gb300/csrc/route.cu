@@ -86,40 +86,44 @@ struct RouteArgs {
 };
 
 __device__ __forceinline__ float logit_at(const RouteArgs &A, long long row, int e) {
+  if (!BOUTE_INB(e, A.E) || !BOUTE_INB(row, A.rows)) return -INFINITY;
   const long long i = row * A.ld + e;
   if (A.dtype == BOUTE_F32) return ((const float *)A.logits)[i];
   if (A.dtype == BOUTE_F16) return __half2float(((const __half *)A.logits)[i]);
   return __bfloat162float(((const __nv_bfloat16 *)A.logits)[i]);
 }
 // N words of 4-byte (PER = 1) or pairs of 2-byte logits from e0 on, by vectors of up to 16 bytes
-// where rows allow (`vec`); `none` beyond E.
+// where rows allow (`vec`); `none` from `end` on, of a row of E.
 template <int N, int PER>
-__device__ __forceinline__ void load_words(uint32_t *w, const void *row, int e0, int E, bool vec,
-                                           uint32_t none) {
+__device__ __forceinline__ void load_words(uint32_t *w, const void *row, int e0, int end, int E,
+                                           bool vec, uint32_t none) {
   static_assert(N == 1 || N == 2 || N % 4 == 0, "whole vectors");
   if (vec && N == 1) {
-    w[0] = e0 < E ? *((const uint32_t *)row + e0 / PER) : none;
+    w[0] = e0 < end && BOUTE_INB(e0 + PER - 1, E) ? *((const uint32_t *)row + e0 / PER) : none;
   } else if (vec && N == 2) {
     uint2 v = {none, none};
-    if (e0 < E) v = *(const uint2 *)((const uint32_t *)row + e0 / PER);
+    if (e0 < end && BOUTE_INB(e0 + 2 * PER - 1, E))
+      v = *(const uint2 *)((const uint32_t *)row + e0 / PER);
     w[0] = v.x, w[N - 1] = v.y;
   } else if (vec) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
       uint4 v = {none, none, none, none};
-      if (e0 + 4 * PER * i < E) v = *(const uint4 *)((const uint32_t *)row + e0 / PER + 4 * i);
+      if (e0 + 4 * PER * i < end && BOUTE_INB(e0 + 4 * PER * (i + 1) - 1, E))
+        v = *(const uint4 *)((const uint32_t *)row + e0 / PER + 4 * i);
       w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
     }
   } else if constexpr (PER == 1) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = e0 + i < E ? ((const uint32_t *)row)[e0 + i] : none;
+    for (int i = 0; i < N; ++i)
+      w[i] = e0 + i < end && BOUTE_INB(e0 + i, E) ? ((const uint32_t *)row)[e0 + i] : none;
   } else {
     const unsigned short *h = (const unsigned short *)row;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int e = e0 + 2 * i;
-      w[i] = (e < E ? (uint32_t)h[e] : none & 0xffffu) |
-             (e + 1 < E ? (uint32_t)h[e + 1] << 16 : none & 0xffff0000u);
+      w[i] = (e < end && BOUTE_INB(e, E) ? (uint32_t)h[e] : none & 0xffffu) |
+             (e + 1 < end && BOUTE_INB(e + 1, E) ? (uint32_t)h[e + 1] << 16 : none & 0xffff0000u);
     }
   }
 }
@@ -346,7 +350,8 @@ __device__ __forceinline__ unsigned keep_groups(const float *c, float *scores, c
     float a = -INFINITY, b = -INFINITY;
     if (g < A.G)
 #pragma unroll 4
-      for (int i = l % width; i < per; i += width) join_two(a, b, c[g * per + i], -INFINITY);
+      for (int i = l % width; i < per; i += width) 
+        if (BOUTE_INB(g * per + i, A.E)) join_two(a, b, c[g * per + i], -INFINITY);
     for (int o = 1; o < width; o *= 2)
       join_two(a, b, __shfl_xor_sync(kAll, a, o), __shfl_xor_sync(kAll, b, o));
     if (g < A.G && l % width == 0) scores[g] = A.group_top == 2 && b > -INFINITY ? a + b : a;
@@ -396,7 +401,7 @@ __device__ __forceinline__ void apply_groups(const RouteArgs &A, float (&c)[S], 
   }
 #pragma unroll
   for (int s = 0; s < S; ++s)
-    if (e0 + s < end) shared[e0 + s] = c[s];
+    if (e0 + s < end && BOUTE_INB(e0 + s, A.E)) shared[e0 + s] = c[s];
   __syncwarp();
   const unsigned kept = keep_groups<L>(shared, shared + A.E, A, A.E / A.G, l);
   __syncwarp();
@@ -446,12 +451,12 @@ __device__ __forceinline__ void load_logits(const RouteArgs &A, long long row, i
                                             float (&c)[S]) {
   if (A.dtype == BOUTE_F32) {
     uint32_t w[S];
-    load_words<S, 1>(w, (const float *)A.logits + row * A.ld, e0, end, A.vec, 0xff800000u);
+    load_words<S, 1>(w, (const float *)A.logits + row * A.ld, e0, end, A.E, A.vec, 0xff800000u);
 #pragma unroll
     for (int s = 0; s < S; ++s) c[s] = __uint_as_float(w[s]);
   } else {
     uint32_t w[S / 2];
-    load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, end, A.vec,
+    load_words<S / 2, 2>(w, (const unsigned short *)A.logits + row * A.ld, e0, end, A.E, A.vec,
                          A.dtype == BOUTE_F16 ? 0xfc00fc00u : 0xff80ff80u);
 #pragma unroll
     for (int i = 0; i < S / 2; ++i)
@@ -562,6 +567,7 @@ __device__ __forceinline__ void write_chosen(const RouteArgs &A, const Query &q,
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     if (!live || place[j] >= A.k) continue;
+    if (!BOUTE_INB(place[j], A.k) || !BOUTE_INB(row, A.rows)) continue;
     A.idx[row * A.k + place[j]] = e[j];
     A.weight[row * A.k + place[j]] = q.bad ? NAN : A.factor * w[j];
     if (A.load && e[j] >= 0 && BOUTE_INB(e[j], A.E)) atomicAdd(hist + e[j], 1);
@@ -671,7 +677,7 @@ __device__ __forceinline__ void in_order(Key *to, int n, int l, Key (&key)[OWN],
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < OWN; ++j)
-    if (place[j] < n) to[rank[j]] = key[j];
+    if (place[j] < n && BOUTE_INB(rank[j], n)) to[rank[j]] = key[j];
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < OWN; ++j) key[j] = place[j] < n ? to[place[j]] : Key(0);
@@ -711,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 4) route_pairs_kernel(RouteArgs A) {
     P w[S / 2], top;
     {
       uint32_t v[S / 2];
-      load_words<S / 2, 2>(v, logits, e0, E, A.vec, (inf | 0x8000u) * 0x10001u);
+      load_words<S / 2, 2>(v, logits, e0, E, E, A.vec, (inf | 0x8000u) * 0x10001u);
 #pragma unroll
       for (int i = 0; i < S / 2; ++i) w[i].w = v[i];
     }
@@ -733,10 +739,11 @@ __global__ void __launch_bounds__(kThreads, 4) route_pairs_kernel(RouteArgs A) {
       for (int at = first; hit; ++at) {
         const int b = __ffs(hit) - 1, index = e0 + 2 * (b & 15) + (b >> 4);
         hit &= hit - 1u;
+        if (!BOUTE_INB(index, E)) continue;
         unsigned u = logits[index];
         if (u == 0x8000u) u = 0u;
         u ^= u & 0x8000u ? 0xffffu : 0x8000u;
-        to[at] = u << 16 | (0xffffu - (unsigned)index);
+        if (BOUTE_INB(at, kSlots)) to[at] = u << 16 | (0xffffu - (unsigned)index);
       }
       in_order<kOwn>(to, n, l, key, place);
     } else {  // all as keys; a NaN is largest, +inf next, -inf smallest
@@ -826,7 +833,8 @@ __global__ void __launch_bounds__(kThreads, S > 16 ? 4 : 5) route_bound_kernel(R
       for (int at = first; hit; ++at) {
         const int i = e0 + __ffs(hit) - 1;
         hit &= hit - 1u;
-        to[at] = make_key(q.value(A, logit_at(A, row, i), i), (unsigned)i);
+        if (BOUTE_INB(i, E) && BOUTE_INB(at, kSlots))
+          to[at] = make_key(q.value(A, logit_at(A, row, i), i), (unsigned)i);
       }
       in_order<kOwn>(to, n, l, key, place);
     } else {  // many equal ones: the largest, k times
@@ -956,7 +964,7 @@ struct Raw {
   __device__ __forceinline__ void load(const T *x, int E, bool vec) {
     const int e0 = (threadIdx.x & 31) * S;
     if (vec) {
-      if (e0 < E) {
+      if (e0 < E && BOUTE_INB(e0 + S - 1, E)) {
         if constexpr (kWords >= 4) {
 #pragma unroll
           for (int i = 0; i < kWords / 4; ++i) ((uint4 *)w)[i] = ((const uint4 *)(x + e0))[i];
@@ -1000,7 +1008,8 @@ __device__ __forceinline__ void clear_run(T *p, int n, int lane) {
   const int head = min(n, (int)((16 - (uintptr_t)p % 16) % 16 / sizeof(T)));
   const int whole = (n - head) / kOf, tail = head + whole * kOf;
   uint4 *v = (uint4 *)(p + head);
-  for (int i = lane; i < whole; i += 32) v[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = lane; i < whole; i += 32)
+    if (BOUTE_INB(head + (i + 1) * kOf - 1, n)) v[i] = make_uint4(0u, 0u, 0u, 0u);
   if (lane < head) p[lane] = from_float<T>(0.f);
   if (tail + lane < n) p[tail + lane] = from_float<T>(0.f);
 }
@@ -1015,6 +1024,7 @@ __device__ __forceinline__ void for_run(const T *p, int n, int lane, Go go) {
   const uint4 *v = (const uint4 *)(p + head);
 #pragma unroll 4
   for (int i = lane; i < whole; i += 32) {
+    if (!BOUTE_INB(head + (i + 1) * kOf - 1, n)) continue;
     const uint4 w = v[i];
     T t[kOf];
     memcpy(t, &w, 16);
@@ -1104,7 +1114,7 @@ __global__ void __launch_bounds__(kThreads, SOFT ? 6 : 0)
     // 31; of 61 bf16 without one: 13.2 element by element, 6.7 looking for the run's ends)
     if (A.vec && A.ldd == A.E) {  // the rows are one run of 16-byte vectors
       uint4 *p = (uint4 *)(dlogits + row0 * A.E);
-      const int vectors = n * A.E / (16 / (int)sizeof(T));
+      const int vectors = BOUTE_INB((uintptr_t)p % 16, 1) ? n * A.E / (16 / (int)sizeof(T)) : 0;
       for (int i = lane; i < vectors; i += 32) p[i] = make_uint4(0u, 0u, 0u, 0u);
     } else if (A.ldd == A.E) {
       clear_run(dlogits + row0 * A.E, n * A.E, lane);
@@ -1114,7 +1124,8 @@ __global__ void __launch_bounds__(kThreads, SOFT ? 6 : 0)
           dlogits[(row0 + i) * A.ldd + j] = from_float<T>(0.f);
     }
     __syncwarp();
-    if (e >= 0) dlogits[row * A.ldd + e] = from_float<T>(d);
+    if (e >= 0 && BOUTE_INB(e, A.E) && BOUTE_INB(row, A.rows))
+      dlogits[row * A.ldd + e] = from_float<T>(d);
   }
 }
 
@@ -1162,7 +1173,7 @@ __global__ void __launch_bounds__(kThreads)
     uint32_t w[kWords];
     memcpy(w, out, sizeof(w));
     if (A.vec) {
-      if (lane * S < E) {
+      if (lane * S < E && BOUTE_INB(lane * S + S - 1, E)) {
         if constexpr (kWords >= 4) {
 #pragma unroll
           for (int i = 0; i < kWords / 4; ++i) ((uint4 *)dx)[i] = ((uint4 *)w)[i];
@@ -1178,7 +1189,7 @@ __global__ void __launch_bounds__(kThreads)
         if (lane * S + s < E) dx[s] = out[s];
     }
     __syncwarp();
-    if (e >= 0) dlogits[row * A.ldd + e] = from_float<T>(v * (ds - dot));
+    if (e >= 0 && BOUTE_INB(e, E)) dlogits[row * A.ldd + e] = from_float<T>(v * (ds - dot));
   }
 }
 

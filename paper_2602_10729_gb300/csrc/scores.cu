@@ -68,7 +68,9 @@ struct Answers {
       const int at0 = (int)(t0 - from);
       float l[kUnroll], h[kUnroll];
       bool in[kUnroll];
+      if (!BOUTE_INB(t0, T)) break;
       if (t0 + (kUnroll - 1) * BY < b) {
+        if (!BOUTE_INB(t0 + (kUnroll - 1) * BY, T)) break;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           l[u] = pl[u * BY];
@@ -78,7 +80,7 @@ struct Answers {
       } else {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-          in[u] = t0 + u * BY < b;
+          in[u] = t0 + u * BY < b && BOUTE_INB(t0 + u * BY, T);
           if (!in[u]) continue;
           l[u] = pl[u * BY];
           h[u] = ph[u * BY];
@@ -146,7 +148,7 @@ __device__ __forceinline__ Part cluster_join(Part p, int rank, int cluster, Part
                                              Part *parts) {
   p = block_join(p, red);
   cluster_runs();
-  if (threadIdx.x < cluster) {
+  if (threadIdx.x < cluster && BOUTE_INB(rank, kMaxCluster)) {
     const uint32_t to = peer(&parts[rank], threadIdx.x);
     store_peer(to, p.lo);
     store_peer(to + 8, p.hi);
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 5)
     answer_scores_kernel(Answers A, float *scores, int *counts) {
   for_answers<TEAM>(A, [&](long long q, long long from, const Part &p, long long a, long long b,
                            unsigned long long on, int i, auto by) {
-    if (i != 0 || a != from) return;
+    if (i != 0 || a != from || !BOUTE_INB(q, A.Q)) return;
     const float n = (float)p.n;
     counts[q] = p.n;
     scores[4 * q] = p.n ? p.lp / n : 0.f;
@@ -233,6 +235,7 @@ __global__ void __launch_bounds__(kThreads, 5)
                            unsigned long long on, int i, auto by) {
     constexpr int BY = decltype(by)::value;
     const float n = p.n ? (float)p.n : 1.f;
+    if (!BOUTE_INB(q, A.Q)) return;
     const float *g = g_scores + 4 * q;
     const float g0 = g[0] / n, g1 = g[1], g2 = g[2] / n, g3 = g[3];
     const int lo = key_position(p.lo), hi = key_position(p.hi);  // from `from` on
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 5)
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        if (u * BY >= left) break;
+        if (u * BY >= left || !BOUTE_INB(t0 + u * BY, A.T)) break;
         const bool in = bits >> u & 1u;
         pl[u * BY] = in ? g0 + (at0 + u * BY == lo ? g1 : 0.f) : 0.f;
         ph[u * BY] = in ? g2 + (at0 + u * BY == hi ? g3 : 0.f) : 0.f;

@@ -1,5 +1,10 @@
 """The operators over a model's answers where their inputs or launches are at a limit, against plain
 64-bit forms."""
+import os
+import subprocess
+import sys
+import textwrap
+
 import numpy as np
 import pytest
 import torch
@@ -260,3 +265,53 @@ def test_weights_and_gradient_agree_where_a_softmax_underflows():
     dx = torch.full_like(x, 9.0)
     bt.boute_route_grad(x, SOFT, True, 1.0, idx, torch.tensor([[1.0, -2.0]]).cuda(), dx)
     assert (dx == 0).all()
+
+
+# ---------------------------------------------------------------- the bounds-checked build
+CHILD = textwrap.dedent(r"""
+    import sys
+    sys.path.insert(0, ROOT); sys.path.insert(0, HERE)
+    from paper_2602_10729_gb300 import boute as bt, build as bld
+    bt.load(bld.build(debug=True))
+    import test_gpu_answers as ta, test_gpu_answers_limits as tl, test_gpu_routing as tr
+
+    ok = True
+    def run(test, *a):
+        global ok
+        test(*a)
+        r = bt.boute_bounds_report()
+        if r is not None:
+            ok = False
+            print(test.__name__, a, f"VIOLATION unit={r[0]} line={r[1]} index={r[2]} extent={r[3]}")
+
+    for T, V, scale, pitch, shift, ent in [(1, 1, 1.0, 0, 0, True), (4, 255, 1.25, 1, 5, True),
+                                           (6, 1001, 1 / 0.7, 0, 3, True),
+                                           (2, 50021, 1.0, 0, 0, True), (200, 300, 1.0, 0, 0, True)]:
+        for dt in ("f32", "bf16"):
+            run(ta.test_gradient_against_the_formula, dt, T, V, scale, pitch, shift, ent)
+    run(tl.test_gradient_of_logits_far_from_zero, "bf16", 0.7, 4, 70001, True)
+    run(ta.test_forward_many_short_rows, "f16", 7001, 8)
+    run(tl.test_clusters_of_empty_answers)
+    for E, k in ((48, 6), (256, 4), (256, 8), (200, 7)):
+        for dt in ("f32", "bf16"):
+            run(tr.test_many_queries_broken_rows, tr.SOFT, dt, E, k)
+    for shape in tr.SHAPES + [(61, 190, 10, 4, 2, 6), (61, 192, 8, 4, 2, 6), (61, 254, 2, 1, 1, 5)]:
+        run(tr.test_many_queries, tr.SIG, "f16", *shape)
+    for T, E, k, pitch in [(1, 1, 1, 0), (4, 7, 3, 1), (37, 64, 2, 0), (5, 100, 10, 3), (3, 1024, 32, 0),
+                           (9, 333, 6, 0), (1500, 48, 4, 8)]:
+        for mode in (tr.SOFT, tr.SIG):
+            for renorm in (True, False):
+                run(tr.test_gradient_against_the_formula, mode, renorm, "bf16", T, E, k, pitch)
+    for E, T, load in [(12, 9000, True), (250, 9000, True), (300, None, True)]:
+        run(tl.test_choice_among_scores_that_fp32_hardly_holds, tr.SIG, False, E, T, load)
+        run(tl.test_choice_among_scores_that_fp32_hardly_holds, tr.SOFT, True, E, T, load)
+    print("BOUNDS_OK" if ok else "BOUNDS_BAD")
+""")
+
+
+def test_no_index_outside_its_extent():
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = f"ROOT = {os.path.dirname(here)!r}; HERE = {here!r}\n" + CHILD
+    p = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=900)
+    assert p.returncode == 0, p.stdout + p.stderr
+    assert "BOUNDS_OK" in p.stdout, p.stdout
