@@ -44,6 +44,14 @@ __device__ __forceinline__ void add(Part &p, const Part &o) {
   p.hi = max(p.hi, o.hi);
 }
 
+// A block's threads may have any number of positions each: a chain of n equal terms can be off by n /
+// 2 roundings (a million of them, by 1 %), so what an addition loses goes to the next (Kahan's sum).
+__device__ __forceinline__ void add_exact(float &sum, float v, float &lost) {
+  const float y = v - lost, t = sum + y;
+  lost = (t - sum) - y;
+  sum = t;
+}
+
 struct Answers {
   const float *logprob, *entropy;
   const long long *targets, *offsets;
@@ -62,6 +70,7 @@ struct Answers {
     on = 0ull;
     float lo = INFINITY, hi = -INFINITY;
     int lo_at = -1, hi_at = -1, first = 0;  // of this round, in the thread's order
+    float lost_lp = 0.f, lost_ent = 0.f;
     for (long long t0 = a + i; t0 < b; t0 += kUnroll * BY, first += kUnroll) {
       const float *pl = logprob + t0, *ph = entropy + t0;
       const long long *pt = targets + t0;
@@ -88,14 +97,22 @@ struct Answers {
         }
       }
       unsigned bits = 0u;
+      float lp = 0.f, ent = 0.f;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         if (!in[u]) continue;
         bits |= 1u << u;
-        p.lp += l[u];
-        p.ent += h[u];
+        lp += l[u];
+        ent += h[u];
         if (l[u] < lo) lo = l[u], lo_at = at0 + u * BY;
         if (h[u] > hi) hi = h[u], hi_at = at0 + u * BY;
+      }
+      if (BY == kThreads) {
+        add_exact(p.lp, lp, lost_lp);
+        add_exact(p.ent, ent, lost_ent);
+      } else {
+        p.lp += lp;
+        p.ent += ent;
       }
       p.n += __popc(bits);
       if (first < 64) on |= (unsigned long long)bits << first;
@@ -106,8 +123,11 @@ struct Answers {
       p.hi = ((unsigned long long)extreme_bits(hi) << 32) | (0xffffffffu - (unsigned)hi_at);
       return p;
     }
+    p.lp = p.ent = 0.f;  // (what is lost of an infinity is a NaN)
     for (long long t = a + i; t < b; t += BY) {
       if (!counts(t)) continue;
+      p.lp += logprob[t];
+      p.ent += entropy[t];
       const unsigned at = 0xffffffffu - (unsigned)(t - from);
       p.lo = max(p.lo, ((unsigned long long)extreme_bits(-logprob[t]) << 32) | at);
       p.hi = max(p.hi, ((unsigned long long)extreme_bits(entropy[t]) << 32) | at);

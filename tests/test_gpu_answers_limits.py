@@ -315,3 +315,21 @@ def test_no_index_outside_its_extent():
     p = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=900)
     assert p.returncode == 0, p.stdout + p.stderr
     assert "BOUNDS_OK" in p.stdout, p.stdout
+
+
+# ---------------------------------------------------------------- very long answers
+@pytest.mark.parametrize("lengths", [[100_000_000], [3] * 200_000 + [30_000_000] + [0, 2] * 500])
+def test_means_of_very_long_answers(lengths):
+    """Equal values, whose roundings all go the same way. Four positions join with 3 U, a thread's
+    fours with 2 U (what an addition loses goes to the next), threads, warps and blocks in 21
+    additions, then the count and the quotient: a mean is within 40 U of the value."""
+    off = torch.tensor([0] + lengths).cumsum(0)
+    T, Q = int(off[-1]), len(lengths)
+    lp, ent = torch.full((T,), -0.1, device="cuda"), torch.full((T,), 0.3, device="cuda")
+    s, n = torch.full((Q, 4), 9.0, device="cuda"), torch.zeros(Q, dtype=torch.int32, device="cuda")
+    bt.boute_answer_scores(lp, ent, None, off.cuda(), s, n)
+    assert n.tolist() == lengths
+    some = s.cpu().double().numpy()[np.array(lengths) > 0]
+    v = np.array([float(np.float32(-0.1)), float(np.float32(0.3))])
+    assert (np.abs(some[:, [0, 2]] - v) <= 40 * U * np.abs(v)).all()
+    assert (some[:, [1, 3]] == v).all()
