@@ -204,12 +204,14 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   return {m, a.s + b.s, a.u + b.u};
 }
 
-// Adds a piece to pairs of partial sums; CLAMP: with logits so far below m that (x - m) c
+// A piece's pairs of partial sums (which join the running ones once: a lane's terms, some hundreds of
+// a long row, added one after another would round at the running sum's size each time); CLAMP: with logits so far below m that (x - m) c
 // overflows (-inf, masks of the type's lowest value), whose y 2^y is else a NaN.
 template <bool CLAMP, class T>
-__device__ __forceinline__ void add_piece(const Piece<T> &p, float m, float c,
+__device__ __forceinline__ void sum_piece(const Piece<T> &p, float m, float c,
                                           unsigned long long &s2, unsigned long long &u2) {
   const unsigned long long m2 = f2_dup(m), c2 = f2_dup(c);
+  s2 = u2 = 0ull;
 #pragma unroll
   for (int j = 0; j < Piece<T>::N / 2; ++j) {
     float a, b;
@@ -330,19 +332,19 @@ __global__ void __launch_bounds__(kThreads, 4)
       u2 = f2_pack(a.u, b.u);
       m = max_nan(m, g);
     }
+    unsigned long long s = 0ull, u = 0ull;
     if (whole && !clamp) {
-      unsigned long long s = s2, u = u2;
-      add_piece<false>(p, m, c, s, u);
+      sum_piece<false>(p, m, c, s, u);
       float a, b;
       f2_split(u, a, b);
       clamp = __any_sync(kAll, isnan(a + b));
-      if (!clamp) {
-        s2 = s;
-        u2 = u;
-        continue;
-      }
     }
-    if (m > -INFINITY) add_piece<true>(p, m, c, s2, u2);
+    if (!whole || clamp) {
+      if (!(m > -INFINITY)) continue;
+      sum_piece<true>(p, m, c, s, u);
+    }
+    s2 = f2_add(s2, s);
+    u2 = f2_add(u2, u);
   }
   {
     float a, b;
@@ -553,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 4)
       const float top = fmaxf(a.m, lane_max(p));
       a.move(top, c);
       unsigned long long s2 = 0ull, u2 = 0ull;
-      if (top > -INFINITY) add_piece<true>(p, top, c, s2, u2);
+      if (top > -INFINITY) sum_piece<true>(p, top, c, s2, u2);
       float s, t2;
       f2_split(s2, s, t2);
       a.s += s + t2;

@@ -333,3 +333,22 @@ def test_means_of_very_long_answers(lengths):
     v = np.array([float(np.float32(-0.1)), float(np.float32(0.3))])
     assert (np.abs(some[:, [0, 2]] - v) <= 40 * U * np.abs(v)).all()
     assert (some[:, [1, 3]] == v).all()
+
+
+# ---------------------------------------------------------------- long rows
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_of_long_rows_of_equal_terms(dtype):
+    """Rows of one block, of one logit but for a few tokens of logit 0 that every warp meets: the
+    roundings of equal terms all go the same way. A lane's 16 or 32 of a piece of the row join in two chains (8 U), up to
+    64 pieces in another (32 U), chains, lanes and warps in 9 additions; the exponential's argument and
+    the exponential have 6 U. ln s has an error of those 55 U and 2 U of its own size, 12: 80 U."""
+    T, V = 700, 131072
+    c = -(torch.arange(T) % 55 + 3).float() / 64
+    x = torch.empty((T, V), dtype=DT[dtype], device="cuda")
+    x[:] = c.cuda()[:, None]
+    x[:, 5:4096:512] = 0.0
+    t = torch.full((T,), 517, device="cuda")
+    lp, H, lse, _, _ = forward(x, t, 1.0, 0)
+    want = np.log(8.0 + (V - 8) * np.exp(c.double().numpy()))
+    assert (np.abs(lse.cpu().double().numpy() - want) <= 80 * U).all()
+    assert (np.abs(lp.cpu().double().numpy() + want) <= 80 * U).all()
