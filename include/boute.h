@@ -590,7 +590,8 @@ int boute_mobo_run(const boute_mobo_config *cfg, int d, int m, const float *cand
  * Sums, maxima and softmax statistics are held in fp32.
  *
  * Per position of an answer, with z = scale * logits rounded once to fp32 (scale =
- * 1 / temperature, finite and > 0), over the V tokens of a vocabulary:
+ * 1 / temperature, finite and > 0; the sums take scale * (logit - largest logit) in place of
+ * z - max z, so that logits far from 0 lose nothing in them), over the V tokens of a vocabulary:
  *   lse = ln sum_j exp(z_j),  logprob = z_target - lse,
  *   entropy = -sum_j p_j ln p_j with p_j = exp(z_j - lse) and 0 ln 0 = 0,
  *   the k tokens of the largest z in the order (value descending, -0 as +0,
@@ -615,7 +616,8 @@ int boute_token_logprobs(const void *logits, int dtype, long long T, int V, long
  * entropy and the outputs' gradients g_logprob and g_entropy (T fp32 each;
  * g_entropy, and entropy with it, may be NULL):
  *   dlogits_j = scale (g_logprob ([j = target] - p_j) - g_entropy p_j (ln p_j + entropy)),
- * rounded once to the logits' type. A position without a token takes g_logprob
+ * rounded once to the logits' type (ln p_j = scale * logit_j - lse; where |lse| is over 1024,
+ * and its rounding would show, from the row's own sum). A position without a token takes g_logprob
  * as 0; a row without a token left (lse = -inf) has gradient 0; a target >= V
  * and a row without a distribution (lse NaN) have gradient NaN. dlogits: T rows
  * of V with pitch ldd; it may be logits itself (with ldd = ld). */

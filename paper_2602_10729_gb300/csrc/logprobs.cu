@@ -12,10 +12,11 @@
 // cache, through which the loads in flight pass: with 16 KB a block for the parts
 // themselves, reads were 10 % slower.
 //
-// Memory bounds the large calls: 8192 rows of 131072 bf16 logits, k = 20: 335 us
-// (6.4 TB/s, 0.95 of the copy rate; k = 0: 305 us, 1.04); their gradient, which writes
-// as much as it reads, 640 us (0.99). Rows that do not fill whole waves of blocks pay for
-// the last one: 2039 rows of 50021 fp16, k = 8: 43 us (0.70). What follows a row's loads
+// Memory bounds the large calls: 8192 rows of 131072 bf16 logits, k = 20: 339 us
+// (6.3 TB/s, 0.93 of the copy rate; k = 0: 306 us, 1.04; 4096 rows of fp32: 327); their
+// gradient, which writes as much as it reads, 640 us (0.99; fp32 655). Rows that do not
+// fill whole waves of blocks pay for the last one: 2039 rows of 50021 fp16, k = 8: 43 us
+// (0.70). What follows a row's loads
 // (joining, the bound, the second look, the ranks) is 4 us of latency, which bounds the
 // small calls: one row of 50021, k = 5: 5.2 us; 64 of 131072 fp32, k = 20: 10.8.
 #include <float.h>

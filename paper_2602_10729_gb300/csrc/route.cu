@@ -1,8 +1,8 @@
 // Routing of queries to experts: scores, the choice within the best groups,
 // the weights and the load; and the gradient of the weights.
 //
-// Arithmetic bounds it: a query's logits are one or two lines, its choice some hundred
-// instructions. So as little as possible is compared:
+// Instructions bound it, and the wait for each round's logits: a query's are one or two lines,
+// its choice some hundred instructions. So as little as possible is compared:
 //  - Teams of 8 lanes to a query, four queries to a warp, take up to 8 of up to 256 experts.
 //    Each lane's values are parts, 4 K in all, whose maxima's K-th largest is a bound that K
 //    values reach, and few others; those alone become keys (order bits over the expert's
@@ -14,9 +14,10 @@
 //    each lane sorts its own, and k rounds take the largest of the 32 heads.
 // Without a bias the logits themselves are compared, which have the order of the scores:
 // only the chosen scores are computed then, and a softmax's sum only where the weights are
-// not renormalised. 262144 queries of 256 bf16 logits, k = 4: 35 us (4.1 TB/s; a floor of
-// 21); 131072 of 256, logistic with bias, k = 4: 37, in 8 groups with k = 8: 63.
-// The gradient moves bytes: 131072 queries of 160 fp32, k = 6: 26.3 us where they take 25.7.
+// not renormalised. 262144 queries of 256 bf16 logits, k = 4: 35.5 us (4.0 TB/s; a floor of
+// 21), k = 1: 35.3; 131072 of 256, logistic with bias, k = 4: 37.6, in 8 groups with k = 8: 61.
+// The gradient moves bytes: 131072 queries of 160 fp32, k = 6: 26.4 us where they take 25.7; a
+// softmax's 29.8 renormalised and 45.8 without.
 #include <float.h>
 #include <math.h>
 
@@ -350,7 +351,7 @@ __device__ __forceinline__ unsigned keep_groups(const float *c, float *scores, c
     float a = -INFINITY, b = -INFINITY;
     if (g < A.G)
 #pragma unroll 4
-      for (int i = l % width; i < per; i += width) 
+      for (int i = l % width; i < per; i += width)
         if (BOUTE_INB(g * per + i, A.E)) join_two(a, b, c[g * per + i], -INFINITY);
     for (int o = 1; o < width; o *= 2)
       join_two(a, b, __shfl_xor_sync(kAll, a, o), __shfl_xor_sync(kAll, b, o));
@@ -1275,8 +1276,9 @@ extern "C" int boute_route(const void *logits, int dtype, long long T, int E, lo
     return launch_cluster(kernel, grid, kThreads, 1, smem, s, A);
   };
   // Teams for pairs, and for other values where the queries give most SMs a block or two; and where
-  // one block of them takes all queries, which then needs no launch to clear the load (32 queries
-  // of 64 fp32: 2.2 and one launch, 2.5 and two). (us by
+  // one block of them takes all queries, which then needs no launch to clear the load (of 64 fp32,
+  // 32 queries: 2.5 us on the device with one launch or two, 64: 3.8 and 2.5, but a launch takes the
+  // host 2). (us by
   // team and by warp: 131072 x 256 bf16 with bias, k = 4: 37, 60, in 8 groups, k = 8: 63, 107; 131072
   // x 64, 8 groups, k = 4: 29, 66; 256 experts, 8 groups, k = 8, of 300, 2000, 4099 and 10000
   // queries: 7.2, 4.1; 7.3, 5.7; 7.4, 8.4; 10.6, 13.9; 64 experts, k = 4, of 300, 2000 and 4099: 3.8,

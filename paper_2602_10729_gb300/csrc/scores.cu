@@ -5,9 +5,10 @@
 // Lengths are ragged: what is too long for a team is taken by its block afterwards, and
 // where answers are long in the mean, by up to eight blocks of a cluster. Latency bounds
 // it: the offsets, then the positions, are one trip to memory each, and the longest
-// answer's rounds another each. 4096 answers of 200 positions in the mean: 7.6 us (13 MB,
-// a floor of 2), their gradient 9.4; 96 of 16384: 9 to 11 and 12 to 18, as the longest
-// has it (floors of 3.7 and 5.6). Blocks of 512 or 1024 threads: 12.5 and 23 to 30.
+// answer's rounds another each. 4096 answers of 200 positions in the mean: 7.4 us (13 MB,
+// a floor of 2), their gradient 9.4; 96 of 16384: 12 to 13 and 16 to 19, as the longest
+// has it (floors of 3.7 and 5.6). An answer of 2^20 takes 49 us alone and 601 among 4096
+// of 200, where it is one block's. Blocks of 512 or 1024 threads: 12.5 and 23 to 30.
 #include <math.h>
 
 #include <algorithm>
@@ -309,7 +310,7 @@ static int sizes_ok(long long T, long long Q, const float *logprob, const float 
 
 // Teams by the mean length: 8 lanes up to 24 positions, 32 up to 512, else a block; and up to the
 // eight blocks of a cluster for answers over 1024 positions a block that are too few to fill the
-// SMs. (13665 answers of 31: 6.4 us with 32 lanes, 8.3 with 8; 2245 of 682: 10.5 with a block, 15.4
+// SMs. (13665 answers of 31: 6.3 us with 32 lanes, 8.0 with 8; 2245 of 682: 11.7 with a block, 14.1
 // with 32 lanes.)
 template <class Go>
 static int with_team(long long T, long long Q, Go go) {
