@@ -352,7 +352,7 @@ int boute_selftest_wait(int complete, unsigned long long limit_ns, void *stream)
  * operand images, the outputs, the strips and boxes, the selection). This
  * call waits for the device, returns 1 and fills rec (4 words: the source
  * unit 1 posterior, 2 in-sample, 3 acquisition, 4 front, 5 fit, 6 top-k,
- * 7 log-probabilities, 8 answer scores, 9 routing; the source line; the index; the extent) when some unit recorded one since
+ * 7 log-probabilities, 8 answer scores, 9 routing, 10 experts' rows; the source line; the index; the extent) when some unit recorded one since
  * the last call, else 0; it clears the records. The product library returns
  * BOUTE_ERR_UNSUPPORTED (its checks compile to nothing). */
 int boute_bounds_report(long long *rec);
@@ -687,6 +687,47 @@ int boute_route(const void *logits, int dtype, long long T, int E, long long ld,
 int boute_route_grad(const void *logits, int dtype, long long T, int E, long long ld, int mode,
                      int k, int renorm, float factor, const int *idx, const float *g_weight,
                      void *dlogits, long long ldd, void *stream);
+
+/* The choices of a routing in the order of their experts, and the queries' rows (of features,
+ * or of a model's hidden states) there and back. Choice c = t k + i is query t's i-th; idx
+ * (T x k int32, as boute_route writes it) names its expert, and what is not in [0, E) is no
+ * choice. The n choices that there are take places 0 .. n - 1 by ascending expert, those of an
+ * expert by ascending c (also where a query names it twice):
+ *   offsets (E + 1 int32): expert e's places are offsets[e] .. offsets[e + 1] - 1, n = offsets[E];
+ *   source (T k int32): the choice at a place, -1 for places >= n;
+ *   place (T x k int32): the place of a choice, -1 for none.
+ * The order is the same on every run. E <= BOUTE_MAX_EXPERTS, k <= BOUTE_MAX_CHOICES, 0 <= T k <
+ * 2^31. */
+int boute_expert_sort(const int *idx, long long T, int k, int E, int *offsets, int *source,
+                      int *place, void *stream);
+/* The rows of the choices, x_t at each of query t's places, and the gradient of x:
+ *   rows[place[t, i]] = x[t],   dx[t] = sum_i g_rows[place[t, i]].
+ * In this call and the next two, place holds T x k places within R rows of D elements; one that is
+ * not in [0, R) is none: its row is neither read nor written, and adds nothing (with R below the
+ * number of choices, those of the last places are left out). Rows without a choice are left as they
+ * were. x, dx: T rows of pitch ldx; rows, g_rows: R rows of pitch ldr (in elements; of one type,
+ * fp32, fp16 or bf16; any element-aligned address will do). Sums are taken in fp32 in the order of
+ * i and rounded once. D <= BOUTE_MAX_ROW. */
+#define BOUTE_MAX_ROW (1 << 20)
+int boute_expert_dispatch(const void *x, int dtype, long long T, int D, long long ldx,
+                          const int *place, int k, void *rows, long long R, long long ldr,
+                          void *stream);
+int boute_expert_dispatch_grad(const void *g_rows, int dtype, long long R, int D, long long ldr,
+                               const int *place, long long T, int k, void *dx, long long ldx,
+                               void *stream);
+/* The experts' rows back to the queries, with the routing's weights (T x k fp32; those of no
+ * choice are not read): out[t] = sum_i weight[t, i] rows[place[t, i]], 0 without a choice. */
+int boute_expert_combine(const void *rows, int dtype, long long R, int D, long long ldr,
+                         const int *place, const float *weight, long long T, int k, void *out,
+                         long long ldo, void *stream);
+/* Its gradients, for different places:
+ *   g_rows[place[t, i]] = weight[t, i] g_out[t],   g_weight[t, i] = <g_out[t], rows[place[t, i]]>
+ * (0 for no choice). g_rows: R rows of pitch ldg; it may be rows itself (with ldg = ldr).
+ * g_weight: T x k fp32, the input of boute_route_grad. */
+int boute_expert_combine_grad(const void *g_out, int dtype, long long T, int D, long long ldo,
+                              const void *rows, long long R, long long ldr, const int *place,
+                              const float *weight, int k, void *g_rows, long long ldg,
+                              float *g_weight, void *stream);
 
 #ifdef __cplusplus
 }

@@ -41,6 +41,8 @@ SYMBOLS = (
     "boute_engine_free",
     "boute_token_logprobs", "boute_token_logprobs_grad", "boute_answer_scores",
     "boute_answer_scores_grad", "boute_route", "boute_route_grad",
+    "boute_expert_sort", "boute_expert_dispatch", "boute_expert_dispatch_grad",
+    "boute_expert_combine", "boute_expert_combine_grad",
 )
 #: stage names of boute_engine_stage_times, in order
 STAGES = ("fit", "front", "posterior", "acquisition", "topk")
@@ -150,6 +152,12 @@ def load(path: str | None = None):
                          _vp], _i),
         "boute_route_grad": ([_vp, _i, _ll, _i, _ll, _i, _i, _i, _f, _vp, _vp, _vp, _ll, _vp],
                              _i),
+        "boute_expert_sort": ([_vp, _ll, _i, _i, _vp, _vp, _vp, _vp], _i),
+        "boute_expert_dispatch": ([_vp, _i, _ll, _i, _ll, _vp, _i, _vp, _ll, _ll, _vp], _i),
+        "boute_expert_dispatch_grad": ([_vp, _i, _ll, _i, _ll, _vp, _ll, _i, _vp, _ll, _vp], _i),
+        "boute_expert_combine": ([_vp, _i, _ll, _i, _ll, _vp, _vp, _ll, _i, _vp, _ll, _vp], _i),
+        "boute_expert_combine_grad": ([_vp, _i, _ll, _i, _ll, _vp, _ll, _ll, _vp, _vp, _i, _vp,
+                                       _ll, _vp, _vp], _i),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -769,3 +777,65 @@ def boute_route_grad(logits, mode, renorm, factor, idx, g_weight, dlogits, strea
                                    _pn(g_weight, torch.float32, (T, k), dev), dx, ldd,
                                    _s_on(stream, dev)),
            "boute_route_grad")
+
+
+def boute_expert_sort(idx, offsets, source, place, stream=None):
+    """idx: T x k int32, the chosen experts (none where not in [0, E)); offsets: E + 1 int32;
+    source: T k int32; place: T x k int32."""
+    i32, dev = torch.int32, idx.get_device()
+    T, k = idx.shape
+    E = offsets.shape[0] - 1
+    _check(load().boute_expert_sort(_pn(idx, i32, (T, k), dev), T, k, E,
+                                    _pn(offsets, i32, (E + 1,), dev),
+                                    _pn(source, i32, (T * k,), dev), _pn(place, i32, (T, k), dev),
+                                    _s_on(stream, dev)), "boute_expert_sort")
+
+
+def _expert_rows(x, rows, place):
+    """(the queries' rows, the experts' rows, place's pointer, k), each of _rows, checked."""
+    a = _rows(x)
+    dev, T, D = a[1], a[3], a[4]
+    if rows.dtype != x.dtype:
+        raise TypeError(f"rows of {x.dtype} and {rows.dtype}")
+    b = _rows(rows, dev)
+    if b[4] != D:
+        raise ValueError(f"rows of {D} and {b[4]} elements")
+    k = place.shape[-1]
+    return a, b, _pn(place, torch.int32, (T, k), dev), k
+
+
+def boute_expert_dispatch(x, place, rows, stream=None):
+    """x: T x D (fp32, fp16 or bf16, rows contiguous); place: T x k int32, of
+    boute_expert_sort; rows: R x D of x's dtype, written where a choice has its place."""
+    (x, dev, code, T, D, ldx), (rows, _, _, R, _, ldr), place, k = _expert_rows(x, rows, place)
+    _check(load().boute_expert_dispatch(x, code, T, D, ldx, place, k, rows, R, ldr,
+                                        _s_on(stream, dev)), "boute_expert_dispatch")
+
+
+def boute_expert_dispatch_grad(g_rows, place, dx, stream=None):
+    """g_rows: R x D; dx: T x D of the same dtype, the sums of the choices' rows."""
+    (dx, dev, code, T, D, ldx), (g, _, _, R, _, ldr), place, k = _expert_rows(dx, g_rows, place)
+    _check(load().boute_expert_dispatch_grad(g, code, R, D, ldr, place, T, k, dx, ldx,
+                                             _s_on(stream, dev)), "boute_expert_dispatch_grad")
+
+
+def boute_expert_combine(rows, place, weight, out, stream=None):
+    """rows: R x D; place: T x k int32; weight: T x k fp32; out: T x D of the rows' dtype."""
+    (out, dev, code, T, D, ldo), (rows, _, _, R, _, ldr), place, k = _expert_rows(out, rows, place)
+    _check(load().boute_expert_combine(rows, code, R, D, ldr, place,
+                                       _pn(weight, torch.float32, (T, k), dev), T, k, out, ldo,
+                                       _s_on(stream, dev)), "boute_expert_combine")
+
+
+def boute_expert_combine_grad(g_out, rows, place, weight, g_rows, g_weight, stream=None):
+    """g_out: T x D; rows: R x D of its dtype; weight: T x k fp32; g_rows: as rows (it may be
+    rows), written where a choice has its place; g_weight: T x k fp32."""
+    f32 = torch.float32
+    gr = _rows(g_rows, None, rows)
+    (go, dev, code, T, D, ldo), (x, _, _, R, _, ldr), p, k = _expert_rows(g_out, rows, place)
+    if gr[1] != dev:
+        raise ValueError(f"tensors on devices {dev} and {gr[1]}")
+    _check(load().boute_expert_combine_grad(go, code, T, D, ldo, x, R, ldr, p,
+                                            _pn(weight, f32, (T, k), dev), k, gr[0], gr[5],
+                                            _pn(g_weight, f32, (T, k), dev), _s_on(stream, dev)),
+           "boute_expert_combine_grad")
