@@ -352,7 +352,7 @@ int boute_selftest_wait(int complete, unsigned long long limit_ns, void *stream)
  * operand images, the outputs, the strips and boxes, the selection). This
  * call waits for the device, returns 1 and fills rec (4 words: the source
  * unit 1 posterior, 2 in-sample, 3 acquisition, 4 front, 5 fit, 6 top-k,
- * 7 log-probabilities, 8 answer scores, 9 routing, 10 experts' rows; the source line; the index; the extent) when some unit recorded one since
+ * 7 log-probabilities, 8 answer scores, 9 routing, 10 experts' rows, 11 hidden states; the source line; the index; the extent) when some unit recorded one since
  * the last call, else 0; it clears the records. The product library returns
  * BOUTE_ERR_UNSUPPORTED (its checks compile to nothing). */
 int boute_bounds_report(long long *rec);
@@ -728,6 +728,43 @@ int boute_expert_combine_grad(const void *g_out, int dtype, long long T, int D, 
                               const void *rows, long long R, long long ldr, const int *place,
                               const float *weight, int k, void *g_rows, long long ldg,
                               float *g_weight, void *stream);
+
+/* boute_token_logprobs for a caller who has the last hidden states and the vocabulary's weight:
+ * logprob, entropy and lse for the logits hidden . weight^T (products of 16-bit numbers, summed in
+ * fp32), which are never in memory, with its scale, its targets and its rules for what is masked,
+ * NaN or infinite. The outputs are boute_answer_scores' inputs, its gradients this gradient's.
+ *   hidden: T rows of D (pitch ldh), weight: V rows of D (pitch ldw), both fp16 or both bf16 (fp32
+ *   is refused: BOUTE_ERR_UNSUPPORTED); any 2-byte-aligned address and any pitch >= D, but rows at
+ *   multiples of 16 bytes are read in place, others by way of an aligned copy in the workspace.
+ *   workspace: device memory, 256-byte aligned, of the bytes that boute_hidden_logprobs_workspace
+ *   gives for the same arguments (grad: for which of the calls); its contents need not be kept
+ *   between calls. Calls that may run at the same time need one each.
+ * A device-side wait that gives up (2 s; nothing hangs) makes all outputs of the call NaN, but for
+ * dweight, of which a part is then not written.
+ * 0 <= T <= BOUTE_MAX_HIDDEN, 1 <= D <= BOUTE_MAX_HIDDEN_SIZE, 1 <= V <= BOUTE_MAX_VOCAB. */
+#define BOUTE_MAX_HIDDEN (1 << 20)
+#define BOUTE_MAX_HIDDEN_SIZE (1 << 16)
+int boute_hidden_logprobs_workspace(const void *hidden, int dtype, long long T, int D,
+                                    long long ldh, const void *weight, int V, long long ldw,
+                                    int grad, long long *bytes);
+int boute_hidden_logprobs(const void *hidden, int dtype, long long T, int D, long long ldh,
+                          const void *weight, int V, long long ldw, const long long *targets,
+                          float scale, float *logprob, float *entropy, float *lse,
+                          void *workspace, long long bytes, void *stream);
+/* Its gradient with respect to both: with dlogits as boute_token_logprobs_grad has them, from the
+ * forward call's lse and entropy and the outputs' gradients (g_entropy, and entropy with it, may be
+ * NULL),
+ *   dhidden = dlogits weight (T rows of D, pitch lddh), dweight = dlogits^T hidden (V rows, lddw),
+ * rounded once to the type from fp32 sums. The products take each dlogits_tj rounded to the type
+ * (fp16: times a power of two, by which the largest coefficient that the gradients allow comes near
+ * 2^14; what is less than 2^-28 of it loses bits). At most 256 MB of them are held at a time
+ * (512 bytes a position, if that is more). dhidden and dweight overlap no input. */
+int boute_hidden_logprobs_grad(const void *hidden, int dtype, long long T, int D, long long ldh,
+                               const void *weight, int V, long long ldw, const long long *targets,
+                               float scale, const float *lse, const float *entropy,
+                               const float *g_logprob, const float *g_entropy, void *dhidden,
+                               long long lddh, void *dweight, long long lddw, void *workspace,
+                               long long bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -43,6 +43,7 @@ SYMBOLS = (
     "boute_answer_scores_grad", "boute_route", "boute_route_grad",
     "boute_expert_sort", "boute_expert_dispatch", "boute_expert_dispatch_grad",
     "boute_expert_combine", "boute_expert_combine_grad",
+    "boute_hidden_logprobs_workspace", "boute_hidden_logprobs", "boute_hidden_logprobs_grad",
 )
 #: stage names of boute_engine_stage_times, in order
 STAGES = ("fit", "front", "posterior", "acquisition", "topk")
@@ -158,6 +159,12 @@ def load(path: str | None = None):
         "boute_expert_combine": ([_vp, _i, _ll, _i, _ll, _vp, _vp, _ll, _i, _vp, _ll, _vp], _i),
         "boute_expert_combine_grad": ([_vp, _i, _ll, _i, _ll, _vp, _ll, _ll, _vp, _vp, _i, _vp,
                                        _ll, _vp, _vp], _i),
+        "boute_hidden_logprobs_workspace": ([_vp, _i, _ll, _i, _ll, _vp, _i, _ll, _i,
+                                             ctypes.POINTER(_ll)], _i),
+        "boute_hidden_logprobs": ([_vp, _i, _ll, _i, _ll, _vp, _i, _ll, _vp, _f, _vp, _vp, _vp,
+                                   _vp, _ll, _vp], _i),
+        "boute_hidden_logprobs_grad": ([_vp, _i, _ll, _i, _ll, _vp, _i, _ll, _vp, _f, _vp, _vp,
+                                        _vp, _vp, _vp, _ll, _vp, _ll, _vp, _ll, _vp], _i),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -839,3 +846,66 @@ def boute_expert_combine_grad(g_out, rows, place, weight, g_rows, g_weight, stre
                                             _pn(weight, f32, (T, k), dev), k, gr[0], gr[5],
                                             _pn(g_weight, f32, (T, k), dev), _s_on(stream, dev)),
            "boute_expert_combine_grad")
+
+
+def _hidden(hidden, weight):
+    """_rows of the hidden states (T x D) and of the weight (V x D), checked."""
+    h = _rows(hidden)
+    if weight.dtype != hidden.dtype:
+        raise TypeError(f"hidden states of {hidden.dtype}, weight of {weight.dtype}")
+    w = _rows(weight, h[1])
+    if w[4] != h[4]:
+        raise ValueError(f"hidden states of {h[4]} elements, weight of {w[4]}")
+    return h, w
+
+
+def _bytes_on(workspace, dev):
+    """(pointer, bytes) of a contiguous CUDA tensor on device dev."""
+    if not workspace.is_contiguous():
+        raise ValueError("tensors must be contiguous")
+    if workspace.get_device() != dev:
+        raise ValueError(f"tensors on devices {dev} and {workspace.get_device()}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def boute_hidden_logprobs_workspace(hidden, weight, grad=False) -> int:
+    """Bytes of workspace that boute_hidden_logprobs (grad: its gradient) needs for these."""
+    (h, dev, code, T, D, ldh), (w, _, _, V, _, ldw) = _hidden(hidden, weight)
+    n = _ll()
+    _check(load().boute_hidden_logprobs_workspace(h, code, T, D, ldh, w, V, ldw, bool(grad),
+                                                  ctypes.byref(n)),
+           "boute_hidden_logprobs_workspace")
+    return n.value
+
+
+def boute_hidden_logprobs(hidden, weight, targets, scale, logprob, entropy, lse, workspace,
+                          stream=None):
+    """hidden: T x D, weight: V x D (both fp16 or both bf16, rows contiguous); targets: T int64
+    (< 0: no token); logprob, entropy, lse: T fp32, as boute_token_logprobs has them for the
+    logits hidden @ weight.T; workspace: of boute_hidden_logprobs_workspace's bytes."""
+    f32 = torch.float32
+    (h, dev, code, T, D, ldh), (w, _, _, V, _, ldw) = _hidden(hidden, weight)
+    ws, n = _bytes_on(workspace, dev)
+    _check(load().boute_hidden_logprobs(h, code, T, D, ldh, w, V, ldw,
+                                        _pn(targets, torch.int64, (T,), dev), scale,
+                                        _pn(logprob, f32, (T,), dev), _pn(entropy, f32, (T,), dev),
+                                        _pn(lse, f32, (T,), dev), ws, n, _s_on(stream, dev)),
+           "boute_hidden_logprobs")
+
+
+def boute_hidden_logprobs_grad(hidden, weight, targets, scale, lse, entropy, g_logprob, g_entropy,
+                               dhidden, dweight, workspace, stream=None):
+    """entropy and g_entropy may be None; dhidden: T x D, dweight: V x D of the hidden states'
+    dtype; workspace: of boute_hidden_logprobs_workspace(hidden, weight, True) bytes."""
+    f32 = torch.float32
+    (h, dev, code, T, D, ldh), (w, _, _, V, _, ldw) = _hidden(hidden, weight)
+    dh, _, _, _, _, lddh = _rows(dhidden, dev, hidden)
+    dw, _, _, _, _, lddw = _rows(dweight, dev, weight)
+    ws, n = _bytes_on(workspace, dev)
+    _check(load().boute_hidden_logprobs_grad(h, code, T, D, ldh, w, V, ldw,
+                                             _pn(targets, torch.int64, (T,), dev), scale,
+                                             _pn(lse, f32, (T,), dev), _pn(entropy, f32, (T,), dev),
+                                             _pn(g_logprob, f32, (T,), dev),
+                                             _pn(g_entropy, f32, (T,), dev), dh, lddh, dw, lddw,
+                                             ws, n, _s_on(stream, dev)),
+           "boute_hidden_logprobs_grad")

@@ -1186,7 +1186,7 @@ int boute_bounds_report(long long *rec) {
   int (*readers[])(long long *) = {bounds_read_posterior, bounds_read_insample, bounds_read_acq,
                                    bounds_read_front,     bounds_read_fit,      bounds_read_topk,
                                    bounds_read_logprobs,  bounds_read_scores,   bounds_read_route,
-                                   bounds_read_experts};
+                                   bounds_read_experts,   bounds_read_hidden};
   int found = 0;
   rec[0] = rec[1] = rec[2] = rec[3] = 0;
   for (int u = 0; u < (int)(sizeof(readers) / sizeof(readers[0])); ++u) {

@@ -137,6 +137,7 @@ int bounds_read_logprobs(long long *out);
 int bounds_read_scores(long long *out);
 int bounds_read_route(long long *out);
 int bounds_read_experts(long long *out);
+int bounds_read_hidden(long long *out);
 // codes: outcome transforms before standardising (objective_code)
 int launch_standardize(const double *Y, int B, int n, int m, int codes, double *Ys,
                        cudaStream_t s);
