@@ -32,10 +32,13 @@ constexpr float kLowest = -200.f;  // 2^kLowest = 0 in fp32
 
 enum Mode { kStats = 0, kCoef = 1, kDHidden = 2, kDWeight = 3 };
 
-// Of a call's workspace, cleared before its first kernel.
+// At the start of a call's workspace.
+constexpr int kBlocks = 256;  // of a launch at most
 struct Header {
-  int status;        // BOUTE_ERR_TIMEOUT when a wait ran out
-  unsigned largest;  // bits of the largest bound of a coefficient
+  // BOUTE_ERR_TIMEOUT where a wait ran out: of each block of the statistics' launch, which writes
+  // its own; of all launches of the gradient, which clears it first
+  int status[kBlocks];
+  unsigned largest;  // bits of the largest bound of a coefficient (gradient)
 };
 // What the coefficients of a position need.
 struct Position {
@@ -53,8 +56,8 @@ __device__ __forceinline__ float coef_scale(unsigned largest, bool inverse) {
 
 struct Work {
   int M, N, K;             // rows, columns, reduction
-  int tile_n, nM, nN, splits;
-  int stages, stage_bytes;
+  int tile_m, tile_n, nM, nN, splits;  // (tile_m: rows of a block, 128 but for few positions)
+  int stages, stage_bytes, tx_bytes;  // (of a block; what its copies bring)
   Header *head;
   // statistics
   float c2;
@@ -80,10 +83,17 @@ struct Unit {
   int m, n, k0, k1;  // tiles; blocks of the reduction
 };
 __device__ __forceinline__ Unit unit_of(const Work &W, int u) {
-  const int per = W.nM * W.nN, s = u / per, r = u - s * per;
-  const int kb = (W.K + kBlockK - 1) / kBlockK;
-  return {r / W.nN, r % W.nN, (int)((long long)s * kb / W.splits),
-          (int)((long long)(s + 1) * kb / W.splits)};
+  const int kb = (W.K + kBlockK - 1) / kBlockK;  // (times a split: 2^14 x 64 at most)
+  int s = 0, r = u, k0 = 0, k1 = kb;
+  if (W.splits > 1) {
+    const int per = W.nM * W.nN;
+    s = u / per;
+    r = u - s * per;
+    k0 = s * kb / W.splits;
+    k1 = (s + 1) * kb / W.splits;
+  }
+  const int m = r / W.nN;
+  return {m, r - m * W.nN, k0, k1};
 }
 
 __device__ __forceinline__ uint32_t pack2(__half, float a, float b) { return pack_f16x2(a, b); }
@@ -184,12 +194,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t phase = 0;
       for (int u = pair; u < units && !*abort; u += pairs) {
         const Unit t = unit_of(W, u);
-        const int m0 = t.m * kPairM + rank * 128, n0 = t.n * W.tile_n + rank * half_n;
+        const int m0 = (t.m * 2 + rank) * W.tile_m, n0 = t.n * W.tile_n + rank * half_n;
         for (int kb = t.k0; kb < t.k1; ++kb) {
           if (!pair_wait(&empty[s], phase ^ 1u, abort)) break;
           uint8_t *a = ring + (size_t)s * W.stage_bytes, *b = a + kABytes;
           const uint32_t bar = peer(&full[s], 0);
-          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * (uint32_t)W.stage_bytes);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * (uint32_t)W.tx_bytes);
           const int k = kb * kBlockK;
           if constexpr (kAMn) {
             load_box(a, &map_a, m0, k, bar);
@@ -211,32 +221,45 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------------- products
-    if (lane == 0 && rank == 0) {
+    // (The warp stays together, so that descriptors are in uniform registers: with one lane alone in
+    // the loop, issuing took longer than the products.)
+    if (rank == 0) {
       constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
       const uint32_t idesc = pair_idesc(kBf16, kAMn, kBMn, W.tile_n);
+      const bool issuer = elect_one();
+      const uint64_t ad0 = operand_desc<kAMn>(smem_u32(ring));
+      const uint64_t bd0 = operand_desc<kBMn>(smem_u32(ring) + kABytes);
       int s = 0;
       uint32_t phase = 0, seq = 0;
-      for (int u = pair; u < units && !*abort; u += pairs, ++seq) {
+      bool ok = true;
+      for (int u = pair; u < units && ok; u += pairs, ++seq) {
         const Unit t = unit_of(W, u);
-        const uint32_t acc = seq & 1u;
-        if (!pair_wait(&acc_empty[acc], ((seq >> 1) & 1u) ^ 1u, abort)) break;
+        const uint32_t acc = seq & 1u, to = tmem + acc * kMaxTileN;
+        ok = __all_sync(kAll, pair_wait<true>(&acc_empty[acc], ((seq >> 1) & 1u) ^ 1u, abort));
+        if (!ok) break;
         tc_fence_after();
         for (int kb = t.k0; kb < t.k1; ++kb) {
-          if (!pair_wait(&full[s], phase, abort)) break;
+          ok = __all_sync(kAll, pair_wait(&full[s], phase, abort));
+          if (!ok) break;
           tc_fence_after();
-          const uint32_t a = smem_u32(ring + (size_t)s * W.stage_bytes);
-          const uint64_t ad = operand_desc<kAMn>(a), bd = operand_desc<kBMn>(a + kABytes);
-          const int steps = min(kBlockK, W.K - kb * kBlockK + 15) / 16;
-          for (int k = 0; k < steps; ++k)
-            pair_mma(tmem + acc * kMaxTileN, ad + k * kDescStep<kAMn>, bd + k * kDescStep<kBMn>,
-                     idesc, kb > t.k0 || k > 0);
-          pair_commit(&empty[s]);
+          if (issuer) {
+            const uint64_t at = (uint64_t)((uint32_t)(s * W.stage_bytes) >> 4);
+            const uint64_t ad = ad0 + at, bd = bd0 + at;
+            const int left = W.K - kb * kBlockK;  // (of a short last block, the steps with data)
+#pragma unroll
+            for (int k = 0; k < kBlockK / 16; ++k)
+              if (k * 16 < left)
+                pair_mma(to, ad + k * kDescStep<kAMn>, bd + k * kDescStep<kBMn>, idesc,
+                         kb > t.k0 || k > 0);
+            pair_commit(&empty[s]);
+          }
+          __syncwarp();
           if (++s == W.stages) s = 0, phase ^= 1u;
         }
-        if (*abort) break;
-        pair_commit(&acc_full[acc]);
+        if (ok && issuer) pair_commit(&acc_full[acc]);
+        __syncwarp();
       }
-      if (*abort) {  // no product in flight when the tensor memory goes
+      if (!ok && issuer) {  // no product in flight when the tensor memory goes
         pair_commit(&drain);
         mbar_wait(&drain, 0);
       }
@@ -258,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int u = pair; u < units; u += pairs, ++seq) {
       if ((seq & 1u) != (uint32_t)group) continue;
       const Unit t = unit_of(W, u);
-      const int row = t.m * kPairM + rank * 128 + quarter * 32, col = t.n * W.tile_n;
+      const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32, col = t.n * W.tile_n;
       // what does not wait for the products
       Position *pos = (Position *)epi + group * kMaxTileN;
       int *tgt = (int *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
@@ -294,7 +317,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int at = col + c * 32 + lane;
           long long target = -1;
           if (at < W.N && BOUTE_INB(at, W.N)) target = W.targets[at];
-          if (row + lane >= W.M)
+          // (rows of the accumulator beyond the block's hold what was in its shared memory)
+          const int rows = min(W.tile_m - quarter * 32, W.M - row);
+          if (lane >= rows)
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = -INFINITY;
 #pragma unroll
@@ -303,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
 #pragma unroll
           for (int i = 0; i < 32; ++i) x[i] = buf[i * kPitch + lane];
-          if (target >= row && target < row + 32 && target < W.M)
+          if (target >= row && target < row + min(rows, 32))
             W.picked[at] = buf[(int)(target - row) * kPitch + lane];
           red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x, W.c2);
           __syncwarp();
@@ -330,14 +355,21 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         } else if constexpr (MODE == kDHidden) {
           if (row + lane < W.M) {
+            const int n = min(32, W.N - col - c * 32);
             float *to = W.sums + ((long long)(u / (W.nM * W.nN)) * W.N + col + c * 32) * W.M + row +
                         lane;
+            if (W.add && BOUTE_INB(row + lane, W.M)) {
+              float was[32];  // (all on their way at once)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              if (col + c * 32 + i >= W.N) break;
-              float *p = to + (long long)i * W.M;
-              if (BOUTE_INB(row + lane, W.M)) *p = W.add ? *p + x[i] : x[i];
+              for (int i = 0; i < 32; ++i)
+                if (i < n) was[i] = to[(long long)i * W.M];
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (i < n) x[i] += was[i];
             }
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i < n && BOUTE_INB(row + lane, W.M)) to[(long long)i * W.M] = x[i];
           }
         } else {
           const int d0 = col + c * 32;
@@ -381,7 +413,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (tid == 0 && *abort) set_status(&W.head->status, BOUTE_ERR_TIMEOUT);
+  if (tid == 0 && MODE == kStats) W.head->status[blockIdx.x] = *abort ? BOUTE_ERR_TIMEOUT : 0;
+  if (tid == 0 && MODE != kStats && *abort) set_status(W.head->status, BOUTE_ERR_TIMEOUT);
   cluster_sync();
   if (warp == 1) pair_tmem_dealloc(tmem, 512);
 }
@@ -389,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // The pieces' sums of 32 positions a block: lanes over the positions, warps over the pieces.
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
-    hidden_join_kernel(const Header *head, const float *part, const float *picked,
+    hidden_join_kernel(const Header *head, int blocks, const float *part, const float *picked,
                        const long long *targets, long long T, long long Tp, int parts, int V,
                        float scale, float c2, float *logprob, float *entropy, float *lse) {
   __shared__ Stat red[kJoinWarps][32];
@@ -398,12 +431,21 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   const long long t = blockIdx.x * 32ll + lane, all = parts * Tp;
   Stat a = {-INFINITY, 0.f, 0.f};
-  if (t < T)
-#pragma unroll 4
-    for (int p = warp; p < parts; p += kJoinWarps) {
+  constexpr int kAtOnce = 8;  // parts on their way to a thread
+  for (int p0 = warp; p0 < parts; p0 += kAtOnce * kJoinWarps) {
+    Stat b[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int p = p0 + i * kJoinWarps;
       const long long at = p * Tp + t;
-      if (BOUTE_INB(at, all)) join(a, {part[at], part[all + at], part[2 * all + at]}, c2);
+      b[i] = {-INFINITY, 0.f, 0.f};
+      if (p < parts && t < T && BOUTE_INB(at, all))
+        b[i] = {part[at], part[all + at], part[2 * all + at]};
     }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) join(a, b[i], c2);
+  }
+  const bool late = __syncthreads_or(threadIdx.x < blocks && head->status[threadIdx.x] != 0);
   red[warp][lane] = a;
   __syncthreads();
   for (int n = kJoinWarps / 2; n > 0; n /= 2) {
@@ -427,7 +469,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
     l = H = NAN;
     if (target >= 0) lp = NAN;
   }
-  if (head->status != 0) l = H = lp = NAN;
+  if (late) l = H = lp = NAN;
   logprob[t] = lp;
   entropy[t] = H;
   lse[t] = l;
@@ -472,7 +514,7 @@ __global__ void __launch_bounds__(256)
   for (int s = 0; s < splits; ++s)
     if (BOUTE_INB(s * n + i, splits * n)) v += sums[s * n + i];
   v *= coef_scale(head->largest, true);
-  if (head->status != 0) v = NAN;
+  if (head->status[0] != 0) v = NAN;
   dh[i / D * ldd + i % D] = from_float<T>(v);
 }
 
@@ -508,6 +550,14 @@ void tile_columns(int n, int &tiles, int &width) {
   width = (int)up((n + tiles - 1) / tiles, 32);
 }
 
+// A block's rows of a tile, a multiple of 8 up to 128, so that the pairs' rounds over V rows are
+// full: where one tile holds the positions, reading the weight bounds the call.
+int even_rows(int V) {
+  const int pairs = num_sms() / 2;
+  const int rounds = (V + kPairM * pairs - 1) / (kPairM * pairs);
+  return (int)std::min<long long>(128, up((V + 2ll * rounds * pairs - 1) / (2ll * rounds * pairs), 8));
+}
+
 // A matrix as the copies can read it: in place, or aligned in the workspace.
 struct Operand {
   const void *p;
@@ -523,6 +573,7 @@ Operand operand(const void *p, long long rows, int D, long long ld) {
 struct Plan {
   Operand h, w;
   int tiles_t, tile_t;     // of the positions
+  int tile_m;              // a block's tokens of the vocabulary (statistics)
   long long Tp;
   int piece;               // tokens of the vocabulary at once (gradient)
   int splits;              // of dh's reduction
@@ -558,7 +609,8 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   };
   p.header = take(sizeof(Header));
   if (!grad) {
-    p.part = take(3ull * 2 * ((V + kPairM - 1) / kPairM) * p.Tp * sizeof(float));
+    p.tile_m = p.tiles_t == 1 ? even_rows(V) : 128;
+    p.part = take(3ull * 2 * ((V + 2 * p.tile_m - 1) / (2 * p.tile_m)) * p.Tp * sizeof(float));
     p.picked = take(p.Tp * sizeof(float));
   } else {
     p.piece = (int)std::min<long long>(
@@ -583,9 +635,14 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
 size_t set_stages(Work &W, bool b_mn, size_t epi) {
   const int half = W.tile_n / 2;
   W.stage_bytes = kABytes + (b_mn ? (half + 63) / 64 * 64 : half) * 128;
+  W.tx_bytes = W.stage_bytes - (128 - W.tile_m) * 128;
   const size_t room = 232448 - 1024 - 1024 - epi;  // (1 KB of barriers, 1 KB of alignment)
   W.stages = (int)std::min<size_t>(kMaxStages, room / W.stage_bytes);
   return 1024 + (size_t)W.stages * W.stage_bytes + epi;
+}
+
+int pairs_of(long long units) {
+  return (int)std::min<long long>(units, std::min(num_sms(), kBlocks) / 2);
 }
 
 template <Mode MODE>
@@ -596,7 +653,7 @@ int launch(int dtype, const CUtensorMap &a, const CUtensorMap &b, Work W, cudaSt
                                      : 0;
   const size_t smem = set_stages(W, kBMn, epi);
   const long long units = (long long)W.nM * W.nN * W.splits;
-  const int pairs = (int)std::min<long long>(units, num_sms() / 2);
+  const int pairs = pairs_of(units);
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     if constexpr (std::is_same<T, float>::value) {
@@ -694,15 +751,15 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
   if (T == 0) return BOUTE_OK;
   const cudaStream_t s = (cudaStream_t)stream;
   char *ws = (char *)workspace;
-  if (cudaMemsetAsync(ws, 0, sizeof(Header), s) != cudaSuccess) return last_launch_status();
   if (int r = align_operand(p.h, T, D, ldh, ws + p.h_at, s)) return r;
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   CUtensorMap mw, mh;
-  if (int r = make_map(&mw, dtype, p.w.p, D, V, p.w.ld, 128)) return r;
+  if (int r = make_map(&mw, dtype, p.w.p, D, V, p.w.ld, p.tile_m)) return r;
   Work W{};
   W.M = V;
   W.K = D;
-  W.nM = (V + kPairM - 1) / kPairM;
+  W.tile_m = p.tile_m;
+  W.nM = (V + 2 * p.tile_m - 1) / (2 * p.tile_m);
   W.splits = 1;
   W.head = (Header *)(ws + p.header);
   W.c2 = scale * kLog2e;
@@ -719,7 +776,7 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
       return r;
     if (int r = launch<kStats>(dtype, mw, mh, W, s)) return r;
     if (int r = launch_cluster(hidden_join_kernel, (n + 31) / 32, 32 * kJoinWarps, 1, 0, s, W.head,
-                               W.part, W.picked, W.targets, n, W.Tp, 2 * W.nM, V, scale, W.c2,
+                               2 * pairs_of((long long)W.nM * W.nN), W.part, W.picked, W.targets, n, W.Tp, 2 * W.nM, V, scale, W.c2,
                                logprob + t0, entropy + t0, lse + t0))
       return r;
   }
@@ -754,6 +811,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
   W.head = (Header *)(ws + p.header);
+  W.tile_m = 128;
   Position *pos = (Position *)(ws + p.pos);
   int *tgt = (int *)(ws + p.tgt);
   if (int r = launch_cluster(hidden_positions_kernel, (T + 255) / 256, 256, 1, 0, s, W.head,

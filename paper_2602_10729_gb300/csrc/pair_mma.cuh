@@ -23,9 +23,11 @@ int make_map(CUtensorMap *map, int dtype, const void *base, long long inner, lon
 #ifdef __CUDACC__
 // ---- barriers ------------------------------------------------------------------------
 // Waits like mbar_wait, and gives up when *abort is set (which it does where the wait runs out).
-// The acquire covers what the pair's other block released.
+// CLUSTER: for what the pair's other block released, too.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
   auto done = [&]() {
+    if (!CLUSTER) return mbar_try_wait_sleep(bar, parity, 2000u);
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -48,6 +50,16 @@ __device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, volati
       }
     }
   }
+}
+// True in one lane of a whole warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
 }
 // Whether ok holds in all `count` threads that meet at barrier `id`, in each of them.
 __device__ __forceinline__ bool group_all(int id, int count, bool ok) {
