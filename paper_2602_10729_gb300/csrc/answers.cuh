@@ -25,6 +25,21 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) {
   return __float2bfloat16_rn(x);
 }
 
+// A word's two 16-bit elements as floats, and back with one rounding each.
+__device__ __forceinline__ void unpack2(__half, uint32_t w, float &a, float &b) {
+  unpack_f16x2(w, a, b);
+}
+__device__ __forceinline__ void unpack2(__nv_bfloat16, uint32_t w, float &a, float &b) {
+  a = __uint_as_float(w << 16);
+  b = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t pack2(__half, float a, float b) { return pack_f16x2(a, b); }
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16, float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
 // go(T{}) for the element type of a boute_dtype.
 template <class Go>
 inline int with_dtype(int dtype, Go go) {
