@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "pair_mma.cuh"
 
@@ -30,15 +31,19 @@ constexpr int kPitch = 36;  // floats of a row of a warp's 32 x 32 transposition
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -200.f;  // 2^kLowest = 0 in fp32
 
-enum Mode { kStats = 0, kCoef = 1, kDHidden = 2, kDWeight = 3 };
+// What a launch makes of its tiles. The logits come with the vocabulary in the tile's rows and the
+// positions in its columns (any number of positions fills the columns of a tile), or with the
+// positions in its rows (a thread has a position's logits, and no sum crosses threads).
+enum Kind { kStatsCols, kStatsRows, kCoefCols, kCoefRows, kGrads };
 
 // At the start of a call's workspace.
 constexpr int kBlocks = 256;  // of a launch at most
+constexpr int kBounds = 64;
 struct Header {
   // BOUTE_ERR_TIMEOUT where a wait ran out: of each block of the statistics' launch, which writes
   // its own; of all launches of the gradient, which clears it first
   int status[kBlocks];
-  unsigned largest;  // bits of the largest bound of a coefficient (gradient)
+  unsigned largest[kBounds];  // bits of the largest bound of a coefficient, of each block that looked
 };
 // What the coefficients of a position need.
 struct Position {
@@ -46,8 +51,12 @@ struct Position {
 };
 
 // The power of two by which the coefficients are scaled while they are 16-bit numbers: the largest
-// comes to 2^14 (fp16: what is 2^-28 of that has all its bits, and 2^-39 some).
-__device__ __forceinline__ float coef_scale(unsigned largest, bool inverse) {
+// comes to 2^14 (fp16: what is 2^-28 of that has all its bits, and 2^-39 some). For whole warps.
+__device__ __forceinline__ float coef_scale(const Header *head, int bounds, bool inverse) {
+  const int lane = threadIdx.x & 31;
+  unsigned largest = lane < bounds ? head->largest[lane] : 0u;
+  if (lane + 32 < bounds) largest = max(largest, head->largest[lane + 32]);
+  largest = __reduce_max_sync(kAll, largest);
   const int e = (int)(largest >> 23) - 127;  // (the largest is in [2^e, 2^(e + 1)))
   if (largest == 0u || largest >= 0x7f800000u) return 1.f;
   const int k = min(max(13 - e, -126), 126);
@@ -55,45 +64,83 @@ __device__ __forceinline__ float coef_scale(unsigned largest, bool inverse) {
 }
 
 struct Work {
-  int M, N, K;             // rows, columns, reduction
+  int M, N, K;              // rows, columns, reduction
   int tile_m, tile_n, nM, nN, splits;  // (tile_m: rows of a block, 128 but for few positions)
-  int stages, stage_bytes, tx_bytes;  // (of a block; what its copies bring)
+  int a_mn, b_mn, rows_first;  // operands' order; whether neighbouring units differ in their rows
+  int tx_bytes;             // that a block's copies bring for a stage
   Header *head;
+  int bounds;               // values of head->largest
   // statistics
   float c2;
-  float *part;             // 3 x parts x Tp: maxima, s, u
-  float *picked;           // Tp: x of the targets
+  float *part;              // 3 x parts x Tp: maxima, s, u
+  float *picked;            // Tp: x of the targets
   const long long *targets;
-  long long Tp;
+  long long Tp;             // (coefficients: the pitch of coef)
   // coefficients
   const Position *pos;
-  const int *tgt;          // targets, -1 for none
+  const int *tgt;           // targets, -1 for none
   float scale;
-  uint16_t *coef;          // M x Tp
-  int row0;                // of the piece in the vocabulary
+  uint16_t *coef;           // a piece's: tokens x positions, or positions x tokens
+  int row0;                 // of the piece in the vocabulary
   // gradients
-  float *sums;             // splits x N x M
-  int add;                 // to what earlier pieces left there
-  char *out;               // M x N, pitch ldo
+  float *sums;              // dh: splits x N x M, in fp32
+  int add;                  // to what earlier pieces left there
+  char *out;                // dW: M x N, pitch ldo
   long long ldo;
-  int width;               // bytes that the rows' alignment allows in a store
+  int width;                // bytes that the rows' alignment allows in a store
+};
+// A launch's products: one set of tiles, or dh's and behind them dW's.
+struct Job {
+  CUtensorMap a, b;
+  Work w;
+};
+struct Jobs {
+  Job job[2];
+  int units[2], stages, stage_bytes;
+  // The pairs take the first set's units in turn; those that got one fewer (`light`, from pair
+  // light_from on) take `ahead` of the second set first, then all take the rest in turn.
+  int light_from, ahead;
 };
 
 struct Unit {
-  int m, n, k0, k1;  // tiles; blocks of the reduction
+  int job, m, n, k0, k1, split;  // tiles; blocks of the reduction; job < 0: none
 };
-__device__ __forceinline__ Unit unit_of(const Work &W, int u) {
+// The i-th unit of a pair.
+template <Kind KIND>
+__device__ __forceinline__ Unit unit_of(const Jobs &J, int pair, int pairs, int i) {
+  int job = 0, u = pair + i * pairs;
+  if (KIND == kGrads && u >= J.units[0]) {
+    job = 1;
+    const int had = pair < J.units[0] ? (J.units[0] - pair + pairs - 1) / pairs : 0;
+    int j = i - had;
+    const int lights = pairs - J.light_from, l = pair - J.light_from;
+    const int heads = min(J.units[1], lights * J.ahead);
+    if (l < 0) {
+      u = heads + j * pairs + lights + pair;
+    } else {
+      const int mine = l < heads ? (heads - l + lights - 1) / lights : 0;
+      u = j < mine ? j * lights + l : heads + (j - mine) * pairs + l;
+    }
+  }
+  if (u >= J.units[job]) return {-1, 0, 0, 0, 0, 0};
+  const Work &W = J.job[job].w;
   const int kb = (W.K + kBlockK - 1) / kBlockK;  // (times a split: 2^14 x 64 at most)
-  int s = 0, r = u, k0 = 0, k1 = kb;
+  Unit t{job, 0, 0, 0, kb, 0};
   if (W.splits > 1) {
     const int per = W.nM * W.nN;
-    s = u / per;
-    r = u - s * per;
-    k0 = s * kb / W.splits;
-    k1 = (s + 1) * kb / W.splits;
+    t.split = u / per;
+    u -= t.split * per;
+    t.k0 = t.split * kb / W.splits;
+    t.k1 = (t.split + 1) * kb / W.splits;
   }
-  const int m = r / W.nN;
-  return {m, r - m * W.nN, k0, k1};
+  if (W.rows_first) {
+    t.n = u / W.nM;
+    t.m = u - t.n * W.nM;
+  } else {
+    t.m = u / W.nN;
+    t.n = u - t.m * W.nN;
+  }
+  return t;
 }
 
 // ---- the sums of a tile ----------------------------------------------------------------
@@ -107,16 +154,26 @@ __device__ __forceinline__ Stat stat_of(const float (&x)[32], float c2) {
   for (int i = 1; i < 31; i += 2) m = max_nan(m, x[i], x[i + 1]);
   m = max_nan(m, x[31]);
   if (m == -INFINITY) return {m, 0.f, 0.f};
-  float s[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+  const unsigned long long zero = f2_dup(0.f), less = f2_dup(-m), by = f2_dup(c2);
+  unsigned long long s[2] = {zero, zero}, u[2] = {zero, zero};
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const float y = (x[i] - m) * c2, e = exp2_fast(y);
-    s[i & 3] += e;
-    u[i & 3] = fmaf(y, e, u[i & 3]);
+  for (int i = 0; i < 32; i += 2) {
+    const unsigned long long y = f2_mul(f2_add(f2_pack(x[i], x[i + 1]), less), by);
+    float y0, y1;
+    f2_split(y, y0, y1);
+    const unsigned long long e = f2_pack(exp2_fast(y0), exp2_fast(y1));
+    s[i / 2 & 1] = f2_add(s[i / 2 & 1], e);
+    u[i / 2 & 1] = f2_fma(y, e, u[i / 2 & 1]);
   }
-  Stat r = {m, (s[0] + s[1]) + (s[2] + s[3]), (u[0] + u[1]) + (u[2] + u[3])};
+  Stat r = {m, 0.f, 0.f};
+  float a, b;
+  f2_split(f2_add(s[0], s[1]), a, b);
+  r.s = a + b;
+  f2_split(f2_add(u[0], u[1]), a, b);
+  r.u = a + b;
   if (isnan(r.u)) {  // (a masked logit: -inf times 0)
     float v = 0.f;
+#pragma unroll
     for (int i = 0; i < 32; ++i) {
       const float y = max_nan((x[i] - m) * c2, kLowest);
       v = fmaf(y, exp2_fast(y), v);
@@ -139,12 +196,20 @@ __device__ __forceinline__ void join(Stat &a, Stat b, float c2) {
   a.m = m;
 }
 
+// 32 values of a thread with one rounding each, to a 32-byte boundary.
+template <class T>
+__device__ __forceinline__ void store_row_of(uint16_t *to, const float (&x)[32]) {
+  uint32_t r[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = pack2(T{}, x[2 * i], x[2 * i + 1]);
+  store32(to, r);
+  store32(to + 16, r + 8);
+}
+
 // ---- the kernel --------------------------------------------------------------------------
-template <Mode MODE, class T>
-__global__ void __launch_bounds__(kThreads, 1)
-    hidden_kernel(const __grid_constant__ CUtensorMap map_a,
-                  const __grid_constant__ CUtensorMap map_b, const Work W) {
-  constexpr bool kAMn = MODE == kDHidden, kBMn = MODE == kDHidden || MODE == kDWeight;
+template <Kind KIND, class T>
+__global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_constant__ Jobs J) {
+  constexpr bool kStats = KIND == kStatsCols || KIND == kStatsRows;
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2],
       drain;
@@ -154,9 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
   const int rank = blockIdx.x & 1, pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   uint8_t *ring = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *epi = ring + (size_t)W.stages * W.stage_bytes;
-  const int units = W.nM * W.nN * W.splits;
-  const int half_n = W.tile_n / 2;
+  uint8_t *epi = ring + (size_t)J.stages * J.stage_bytes;
 
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
@@ -185,28 +248,32 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       int s = 0, used = 0;
       uint32_t phase = 0;
-      for (int u = pair; u < units && !*abort; u += pairs) {
-        const Unit t = unit_of(W, u);
+      for (int i = 0; !*abort; ++i) {
+        const Unit t = unit_of<KIND>(J, pair, pairs, i);
+        if (t.job < 0) break;
+        const Job &job = J.job[KIND == kGrads ? t.job : 0];
+        const Work &W = job.w;
+        const int half_n = W.tile_n / 2;
         const int m0 = (t.m * 2 + rank) * W.tile_m, n0 = t.n * W.tile_n + rank * half_n;
         for (int kb = t.k0; kb < t.k1; ++kb) {
           if (!pair_wait(&empty[s], phase ^ 1u, abort)) break;
-          uint8_t *a = ring + (size_t)s * W.stage_bytes, *b = a + kABytes;
+          uint8_t *a = ring + (size_t)s * J.stage_bytes, *b = a + kABytes;
           const uint32_t bar = peer(&full[s], 0);
           if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * (uint32_t)W.tx_bytes);
           const int k = kb * kBlockK;
-          if constexpr (kAMn) {
-            load_box(a, &map_a, m0, k, bar);
-            load_box(a + kABytes / 2, &map_a, m0 + 64, k, bar);
+          if (KIND == kGrads && W.a_mn) {
+            load_box(a, &job.a, m0, k, bar);
+            load_box(a + kABytes / 2, &job.a, m0 + 64, k, bar);
           } else {
-            load_box(a, &map_a, k, m0, bar);
+            load_box(a, &job.a, k, m0, bar);
           }
-          if constexpr (kBMn) {
-            for (int q = 0; q < half_n; q += 64) load_box(b + q * 128, &map_b, n0 + q, k, bar);
+          if (KIND == kGrads && W.b_mn) {
+            for (int q = 0; q < half_n; q += 64) load_box(b + q * 128, &job.b, n0 + q, k, bar);
           } else {
-            load_box(b, &map_b, k, n0, bar);
+            load_box(b, &job.b, k, n0, bar);
           }
           used = max(used, s + 1);
-          if (++s == W.stages) s = 0, phase ^= 1u;
+          if (++s == J.stages) s = 0, phase ^= 1u;
         }
       }
       if (*abort && rank == 0)  // let the copies land before the blocks' memory goes
@@ -218,17 +285,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     // the loop, issuing took longer than the products.)
     if (rank == 0) {
       constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-      const uint32_t idesc = pair_idesc(kBf16, kAMn, kBMn, W.tile_n);
       const bool issuer = elect_one();
-      const uint64_t ad0 = operand_desc<kAMn>(smem_u32(ring));
-      const uint64_t bd0 = operand_desc<kBMn>(smem_u32(ring) + kABytes);
       int s = 0;
-      uint32_t phase = 0, seq = 0;
+      uint32_t phase = 0;
       bool ok = true;
-      for (int u = pair; u < units && ok; u += pairs, ++seq) {
-        const Unit t = unit_of(W, u);
-        const uint32_t acc = seq & 1u, to = tmem + acc * kMaxTileN;
-        ok = __all_sync(kAll, pair_wait<true>(&acc_empty[acc], ((seq >> 1) & 1u) ^ 1u, abort));
+      for (int i = 0; ok; ++i) {
+        const Unit t = unit_of<KIND>(J, pair, pairs, i);
+        if (t.job < 0) break;
+        const Work &W = J.job[KIND == kGrads ? t.job : 0].w;
+        const bool a_mn = KIND == kGrads && W.a_mn, b_mn = KIND == kGrads && W.b_mn;
+        const uint32_t idesc = pair_idesc(kBf16, a_mn, b_mn, W.tile_n);
+        const uint64_t ad0 = operand_desc(smem_u32(ring), a_mn);
+        const uint64_t bd0 = operand_desc(smem_u32(ring) + kABytes, b_mn);
+        const int a_step = desc_step(a_mn), b_step = desc_step(b_mn);
+        const uint32_t acc = i & 1u, to = tmem + acc * kMaxTileN;
+        ok = __all_sync(kAll, pair_wait<true>(&acc_empty[acc], ((i >> 1) & 1u) ^ 1u, abort));
         if (!ok) break;
         tc_fence_after();
         for (int kb = t.k0; kb < t.k1; ++kb) {
@@ -236,18 +307,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           tc_fence_after();
           if (issuer) {
-            const uint64_t at = (uint64_t)((uint32_t)(s * W.stage_bytes) >> 4);
+            const uint64_t at = (uint64_t)((uint32_t)(s * J.stage_bytes) >> 4);
             const uint64_t ad = ad0 + at, bd = bd0 + at;
             const int left = W.K - kb * kBlockK;  // (of a short last block, the steps with data)
 #pragma unroll
             for (int k = 0; k < kBlockK / 16; ++k)
               if (k * 16 < left)
-                pair_mma(to, ad + k * kDescStep<kAMn>, bd + k * kDescStep<kBMn>, idesc,
-                         kb > t.k0 || k > 0);
+                pair_mma(to, ad + k * a_step, bd + k * b_step, idesc, kb > t.k0 || k > 0);
             pair_commit(&empty[s]);
           }
           __syncwarp();
-          if (++s == W.stages) s = 0, phase ^= 1u;
+          if (++s == J.stages) s = 0, phase ^= 1u;
         }
         if (ok && issuer) pair_commit(&acc_full[acc]);
         __syncwarp();
@@ -267,18 +337,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) arrive_peer(&acc_empty[group], 0);
     };
-    const int chunks = W.tile_n / 32;
     float mul = 1.f;
-    if (MODE != kStats) mul = coef_scale(W.head->largest, MODE != kCoef);
-    uint32_t seq = 0;
-    for (int u = pair; u < units; u += pairs, ++seq) {
-      if ((seq & 1u) != (uint32_t)group) continue;
-      const Unit t = unit_of(W, u);
+    if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
+    for (int i = group;; i += 2) {
+      const Unit t = unit_of<KIND>(J, pair, pairs, i);
+      if (t.job < 0) break;
+      const Work &W = J.job[KIND == kGrads ? t.job : 0].w;
+      const int chunks = W.tile_n / 32;
       const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32, col = t.n * W.tile_n;
       // what does not wait for the products
       Position *pos = (Position *)epi + group * kMaxTileN;
       int *tgt = (int *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
-      if constexpr (MODE == kCoef) {
+      Position own = {1e30f, 0.f, 0.f, 0.f};
+      int target = -1;
+      if constexpr (KIND == kCoefCols) {
         named_barrier_sync(1 + group, kGroup);  // (the last tile's are read)
         for (int c = gtid; c < W.tile_n; c += kGroup) {
           Position p = {1e30f, 0.f, 0.f, 0.f};
@@ -291,114 +363,150 @@ __global__ void __launch_bounds__(kThreads, 1)
           pos[c] = p;
           tgt[c] = j;
         }
+      } else if constexpr (KIND == kCoefRows) {
+        if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+          own = W.pos[row + lane];
+          own.a *= mul, own.b *= mul, own.g *= mul;
+          target = W.tgt[row + lane] - W.row0;
+        }
+      } else if constexpr (KIND == kStatsRows) {
+        if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+          const long long j = W.targets[row + lane];
+          target = j >= 0 && j < W.N ? (int)j : -1;
+        }
       }
       // (where the group meets at a barrier, it goes on or gives up as one)
-      bool ok = __all_sync(kAll, pair_wait(&acc_full[group], (seq >> 1) & 1u, abort));
-      if (MODE == kStats || MODE == kCoef) ok = group_all(1 + group, kGroup, ok);
+      bool ok = __all_sync(kAll, pair_wait(&acc_full[group], (i >> 1) & 1u, abort));
+      if (KIND == kStatsCols || KIND == kCoefCols) ok = group_all(1 + group, kGroup, ok);
       if (!ok) break;
       tc_fence_after();
+      Stat run = {-INFINITY, 0.f, 0.f};
       for (int c = 0; c < chunks; ++c) {
         float x[32];
         tmem_ld32(from + c * 32, x);
         if (c == chunks - 1) release();
-        if (MODE == kDHidden && t.k0 == t.k1)  // (a short piece's empty part)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = 0.f;
-        if constexpr (MODE == kStats) {
+        const int d0 = col + c * 32;
+        if constexpr (KIND == kStatsCols) {
           float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
           Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
-          const int at = col + c * 32 + lane;
-          long long target = -1;
-          if (at < W.N && BOUTE_INB(at, W.N)) target = W.targets[at];
+          const int at = d0 + lane;
+          long long wanted = -1;
+          if (at < W.N && BOUTE_INB(at, W.N)) wanted = W.targets[at];
           // (rows of the accumulator beyond the block's hold what was in its shared memory)
           const int rows = min(W.tile_m - quarter * 32, W.M - row);
           if (lane >= rows)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = -INFINITY;
+            for (int q = 0; q < 32; ++q) x[q] = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            *(float4 *)(buf + lane * kPitch + i) = {x[i], x[i + 1], x[i + 2], x[i + 3]};
+          for (int q = 0; q < 32; q += 4)
+            *(float4 *)(buf + lane * kPitch + q) = {x[q], x[q + 1], x[q + 2], x[q + 3]};
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = buf[i * kPitch + lane];
-          if (target >= row && target < row + min(rows, 32))
-            W.picked[at] = buf[(int)(target - row) * kPitch + lane];
+          for (int q = 0; q < 32; ++q) x[q] = buf[q * kPitch + lane];
+          if (wanted >= row && wanted < row + min(rows, 32))
+            W.picked[at] = buf[(int)(wanted - row) * kPitch + lane];
           red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x, W.c2);
           __syncwarp();
-        } else if constexpr (MODE == kCoef) {
+        } else if constexpr (KIND == kStatsRows) {
+          if (d0 + 32 > W.N)
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (d0 + q >= W.N) x[q] = -INFINITY;
+          if (__any_sync(kAll, target >= d0 && target < d0 + 32))
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (target == d0 + q) W.picked[row + lane] = x[q];
+          join(run, stat_of(x, W.c2), W.c2);
+        } else if constexpr (KIND == kCoefCols) {
           const int j = tgt[c * 32 + lane];
           unsigned here = __ballot_sync(kAll, j >= row && j < row + 32);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const Position p = pos[c * 32 + i];
-            const float lp = max_nan(fmaf(x[i], W.scale, -p.lse), -1e4f);
-            x[i] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
+          for (int q = 0; q < 32; ++q) {
+            const Position p = pos[c * 32 + q];
+            const float lp = max_nan(fmaf(x[q], W.scale, -p.lse), -1e4f);
+            x[q] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
           }
           if (here)
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if ((here >> i & 1u) && tgt[c * 32 + i] == row + lane) x[i] += pos[c * 32 + i].g;
-          if (row + lane < W.M && BOUTE_INB(col + c * 32 + 31, W.Tp)) {
-            uint32_t r[16];
+            for (int q = 0; q < 32; ++q)
+              if ((here >> q & 1u) && tgt[c * 32 + q] == row + lane) x[q] += pos[c * 32 + q].g;
+          if (row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp))
+            store_row_of<T>(W.coef + (row + lane) * W.Tp + d0, x);
+        } else if constexpr (KIND == kCoefRows) {
+          const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.lse);
+          const unsigned long long a2 = f2_dup(own.a), b2 = f2_dup(own.b), l2e = f2_dup(kLog2e);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) r[i] = pack2(T{}, x[2 * i], x[2 * i + 1]);
-            uint16_t *to = W.coef + (row + lane) * W.Tp + col + c * 32;
-            store32(to, r);
-            store32(to + 16, r + 8);
+          for (int q = 0; q < 32; q += 2) {
+            float l0, l1, y0, y1;
+            f2_split(f2_fma(f2_pack(x[q], x[q + 1]), by, less), l0, l1);
+            const unsigned long long lp = f2_pack(max_nan(l0, -1e4f), max_nan(l1, -1e4f));
+            f2_split(f2_mul(lp, l2e), y0, y1);
+            f2_split(f2_mul(f2_pack(exp2_fast(y0), exp2_fast(y1)), f2_fma(b2, lp, a2)), x[q],
+                     x[q + 1]);
           }
-        } else if constexpr (MODE == kDHidden) {
-          if (row + lane < W.M) {
-            const int n = min(32, W.N - col - c * 32);
-            float *to = W.sums + ((long long)(u / (W.nM * W.nN)) * W.N + col + c * 32) * W.M + row +
-                        lane;
-            if (W.add && BOUTE_INB(row + lane, W.M)) {
+          if (__any_sync(kAll, target >= d0 && target < d0 + 32))
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (target == d0 + q) x[q] += own.g;
+          if (row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp))
+            store_row_of<T>(W.coef + (row + lane) * W.Tp + d0, x);
+        } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
+          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+            const int n = min(32, W.N - d0);
+            float *to = W.sums + ((long long)t.split * W.N + d0) * W.M + row + lane;
+            if (t.k0 == t.k1)  // (a short piece's empty part)
+#pragma unroll
+              for (int q = 0; q < 32; ++q) x[q] = 0.f;
+            if (W.add) {
               float was[32];  // (all on their way at once)
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (i < n) was[i] = to[(long long)i * W.M];
+              for (int q = 0; q < 32; ++q)
+                if (q < n) was[q] = to[(long long)q * W.M];
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (i < n) x[i] += was[i];
+              for (int q = 0; q < 32; ++q)
+                if (q < n) x[q] += was[q];
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i < n && BOUTE_INB(row + lane, W.M)) to[(long long)i * W.M] = x[i];
+            for (int q = 0; q < 32; ++q)
+              if (q < n) to[(long long)q * W.M] = x[q];
           }
-        } else {
-          const int d0 = col + c * 32;
-          if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {
-            T *to = (T *)W.out + (row + lane) * W.ldo + d0;
-            uint32_t r[16];
+        } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {  // dW
+          T *to = (T *)W.out + (row + lane) * W.ldo + d0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) r[i] = pack2(T{}, mul * x[2 * i], mul * x[2 * i + 1]);
-            if (d0 + 32 <= W.N && W.width >= 32) {
-              store32(to, r);
-              store32(to + 16, r + 8);
-            } else if (d0 + 32 <= W.N && W.width >= 16) {
+          for (int q = 0; q < 32; ++q) x[q] *= mul;
+          if (d0 + 32 <= W.N && W.width >= 32) {
+            store_row_of<T>((uint16_t *)to, x);
+          } else if (d0 + 32 <= W.N && W.width >= 16) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                *(uint4 *)(to + 8 * i) = {r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]};
-            } else {
+            for (int q = 0; q < 32; q += 8)
+              *(uint4 *)(to + q) = {pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
+                                    pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
+          } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (d0 + i < W.N) to[i] = from_float<T>(mul * x[i]);
-            }
+            for (int q = 0; q < 32; ++q)
+              if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
           }
         }
       }
-      if constexpr (MODE == kStats) {
-        named_barrier_sync(1 + group, kGroup);
-        const Stat *red =
-            (const Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
-        const long long parts = 2ll * W.nM, all = parts * W.Tp;
-        for (int c = gtid; c < W.tile_n; c += kGroup) {
-          Stat a = red[c];
-          for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + c], W.c2);
-          const long long at = (2ll * t.m + rank) * W.Tp + col + c;
-          if (col + c >= W.N || !BOUTE_INB(at, all)) continue;
+      if constexpr (kStats) {
+        const long long parts = KIND == kStatsCols ? 2ll * W.nM : W.nN, all = parts * W.Tp;
+        auto write = [&](Stat a, long long at) {
+          if (!BOUTE_INB(at, all)) return;
           W.part[at] = a.m;
           W.part[all + at] = a.s;
           W.part[2 * all + at] = a.u;
+        };
+        if constexpr (KIND == kStatsCols) {
+          named_barrier_sync(1 + group, kGroup);
+          const Stat *red =
+              (const Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
+          for (int c = gtid; c < W.tile_n; c += kGroup) {
+            Stat a = red[c];
+            for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + c], W.c2);
+            if (col + c < W.N) write(a, (2ll * t.m + rank) * W.Tp + col + c);
+          }
+        } else if (row + lane < W.M) {
+          write(run, t.n * W.Tp + row + lane);
         }
       }
     }
@@ -406,8 +514,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (tid == 0 && MODE == kStats) W.head->status[blockIdx.x] = *abort ? BOUTE_ERR_TIMEOUT : 0;
-  if (tid == 0 && MODE != kStats && *abort) set_status(W.head->status, BOUTE_ERR_TIMEOUT);
+  Header *head = J.job[0].w.head;
+  if (tid == 0 && kStats) head->status[blockIdx.x] = *abort ? BOUTE_ERR_TIMEOUT : 0;
+  if (tid == 0 && !kStats && *abort) set_status(head->status, BOUTE_ERR_TIMEOUT);
   cluster_sync();
   if (warp == 1) pair_tmem_dealloc(tmem, 512);
 }
@@ -475,40 +584,68 @@ __global__ void __launch_bounds__(256)
                             float scale, const float *lse, const float *entropy,
                             const float *g_logprob, const float *g_entropy, Position *pos,
                             int *tgt) {
+  __shared__ unsigned red[8];
   pdl_wait();
   pdl_trigger();
-  const long long t = blockIdx.x * 256ll + threadIdx.x;
   float bound = 0.f;
-  if (t < T && BOUTE_INB(t, T)) {
+  bool nan = false;
+  for (long long t = blockIdx.x * 256ll + threadIdx.x; t < T; t += gridDim.x * 256ll) {
+    if (!BOUTE_INB(t, T)) break;
     const long long target = targets[t];
     const float g = target < 0 ? 0.f : g_logprob[t], gh = g_entropy ? g_entropy[t] : 0.f;
     Position p = {lse[t], -scale * g, -scale * gh, scale * g};
     if (g_entropy) p.a -= scale * gh * entropy[t];
-    bound = scale * (fabsf(g) + 4.f * fabsf(gh));
+    const float most = scale * (fabsf(g) + 4.f * fabsf(gh));
+    bound = fmaxf(bound, most);
+    nan |= isnan(most);
     if (p.lse == -INFINITY) p = {1e30f, 0.f, 0.f, 0.f};  // a row without a token left
     if (target >= V) p.a = NAN;
     pos[t] = p;
     tgt[t] = target >= 0 && target < V ? (int)target : -1;
   }
-  const unsigned most = __reduce_max_sync(kAll, __float_as_uint(bound));
-  if ((threadIdx.x & 31) == 0 && most) atomicMax(&head->largest, most);
+  const unsigned most =
+      __reduce_max_sync(kAll, nan ? 0x7fffffffu : __float_as_uint(bound));
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned all = 0;
+    for (int w = 0; w < 8; ++w) all = max(all, red[w]);
+    head->largest[blockIdx.x] = all;
+    if (blockIdx.x == 0) head->status[0] = 0;
+  }
 }
 
-// dh from the sums of its splits.
-template <class T>
+// dh from the sums of its splits: E neighbouring elements a thread.
+template <class T, int E>
 __global__ void __launch_bounds__(256)
-    hidden_dh_kernel(const Header *head, const float *sums, int splits, long long rows, int D,
-                     T *dh, long long ldd) {
+    hidden_dh_kernel(const Header *head, int bounds, const float *sums, int splits,
+                     long long rows, int D, T *dh, long long ldd) {
   pdl_wait();
   pdl_trigger();
-  const long long i = blockIdx.x * 256ll + threadIdx.x, n = rows * D;
+  const float mul = coef_scale(head, bounds, true);
+  const long long i = (blockIdx.x * 256ll + threadIdx.x) * E, n = rows * D;
   if (i >= n) return;
-  float v = 0.f;
-  for (int s = 0; s < splits; ++s)
-    if (BOUTE_INB(s * n + i, splits * n)) v += sums[s * n + i];
-  v *= coef_scale(head->largest, true);
-  if (head->status[0] != 0) v = NAN;
-  dh[i / D * ldd + i % D] = from_float<T>(v);
+  const long long t = i / D;
+  const int d = (int)(i - t * D);
+  float v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    if (!BOUTE_INB(s * n + i, splits * n)) break;
+    float x[E];
+    if constexpr (E == 4) {
+      const float4 q = *(const float4 *)(sums + s * n + i);
+      x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
+    } else {
+      x[0] = sums[s * n + i];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] += x[e];
+  }
+  const bool late = head->status[0] != 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dh[t * ldd + d + e] = from_float<T>(late ? NAN : mul * v[e]);
 }
 
 // Rows of D 16-bit elements to a pitch of whole vectors, with zeros behind them.
@@ -543,6 +680,12 @@ void tile_columns(int n, int &tiles, int &width) {
   width = (int)up((n + tiles - 1) / tiles, 32);
 }
 
+// Whether the positions are the tiles' rows, of which 256 are a tile's whatever there are.
+bool in_rows(long long T, int D) {
+  const long long t = up(T, kPairM);
+  return D < 512 ? 2 * t <= 3 * T : 10 * t <= 11 * T;
+}
+
 // A block's rows of a tile, a multiple of 8 up to 128, so that the pairs' rounds over V rows are
 // full: where one tile holds the positions, reading the weight bounds the call.
 int even_rows(int V) {
@@ -568,33 +711,39 @@ Operand operand(const void *p, long long rows, int D, long long ld, bool lines) 
 
 struct Plan {
   Operand h, w;
-  int tiles_t, tile_t;     // of the positions
-  int tile_m;              // a block's tokens of the vocabulary (statistics)
-  long long Tp;
+  bool rows;               // positions in the tiles' rows
+  int tiles_t, tile_t;     // of the positions in columns
+  int tile_m;              // a block's tokens of the vocabulary (statistics in columns)
+  long long Tp;            // the positions with what the last tile has beyond them
   int piece;               // tokens of the vocabulary at once (gradient)
   int splits;              // of dh's reduction
   size_t header, part, picked, pos, tgt, coef, sums, h_at, w_at, bytes;
 };
 
-// The number of parts of dh's reduction, of which each is a product of its own: the pairs' rounds
-// over them, each 1 / splits as long, and 1 % for every part's sums.
-int dh_splits(long long units, int blocks, size_t each, int pairs) {
-  int best = 1;
-  double least = 1e30;
-  for (int s = 1; s <= 64 && s * 8 <= std::max(blocks, 8); ++s) {
-    if (s > 1 && s * each > kSumBytes) break;
-    const double cost = (double)((units * s + pairs - 1) / pairs) / s * (1.0 + 0.01 * s);
-    if (cost < least) least = cost, best = s;
-  }
-  return best;
+int pairs_of(long long units) {
+  return (int)std::min<long long>(units, std::min(num_sms(), kBlocks) / 2);
+}
+int blocks_of(int k) { return (k + kBlockK - 1) / kBlockK; }
+
+// The number of parts of dh's reduction over a piece, each a unit of its own of the pairs: the
+// fewest whose units are small beside a pair's share of the whole launch (other: dW's part of it),
+// so that dW's units even the pairs out.
+int dh_splits(long long tiles, int blocks, int width, double other, size_t each, int pairs) {
+  const double share = (tiles * (double)blocks * width + other) / pairs;
+  int s = 1;
+  while (s < 64 && (s + 1) * 4 <= blocks && (s + 1) * each <= kSumBytes &&
+         blocks * (double)width / s > 0.7 * share)
+    ++s;
+  return s;
 }
 
 Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, int V,
                long long ldw, bool grad) {
   Plan p{};
-  const long long t = grad ? T : std::min(T, kAtOnce);
-  tile_columns((int)std::max(t, 1ll), p.tiles_t, p.tile_t);
-  p.Tp = (long long)p.tiles_t * p.tile_t;
+  const long long t = std::max(1ll, grad ? T : std::min(T, kAtOnce));
+  tile_columns((int)t, p.tiles_t, p.tile_t);
+  p.rows = in_rows(t, D);
+  p.Tp = p.rows ? up(t, kPairM) : (long long)p.tiles_t * p.tile_t;
   // The hidden states are read once for every 256 tokens of the vocabulary (515 positions of 1000
   // elements, 50021 tokens: 70 us in place, 61 by way of whole lines; 4096: 305 and 259; gradient of
   // 515: 223 and 202). The weight is read once for every 256 positions, too seldom for a copy to pay
@@ -610,16 +759,21 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   p.header = take(sizeof(Header));
   if (!grad) {
     p.tile_m = p.tiles_t == 1 ? even_rows(V) : 128;
-    p.part = take(3ull * 2 * ((V + 2 * p.tile_m - 1) / (2 * p.tile_m)) * p.Tp * sizeof(float));
+    const long long parts = p.rows ? (V + kMaxTileN - 1) / kMaxTileN
+                                   : 2ll * ((V + 2 * p.tile_m - 1) / (2 * p.tile_m));
+    p.part = take(3ull * parts * p.Tp * sizeof(float));
     p.picked = take(p.Tp * sizeof(float));
   } else {
     p.piece = (int)std::min<long long>(
-        V, std::max<long long>(kPairM, (long long)(kCoefBytes / (2 * p.Tp)) / kPairM * kPairM));
-    int tiles_d = (D + kPairM - 1) / kPairM;
+        up(V, kPairM),
+        std::max<long long>(kPairM, (long long)(kCoefBytes / (2 * p.Tp)) / kPairM * kPairM));
     const size_t each = (size_t)T * D * sizeof(float);
-    p.splits = dh_splits((long long)tiles_d * p.tiles_t, (p.piece + kBlockK - 1) / kBlockK, each,
+    int tiles_d, tile_d;
+    tile_columns(D, tiles_d, tile_d);
+    p.splits = dh_splits((long long)((D + kPairM - 1) / kPairM) * p.tiles_t, blocks_of(p.piece),
+                         p.tile_t,
+                         (double)(p.piece / kPairM) * tiles_d * blocks_of((int)t) * tile_d, each,
                          num_sms() / 2);
-    // (a last piece that is shorter than the splits leaves some of them nothing to add)
     p.pos = take(p.Tp * sizeof(Position));
     p.tgt = take(p.Tp * sizeof(int));
     p.coef = take((size_t)p.piece * p.Tp * 2);
@@ -631,39 +785,54 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   return p;
 }
 
-// The rings of a launch: as many stages as fit beside the epilogue's shared memory.
-size_t set_stages(Work &W, bool b_mn, size_t epi) {
+// A block's bytes of a stage.
+int stage_of(const Work &W) {
   const int half = W.tile_n / 2;
-  W.stage_bytes = kABytes + (b_mn ? (half + 63) / 64 * 64 : half) * 128;
-  W.tx_bytes = W.stage_bytes - (128 - W.tile_m) * 128;
-  const size_t room = 232448 - 1024 - 1024 - epi;  // (1 KB of barriers, 1 KB of alignment)
-  W.stages = (int)std::min<size_t>(kMaxStages, room / W.stage_bytes);
-  return 1024 + (size_t)W.stages * W.stage_bytes + epi;
+  return kABytes + (W.b_mn ? (half + 63) / 64 * 64 : half) * 128;
 }
 
-int pairs_of(long long units) {
-  return (int)std::min<long long>(units, std::min(num_sms(), kBlocks) / 2);
-}
-
-template <Mode MODE>
-int launch(int dtype, const CUtensorMap &a, const CUtensorMap &b, Work W, cudaStream_t s) {
-  constexpr bool kBMn = MODE == kDHidden || MODE == kDWeight;
-  const size_t epi = MODE == kStats ? kEpiWarps * 32 * kPitch * 4 + 2 * 4 * kMaxTileN * sizeof(Stat)
-                     : MODE == kCoef ? 2 * kMaxTileN * (sizeof(Position) + sizeof(int))
-                                     : 0;
-  const size_t smem = set_stages(W, kBMn, epi);
-  const long long units = (long long)W.nM * W.nN * W.splits;
-  const int pairs = pairs_of(units);
+template <Kind KIND>
+int launch(int dtype, Jobs &J, cudaStream_t s) {
+  constexpr size_t kEpi =
+      KIND == kStatsCols  ? kEpiWarps * 32 * kPitch * 4 + 2 * 4 * kMaxTileN * sizeof(Stat)
+      : KIND == kCoefCols ? 2 * kMaxTileN * (sizeof(Position) + sizeof(int))
+                          : 0;
+  // as many stages as fit beside the epilogue's shared memory, 1 KB of barriers and 1 KB of alignment
+  constexpr size_t kSmem = 232448 - 1024;
+  J.stage_bytes = 0;
+  for (int i = 0; i < (KIND == kGrads ? 2 : 1); ++i) {
+    Work &W = J.job[i].w;
+    J.units[i] = W.nM * W.nN * W.splits;
+    J.stage_bytes = std::max(J.stage_bytes, stage_of(W));
+    W.tx_bytes = stage_of(W) - (128 - W.tile_m) * 128;
+  }
+  if (KIND != kGrads) J.units[1] = 0;
+  J.stages = (int)std::min<size_t>(kMaxStages, (kSmem - 1024 - kEpi) / J.stage_bytes);
+  const int pairs = pairs_of((long long)J.units[0] + J.units[1]);
+  J.light_from = J.units[0] % pairs;
+  J.ahead = 0;
+  if (KIND == kGrads && J.light_from > 0) {
+    const Work &A = J.job[0].w, &B = J.job[1].w;
+    J.ahead = (int)((double)blocks_of(A.K) * A.tile_n / A.splits / (blocks_of(B.K) * B.tile_n));
+  }
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     if constexpr (std::is_same<T, float>::value) {
       return (int)BOUTE_ERR_INVALID_ARG;
     } else {
-      if (cudaFuncSetAttribute((const void *)hidden_kernel<MODE, T>,
-                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
-          cudaSuccess)
-        return last_launch_status();
-      return launch_cluster(hidden_kernel<MODE, T>, 2 * pairs, kThreads, 2, smem, s, a, b, W);
+      static std::atomic<unsigned long long> allowed{0};  // of the first 64 devices
+      int dev = 0;
+      if (cudaGetDevice(&dev) != cudaSuccess) return last_launch_status();
+      const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+      if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute((const void *)hidden_kernel<KIND, T>,
+                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)kSmem) != cudaSuccess)
+          return last_launch_status();
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+      }
+      const size_t smem = 1024 + (size_t)J.stages * J.stage_bytes + kEpi;
+      return launch_cluster(hidden_kernel<KIND, T>, 2 * pairs, kThreads, 2, smem, s, J);
     }
   });
 }
@@ -753,31 +922,42 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
   char *ws = (char *)workspace;
   if (int r = align_operand(p.h, T, D, ldh, ws + p.h_at, s)) return r;
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
-  CUtensorMap mw, mh;
-  if (int r = make_map(&mw, dtype, p.w.p, D, V, p.w.ld, p.tile_m)) return r;
-  Work W{};
-  W.M = V;
+  const int tile_m = p.rows ? 128 : p.tile_m;
+  Jobs J{};
+  Work &W = J.job[0].w;
   W.K = D;
-  W.tile_m = p.tile_m;
-  W.nM = (V + 2 * p.tile_m - 1) / (2 * p.tile_m);
+  W.tile_m = tile_m;
   W.splits = 1;
   W.head = (Header *)(ws + p.header);
   W.c2 = scale * kLog2e;
   W.part = (float *)(ws + p.part);
   W.picked = (float *)(ws + p.picked);
   W.Tp = p.Tp;
+  CUtensorMap *mh = p.rows ? &J.job[0].a : &J.job[0].b, *mw = p.rows ? &J.job[0].b : &J.job[0].a;
+  if (int r = make_map(mw, dtype, p.w.p, D, V, p.w.ld, p.rows ? kMaxTileN / 2 : tile_m)) return r;
   for (long long t0 = 0; t0 < T; t0 += kAtOnce) {
     const int n = (int)std::min(kAtOnce, T - t0);
-    W.N = n;
-    tile_columns(n, W.nN, W.tile_n);
     W.targets = targets + t0;
-    if (int r = make_map(&mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
-                         W.tile_n / 2))
+    int parts;
+    if (p.rows) {
+      W.M = n, W.N = V;
+      W.nM = (n + kPairM - 1) / kPairM;
+      W.nN = parts = (V + kMaxTileN - 1) / kMaxTileN;
+      W.tile_n = kMaxTileN;
+      W.rows_first = 1;
+    } else {
+      W.M = V, W.N = n;
+      W.nM = (V + 2 * tile_m - 1) / (2 * tile_m);
+      parts = 2 * W.nM;
+      tile_columns(n, W.nN, W.tile_n);
+    }
+    if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
+                         p.rows ? 128 : W.tile_n / 2))
       return r;
-    if (int r = launch<kStats>(dtype, mw, mh, W, s)) return r;
+    if (int r = p.rows ? launch<kStatsRows>(dtype, J, s) : launch<kStatsCols>(dtype, J, s)) return r;
     if (int r = launch_cluster(hidden_join_kernel, (n + 31) / 32, 32 * kJoinWarps, 1, 0, s, W.head,
-                               2 * pairs_of((long long)W.nM * W.nN), W.part, W.picked, W.targets, n, W.Tp, 2 * W.nM, V, scale, W.c2,
-                               logprob + t0, entropy + t0, lse + t0))
+                               2 * pairs_of(J.units[0]), W.part, W.picked, W.targets, n, W.Tp,
+                               parts, V, scale, W.c2, logprob + t0, entropy + t0, lse + t0))
       return r;
   }
   return BOUTE_OK;
@@ -806,65 +986,82 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
                ? BOUTE_OK
                : last_launch_status();
   char *ws = (char *)workspace;
-  if (cudaMemsetAsync(ws, 0, sizeof(Header), s) != cudaSuccess) return last_launch_status();
   if (int r = align_operand(p.h, T, D, ldh, ws + p.h_at, s)) return r;
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
   W.head = (Header *)(ws + p.header);
+  W.bounds = (int)std::min<long long>(kBounds, (T + 255) / 256);
   W.tile_m = 128;
+  W.splits = 1;
   Position *pos = (Position *)(ws + p.pos);
   int *tgt = (int *)(ws + p.tgt);
-  if (int r = launch_cluster(hidden_positions_kernel, (T + 255) / 256, 256, 1, 0, s, W.head,
-                             targets, T, V, scale, lse, entropy, g_logprob, g_entropy, pos, tgt))
+  if (int r = launch_cluster(hidden_positions_kernel, W.bounds, 256, 1, 0, s, W.head, targets, T, V,
+                             scale, lse, entropy, g_logprob, g_entropy, pos, tgt))
     return r;
   W.pos = pos;
   W.tgt = tgt;
   W.scale = scale;
-  W.Tp = p.Tp;
   W.coef = (uint16_t *)(ws + p.coef);
   W.sums = (float *)(ws + p.sums);
+  // a piece's coefficients: tokens x positions, or (positions in the tiles' rows) positions x tokens
+  W.Tp = p.rows ? p.piece : p.Tp;
   CUtensorMap h_k, h_mn;
-  if (int r = make_map(&h_k, dtype, p.h.p, D, T, p.h.ld, p.tile_t / 2)) return r;
+  if (int r = make_map(&h_k, dtype, p.h.p, D, T, p.h.ld, p.rows ? 128 : p.tile_t / 2)) return r;
   if (int r = make_map(&h_mn, dtype, p.h.p, D, T, p.h.ld, kBlockK)) return r;
   for (int v0 = 0; v0 < V; v0 += p.piece) {
-    const int n = std::min(p.piece, V - v0);
+    const int n = std::min(p.piece, V - v0), tiles_v = (n + kPairM - 1) / kPairM;
     const char *w = (const char *)p.w.p + (size_t)v0 * p.w.ld * 2;
-    CUtensorMap w_k, w_mn, c_k, c_mn;
-    if (int r = make_map(&w_k, dtype, w, D, n, p.w.ld, 128)) return r;
-    if (int r = make_map(&w_mn, dtype, w, D, n, p.w.ld, kBlockK)) return r;
-    if (int r = make_map(&c_k, dtype, W.coef, T, n, p.Tp, 128)) return r;
-    if (int r = make_map(&c_mn, dtype, W.coef, T, n, p.Tp, kBlockK)) return r;
-    const int tiles_v = (n + kPairM - 1) / kPairM;
-    Work C = W;  // the coefficients of the piece
-    C.M = n, C.N = (int)T, C.K = D;
-    C.nM = tiles_v, C.nN = p.tiles_t, C.tile_n = p.tile_t, C.splits = 1;
-    C.row0 = v0;
-    if (int r = launch<kCoef>(dtype, w_k, h_k, C, s)) return r;
-    Work G = W;  // dh: rows of its elements, columns of the positions
-    G.M = D, G.N = (int)T, G.K = n;
-    G.nM = (D + kPairM - 1) / kPairM, G.nN = p.tiles_t, G.tile_n = p.tile_t;
-    G.splits = p.splits;
-    G.add = v0 > 0;
-    if (int r = launch<kDHidden>(dtype, w_mn, c_mn, G, s)) return r;
-    Work O = W;  // dW of the piece
-    O.M = n, O.N = D, O.K = (int)T;
-    O.nM = tiles_v;
-    tile_columns(D, O.nN, O.tile_n);
-    O.splits = 1;
-    O.out = (char *)dweight + (size_t)v0 * lddw * 2;
-    O.ldo = lddw;
+    const long long inner = p.rows ? n : T, outer = p.rows ? T : n;  // of the coefficients
+    Jobs J{};
+    Job &c = J.job[0];
+    c.w = W;
+    c.w.K = D, c.w.row0 = v0;
+    CUtensorMap *mw = p.rows ? &c.b : &c.a;
+    if (int r = make_map(mw, dtype, w, D, n, p.w.ld, 128)) return r;
+    (p.rows ? c.a : c.b) = h_k;
+    if (p.rows) {
+      c.w.M = (int)T, c.w.N = n;
+      c.w.nM = (int)((T + kPairM - 1) / kPairM), c.w.nN = tiles_v, c.w.tile_n = kMaxTileN;
+      c.w.rows_first = 1;
+    } else {
+      c.w.M = n, c.w.N = (int)T;
+      c.w.nM = tiles_v, c.w.nN = p.tiles_t, c.w.tile_n = p.tile_t;
+    }
+    if (int r = p.rows ? launch<kCoefRows>(dtype, J, s) : launch<kCoefCols>(dtype, J, s)) return r;
+    Job &g = J.job[0], &o = J.job[1];
+    g.w = W;  // dh: rows of its elements, columns of the positions
+    g.w.M = D, g.w.N = (int)T, g.w.K = n;
+    g.w.nM = (D + kPairM - 1) / kPairM, g.w.nN = p.tiles_t, g.w.tile_n = p.tile_t;
+    g.w.splits = p.splits;
+    g.w.add = v0 > 0;
+    g.w.a_mn = 1, g.w.b_mn = !p.rows;
+    if (int r = make_map(&g.a, dtype, w, D, n, p.w.ld, kBlockK)) return r;
+    if (int r = make_map(&g.b, dtype, W.coef, inner, outer, W.Tp, p.rows ? p.tile_t / 2 : kBlockK))
+      return r;
+    o.w = W;  // dW of the piece
+    o.w.M = n, o.w.N = D, o.w.K = (int)T;
+    o.w.nM = tiles_v;
+    tile_columns(D, o.w.nN, o.w.tile_n);
+    o.w.a_mn = p.rows, o.w.b_mn = 1;
+    if (int r = make_map(&o.a, dtype, W.coef, inner, outer, W.Tp, p.rows ? kBlockK : 128)) return r;
+    o.b = h_mn;
+    o.w.out = (char *)dweight + (size_t)v0 * lddw * 2;
+    o.w.ldo = lddw;
     const uint64_t bits = (uintptr_t)dweight | (uint64_t)(lddw * 2);
-    O.width = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
-    if (int r = launch<kDWeight>(dtype, c_k, h_mn, O, s)) return r;
+    o.w.width = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
+    if (int r = launch<kGrads>(dtype, J, s)) return r;
   }
-  const long long n = T * D;
   return with_dtype(dtype, [&](auto t) {
     using E = decltype(t);
     if constexpr (std::is_same<E, float>::value) {
       return (int)BOUTE_ERR_INVALID_ARG;
     } else {
-      return launch_cluster(hidden_dh_kernel<E>, (n + 255) / 256, 256, 1, 0, s, W.head, W.sums,
-                            p.splits, T, D, (E *)dhidden, lddh);
+      const long long n = T * D;
+      if (D % 4 == 0)
+        return launch_cluster(hidden_dh_kernel<E, 4>, (n / 4 + 255) / 256, 256, 1, 0, s, W.head,
+                              W.bounds, W.sums, p.splits, T, D, (E *)dhidden, lddh);
+      return launch_cluster(hidden_dh_kernel<E, 1>, (n + 255) / 256, 256, 1, 0, s, W.head, W.bounds,
+                            W.sums, p.splits, T, D, (E *)dhidden, lddh);
     }
   });
 }

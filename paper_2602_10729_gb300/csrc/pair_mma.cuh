@@ -110,14 +110,13 @@ __device__ __forceinline__ void pair_tmem_dealloc(uint32_t taddr, uint32_t ncols
 // operand row, and 16 of them are 32 bytes on. Where the operand's rows are contiguous (MN-major),
 // a row holds one reduction column of 64 operand rows, blocks of 64 operand rows follow one another
 // kBlockK rows apart, and 16 reduction columns are 2048 bytes on.
-template <bool MN>
-__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn) {
   uint64_t d = sdesc_sw128(saddr);
-  if (MN) d = (d & ~((uint64_t)0x3fff << 16)) | (uint64_t)((kBlockK * 128) >> 4) << 16;
+  if (mn) d = (d & ~((uint64_t)0x3fff << 16)) | (uint64_t)((kBlockK * 128) >> 4) << 16;
   return d;
 }
-template <bool MN>
-constexpr int kDescStep = MN ? 2048 >> 4 : 32 >> 4;  // of 16 reduction columns
+// Of 16 reduction columns.
+__device__ __forceinline__ int desc_step(bool mn) { return mn ? 2048 >> 4 : 32 >> 4; }
 
 // kind::f16, fp32 accumulators, 256 x n; A and B of one type, each MN-major or not.
 __host__ __device__ constexpr uint32_t pair_idesc(bool bf16, bool a_mn, bool b_mn, int n) {
