@@ -40,6 +40,20 @@ __device__ __forceinline__ uint32_t pack2(__nv_bfloat16, float a, float b) {
   return r;
 }
 
+// The 16 bytes from byte sh (even, below 16) of the words a and b on.
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int sh) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (sh & 8)
+#pragma unroll
+    for (int q = 0; q < 6; ++q) w[q] = w[q + 2];
+  if (sh & 4)
+#pragma unroll
+    for (int q = 0; q < 5; ++q) w[q] = w[q + 1];
+  const int bits = 8 * (sh & 3);
+  return {__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+          __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits)};
+}
+
 // go(T{}) for the element type of a boute_dtype.
 template <class Go>
 inline int with_dtype(int dtype, Go go) {

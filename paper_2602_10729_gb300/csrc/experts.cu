@@ -389,17 +389,7 @@ struct Chunks {
   }
   __device__ __forceinline__ uint4 take(int u) const {
     if (ALIGNED) return a[u];
-    const uint4 x = a[u], y = b[ALIGNED ? 0 : u];
-    uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-    if (sh & 8)
-#pragma unroll
-      for (int q = 0; q < 6; ++q) w[q] = w[q + 2];
-    if (sh & 4)
-#pragma unroll
-      for (int q = 0; q < 5; ++q) w[q] = w[q + 1];
-    const int bits = 8 * (sh & 3);
-    return {__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
-            __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits)};
+    return shifted(a[u], b[ALIGNED ? 0 : u], sh);
   }
 };
 

@@ -88,10 +88,11 @@ struct Work {
   char *out;                // dW: M x N, pitch ldo
   long long ldo;
   int width;                // bytes that the rows' alignment allows in a store
+  int boxes;                // whether `out` has a map
 };
 // A launch's products: one set of tiles, or dh's and behind them dW's.
 struct Job {
-  CUtensorMap a, b;
+  CUtensorMap a, b, out;  // out: where boxes are stored
   Work w;
 };
 struct Jobs {
@@ -142,6 +143,17 @@ __device__ __forceinline__ Unit unit_of(const Jobs &J, int pair, int pairs, int 
   }
   return t;
 }
+
+// Shared memory behind the ring: what a kind needs, and from kBoxes on a box for each warp that
+// stores them.
+constexpr int kBoxBytes = 4096;
+template <Kind KIND>
+constexpr int kBoxes = KIND == kStatsCols ? kEpiWarps * 32 * kPitch * 4 + 2 * 4 * kMaxTileN * 12
+                       : KIND == kCoefCols
+                           ? 2 * kMaxTileN * (int)(sizeof(Position) + sizeof(int))
+                           : 0;
+template <Kind KIND>
+constexpr int kEpi = kBoxes<KIND> + (KIND == kStatsCols || KIND == kStatsRows ? 0 : kEpiWarps * kBoxBytes);
 
 // ---- the sums of a tile ----------------------------------------------------------------
 struct Stat {
@@ -204,6 +216,17 @@ __device__ __forceinline__ void store_row_of(uint16_t *to, const float (&x)[32])
   for (int i = 0; i < 16; ++i) r[i] = pack2(T{}, x[2 * i], x[2 * i + 1]);
   store32(to, r);
   store32(to + 16, r + 8);
+}
+
+// The same to a half (0 or 1) of a row of a box, the lane's.
+template <class T>
+__device__ __forceinline__ void box_row(uint8_t *box, int half, const float (&x)[32]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    *(uint4 *)(box + lane * 128 + (((half * 4 + q) ^ (lane & 7)) << 4)) = {
+        pack2(T{}, x[8 * q], x[8 * q + 1]), pack2(T{}, x[8 * q + 2], x[8 * q + 3]),
+        pack2(T{}, x[8 * q + 4], x[8 * q + 5]), pack2(T{}, x[8 * q + 6], x[8 * q + 7])};
 }
 
 // ---- the kernel --------------------------------------------------------------------------
@@ -381,11 +404,30 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
       if (!ok) break;
       tc_fence_after();
       Stat run = {-INFINITY, 0.f, 0.f};
+      // 64 columns of 32 rows go out as a box (all of their row's bytes at once: 268 MB of dW took 77
+      // us by each thread's 32 bytes of its row), a last half by the threads
+      uint8_t *box = epi + kBoxes<KIND> + (warp - 2) * kBoxBytes;
+      auto send = [&](int c, const float (&x)[32]) {
+        const CUtensorMap *out = &J.job[KIND == kGrads ? t.job : 0].out;
+        if (c % 2 == 0) {
+          if (lane == 0) bulk_wait_read();
+          __syncwarp();
+        }
+        box_row<T>(box, c & 1, x);
+        if (c % 2 == 0) return;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          store_box(out, box, col + (c - 1) * 32, row);
+          bulk_commit();
+        }
+      };
       for (int c = 0; c < chunks; ++c) {
         float x[32];
         tmem_ld32(from + c * 32, x);
         if (c == chunks - 1) release();
         const int d0 = col + c * 32;
+        const bool boxed = c < (chunks & ~1);
         if constexpr (KIND == kStatsCols) {
           float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
           Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
@@ -430,7 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
 #pragma unroll
             for (int q = 0; q < 32; ++q)
               if ((here >> q & 1u) && tgt[c * 32 + q] == row + lane) x[q] += pos[c * 32 + q].g;
-          if (row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp))
+          if (boxed) send(c, x);
+          else if (row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp))
             store_row_of<T>(W.coef + (row + lane) * W.Tp + d0, x);
         } else if constexpr (KIND == kCoefRows) {
           const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.lse);
@@ -448,8 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
 #pragma unroll
             for (int q = 0; q < 32; ++q)
               if (target == d0 + q) x[q] += own.g;
-          if (row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp))
-            store_row_of<T>(W.coef + (row + lane) * W.Tp + d0, x);
+          send(c, x);
         } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
           if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
             const int n = min(32, W.N - d0);
@@ -470,23 +512,45 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
             for (int q = 0; q < 32; ++q)
               if (q < n) to[(long long)q * W.M] = x[q];
           }
-        } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {  // dW
-          T *to = (T *)W.out + (row + lane) * W.ldo + d0;
+        } else {  // dW
 #pragma unroll
           for (int q = 0; q < 32; ++q) x[q] *= mul;
-          if (d0 + 32 <= W.N && W.width >= 32) {
-            store_row_of<T>((uint16_t *)to, x);
-          } else if (d0 + 32 <= W.N && W.width >= 16) {
+          T *to = (T *)W.out + (row + lane) * W.ldo + d0;
+          if (boxed && W.boxes) {
+            send(c, x);
+          } else if (boxed) {  // rows at any address: by way of the box, a row's neighbours together
+            if (c % 2 == 0) __syncwarp();
+            box_row<T>(box, c & 1, x);
+            if (c % 2 == 1) {
+              __syncwarp();
+              const int rows = min(32, W.M - row);
+              for (int r = 0; r < rows; ++r) {
+                T *line = (T *)W.out + (row + r) * W.ldo + d0 - 32;
 #pragma unroll
-            for (int q = 0; q < 32; q += 8)
-              *(uint4 *)(to + q) = {pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
-                                    pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
-          } else {
+                for (int h = 0; h < 2; ++h) {
+                  const int e = h * 32 + lane;
+                  const T v = *(const T *)(box + r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2);
+                  if (d0 - 32 + e < W.N && BOUTE_INB(row + r, W.M)) line[e] = v;
+                }
+              }
+            }
+          } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {
+            if (d0 + 32 <= W.N && W.width >= 32) {
+              store_row_of<T>((uint16_t *)to, x);
+            } else if (d0 + 32 <= W.N && W.width >= 16) {
 #pragma unroll
-            for (int q = 0; q < 32; ++q)
-              if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
+              for (int q = 0; q < 32; q += 8)
+                *(uint4 *)(to + q) = {
+                    pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
+                    pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
+            } else {
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
+            }
           }
         }
+        __syncwarp();
       }
       if constexpr (kStats) {
         const long long parts = KIND == kStatsCols ? 2ll * W.nM : W.nN, all = parts * W.Tp;
@@ -511,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
       }
     }
   }
+  if (warp >= 2 && lane == 0) bulk_wait();
   __syncwarp();
   tc_fence_before();
   __syncthreads();
@@ -659,10 +724,17 @@ __global__ void __launch_bounds__(256)
   if (i >= rows * per) return;
   const long long r = i / per;
   const int d0 = (int)(i % per) * 8;
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  const char *from = (const char *)(x + r * ld + d0);
+  const int sh = (int)((uintptr_t)from & 15), left = 2 * (D - d0);  // bytes of the row from here on
+  uint4 a = {0u, 0u, 0u, 0u}, b = a;
+  // (words that hold a byte of the row)
+  if (left > 0 && BOUTE_INB(d0, ld)) a = *(const uint4 *)(from - sh);
+  if (sh != 0 && 16 - sh < left) b = *(const uint4 *)(from - sh + 16);
+  a = shifted(a, b, sh);
+  uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (d0 + e < D && BOUTE_INB(d0 + e, ld)) w[e / 2] |= (uint32_t)x[r * ld + d0 + e] << 16 * (e & 1);
+  for (int e = 0; e < 4; ++e)
+    w[e] = left >= 4 * e + 4 ? w[e] : left >= 4 * e + 2 ? w[e] & 0xffffu : 0u;
   *(uint4 *)(out + r * ldo + d0) = {w[0], w[1], w[2], w[3]};
 }
 
@@ -793,10 +865,7 @@ int stage_of(const Work &W) {
 
 template <Kind KIND>
 int launch(int dtype, Jobs &J, cudaStream_t s) {
-  constexpr size_t kEpi =
-      KIND == kStatsCols  ? kEpiWarps * 32 * kPitch * 4 + 2 * 4 * kMaxTileN * sizeof(Stat)
-      : KIND == kCoefCols ? 2 * kMaxTileN * (sizeof(Position) + sizeof(int))
-                          : 0;
+  static_assert(kBoxes<KIND> % 1024 == 0 && sizeof(Stat) == 12, "");
   // as many stages as fit beside the epilogue's shared memory, 1 KB of barriers and 1 KB of alignment
   constexpr size_t kSmem = 232448 - 1024;
   J.stage_bytes = 0;
@@ -807,7 +876,7 @@ int launch(int dtype, Jobs &J, cudaStream_t s) {
     W.tx_bytes = stage_of(W) - (128 - W.tile_m) * 128;
   }
   if (KIND != kGrads) J.units[1] = 0;
-  J.stages = (int)std::min<size_t>(kMaxStages, (kSmem - 1024 - kEpi) / J.stage_bytes);
+  J.stages = (int)std::min<size_t>(kMaxStages, (kSmem - 1024 - kEpi<KIND>) / J.stage_bytes);
   const int pairs = pairs_of((long long)J.units[0] + J.units[1]);
   J.light_from = J.units[0] % pairs;
   J.ahead = 0;
@@ -831,7 +900,7 @@ int launch(int dtype, Jobs &J, cudaStream_t s) {
           return last_launch_status();
         allowed.fetch_or(bit, std::memory_order_relaxed);
       }
-      const size_t smem = 1024 + (size_t)J.stages * J.stage_bytes + kEpi;
+      const size_t smem = 1024 + (size_t)J.stages * J.stage_bytes + kEpi<KIND>;
       return launch_cluster(hidden_kernel<KIND, T>, 2 * pairs, kThreads, 2, smem, s, J);
     }
   });
@@ -1027,6 +1096,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
       c.w.M = n, c.w.N = (int)T;
       c.w.nM = tiles_v, c.w.nN = p.tiles_t, c.w.tile_n = p.tile_t;
     }
+    if (int r = make_map(&c.out, dtype, W.coef, inner, outer, W.Tp, 32)) return r;
     if (int r = p.rows ? launch<kCoefRows>(dtype, J, s) : launch<kCoefCols>(dtype, J, s)) return r;
     Job &g = J.job[0], &o = J.job[1];
     g.w = W;  // dh: rows of its elements, columns of the positions
@@ -1049,6 +1119,8 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     o.w.ldo = lddw;
     const uint64_t bits = (uintptr_t)dweight | (uint64_t)(lddw * 2);
     o.w.width = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
+    o.w.boxes = bits % 16 == 0;
+    if (int r = o.w.boxes ? make_map(&o.out, dtype, o.w.out, D, n, lddw, 32) : 0) return r;
     if (int r = launch<kGrads>(dtype, J, s)) return r;
   }
   return with_dtype(dtype, [&](auto t) {

@@ -160,6 +160,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// 32 rows of 64 16-bit elements from shared memory (4 KB on a 1 KB boundary, swizzled) to column x (a
+// multiple of 8) and row y on; what lies outside is not written.
+__device__ __forceinline__ void store_box(const CUtensorMap *map, const void *src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                   map),
+               "r"(x), "r"(y), "r"(smem_u32(src))
+               : "memory");
+}
+
 // 32 bytes to a 32-byte boundary.
 __device__ __forceinline__ void store32(void *p, const uint32_t *r) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]),
