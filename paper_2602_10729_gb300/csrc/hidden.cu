@@ -586,24 +586,35 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
   if (warp == 1) pair_tmem_dealloc(tmem, 512);
 }
 
-// The pieces' sums of 32 positions a block: lanes over the positions, warps over the pieces.
-constexpr int kJoinWarps = 32;
+// The pieces' sums of kJoinAt positions a block (a sector of each piece's): a warp's lanes are four
+// pieces of each, and its warps 32 times those.
+constexpr int kJoinWarps = 32, kJoinAt = 8;
+__device__ __forceinline__ Stat join_lanes(Stat a, int from, float c2) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (o >= from)
+      join(a, {__shfl_xor_sync(kAll, a.m, o), __shfl_xor_sync(kAll, a.s, o),
+               __shfl_xor_sync(kAll, a.u, o)}, c2);
+  return a;
+}
 __global__ void __launch_bounds__(32 * kJoinWarps)
     hidden_join_kernel(const Header *head, int blocks, const float *part, const float *picked,
                        const long long *targets, long long T, long long Tp, int parts, int V,
                        float scale, float c2, float *logprob, float *entropy, float *lse) {
-  __shared__ Stat red[kJoinWarps][32];
+  __shared__ Stat red[kJoinAt][kJoinWarps + 1];
   pdl_wait();
   pdl_trigger();
+  constexpr int kPieces = 32 / kJoinAt, kAtOnce = 4;  // of a warp; on their way to a thread
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const long long t = blockIdx.x * 32ll + lane, all = parts * Tp;
+  const long long t0 = (long long)blockIdx.x * kJoinAt, all = parts * Tp;
+  long long t = t0 + lane % kJoinAt;
   Stat a = {-INFINITY, 0.f, 0.f};
-  constexpr int kAtOnce = 8;  // parts on their way to a thread
-  for (int p0 = warp; p0 < parts; p0 += kAtOnce * kJoinWarps) {
+  for (int p0 = warp * kPieces + lane / kJoinAt; p0 < parts;
+       p0 += kAtOnce * kJoinWarps * kPieces) {
     Stat b[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const int p = p0 + i * kJoinWarps;
+      const int p = p0 + i * kJoinWarps * kPieces;
       const long long at = p * Tp + t;
       b[i] = {-INFINITY, 0.f, 0.f};
       if (p < parts && t < T && BOUTE_INB(at, all))
@@ -612,18 +623,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) join(a, b[i], c2);
   }
+  a = join_lanes(a, kJoinAt, c2);
+  if (lane < kJoinAt) red[lane][warp] = a;
   const bool late = __syncthreads_or(threadIdx.x < blocks && head->status[threadIdx.x] != 0);
-  red[warp][lane] = a;
-  __syncthreads();
-  for (int n = kJoinWarps / 2; n > 0; n /= 2) {
-    if (warp < n) {
-      a = red[warp][lane];
-      join(a, red[warp + n][lane], c2);
-      red[warp][lane] = a;
-    }
-    __syncthreads();
-  }
-  if (warp != 0 || t >= T || !BOUTE_INB(t, T)) return;
+  if (warp >= kJoinAt) return;
+  a = join_lanes(red[warp][lane], 1, c2);  // a warp's position
+  t = t0 + warp;
+  if (lane != 0 || t >= T || !BOUTE_INB(t, T)) return;
   const long long target = targets[t];
   const float ls = logf(a.s);
   float l = scale * a.m + ls, H = ls - kLn2 * (a.u / a.s), lp;
@@ -695,18 +701,26 @@ __global__ void __launch_bounds__(256)
   float v[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    if (!BOUTE_INB(s * n + i, splits * n)) break;
-    float x[E];
-    if constexpr (E == 4) {
-      const float4 q = *(const float4 *)(sums + s * n + i);
-      x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
-    } else {
-      x[0] = sums[s * n + i];
+  constexpr int kAtOnce = E == 1 ? 16 : 4;  // splits on their way to a thread
+  for (int s0 = 0; s0 < splits; s0 += kAtOnce) {
+    float x[kAtOnce][E];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const long long at = (s0 + j) * n + i;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[j][e] = 0.f;
+      if (s0 + j >= splits || !BOUTE_INB(at, splits * n)) continue;
+      if constexpr (E == 4) {
+        const float4 q = *(const float4 *)(sums + at);
+        x[j][0] = q.x, x[j][1] = q.y, x[j][2] = q.z, x[j][3] = q.w;
+      } else {
+        x[j][0] = sums[at];
+      }
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += x[e];
+    for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += x[j][e];
   }
   const bool late = head->status[0] != 0;
 #pragma unroll
@@ -1024,7 +1038,7 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
                          p.rows ? 128 : W.tile_n / 2))
       return r;
     if (int r = p.rows ? launch<kStatsRows>(dtype, J, s) : launch<kStatsCols>(dtype, J, s)) return r;
-    if (int r = launch_cluster(hidden_join_kernel, (n + 31) / 32, 32 * kJoinWarps, 1, 0, s, W.head,
+    if (int r = launch_cluster(hidden_join_kernel, (n + kJoinAt - 1) / kJoinAt, 32 * kJoinWarps, 1, 0, s, W.head,
                                2 * pairs_of(J.units[0]), W.part, W.picked, W.targets, n, W.Tp,
                                parts, V, scale, W.c2, logprob + t0, entropy + t0, lse + t0))
       return r;
@@ -1129,7 +1143,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
       return (int)BOUTE_ERR_INVALID_ARG;
     } else {
       const long long n = T * D;
-      if (D % 4 == 0)
+      if (D % 4 == 0 && n >= 1 << 18)  // (few elements take a thread each, to be read by more SMs)
         return launch_cluster(hidden_dh_kernel<E, 4>, (n / 4 + 255) / 256, 256, 1, 0, s, W.head,
                               W.bounds, W.sums, p.splits, T, D, (E *)dhidden, lddh);
       return launch_cluster(hidden_dh_kernel<E, 1>, (n + 255) / 256, 256, 1, 0, s, W.head, W.bounds,
