@@ -13,6 +13,7 @@
 // products, and two groups of four warps taking the accumulators' tiles in turn, so that a tile's
 // sums or stores go on behind the next one's products.
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -26,6 +27,11 @@ namespace {
 
 constexpr int kThreads = 320, kEpiWarps = 8, kGroup = 128;  // two warps of roles, two groups
 constexpr int kMaxStages = 12;
+// Blocks of the reduction that a logit of the statistics takes on the tensor cores at once. Their sums
+// cut off what fp32 does not hold, step by step; the parts are added up, rounded, in registers.
+// (4096 positions of 32768 tokens, 4096 elements, entropies in one part 2.5e-6 off, in parts of 16
+// blocks 5.4e-7, of 8 2.4e-7, for 1, 1 and 7 % of the time.)
+constexpr int kPart = 16;
 constexpr int kABytes = 128 * kBlockK * 2;  // a block's half of a stage's rows
 constexpr int kPitch = 36;  // floats of a row of a warp's 32 x 32 transposition
 constexpr float kLn2 = 0.6931471805599453f;
@@ -230,9 +236,13 @@ __device__ __forceinline__ void box_row(uint8_t *box, int half, const float (&x)
 }
 
 // ---- the kernel --------------------------------------------------------------------------
-template <Kind KIND, class T>
+// MINE > 0: statistics over a reduction of several parts, whose tiles both groups of warps take
+// together, up to MINE chunks of 32 columns each.
+template <Kind KIND, class T, int MINE>
 __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_constant__ Jobs J) {
   constexpr bool kStats = KIND == kStatsCols || KIND == kStatsRows;
+  constexpr bool kParted = MINE > 0;
+  static_assert(kStats || !kParted, "");
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2],
       drain;
@@ -251,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], kEpiWarps);  // a group's four warps of both blocks
+      mbar_init(&acc_empty[i], kParted ? 2 * kEpiWarps : kEpiWarps);  // who reads it, of both blocks
     }
     mbar_init(&drain, 1);
     abort_flag = 0;
@@ -310,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
       constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
       const bool issuer = elect_one();
       int s = 0;
-      uint32_t phase = 0;
+      uint32_t phase = 0, seq = 0;  // seq: accumulators so far
       bool ok = true;
       for (int i = 0; ok; ++i) {
         const Unit t = unit_of<KIND>(J, pair, pairs, i);
@@ -321,29 +331,38 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
         const uint64_t ad0 = operand_desc(smem_u32(ring), a_mn);
         const uint64_t bd0 = operand_desc(smem_u32(ring) + kABytes, b_mn);
         const int a_step = desc_step(a_mn), b_step = desc_step(b_mn);
-        const uint32_t acc = i & 1u, to = tmem + acc * kMaxTileN;
-        ok = __all_sync(kAll, pair_wait<true>(&acc_empty[acc], ((i >> 1) & 1u) ^ 1u, abort));
-        if (!ok) break;
-        tc_fence_after();
-        for (int kb = t.k0; kb < t.k1; ++kb) {
-          ok = __all_sync(kAll, pair_wait(&full[s], phase, abort));
+        const int part = kParted ? kPart : INT_MAX;
+        for (int k0 = t.k0; ok && (k0 < t.k1 || k0 == t.k0); ++seq) {
+          const int k1 = part < t.k1 - k0 ? k0 + part : t.k1;
+          const uint32_t acc = seq & 1u, to = tmem + acc * kMaxTileN;
+          ok = __all_sync(kAll, pair_wait<true>(&acc_empty[acc], ((seq >> 1) & 1u) ^ 1u, abort));
           if (!ok) break;
           tc_fence_after();
-          if (issuer) {
-            const uint64_t at = (uint64_t)((uint32_t)(s * J.stage_bytes) >> 4);
-            const uint64_t ad = ad0 + at, bd = bd0 + at;
-            const int left = W.K - kb * kBlockK;  // (of a short last block, the steps with data)
+          for (int kb = k0; kb < k1; ++kb) {
+            ok = __all_sync(kAll, pair_wait(&full[s], phase, abort));
+            if (!ok) break;
+            tc_fence_after();
+            if (issuer) {
+              const uint64_t at = (uint64_t)((uint32_t)(s * J.stage_bytes) >> 4);
+              const uint64_t ad = ad0 + at, bd = bd0 + at;
+              const int left = W.K - kb * kBlockK;  // (of a short last block, the steps with data)
 #pragma unroll
-            for (int k = 0; k < kBlockK / 16; ++k)
-              if (k * 16 < left)
-                pair_mma(to, ad + k * a_step, bd + k * b_step, idesc, kb > t.k0 || k > 0);
-            pair_commit(&empty[s]);
+              for (int k = 0; k < kBlockK / 16; ++k)
+                if (k * 16 < left)
+                  pair_mma(to, ad + k * a_step, bd + k * b_step, idesc, kb > k0 || k > 0);
+              pair_commit(&empty[s]);
+            }
+            __syncwarp();
+            if (++s == J.stages) s = 0, phase ^= 1u;
           }
+          if (ok && issuer) pair_commit(&acc_full[acc]);
           __syncwarp();
-          if (++s == J.stages) s = 0, phase ^= 1u;
+          if (k1 == t.k0) {  // (an empty part of dh's)
+            ++seq;
+            break;
+          }
+          k0 = k1;
         }
-        if (ok && issuer) pair_commit(&acc_full[acc]);
-        __syncwarp();
       }
       if (!ok && issuer) {  // no product in flight when the tensor memory goes
         pair_commit(&drain);
@@ -354,12 +373,113 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
     // ------------------------------------------------------------ accumulators' tiles
     const int group = (warp - 2) / 4, quarter = warp & 3;
     const int gtid = tid - 64 - group * kGroup;
-    const uint32_t from = tmem + ((uint32_t)quarter << 21) + group * kMaxTileN;
-    auto release = [&]() {  // the group's accumulator, to the issuing warp
+    const uint32_t from = tmem + ((uint32_t)quarter << 21);
+    auto release = [&](int acc) {  // an accumulator, to the issuing warp
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) arrive_peer(&acc_empty[group], 0);
+      if (lane == 0) arrive_peer(&acc_empty[acc], 0);
     };
+    if constexpr (kParted) {
+      // Both groups take each tile, the first half of its columns one and the rest the other.
+      const Work &W = J.job[0].w;
+      const int half = (W.tile_n / 32 + 1) / 2, chunk0 = group * half;
+      const int chunks = group == 0 ? half : W.tile_n / 32 - half;
+      uint32_t seq = 0;
+      for (int i = 0;; ++i) {
+        const Unit t = unit_of<KIND>(J, pair, pairs, i);
+        if (t.job < 0) break;
+        const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32;
+        const int col = t.n * W.tile_n + chunk0 * 32;
+        // the token wanted of a position
+        auto wanted_at = [&](int at, int end) {
+          return at < end && BOUTE_INB(at, end)
+                     ? (int)min(max(W.targets[at], -1ll), (long long)INT_MAX)
+                     : -1;
+        };
+        float x[kParted ? MINE : 1][32];
+        bool ok = true;
+        for (int k0 = t.k0; k0 < t.k1; k0 += kPart, ++seq) {
+          const int acc = seq & 1u;
+          ok = __all_sync(kAll, pair_wait(&acc_full[acc], (seq >> 1) & 1u, abort));
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < MINE; ++c) {
+            if (c >= chunks) continue;
+#pragma unroll
+            for (int h = 0; h < 32; h += 16) {
+              float v[16];
+              tmem_ld16(from + acc * kMaxTileN + (chunk0 + c) * 32 + h, v);
+              if (k0 == t.k0)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) x[c][h + q] = 0.f;
+#pragma unroll
+              for (int q = 0; q < 16; ++q) x[c][h + q] += v[q];
+            }
+          }
+          release(acc);
+        }
+        // (where the group meets at a barrier, it goes on or gives up as one)
+        if (KIND == kStatsCols) ok = group_all(1 + group, kGroup, ok);
+        if (!ok) break;
+        const long long parts = KIND == kStatsCols ? 2ll * W.nM : 2ll * W.nN, all = parts * W.Tp;
+        auto write = [&](Stat a, long long at) {
+          if (!BOUTE_INB(at, all)) return;
+          W.part[at] = a.m;
+          W.part[all + at] = a.s;
+          W.part[2 * all + at] = a.u;
+        };
+        if constexpr (KIND == kStatsCols) {
+          float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
+          Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + chunk0 * 32;
+          // (rows of the accumulator beyond the block's hold what was in its shared memory)
+          const int rows = min(W.tile_m - quarter * 32, W.M - row);
+#pragma unroll
+          for (int c = 0; c < MINE; ++c) {
+            if (c >= chunks) continue;
+            if (lane >= rows)
+#pragma unroll
+              for (int q = 0; q < 32; ++q) x[c][q] = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < 32; q += 4)
+              *(float4 *)(buf + lane * kPitch + q) = {x[c][q], x[c][q + 1], x[c][q + 2],
+                                                      x[c][q + 3]};
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[c][q] = buf[q * kPitch + lane];
+            const int wanted = wanted_at(col + c * 32 + lane, W.N);
+            if (wanted >= row && wanted < row + min(rows, 32))
+              W.picked[col + c * 32 + lane] = buf[(wanted - row) * kPitch + lane];
+            red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x[c], W.c2);
+            __syncwarp();
+          }
+          named_barrier_sync(1 + group, kGroup);
+          if (gtid < chunks * 32 && col + gtid < W.N) {
+            Stat a = red[gtid];
+            for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + gtid], W.c2);
+            write(a, (2ll * t.m + rank) * W.Tp + col + gtid);
+          }
+        } else {
+          Stat run = {-INFINITY, 0.f, 0.f};
+          const int wanted = wanted_at(row + lane, W.M);
+#pragma unroll
+          for (int c = 0; c < MINE; ++c) {
+            if (c >= chunks) continue;
+            const int d0 = col + c * 32;
+            if (d0 + 32 > W.N)
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (d0 + q >= W.N) x[c][q] = -INFINITY;
+            if (__any_sync(kAll, wanted >= d0 && wanted < d0 + 32))
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (wanted == d0 + q && d0 + q < W.N) W.picked[row + lane] = x[c][q];
+            join(run, stat_of(x[c], W.c2), W.c2);
+          }
+          if (row + lane < W.M) write(run, (2ll * t.n + group) * W.Tp + row + lane);
+        }
+      }
+    } else {
     float mul = 1.f;
     if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
     for (int i = group;; i += 2) {
@@ -424,8 +544,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
       };
       for (int c = 0; c < chunks; ++c) {
         float x[32];
-        tmem_ld32(from + c * 32, x);
-        if (c == chunks - 1) release();
+        tmem_ld32(from + group * kMaxTileN + c * 32, x);
+        if (c == chunks - 1) release(group);
         const int d0 = col + c * 32;
         const bool boxed = c < (chunks & ~1);
         if constexpr (KIND == kStatsCols) {
@@ -573,6 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
           write(run, t.n * W.Tp + row + lane);
         }
       }
+    }
     }
   }
   if (warp >= 2 && lane == 0) bulk_wait();
@@ -845,7 +966,7 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   p.header = take(sizeof(Header));
   if (!grad) {
     p.tile_m = p.tiles_t == 1 ? even_rows(V) : 128;
-    const long long parts = p.rows ? (V + kMaxTileN - 1) / kMaxTileN
+    const long long parts = p.rows ? 2ll * ((V + kMaxTileN - 1) / kMaxTileN)
                                    : 2ll * ((V + 2 * p.tile_m - 1) / (2 * p.tile_m));
     p.part = take(3ull * parts * p.Tp * sizeof(float));
     p.picked = take(p.Tp * sizeof(float));
@@ -877,7 +998,7 @@ int stage_of(const Work &W) {
   return kABytes + (W.b_mn ? (half + 63) / 64 * 64 : half) * 128;
 }
 
-template <Kind KIND>
+template <Kind KIND, int MINE = 0>
 int launch(int dtype, Jobs &J, cudaStream_t s) {
   static_assert(kBoxes<KIND> % 1024 == 0 && sizeof(Stat) == 12, "");
   // as many stages as fit beside the epilogue's shared memory, 1 KB of barriers and 1 KB of alignment
@@ -908,14 +1029,14 @@ int launch(int dtype, Jobs &J, cudaStream_t s) {
       if (cudaGetDevice(&dev) != cudaSuccess) return last_launch_status();
       const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
       if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute((const void *)hidden_kernel<KIND, T>,
+        if (cudaFuncSetAttribute((const void *)hidden_kernel<KIND, T, MINE>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)kSmem) != cudaSuccess)
           return last_launch_status();
         allowed.fetch_or(bit, std::memory_order_relaxed);
       }
       const size_t smem = 1024 + (size_t)J.stages * J.stage_bytes + kEpi<KIND>;
-      return launch_cluster(hidden_kernel<KIND, T>, 2 * pairs, kThreads, 2, smem, s, J);
+      return launch_cluster(hidden_kernel<KIND, T, MINE>, 2 * pairs, kThreads, 2, smem, s, J);
     }
   });
 }
@@ -1037,7 +1158,14 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
     if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
                          p.rows ? 128 : W.tile_n / 2))
       return r;
-    if (int r = p.rows ? launch<kStatsRows>(dtype, J, s) : launch<kStatsCols>(dtype, J, s)) return r;
+    const bool parted = blocks_of(D) > kPart;
+    if (parted && p.rows) parts *= 2;  // (of both groups' columns)
+    int (*start)(int, Jobs &, cudaStream_t) =
+        p.rows ? (parted ? launch<kStatsRows, 4> : launch<kStatsRows>)
+                       : !parted         ? launch<kStatsCols>
+                       : W.tile_n <= 64 ? launch<kStatsCols, 1>
+                                        : launch<kStatsCols, 4>;
+    if (int r = start(dtype, J, s)) return r;
     if (int r = launch_cluster(hidden_join_kernel, (n + kJoinAt - 1) / kJoinAt, 32 * kJoinWarps, 1, 0, s, W.head,
                                2 * pairs_of(J.units[0]), W.part, W.picked, W.targets, n, W.Tp,
                                parts, V, scale, W.c2, logprob + t0, entropy + t0, lse + t0))
