@@ -74,9 +74,11 @@ __device__ __forceinline__ bool group_all(int id, int count, bool ok) {
       : "memory");
   return r != 0;
 }
-// One arrival at a barrier of the pair's block r.
+// One arrival at a barrier of the pair's block r, which hands over tensor memory (that its loads are
+// done is for tc_fence_before): no memory of this thread's, whose stores it would wait for at the
+// scope of the cluster.
 __device__ __forceinline__ void arrive_peer(uint64_t *bar, int r) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer(bar, r))
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer(bar, r))
                : "memory");
 }
 
