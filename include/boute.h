@@ -755,10 +755,11 @@ int boute_hidden_logprobs(const void *hidden, int dtype, long long T, int D, lon
  * forward call's lse and entropy and the outputs' gradients (g_entropy, and entropy with it, may be
  * NULL),
  *   dhidden = dlogits weight (T rows of D, pitch lddh), dweight = dlogits^T hidden (V rows, lddw),
- * rounded once to the type from fp32 sums. The products take each dlogits_tj rounded to the type
- * (fp16: times a power of two, by which the largest coefficient that the gradients allow comes near
- * 2^14; what is less than 2^-28 of it loses bits). At most 256 MB of them are held at a time
- * (512 bytes a position, if that is more). dhidden and dweight overlap no input. */
+ * rounded once to the type from fp32 sums. The products take each dlogits_tj rounded to the type, of
+ * up to 32 positions as the sum of two such numbers (times a power of two, by which the largest
+ * coefficient that the gradients allow comes near 2^14; what is less than 2^-28 of it loses bits in
+ * fp16). At most 256 MB of them are held at a time (512 bytes a position, if that is more). dhidden
+ * and dweight overlap no input. */
 int boute_hidden_logprobs_grad(const void *hidden, int dtype, long long T, int D, long long ldh,
                                const void *weight, int V, long long ldw, const long long *targets,
                                float scale, const float *lse, const float *entropy,

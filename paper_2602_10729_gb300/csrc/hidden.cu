@@ -87,6 +87,7 @@ struct Work {
   const int *tgt;           // targets, -1 for none
   float scale;
   uint16_t *coef;           // a piece's: tokens x positions, or positions x tokens
+  int low;                  // columns on, what rounding left of each follows (0: none kept)
   int row0;                 // of the piece in the vocabulary
   // gradients
   float *sums;              // dh: splits x N x M, in fp32
@@ -301,7 +302,11 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
             load_box(a, &job.a, k, m0, bar);
           }
           if (KIND == kGrads && W.b_mn) {
-            for (int q = 0; q < half_n; q += 64) load_box(b + q * 128, &job.b, n0 + q, k, bar);
+            for (int q = 0; q < half_n; q += 64) {
+              load_box(b + q * 128, &job.b, n0 + q, k, bar);
+              if (t.job == 1 && W.low > 0)  // (a box of the first half: the second is the same)
+                load_box(b + q * 128 + kBlockK / 2 * 128, &job.b, n0 + q, k, bar);
+            }
           } else {
             load_box(b, &job.b, k, n0, bar);
           }
@@ -480,220 +485,230 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
         }
       }
     } else {
-    float mul = 1.f;
-    if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
-    for (int i = group;; i += 2) {
-      const Unit t = unit_of<KIND>(J, pair, pairs, i);
-      if (t.job < 0) break;
-      const Work &W = J.job[KIND == kGrads ? t.job : 0].w;
-      const int chunks = W.tile_n / 32;
-      const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32, col = t.n * W.tile_n;
-      // what does not wait for the products
-      Position *pos = (Position *)epi + group * kMaxTileN;
-      int *tgt = (int *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
-      Position own = {1e30f, 0.f, 0.f, 0.f};
-      int target = -1;
-      if constexpr (KIND == kCoefCols) {
-        named_barrier_sync(1 + group, kGroup);  // (the last tile's are read)
-        for (int c = gtid; c < W.tile_n; c += kGroup) {
-          Position p = {1e30f, 0.f, 0.f, 0.f};
-          int j = -1;
-          if (col + c < W.N && BOUTE_INB(col + c, W.N)) {
-            p = W.pos[col + c];
-            p.a *= mul, p.b *= mul, p.g *= mul;
-            j = W.tgt[col + c] - W.row0;
-          }
-          pos[c] = p;
-          tgt[c] = j;
-        }
-      } else if constexpr (KIND == kCoefRows) {
-        if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
-          own = W.pos[row + lane];
-          own.a *= mul, own.b *= mul, own.g *= mul;
-          target = W.tgt[row + lane] - W.row0;
-        }
-      } else if constexpr (KIND == kStatsRows) {
-        if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
-          const long long j = W.targets[row + lane];
-          target = j >= 0 && j < W.N ? (int)j : -1;
-        }
-      }
-      // (where the group meets at a barrier, it goes on or gives up as one)
-      bool ok = __all_sync(kAll, pair_wait(&acc_full[group], (i >> 1) & 1u, abort));
-      if (KIND == kStatsCols || KIND == kCoefCols) ok = group_all(1 + group, kGroup, ok);
-      if (!ok) break;
-      tc_fence_after();
-      Stat run = {-INFINITY, 0.f, 0.f};
-      // 64 columns of 32 rows go out as a box (all of their row's bytes at once: 268 MB of dW took 77
-      // us by each thread's 32 bytes of its row), a last half by the threads
-      uint8_t *box = epi + kBoxes<KIND> + (warp - 2) * kBoxBytes;
-      auto send = [&](int c, const float (&x)[32]) {
-        const CUtensorMap *out = &J.job[KIND == kGrads ? t.job : 0].out;
-        if (c % 2 == 0) {
-          if (lane == 0) bulk_wait_read();
-          __syncwarp();
-        }
-        box_row<T>(box, c & 1, x);
-        if (c % 2 == 0) return;
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          store_box(out, box, col + (c - 1) * 32, row);
-          bulk_commit();
-        }
-      };
-      for (int c = 0; c < chunks; ++c) {
-        float x[32];
-        tmem_ld32(from + group * kMaxTileN + c * 32, x);
-        if (c == chunks - 1) release(group);
-        const int d0 = col + c * 32;
-        const bool boxed = c < (chunks & ~1);
-        if constexpr (KIND == kStatsCols) {
-          float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
-          Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
-          const int at = d0 + lane;
-          long long wanted = -1;
-          if (at < W.N && BOUTE_INB(at, W.N)) wanted = W.targets[at];
-          // (rows of the accumulator beyond the block's hold what was in its shared memory)
-          const int rows = min(W.tile_m - quarter * 32, W.M - row);
-          if (lane >= rows)
-#pragma unroll
-            for (int q = 0; q < 32; ++q) x[q] = -INFINITY;
-#pragma unroll
-          for (int q = 0; q < 32; q += 4)
-            *(float4 *)(buf + lane * kPitch + q) = {x[q], x[q + 1], x[q + 2], x[q + 3]};
-          __syncwarp();
-#pragma unroll
-          for (int q = 0; q < 32; ++q) x[q] = buf[q * kPitch + lane];
-          if (wanted >= row && wanted < row + min(rows, 32))
-            W.picked[at] = buf[(int)(wanted - row) * kPitch + lane];
-          red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x, W.c2);
-          __syncwarp();
-        } else if constexpr (KIND == kStatsRows) {
-          if (d0 + 32 > W.N)
-#pragma unroll
-            for (int q = 0; q < 32; ++q)
-              if (d0 + q >= W.N) x[q] = -INFINITY;
-          if (__any_sync(kAll, target >= d0 && target < d0 + 32))
-#pragma unroll
-            for (int q = 0; q < 32; ++q)
-              if (target == d0 + q) W.picked[row + lane] = x[q];
-          join(run, stat_of(x, W.c2), W.c2);
-        } else if constexpr (KIND == kCoefCols) {
-          const int j = tgt[c * 32 + lane];
-          unsigned here = __ballot_sync(kAll, j >= row && j < row + 32);
-#pragma unroll
-          for (int q = 0; q < 32; ++q) {
-            const Position p = pos[c * 32 + q];
-            const float lp = max_nan(fmaf(x[q], W.scale, -p.lse), -1e4f);
-            x[q] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
-          }
-          if (here)
-#pragma unroll
-            for (int q = 0; q < 32; ++q)
-              if ((here >> q & 1u) && tgt[c * 32 + q] == row + lane) x[q] += pos[c * 32 + q].g;
-          if (boxed) send(c, x);
-          else if (row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp))
-            store_row_of<T>(W.coef + (row + lane) * W.Tp + d0, x);
-        } else if constexpr (KIND == kCoefRows) {
-          const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.lse);
-          const unsigned long long a2 = f2_dup(own.a), b2 = f2_dup(own.b), l2e = f2_dup(kLog2e);
-#pragma unroll
-          for (int q = 0; q < 32; q += 2) {
-            float l0, l1, y0, y1;
-            f2_split(f2_fma(f2_pack(x[q], x[q + 1]), by, less), l0, l1);
-            const unsigned long long lp = f2_pack(max_nan(l0, -1e4f), max_nan(l1, -1e4f));
-            f2_split(f2_mul(lp, l2e), y0, y1);
-            f2_split(f2_mul(f2_pack(exp2_fast(y0), exp2_fast(y1)), f2_fma(b2, lp, a2)), x[q],
-                     x[q + 1]);
-          }
-          if (__any_sync(kAll, target >= d0 && target < d0 + 32))
-#pragma unroll
-            for (int q = 0; q < 32; ++q)
-              if (target == d0 + q) x[q] += own.g;
-          send(c, x);
-        } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
-          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
-            const int n = min(32, W.N - d0);
-            float *to = W.sums + ((long long)t.split * W.N + d0) * W.M + row + lane;
-            if (t.k0 == t.k1)  // (a short piece's empty part)
-#pragma unroll
-              for (int q = 0; q < 32; ++q) x[q] = 0.f;
-            if (W.add) {
-              float was[32];  // (all on their way at once)
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (q < n) was[q] = to[(long long)q * W.M];
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (q < n) x[q] += was[q];
+      float mul = 1.f;
+      if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
+      for (int i = group;; i += 2) {
+        const Unit t = unit_of<KIND>(J, pair, pairs, i);
+        if (t.job < 0) break;
+        const Work &W = J.job[KIND == kGrads ? t.job : 0].w;
+        const int chunks = W.tile_n / 32;
+        const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32, col = t.n * W.tile_n;
+        // what does not wait for the products
+        Position *pos = (Position *)epi + group * kMaxTileN;
+        int *tgt = (int *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
+        Position own = {1e30f, 0.f, 0.f, 0.f};
+        int target = -1;
+        if constexpr (KIND == kCoefCols) {
+          named_barrier_sync(1 + group, kGroup);  // (the last tile's are read)
+          for (int c = gtid; c < W.tile_n; c += kGroup) {
+            Position p = {1e30f, 0.f, 0.f, 0.f};
+            int j = -1;
+            if (col + c < W.N && BOUTE_INB(col + c, W.N)) {
+              p = W.pos[col + c];
+              p.a *= mul, p.b *= mul, p.g *= mul;
+              j = W.tgt[col + c] - W.row0;
             }
-#pragma unroll
-            for (int q = 0; q < 32; ++q)
-              if (q < n) to[(long long)q * W.M] = x[q];
+            pos[c] = p;
+            tgt[c] = j;
           }
-        } else {  // dW
+        } else if constexpr (KIND == kCoefRows) {
+          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+            own = W.pos[row + lane];
+            own.a *= mul, own.b *= mul, own.g *= mul;
+            target = W.tgt[row + lane] - W.row0;
+          }
+        } else if constexpr (KIND == kStatsRows) {
+          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+            const long long j = W.targets[row + lane];
+            target = j >= 0 && j < W.N ? (int)j : -1;
+          }
+        }
+        // (where the group meets at a barrier, it goes on or gives up as one)
+        bool ok = __all_sync(kAll, pair_wait(&acc_full[group], (i >> 1) & 1u, abort));
+        if (KIND == kStatsCols || KIND == kCoefCols) ok = group_all(1 + group, kGroup, ok);
+        if (!ok) break;
+        tc_fence_after();
+        Stat run = {-INFINITY, 0.f, 0.f};
+        // 64 columns of 32 rows go out as a box (all of their row's bytes at once: 268 MB of dW took 77
+        // us by each thread's 32 bytes of its row), a last half by the threads
+        uint8_t *box = epi + kBoxes<KIND> + (warp - 2) * kBoxBytes;
+        auto send = [&](int c, const float (&x)[32]) {
+          const CUtensorMap *out = &J.job[KIND == kGrads ? t.job : 0].out;
+          if (c % 2 == 0) {
+            if (lane == 0) bulk_wait_read();
+            __syncwarp();
+          }
+          box_row<T>(box, c & 1, x);
+          if (c % 2 == 0) return;
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            store_box(out, box, col + (c - 1) * 32, row);
+            bulk_commit();
+          }
+        };
+        for (int c = 0; c < chunks; ++c) {
+          float x[32];
+          tmem_ld32(from + group * kMaxTileN + c * 32, x);
+          if (c == chunks - 1) release(group);
+          const int d0 = col + c * 32;
+          const bool boxed = c < (chunks & ~1);
+          if constexpr (KIND == kStatsCols) {
+            float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
+            Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
+            const int at = d0 + lane;
+            long long wanted = -1;
+            if (at < W.N && BOUTE_INB(at, W.N)) wanted = W.targets[at];
+            // (rows of the accumulator beyond the block's hold what was in its shared memory)
+            const int rows = min(W.tile_m - quarter * 32, W.M - row);
+            if (lane >= rows)
 #pragma unroll
-          for (int q = 0; q < 32; ++q) x[q] *= mul;
-          T *to = (T *)W.out + (row + lane) * W.ldo + d0;
-          if (boxed && W.boxes) {
+              for (int q = 0; q < 32; ++q) x[q] = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < 32; q += 4)
+              *(float4 *)(buf + lane * kPitch + q) = {x[q], x[q + 1], x[q + 2], x[q + 3]};
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] = buf[q * kPitch + lane];
+            if (wanted >= row && wanted < row + min(rows, 32))
+              W.picked[at] = buf[(int)(wanted - row) * kPitch + lane];
+            red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x, W.c2);
+            __syncwarp();
+          } else if constexpr (KIND == kStatsRows) {
+            if (d0 + 32 > W.N)
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (d0 + q >= W.N) x[q] = -INFINITY;
+            if (__any_sync(kAll, target >= d0 && target < d0 + 32))
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (target == d0 + q) W.picked[row + lane] = x[q];
+            join(run, stat_of(x, W.c2), W.c2);
+          } else if constexpr (KIND == kCoefCols) {
+            const int j = tgt[c * 32 + lane];
+            unsigned here = __ballot_sync(kAll, j >= row && j < row + 32);
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+              const Position p = pos[c * 32 + q];
+              const float lp = max_nan(fmaf(x[q], W.scale, -p.lse), -1e4f);
+              x[q] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
+            }
+            if (here)
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if ((here >> q & 1u) && tgt[c * 32 + q] == row + lane) x[q] += pos[c * 32 + q].g;
+            if (d0 + 32 > W.N)  // (columns of no position, which a token of infinities makes NaN)
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (d0 + q >= W.N) x[q] = 0.f;
+            uint16_t *to = W.coef + (row + lane) * W.Tp + d0;
+            const bool mine = row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp);
+            if (boxed) send(c, x);
+            else if (mine) store_row_of<T>(to, x);
+            if (W.low > 0 && mine && BOUTE_INB(d0 + W.low + 31, W.Tp)) {
+#pragma unroll
+              for (int q = 0; q < 32; ++q) x[q] -= to_float(from_float<T>(x[q]));
+              store_row_of<T>(to + W.low, x);
+            }
+          } else if constexpr (KIND == kCoefRows) {
+            const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.lse);
+            const unsigned long long a2 = f2_dup(own.a), b2 = f2_dup(own.b), l2e = f2_dup(kLog2e);
+#pragma unroll
+            for (int q = 0; q < 32; q += 2) {
+              float l0, l1, y0, y1;
+              f2_split(f2_fma(f2_pack(x[q], x[q + 1]), by, less), l0, l1);
+              const unsigned long long lp = f2_pack(max_nan(l0, -1e4f), max_nan(l1, -1e4f));
+              f2_split(f2_mul(lp, l2e), y0, y1);
+              f2_split(f2_mul(f2_pack(exp2_fast(y0), exp2_fast(y1)), f2_fma(b2, lp, a2)), x[q],
+                       x[q + 1]);
+            }
+            if (__any_sync(kAll, target >= d0 && target < d0 + 32))
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (target == d0 + q) x[q] += own.g;
             send(c, x);
-          } else if (boxed) {  // rows at any address: by way of the box, a row's neighbours together
-            if (c % 2 == 0) __syncwarp();
-            box_row<T>(box, c & 1, x);
-            if (c % 2 == 1) {
-              __syncwarp();
-              const int rows = min(32, W.M - row);
-              for (int r = 0; r < rows; ++r) {
-                T *line = (T *)W.out + (row + r) * W.ldo + d0 - 32;
+          } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
+            if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+              const int n = min(32, W.N - d0);
+              float *to = W.sums + ((long long)t.split * W.N + d0) * W.M + row + lane;
+              if (t.k0 == t.k1)  // (a short piece's empty part)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const int e = h * 32 + lane;
-                  const T v = *(const T *)(box + r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2);
-                  if (d0 - 32 + e < W.N && BOUTE_INB(row + r, W.M)) line[e] = v;
+                for (int q = 0; q < 32; ++q) x[q] = 0.f;
+              if (W.add) {
+                float was[32];  // (all on their way at once)
+#pragma unroll
+                for (int q = 0; q < 32; ++q)
+                  if (q < n) was[q] = to[(long long)q * W.M];
+#pragma unroll
+                for (int q = 0; q < 32; ++q)
+                  if (q < n) x[q] += was[q];
+              }
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (q < n) to[(long long)q * W.M] = x[q];
+            }
+          } else {  // dW
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] *= mul;
+            T *to = (T *)W.out + (row + lane) * W.ldo + d0;
+            if (boxed && W.boxes) {
+              send(c, x);
+            } else if (boxed) {  // rows at any address: by way of the box, a row's neighbours together
+              if (c % 2 == 0) __syncwarp();
+              box_row<T>(box, c & 1, x);
+              if (c % 2 == 1) {
+                __syncwarp();
+                const int rows = min(32, W.M - row);
+                for (int r = 0; r < rows; ++r) {
+                  T *line = (T *)W.out + (row + r) * W.ldo + d0 - 32;
+#pragma unroll
+                  for (int h = 0; h < 2; ++h) {
+                    const int e = h * 32 + lane;
+                    const T v = *(const T *)(box + r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2);
+                    if (d0 - 32 + e < W.N && BOUTE_INB(row + r, W.M)) line[e] = v;
+                  }
                 }
               }
-            }
-          } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {
-            if (d0 + 32 <= W.N && W.width >= 32) {
-              store_row_of<T>((uint16_t *)to, x);
-            } else if (d0 + 32 <= W.N && W.width >= 16) {
+            } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {
+              if (d0 + 32 <= W.N && W.width >= 32) {
+                store_row_of<T>((uint16_t *)to, x);
+              } else if (d0 + 32 <= W.N && W.width >= 16) {
 #pragma unroll
-              for (int q = 0; q < 32; q += 8)
-                *(uint4 *)(to + q) = {
-                    pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
-                    pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
-            } else {
+                for (int q = 0; q < 32; q += 8)
+                  *(uint4 *)(to + q) = {
+                      pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
+                      pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
+              } else {
 #pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
+                for (int q = 0; q < 32; ++q)
+                  if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
+              }
             }
           }
+          __syncwarp();
         }
-        __syncwarp();
-      }
-      if constexpr (kStats) {
-        const long long parts = KIND == kStatsCols ? 2ll * W.nM : W.nN, all = parts * W.Tp;
-        auto write = [&](Stat a, long long at) {
-          if (!BOUTE_INB(at, all)) return;
-          W.part[at] = a.m;
-          W.part[all + at] = a.s;
-          W.part[2 * all + at] = a.u;
-        };
-        if constexpr (KIND == kStatsCols) {
-          named_barrier_sync(1 + group, kGroup);
-          const Stat *red =
-              (const Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
-          for (int c = gtid; c < W.tile_n; c += kGroup) {
-            Stat a = red[c];
-            for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + c], W.c2);
-            if (col + c < W.N) write(a, (2ll * t.m + rank) * W.Tp + col + c);
+        if constexpr (kStats) {
+          const long long parts = KIND == kStatsCols ? 2ll * W.nM : W.nN, all = parts * W.Tp;
+          auto write = [&](Stat a, long long at) {
+            if (!BOUTE_INB(at, all)) return;
+            W.part[at] = a.m;
+            W.part[all + at] = a.s;
+            W.part[2 * all + at] = a.u;
+          };
+          if constexpr (KIND == kStatsCols) {
+            named_barrier_sync(1 + group, kGroup);
+            const Stat *red =
+                (const Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
+            for (int c = gtid; c < W.tile_n; c += kGroup) {
+              Stat a = red[c];
+              for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + c], W.c2);
+              if (col + c < W.N) write(a, (2ll * t.m + rank) * W.Tp + col + c);
+            }
+          } else if (row + lane < W.M) {
+            write(run, t.n * W.Tp + row + lane);
           }
-        } else if (row + lane < W.M) {
-          write(run, t.n * W.Tp + row + lane);
         }
       }
-    }
     }
   }
   if (warp >= 2 && lane == 0) bulk_wait();
@@ -807,11 +822,12 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// dh from the sums of its splits: E neighbouring elements a thread.
+// dh from the sums of its splits, `each` elements apart, and with low > 0 of their coefficients' low
+// parts, low elements on: E neighbouring elements a thread.
 template <class T, int E>
 __global__ void __launch_bounds__(256)
-    hidden_dh_kernel(const Header *head, int bounds, const float *sums, int splits,
-                     long long rows, int D, T *dh, long long ldd) {
+    hidden_dh_kernel(const Header *head, int bounds, const float *sums, int splits, long long each,
+                     long long low, long long rows, int D, T *dh, long long ldd) {
   pdl_wait();
   pdl_trigger();
   const float mul = coef_scale(head, bounds, true);
@@ -822,15 +838,17 @@ __global__ void __launch_bounds__(256)
   float v[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = 0.f;
-  constexpr int kAtOnce = E == 1 ? 16 : 4;  // splits on their way to a thread
-  for (int s0 = 0; s0 < splits; s0 += kAtOnce) {
+  constexpr int kAtOnce = E == 1 ? 16 : 4;  // sums on their way to a thread
+  const int all = low > 0 ? 2 * splits : splits;
+  for (int s0 = 0; s0 < all; s0 += kAtOnce) {
     float x[kAtOnce][E];
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
-      const long long at = (s0 + j) * n + i;
+      const int s = s0 + j;
+      const long long at = (s < splits ? s * each : (s - splits) * each + low) + i;
 #pragma unroll
       for (int e = 0; e < E; ++e) x[j][e] = 0.f;
-      if (s0 + j >= splits || !BOUTE_INB(at, splits * n)) continue;
+      if (s >= all || !BOUTE_INB(at, splits * each)) continue;
       if constexpr (E == 4) {
         const float4 q = *(const float4 *)(sums + at);
         x[j][0] = q.x, x[j][1] = q.y, x[j][2] = q.z, x[j][3] = q.w;
@@ -919,12 +937,16 @@ Operand operand(const void *p, long long rows, int D, long long ld, bool lines) 
 struct Plan {
   Operand h, w;
   bool rows;               // positions in the tiles' rows
+  bool fine;               // the coefficients have low parts
   int tiles_t, tile_t;     // of the positions in columns
   int tile_m;              // a block's tokens of the vocabulary (statistics in columns)
   long long Tp;            // the positions with what the last tile has beyond them
   int piece;               // tokens of the vocabulary at once (gradient)
   int splits;              // of dh's reduction
   size_t header, part, picked, pos, tgt, coef, sums, h_at, w_at, bytes;
+  // positions that the coefficients have columns for, and that dh's sums have rows for
+  long long columns() const { return fine ? 2 * Tp : Tp; }
+  long long sum_rows(long long T) const { return fine ? 2 * Tp : T; }
 };
 
 int pairs_of(long long units) {
@@ -956,6 +978,10 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   // 515: 223 and 202). The weight is read once for every 256 positions, too seldom for a copy to pay
   // (another 35 us, also for the 16 reads of 4096 positions).
   p.h = operand(h, T, D, ldh, T > 128);
+  // The coefficients of up to half a block's positions are two 16-bit numbers each, the second in the
+  // block's other half, where the products are made all the same. (One position's gradient would be
+  // its coefficients' rounding off throughout; of many the roundings are apart.)
+  p.fine = grad && T <= kBlockK / 2;
   p.w = operand(w, V, D, ldw, false);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -973,17 +999,20 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   } else {
     p.piece = (int)std::min<long long>(
         up(V, kPairM),
-        std::max<long long>(kPairM, (long long)(kCoefBytes / (2 * p.Tp)) / kPairM * kPairM));
-    const size_t each = (size_t)T * D * sizeof(float);
+        std::max<long long>(kPairM,
+                            (long long)(kCoefBytes / (2 * p.columns())) / kPairM * kPairM));
+    const size_t each = (size_t)p.sum_rows(T) * D * sizeof(float);
     int tiles_d, tile_d;
     tile_columns(D, tiles_d, tile_d);
     p.splits = dh_splits((long long)((D + kPairM - 1) / kPairM) * p.tiles_t, blocks_of(p.piece),
-                         p.tile_t,
-                         (double)(p.piece / kPairM) * tiles_d * blocks_of((int)t) * tile_d, each,
+                         p.fine ? 2 * p.tile_t : p.tile_t,
+                         (double)(p.piece / kPairM) * tiles_d * blocks_of((int)p.sum_rows(t)) *
+                             tile_d,
+                         each,
                          num_sms() / 2);
     p.pos = take(p.Tp * sizeof(Position));
     p.tgt = take(p.Tp * sizeof(int));
-    p.coef = take((size_t)p.piece * p.Tp * 2);
+    p.coef = take((size_t)p.piece * p.columns() * 2);
     p.sums = take(p.splits * each);
   }
   if (p.h.moved) p.h_at = take((size_t)T * p.h.ld * 2);
@@ -1197,6 +1226,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
                ? BOUTE_OK
                : last_launch_status();
   char *ws = (char *)workspace;
+  const long long both = p.sum_rows(T);  // positions, and with low parts as many again
   if (int r = align_operand(p.h, T, D, ldh, ws + p.h_at, s)) return r;
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
@@ -1215,14 +1245,16 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   W.coef = (uint16_t *)(ws + p.coef);
   W.sums = (float *)(ws + p.sums);
   // a piece's coefficients: tokens x positions, or (positions in the tiles' rows) positions x tokens
-  W.Tp = p.rows ? p.piece : p.Tp;
+  W.Tp = p.rows ? p.piece : p.columns();
+  W.low = p.fine ? (int)p.Tp : 0;
   CUtensorMap h_k, h_mn;
   if (int r = make_map(&h_k, dtype, p.h.p, D, T, p.h.ld, p.rows ? 128 : p.tile_t / 2)) return r;
-  if (int r = make_map(&h_mn, dtype, p.h.p, D, T, p.h.ld, kBlockK)) return r;
+  if (int r = make_map(&h_mn, dtype, p.h.p, D, T, p.h.ld, p.fine ? kBlockK / 2 : kBlockK))
+    return r;
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = std::min(p.piece, V - v0), tiles_v = (n + kPairM - 1) / kPairM;
     const char *w = (const char *)p.w.p + (size_t)v0 * p.w.ld * 2;
-    const long long inner = p.rows ? n : T, outer = p.rows ? T : n;  // of the coefficients
+    const long long inner = p.rows ? n : both, outer = p.rows ? T : n;  // of the coefficients
     Jobs J{};
     Job &c = J.job[0];
     c.w = W;
@@ -1242,8 +1274,9 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     if (int r = p.rows ? launch<kCoefRows>(dtype, J, s) : launch<kCoefCols>(dtype, J, s)) return r;
     Job &g = J.job[0], &o = J.job[1];
     g.w = W;  // dh: rows of its elements, columns of the positions
-    g.w.M = D, g.w.N = (int)T, g.w.K = n;
-    g.w.nM = (D + kPairM - 1) / kPairM, g.w.nN = p.tiles_t, g.w.tile_n = p.tile_t;
+    g.w.M = D, g.w.N = (int)both, g.w.K = n;
+    g.w.nM = (D + kPairM - 1) / kPairM, g.w.nN = p.tiles_t;
+    g.w.tile_n = p.fine ? 2 * p.tile_t : p.tile_t;
     g.w.splits = p.splits;
     g.w.add = v0 > 0;
     g.w.a_mn = 1, g.w.b_mn = !p.rows;
@@ -1251,7 +1284,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     if (int r = make_map(&g.b, dtype, W.coef, inner, outer, W.Tp, p.rows ? p.tile_t / 2 : kBlockK))
       return r;
     o.w = W;  // dW of the piece
-    o.w.M = n, o.w.N = D, o.w.K = (int)T;
+    o.w.M = n, o.w.N = D, o.w.K = (int)both;
     o.w.nM = tiles_v;
     tile_columns(D, o.w.nN, o.w.tile_n);
     o.w.a_mn = p.rows, o.w.b_mn = 1;
@@ -1270,12 +1303,12 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     if constexpr (std::is_same<E, float>::value) {
       return (int)BOUTE_ERR_INVALID_ARG;
     } else {
-      const long long n = T * D;
+      const long long n = T * D, each = both * D, low = p.fine ? p.Tp * D : 0;
       if (D % 4 == 0 && n >= 1 << 18)  // (few elements take a thread each, to be read by more SMs)
         return launch_cluster(hidden_dh_kernel<E, 4>, (n / 4 + 255) / 256, 256, 1, 0, s, W.head,
-                              W.bounds, W.sums, p.splits, T, D, (E *)dhidden, lddh);
+                              W.bounds, W.sums, p.splits, each, low, T, D, (E *)dhidden, lddh);
       return launch_cluster(hidden_dh_kernel<E, 1>, (n + 255) / 256, 256, 1, 0, s, W.head, W.bounds,
-                            W.sums, p.splits, T, D, (E *)dhidden, lddh);
+                            W.sums, p.splits, each, low, T, D, (E *)dhidden, lddh);
     }
   });
 }

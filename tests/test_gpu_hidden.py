@@ -102,8 +102,10 @@ class Plain:
         tol = 2 * self.tol * (2 + math.log(V)) + 2 * U * self.H
         assert ((H.double() - self.H).abs() <= tol).all()
 
-    def grad(self, g, gh, dtype):
-        """(dh, dw, their tolerances) of the outputs' gradients, with lse and the entropy rounded to fp32."""
+    def grad(self, g, gh, dtype, coef=None):
+        """(dh, dw, their tolerances) of the outputs' gradients, with lse and the entropy rounded to fp32;
+        coef: the relative error of a coefficient's rounding."""
+        coef = EPS[dtype] if coef is None else coef
         V, D = self.w.shape
         T = len(self.t)
         g = torch.where(self.t >= 0, g, torch.zeros_like(g)).double()
@@ -125,7 +127,7 @@ class Plain:
             dz = STEP * D * size * self.scale + U * (4 * q.abs() + 4 * lse[r, None].abs() + 16)
             e = self.scale * p * ((inner.abs() + 2 * U * (g[r].abs() + gh[r].abs() * (H[r] + 1))[:, None])
                                   * dz + gh[r, None].abs() * (dz + 2 * U * (H[r, None] + q.abs())))
-            e += EPS[dtype] * (c.abs() + e) + low + TINY["bf16"]
+            e += coef * (c.abs() + e) + low + TINY["bf16"]
             dh.append(c @ self.w)
             th.append((e + STEP * V * c.abs()) @ self.w.abs())
             dw += c.t() @ self.h[r]
@@ -173,6 +175,20 @@ def check_grad(T, V, D, dtype, scale, pitch=0, shift=0, ent=True, spread=1.5):
 @pytest.mark.parametrize("T,V,D,dtype,scale,pitch,shift", SIZES)
 def test_gradient(T, V, D, dtype, scale, pitch, shift):
     check_grad(T, V, D, dtype, scale, pitch, shift, ent=(T + V) % 3 != 0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 5, 31, 32])
+def test_gradients_of_few_positions_keep_the_coefficients_low_parts(T, dtype):
+    """Up to 32 positions: a coefficient is two numbers of the type, and off by EPS^2 alone."""
+    h, w, t = inputs(T, 1000, 72, dtype, seed=4, spread=0.5)
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    g, gh = (torch.randn((T,), generator=gen, device="cuda") for _ in range(2))
+    plain = Plain(h, w, t, 1.0)
+    got = backward(h, w, t, 1.0, plain.lse.float(), plain.H.float(), g, gh)
+    dh, dw, th, tw = plain.grad(g, gh, dtype, EPS[dtype] ** 2)
+    assert ((got[0].double() - dh).abs() <= th).all()
+    assert ((got[1].double() - dw).abs() <= tw).all()
 
 
 @pytest.mark.parametrize("T", [8191, 8192, 8193, 8200, 16500])
