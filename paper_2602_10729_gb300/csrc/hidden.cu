@@ -8,10 +8,25 @@
 //   c_tj = scale (g ([j = t] - p_j) - g_H p_j (ln p_j + H)),
 // of which dh = c W and dW = c^T h are two more products.
 //
-// All products run on the tensor cores: a pair of blocks takes tiles of 256 tokens of the
-// vocabulary (rows) x up to 256 positions (columns), one warp bringing operand tiles, one issuing
-// products, and two groups of four warps taking the accumulators' tiles in turn, so that a tile's
-// sums or stores go on behind the next one's products.
+// All products run on the tensor cores. A pair of blocks takes tiles of 256 rows x up to 256
+// columns, one warp bringing operand tiles, one issuing products, and two groups of four warps
+// taking the accumulators' tiles in turn, so that a tile's sums or stores go on behind the next
+// one's products. The logits' pieces are as small as a tile (256 tokens), the coefficients' as
+// large as 256 MB: a piece's reductions and its tail of tiles are long beside what they wait for.
+//
+// Many positions are bound by the tensor cores (96 % of their cycles in the statistics, 94 and 83
+// in the gradient's two launches) and at that by power, which takes the clock to 1.7 GHz: 4096
+// positions x 131072 tokens, 4096 elements, bf16: 2.1 to 2.4 ms from machine to machine (1.86 to
+// 2.1 PFLOP/s; a library product that writes such logits 2.25); the gradient with 2048 elements 3.8
+// to 4.1 ms (1.62 to 1.74). In the gradient, what operands read by columns cost is not hidden
+// (without their copies the launch took 508 us for 627). Few positions are bound by reading the
+// weight: one position of 50021 x 2048 takes 42 us (4.9 TB/s; 36 are the kernel's, the rest its
+// start, the last tile and the join), 64 of 32768 x 4096 51, and 157 for the gradient, which reads
+// the weight twice and writes as much. Between them every 256 tokens ask as many bytes of the L2 as
+// it brings at the tensor cores' pace: 515 x 50021 x 1024 49 us (1.1 PFLOP/s). A weight whose rows
+// are no multiples of 128 bytes is read in pieces of two lines (515 x 50021 x 1000 fp16: gradient
+// 165 us, with 1024 elements 150), one of no multiples of 16 is copied first (64 x 32768 x 1001: 46
+// us, x 1000 22).
 #include <float.h>
 #include <limits.h>
 #include <math.h>
@@ -27,10 +42,11 @@ namespace {
 
 constexpr int kThreads = 320, kEpiWarps = 8, kGroup = 128;  // two warps of roles, two groups
 constexpr int kMaxStages = 12;
-// Blocks of the reduction that a logit of the statistics takes on the tensor cores at once. Their sums
-// cut off what fp32 does not hold, step by step; the parts are added up, rounded, in registers.
-// (4096 positions of 32768 tokens, 4096 elements, entropies in one part 2.5e-6 off, in parts of 16
-// blocks 5.4e-7, of 8 2.4e-7, for 1, 1 and 7 % of the time.)
+// Blocks of the reduction that a logit of the statistics takes on the tensor cores at once. Their
+// sums cut off what fp32 does not hold, step by step; the parts are added up, rounded, in
+// registers.
+// (4096 positions of 32768 tokens, 4096 elements: entropies in one part 2.5e-6 off, in parts of 16
+// blocks 5.4e-7 for 1 % more time, of 8 2.4e-7 for 7 %.)
 constexpr int kPart = 16;
 constexpr int kABytes = 128 * kBlockK * 2;  // a block's half of a stage's rows
 constexpr int kPitch = 36;  // floats of a row of a warp's 32 x 32 transposition
@@ -49,7 +65,8 @@ struct Header {
   // BOUTE_ERR_TIMEOUT where a wait ran out: of each block of the statistics' launch, which writes
   // its own; of all launches of the gradient, which clears it first
   int status[kBlocks];
-  unsigned largest[kBounds];  // bits of the largest bound of a coefficient, of each block that looked
+  // bits of the largest bound of a coefficient, of each block that looked
+  unsigned largest[kBounds];
 };
 // What the coefficients of a position need.
 struct Position {
@@ -160,7 +177,8 @@ constexpr int kBoxes = KIND == kStatsCols ? kEpiWarps * 32 * kPitch * 4 + 2 * 4 
                            ? 2 * kMaxTileN * (int)(sizeof(Position) + sizeof(int))
                            : 0;
 template <Kind KIND>
-constexpr int kEpi = kBoxes<KIND> + (KIND == kStatsCols || KIND == kStatsRows ? 0 : kEpiWarps * kBoxBytes);
+constexpr int kEpi =
+    kBoxes<KIND> + (KIND == kStatsCols || KIND == kStatsRows ? 0 : kEpiWarps * kBoxBytes);
 
 // ---- the sums of a tile ----------------------------------------------------------------
 struct Stat {
@@ -262,7 +280,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], kParted ? 2 * kEpiWarps : kEpiWarps);  // who reads it, of both blocks
+      // (the warps of both blocks that read it)
+      mbar_init(&acc_empty[i], kParted ? 2 * kEpiWarps : kEpiWarps);
     }
     mbar_init(&drain, 1);
     abort_flag = 0;
@@ -319,8 +338,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------------- products
-    // (The warp stays together, so that descriptors are in uniform registers: with one lane alone in
-    // the loop, issuing took longer than the products.)
+    // (The warp stays together, so that descriptors are in uniform registers: with one lane alone
+    // in the loop, issuing took longer than the products, 1.6 PFLOP/s for 2.1.)
     if (rank == 0) {
       constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
       const bool issuer = elect_one();
@@ -529,8 +548,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
         if (!ok) break;
         tc_fence_after();
         Stat run = {-INFINITY, 0.f, 0.f};
-        // 64 columns of 32 rows go out as a box (all of their row's bytes at once: 268 MB of dW took 77
-        // us by each thread's 32 bytes of its row), a last half by the threads
+        // 64 columns of 32 rows go out as a box (a row's bytes at once: 268 MB of dW took 77 us by
+        // each thread's 32 bytes of its row), a last half by the threads
         uint8_t *box = epi + kBoxes<KIND> + (warp - 2) * kBoxBytes;
         auto send = [&](int c, const float (&x)[32]) {
           const CUtensorMap *out = &J.job[KIND == kGrads ? t.job : 0].out;
@@ -653,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
             T *to = (T *)W.out + (row + lane) * W.ldo + d0;
             if (boxed && W.boxes) {
               send(c, x);
-            } else if (boxed) {  // rows at any address: by way of the box, a row's neighbours together
+            } else if (boxed) {  // rows at any address: by way of the box, a row by its lanes
               if (c % 2 == 0) __syncwarp();
               box_row<T>(box, c & 1, x);
               if (c % 2 == 1) {
@@ -664,7 +683,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
 #pragma unroll
                   for (int h = 0; h < 2; ++h) {
                     const int e = h * 32 + lane;
-                    const T v = *(const T *)(box + r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2);
+                    const int at = r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2;
+                    const T v = *(const T *)(box + at);
                     if (d0 - 32 + e < W.N && BOUTE_INB(row + r, W.M)) line[e] = v;
                   }
                 }
@@ -822,8 +842,8 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// dh from the sums of its splits, `each` elements apart, and with low > 0 of their coefficients' low
-// parts, low elements on: E neighbouring elements a thread.
+// dh from the sums of its splits, `each` elements apart, and with low > 0 of their coefficients'
+// low parts, low elements on: E neighbouring elements a thread.
 template <class T, int E>
 __global__ void __launch_bounds__(256)
     hidden_dh_kernel(const Header *head, int bounds, const float *sums, int splits, long long each,
@@ -905,10 +925,15 @@ void tile_columns(int n, int &tiles, int &width) {
   width = (int)up((n + tiles - 1) / tiles, 32);
 }
 
-// Whether the positions are the tiles' rows, of which 256 are a tile's whatever there are.
-bool in_rows(long long T, int D) {
+// Whether the positions are the tiles' rows, of which 256 are a tile's whatever there are. The
+// statistics gain most where the reduction is short (32768 tokens, in us, rows and columns: 300
+// positions of 256 elements 17.3 and 18.5, 515 x 50021 x 1024 48.7 and 49.9, 4096 x 1024 147 and
+// 155), the coefficients pass through shared memory either way (gradients: 384 x 256 46 and 49,
+// x 1024 92 and 89, 700 x 1024 127 and 130).
+bool in_rows(long long T, int D, bool grad) {
   const long long t = up(T, kPairM);
-  return D < 512 ? 2 * t <= 3 * T : 10 * t <= 11 * T;
+  if (grad) return D < 512 ? 2 * t <= 3 * T : 10 * t <= 11 * T;
+  return D < 512 ? 5 * t <= 9 * T : 2 * t <= 3 * T;
 }
 
 // A block's rows of a tile, a multiple of 8 up to 128, so that the pairs' rounds over V rows are
@@ -916,7 +941,8 @@ bool in_rows(long long T, int D) {
 int even_rows(int V) {
   const int pairs = num_sms() / 2;
   const int rounds = (V + kPairM * pairs - 1) / (kPairM * pairs);
-  return (int)std::min<long long>(128, up((V + 2ll * rounds * pairs - 1) / (2ll * rounds * pairs), 8));
+  const long long blocks = 2ll * rounds * pairs;
+  return (int)std::min<long long>(128, up((V + blocks - 1) / blocks, 8));
 }
 
 // A matrix as the copies can read it: in place, or aligned in the workspace. They need rows at
@@ -971,16 +997,18 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
   Plan p{};
   const long long t = std::max(1ll, grad ? T : std::min(T, kAtOnce));
   tile_columns((int)t, p.tiles_t, p.tile_t);
-  p.rows = in_rows(t, D);
+  p.rows = in_rows(t, D, grad);
   p.Tp = p.rows ? up(t, kPairM) : (long long)p.tiles_t * p.tile_t;
-  // The hidden states are read once for every 256 tokens of the vocabulary (515 positions of 1000
-  // elements, 50021 tokens: 70 us in place, 61 by way of whole lines; 4096: 305 and 259; gradient of
-  // 515: 223 and 202). The weight is read once for every 256 positions, too seldom for a copy to pay
-  // (another 35 us, also for the 16 reads of 4096 positions).
+  // The hidden states are read once for every 256 tokens of the vocabulary, by way of whole lines
+  // for more than 128 positions (when it was tried, 515 positions of 1000 elements, 50021 tokens:
+  // 70 us in place, 61 so; 4096: 305 and 259; gradient of 515: 223 and 202). The weight is read
+  // once for every 256 positions, too seldom for a copy to pay (35 us more, also for the 16 times
+  // of 4096 positions).
   p.h = operand(h, T, D, ldh, T > 128);
-  // The coefficients of up to half a block's positions are two 16-bit numbers each, the second in the
-  // block's other half, where the products are made all the same. (One position's gradient would be
-  // its coefficients' rounding off throughout; of many the roundings are apart.)
+  // The coefficients of up to half a block's positions are two 16-bit numbers each, the second in
+  // the block's other half, where the products are made all the same. (One position's gradient
+  // would be its coefficients' rounding off throughout; of many the roundings are apart: 1.35 times
+  // the error of the one rounding at the end.)
   p.fine = grad && T <= kBlockK / 2;
   p.w = operand(w, V, D, ldw, false);
   size_t at = 0;
@@ -1030,7 +1058,7 @@ int stage_of(const Work &W) {
 template <Kind KIND, int MINE = 0>
 int launch(int dtype, Jobs &J, cudaStream_t s) {
   static_assert(kBoxes<KIND> % 1024 == 0 && sizeof(Stat) == 12, "");
-  // as many stages as fit beside the epilogue's shared memory, 1 KB of barriers and 1 KB of alignment
+  // as many stages as fit beside the epilogue's shared memory, 1 KB of barriers, 1 KB of alignment
   constexpr size_t kSmem = 232448 - 1024;
   J.stage_bytes = 0;
   for (int i = 0; i < (KIND == kGrads ? 2 : 1); ++i) {
@@ -1195,9 +1223,10 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
                        : W.tile_n <= 64 ? launch<kStatsCols, 1>
                                         : launch<kStatsCols, 4>;
     if (int r = start(dtype, J, s)) return r;
-    if (int r = launch_cluster(hidden_join_kernel, (n + kJoinAt - 1) / kJoinAt, 32 * kJoinWarps, 1, 0, s, W.head,
-                               2 * pairs_of(J.units[0]), W.part, W.picked, W.targets, n, W.Tp,
-                               parts, V, scale, W.c2, logprob + t0, entropy + t0, lse + t0))
+    if (int r = launch_cluster(hidden_join_kernel, (n + kJoinAt - 1) / kJoinAt, 32 * kJoinWarps, 1,
+                               0, s, W.head, 2 * pairs_of(J.units[0]), W.part, W.picked,
+                               W.targets, n, W.Tp, parts, V, scale, W.c2, logprob + t0,
+                               entropy + t0, lse + t0))
       return r;
   }
   return BOUTE_OK;
@@ -1244,7 +1273,8 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   W.scale = scale;
   W.coef = (uint16_t *)(ws + p.coef);
   W.sums = (float *)(ws + p.sums);
-  // a piece's coefficients: tokens x positions, or (positions in the tiles' rows) positions x tokens
+  // a piece's coefficients: tokens x positions, or, with the positions in the tiles' rows, the
+  // other way round
   W.Tp = p.rows ? p.piece : p.columns();
   W.low = p.fine ? (int)p.Tp : 0;
   CUtensorMap h_k, h_mn;

@@ -31,9 +31,11 @@ def test_workspace_refusals_and_sizes(lib):  # noqa: F811
         return n.value
 
     assert 0 < size() < 1 << 20
-    # no logits: 4096 x 131072 of them are 1 GB in 16 bits
+    # no logits: 4096 x 131072 of them are 1 GB in 16 bits. Three floats for each half of a tile of 256
+    # tokens and each position are 50 MB, an aligned copy of the hidden states 17; the gradient has 256 MB
+    # of coefficients at once and up to 128 of dh's sums.
     big = dict(T=4096, D=2048, ldh=2048, V=131072, ldw=2048)
-    assert size(**big) < 64 << 20 and size(**big, grad=1) < 512 << 20
+    assert size(**big) < 68 << 20 and size(**big, grad=1) < 512 << 20
     # an aligned copy of what is not
     assert size(ldw=65) >= size() + 100 * 64 * 2
     assert size(T=1, ldh=65) == size(T=1)  # (one row has no pitch)
