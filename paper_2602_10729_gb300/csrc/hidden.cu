@@ -788,13 +788,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   if (lane != 0 || t >= T || !BOUTE_INB(t, T)) return;
   const long long target = targets[t];
   const float ls = logf(a.s);
-  float l = scale * a.m + ls, H = ls - kLn2 * (a.u / a.s), lp;
+  const float top = scale * a.m;  // (a scale may take it to an infinity)
+  float l = top + ls, H = ls - kLn2 * (a.u / a.s), lp;
   lp = target >= V ? NAN : target < 0 ? 0.f : scale * (picked[t] - a.m) - ls;
-  if (a.m == -INFINITY) {
+  if (top == -INFINITY) {
     l = -INFINITY;
     H = 0.f;
     lp = target >= V ? NAN : target < 0 ? 0.f : -INFINITY;
-  } else if (isnan(a.s)) {
+  } else if (isnan(a.s) || top == INFINITY) {
     l = H = NAN;
     if (target >= 0) lp = NAN;
   }

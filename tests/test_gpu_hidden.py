@@ -253,6 +253,22 @@ def test_infinite_and_nan_rows():
     assert dh[3].isnan().all() and dh[5].isnan().all()
 
 
+def test_a_scale_that_overflows():
+    """z = scale x beyond fp32: +inf leaves no distribution, -inf masks; what stays finite counts."""
+    V, D = 300, 16
+    h = torch.zeros((3, D), dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((V, D), dtype=torch.bfloat16, device="cuda")
+    h[0, 0], h[1, 1], h[2, 2] = 1.0, 1.0, 1.0
+    w[5, 0] = 2.0 ** 40            # position 0: one logit to +inf
+    w[:, 1] = -2.0 ** 40           # position 1: all to -inf
+    w[:, 2], w[7, 2] = -2.0 ** 40, 2.0 ** -90  # position 2: all but token 7
+    t = torch.tensor([0, 3, 7], device="cuda")
+    lp, H, lse = forward(h, w, t, 2.0 ** 100)
+    assert lp[0].isnan() and H[0].isnan() and lse[0].isnan()
+    assert lse[1] == -float("inf") and H[1] == 0 and lp[1] == -float("inf")
+    assert lse[2] == 2.0 ** 10 and H[2] == 0 and lp[2] == 0
+
+
 def test_a_position_without_a_token_left_has_gradient_0():
     T, V, D = 33, 300, 40
     h, w, t = inputs(T, V, D, "f16")
