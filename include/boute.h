@@ -352,8 +352,8 @@ int boute_selftest_wait(int complete, unsigned long long limit_ns, void *stream)
  * operand images, the outputs, the strips and boxes, the selection). This
  * call waits for the device, returns 1 and fills rec (4 words: the source
  * unit 1 posterior, 2 in-sample, 3 acquisition, 4 front, 5 fit, 6 top-k,
- * 7 log-probabilities, 8 answer scores, 9 routing, 10 experts' rows, 11 hidden states; the source line; the index; the extent) when some unit recorded one since
- * the last call, else 0; it clears the records. The product library returns
+ * 7 log-probabilities, 8 answer scores, 9 routing, 10 experts' rows, 11 hidden states; the source
+ * line; the index; the extent) when some unit recorded one since the last call, else 0; it clears the records. The product library returns
  * BOUTE_ERR_UNSUPPORTED (its checks compile to nothing). */
 int boute_bounds_report(long long *rec);
 
@@ -696,7 +696,7 @@ int boute_route_grad(const void *logits, int dtype, long long T, int E, long lon
  *   offsets (E + 1 int32): expert e's places are offsets[e] .. offsets[e + 1] - 1, n = offsets[E];
  *   source (T k int32): the choice at a place, -1 for places >= n;
  *   place (T x k int32): the place of a choice, -1 for none.
- * The order is the same on every run. E <= BOUTE_MAX_EXPERTS, k <= BOUTE_MAX_CHOICES, 0 <= T k <
+ * The order is the same on every run. The outputs overlap no input. E <= BOUTE_MAX_EXPERTS, k <= BOUTE_MAX_CHOICES, 0 <= T k <
  * 2^31. */
 int boute_expert_sort(const int *idx, long long T, int k, int E, int *offsets, int *source,
                       int *place, void *stream);
@@ -707,7 +707,8 @@ int boute_expert_sort(const int *idx, long long T, int k, int E, int *offsets, i
  * number of choices, those of the last places are left out). Rows without a choice are left as they
  * were. x, dx: T rows of pitch ldx; rows, g_rows: R rows of pitch ldr (in elements; of one type,
  * fp32, fp16 or bf16; any element-aligned address will do). Sums are taken in fp32 in the order of
- * i and rounded once. D <= BOUTE_MAX_ROW. */
+ * i and rounded once. Outputs overlap inputs only where it says that they may.
+ * D <= BOUTE_MAX_ROW. */
 #define BOUTE_MAX_ROW (1 << 20)
 int boute_expert_dispatch(const void *x, int dtype, long long T, int D, long long ldx,
                           const int *place, int k, void *rows, long long R, long long ldr,

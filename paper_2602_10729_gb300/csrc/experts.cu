@@ -744,7 +744,8 @@ extern "C" int boute_expert_sort(const int *idx, long long T, int k, int E, int 
                                  int *source, int *place, void *stream) {
   BOUTE_TRACE();
   if (T < 0 || k < 1 || E < 1 || !array_ok(offsets, 4) ||
-      (T > 0 && (!array_ok(idx, 4) || !array_ok(source, 4) || !array_ok(place, 4))))
+      (T > 0 && (!array_ok(idx, 4) || !array_ok(source, 4) || !array_ok(place, 4) ||
+                 idx == source || idx == place)))  // (read again after they are written)
     return BOUTE_ERR_INVALID_ARG;
   if (T > 0x7fffffff || k > BOUTE_MAX_CHOICES || T * k > 0x7fffffff || E > BOUTE_MAX_EXPERTS)
     return BOUTE_ERR_UNSUPPORTED;
@@ -852,6 +853,7 @@ extern "C" int boute_expert_dispatch(const void *x, int dtype, long long T, int 
                                      const int *place, int k, void *rows, long long R,
                                      long long ldr, void *stream) {
   BOUTE_TRACE();
+  if (T > 0 && x == rows) return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, x, T, D, ldx, rows, R, ldr, place, k)) return r;
   if (T == 0 || R == 0) return BOUTE_OK;
   const int size = (int)dtype_bytes(dtype), bytes = D * size;
@@ -881,6 +883,7 @@ extern "C" int boute_expert_dispatch_grad(const void *g_rows, int dtype, long lo
                                           long long ldr, const int *place, long long T, int k,
                                           void *dx, long long ldx, void *stream) {
   BOUTE_TRACE();
+  if (T > 0 && dx == g_rows) return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, dx, T, D, ldx, g_rows, R, ldr, place, k)) return r;
   if (T == 0) return BOUTE_OK;
   return combine(g_rows, dtype, R, D, ldr, place, nullptr, T, k, dx, ldx, (cudaStream_t)stream);
@@ -890,7 +893,7 @@ extern "C" int boute_expert_combine(const void *rows, int dtype, long long R, in
                                     const int *place, const float *weight, long long T, int k,
                                     void *out, long long ldo, void *stream) {
   BOUTE_TRACE();
-  if (T > 0 && !array_ok(weight, 4)) return BOUTE_ERR_INVALID_ARG;
+  if (T > 0 && (!array_ok(weight, 4) || out == rows)) return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, out, T, D, ldo, rows, R, ldr, place, k)) return r;
   if (T == 0) return BOUTE_OK;
   return combine(rows, dtype, R, D, ldr, place, weight, T, k, out, ldo, (cudaStream_t)stream);
@@ -904,7 +907,7 @@ extern "C" int boute_expert_combine_grad(const void *g_out, int dtype, long long
   BOUTE_TRACE();
   const int size = (int)dtype_bytes(dtype);
   if ((T > 0 && (!array_ok(weight, 4) || !array_ok(g_weight, 4))) || ldg < D ||
-      (R > 0 && !array_ok(g_rows, size)) || (R > 0 && g_rows == rows && ldg != ldr))
+      (R > 0 && (!array_ok(g_rows, size) || g_rows == g_out || (g_rows == rows && ldg != ldr))))
     return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, g_out, T, D, ldo, rows, R, ldr, place, k)) return r;
   if (T == 0) return BOUTE_OK;

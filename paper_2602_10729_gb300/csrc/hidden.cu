@@ -1248,7 +1248,8 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   if (!(scale > 0.f) || !isfinite(scale) || lddh < D || lddw < D || !array_ok(dweight, 2) ||
       !optional_ok(entropy, 4) || !optional_ok(g_entropy, 4) || (g_entropy && !entropy && T > 0) ||
       (T > 0 && (!array_ok(targets, 8) || !array_ok(lse, 4) || !array_ok(g_logprob, 4) ||
-                 !array_ok(dhidden, 2) || !array_ok(workspace, 256))))
+                 !array_ok(dhidden, 2) || !array_ok(workspace, 256) || dhidden == hidden ||
+                 dweight == weight)))
     return BOUTE_ERR_INVALID_ARG;
   if (int r = sizes_ok(hidden, dtype, T, D, ldh, weight, V, ldw)) return r;
   Plan p = make_plan(hidden, T, D, ldh, weight, V, ldw, true);

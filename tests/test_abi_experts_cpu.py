@@ -8,15 +8,15 @@ from paper_2602_10729_gb300 import boute as bt
 from test_abi_answers_cpu import BAD, ODD, P, UNS, call, lib  # noqa: F401
 from test_abi_answers_devices_cpu import On
 
-Q = ctypes.c_void_p(128)
+Q, G = ctypes.c_void_p(128), ctypes.c_void_p(192)
 H = ctypes.c_void_p(66)  # (aligned to 2 bytes alone)
 
 
 def test_sort_refusals(lib):  # noqa: F811
-    good = dict(idx=P, T=4, k=2, E=9, off=P, src=P, place=P, s=None)
+    good = dict(idx=P, T=4, k=2, E=9, off=Q, src=Q, place=Q, s=None)
     f = lib.boute_expert_sort
     for change in (dict(idx=None), dict(idx=ODD), dict(T=-1), dict(k=0), dict(E=0), dict(off=None),
-                   dict(off=H), dict(src=None), dict(place=H)):
+                   dict(off=H), dict(src=None), dict(place=H), dict(place=P), dict(src=P)):
         assert call(f, good, **change) == BAD, change
     for change in (dict(k=33), dict(E=1025), dict(T=1 << 30), dict(T=1 << 62)):
         assert call(f, good, **change) == UNS, change
@@ -28,24 +28,24 @@ def test_rows_refusals(lib):  # noqa: F811
            dict(R=-1), dict(place=None), dict(place=H), dict(rows=None), dict(x=None))
     uns = (dict(k=33), dict(T=1 << 30), dict(R=1 << 31), dict(D=(1 << 20) + 1, ldx=1 << 21, ldr=1 << 21))
     f = lib.boute_expert_dispatch
-    for change in bad + (dict(x=H), dict(rows=H)):
+    for change in bad + (dict(x=H), dict(rows=H), dict(rows=P)):
         assert call(f, good, **change) == BAD, change
     for change in uns:
         assert call(f, good, **change) == UNS, change
     good = dict(rows=P, dtype=2, R=8, D=10, ldr=12, place=P, T=4, k=2, x=Q, ldx=10, s=None)
-    for change in bad:
+    for change in bad + (dict(x=P),):
         assert call(lib.boute_expert_dispatch_grad, good, **change) == BAD, change
     for change in uns:
         assert call(lib.boute_expert_dispatch_grad, good, **change) == UNS, change
     good = dict(rows=P, dtype=1, R=8, D=10, ldr=12, place=P, w=P, T=4, k=2, x=Q, ldx=10, s=None)
-    for change in bad + (dict(w=None), dict(w=H), dict(x=ODD)):
+    for change in bad + (dict(w=None), dict(w=H), dict(x=ODD), dict(x=P)):
         assert call(lib.boute_expert_combine, good, **change) == BAD, change
     for change in uns:
         assert call(lib.boute_expert_combine, good, **change) == UNS, change
-    good = dict(x=P, dtype=0, T=4, D=10, ldx=10, rows=Q, R=8, ldr=12, place=P, w=P, k=2, g=P, ldg=10,
+    good = dict(x=P, dtype=0, T=4, D=10, ldx=10, rows=Q, R=8, ldr=12, place=P, w=P, k=2, g=G, ldg=10,
                 gw=P, s=None)
     for change in bad + (dict(w=None), dict(gw=None), dict(gw=H), dict(g=None), dict(g=H), dict(ldg=9),
-                         dict(g=Q)):  # (in place with another pitch)
+                         dict(g=P), dict(g=Q)):  # (g_out; in place with another pitch)
         assert call(lib.boute_expert_combine_grad, good, **change) == BAD, change
     for change in uns:
         assert call(lib.boute_expert_combine_grad, dict(good, ldg=1 << 21), **change) == UNS, change

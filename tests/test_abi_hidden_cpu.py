@@ -9,7 +9,7 @@ from test_abi_answers_cpu import BAD, ODD, P, UNS, call, lib  # noqa: F401
 from test_abi_answers_devices_cpu import On
 from test_abi_experts_cpu import launched  # noqa: F401
 
-WS = ctypes.c_void_p(1 << 20)
+WS, Q = ctypes.c_void_p(1 << 20), ctypes.c_void_p(128)
 F32, F16, I64, U8 = torch.float32, torch.float16, torch.int64, torch.uint8
 COMMON = (dict(h=None), dict(h=ODD), dict(w=None), dict(w=ODD), dict(dt=3), dict(dt=-1), dict(T=-1),
           dict(D=0), dict(V=0), dict(ldh=63), dict(ldw=63))
@@ -55,11 +55,11 @@ def test_forward_refusals(lib):  # noqa: F811
 
 def test_gradient_refusals(lib):  # noqa: F811
     good = dict(h=P, dt=1, T=4, D=64, ldh=64, w=P, V=100, ldw=64, t=P, scale=1.0, lse=P, H=P, g=P, gh=P,
-                dh=P, lddh=1 << 17, dw=P, lddw=1 << 17, ws=WS, n=1 << 30, s=None)
+                dh=Q, lddh=1 << 17, dw=Q, lddw=1 << 17, ws=WS, n=1 << 30, s=None)
     f = lib.boute_hidden_logprobs_grad
     for change in COMMON + (dict(t=None), dict(scale=-1.0), dict(lse=None), dict(H=None), dict(H=ODD),
                             dict(g=None), dict(gh=ODD), dict(dh=None), dict(dh=ODD), dict(lddh=63),
-                            dict(dw=None), dict(lddw=63), dict(ws=None), dict(ws=P), dict(n=100)):
+                            dict(dw=None), dict(dh=P), dict(dw=P), dict(lddw=63), dict(ws=None), dict(ws=P), dict(n=100)):
         assert call(f, good, **change) == BAD, change
     for change in LIMITS:
         assert call(f, good, **change) == UNS, change
