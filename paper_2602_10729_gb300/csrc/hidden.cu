@@ -42,12 +42,6 @@ namespace {
 
 constexpr int kThreads = 320, kEpiWarps = 8, kGroup = 128;  // two warps of roles, two groups
 constexpr int kMaxStages = 12;
-// Blocks of the reduction that a logit of the statistics takes on the tensor cores at once. Their
-// sums cut off what fp32 does not hold, step by step; the parts are added up, rounded, in
-// registers.
-// (4096 positions of 32768 tokens, 4096 elements: entropies in one part 2.5e-6 off, in parts of 16
-// blocks 5.4e-7 for 1 % more time, of 8 2.4e-7 for 7 %.)
-constexpr int kPart = 16;
 constexpr int kABytes = 128 * kBlockK * 2;  // a block's half of a stage's rows
 constexpr int kPitch = 36;  // floats of a row of a warp's 32 x 32 transposition
 constexpr float kLn2 = 0.6931471805599453f;
@@ -122,6 +116,7 @@ struct Job {
 struct Jobs {
   Job job[2];
   int units[2], stages, stage_bytes;
+  int part;  // blocks of the reduction that an accumulator takes (statistics in parts)
   // The pairs take the first set's units in turn; those that got one fewer (`light`, from pair
   // light_from on) take `ahead` of the second set first, then all take the rest in turn.
   int light_from, ahead;
@@ -355,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
         const uint64_t ad0 = operand_desc(smem_u32(ring), a_mn);
         const uint64_t bd0 = operand_desc(smem_u32(ring) + kABytes, b_mn);
         const int a_step = desc_step(a_mn), b_step = desc_step(b_mn);
-        const int part = kParted ? kPart : INT_MAX;
+        const int part = kParted ? J.part : INT_MAX;
         for (int k0 = t.k0; ok && (k0 < t.k1 || k0 == t.k0); ++seq) {
           const int k1 = part < t.k1 - k0 ? k0 + part : t.k1;
           const uint32_t acc = seq & 1u, to = tmem + acc * kMaxTileN;
@@ -422,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
         };
         float x[kParted ? MINE : 1][32];
         bool ok = true;
-        for (int k0 = t.k0; k0 < t.k1; k0 += kPart, ++seq) {
+        for (int k0 = t.k0; k0 < t.k1; k0 += J.part, ++seq) {
           const int acc = seq & 1u;
           ok = __all_sync(kAll, pair_wait(&acc_full[acc], (seq >> 1) & 1u, abort));
           if (!ok) break;
@@ -981,6 +976,18 @@ int pairs_of(long long units) {
 }
 int blocks_of(int k) { return (k + kBlockK - 1) / kBlockK; }
 
+// Blocks of the reduction that a logit of the statistics takes on the tensor cores at once, as even
+// as they come. Their sums cut off what fp32 does not hold, step by step; the parts are added up,
+// rounded, in registers. (4096 positions of 32768 tokens, 4096 elements: entropies in one part
+// 2.5e-6 off, in parts of 16 blocks 5.4e-7 for 1 % more time, of 8 2.4e-7 for another 1; with 2048
+// elements 8 cost 2 % more than 16, of 515 positions 10, of up to 64, where the weight is waited
+// for, nothing.)
+int part_of(int D, bool few) {
+  const int blocks = blocks_of(D), most = few || blocks > 32 ? 8 : 16;
+  const int parts = (blocks + most - 1) / most;
+  return (blocks + parts - 1) / parts;
+}
+
 // The number of parts of dh's reduction over a piece, each a unit of its own of the pairs: the
 // fewest whose units are small beside a pair's share of the whole launch (other: dW's part of it),
 // so that dW's units even the pairs out.
@@ -1220,7 +1227,8 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
     if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
                          p.rows ? 128 : W.tile_n / 2))
       return r;
-    const bool parted = blocks_of(D) > kPart;
+    J.part = part_of(D, !p.rows && W.tile_n <= 64);
+    const bool parted = J.part < blocks_of(D);
     if (parted && p.rows) parts *= 2;  // (of both groups' columns)
     int (*start)(int, Jobs &, cudaStream_t) =
         p.rows ? (parted ? launch<kStatsRows, 4> : launch<kStatsRows>)
