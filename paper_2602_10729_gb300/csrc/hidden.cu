@@ -979,11 +979,10 @@ int blocks_of(int k) { return (k + kBlockK - 1) / kBlockK; }
 // Blocks of the reduction that a logit of the statistics takes on the tensor cores at once, as even
 // as they come. Their sums cut off what fp32 does not hold, step by step; the parts are added up,
 // rounded, in registers. (4096 positions of 32768 tokens, 4096 elements: entropies in one part
-// 2.5e-6 off, in parts of 16 blocks 5.4e-7 for 1 % more time, of 8 2.4e-7 for another 1; with 2048
-// elements 8 cost 2 % more than 16, of 515 positions 10, of up to 64, where the weight is waited
-// for, nothing.)
+// 2.5e-6 off, in parts of 16 blocks 5.4e-7 for 1 % more time, of 8 2.4e-7 for another 1 to 3, at 515
+// positions 10, up to 64, where the weight is waited for, nothing.)
 int part_of(int D, bool few) {
-  const int blocks = blocks_of(D), most = few || blocks > 32 ? 8 : 16;
+  const int blocks = blocks_of(D), most = few ? 8 : 16;
   const int parts = (blocks + most - 1) / most;
   return (blocks + parts - 1) / parts;
 }
