@@ -77,6 +77,8 @@ inline bool optional_ok(const void *p, size_t bytes) { return p == nullptr || ar
 
 constexpr unsigned kAll = 0xffffffffu;
 constexpr float kLog2e = 1.4426950408889634f;
+// Gradients take ln s and the largest logit from the row itself where |lse| is beyond this.
+constexpr float kLargeLse = 1024.f;
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

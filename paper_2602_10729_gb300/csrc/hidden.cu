@@ -7,6 +7,8 @@
 // The gradient takes the logits again, piece by piece of the vocabulary, as coefficients
 //   c_tj = scale (g ([j = t] - p_j) - g_H p_j (ln p_j + H)),
 // of which dh = c W and dW = c^T h are two more products.
+// Where |lse| is large its rounding would be in every p: the statistics are taken once more before
+// that, in a launch that ends at once where no position needs it.
 //
 // All products run on the tensor cores. A pair of blocks takes tiles of 256 rows x up to 256
 // columns, one warp bringing operand tiles, one issuing products, and two groups of four warps
@@ -54,25 +56,34 @@ enum Kind { kStatsCols, kStatsRows, kCoefCols, kCoefRows, kGrads };
 
 // At the start of a call's workspace.
 constexpr int kBlocks = 256;  // of a launch at most
-constexpr int kBounds = 64;
+constexpr int kBounds = BOUTE_MAX_HIDDEN / 256;
 struct Header {
-  // BOUTE_ERR_TIMEOUT where a wait ran out: of each block of the statistics' launch, which writes
-  // its own; of all launches of the gradient, which clears it first
-  int status[kBlocks];
-  // bits of the largest bound of a coefficient, of each block that looked
+  // BOUTE_ERR_TIMEOUT where a wait ran out: in the gradient's launches, which clear it first; in each
+  // block of the statistics' launch, which writes its own
+  int late, status[kBlocks];
+  // bits of the largest bound of a coefficient, of each 256 positions
   unsigned largest[kBounds];
 };
-// What the coefficients of a position need.
+// What the coefficients of a position need: p = e^lp, lp = (x - m) scale - ls, p (a + b lp), + g at
+// its target.
 struct Position {
-  float lse, a, b, g;  // p (a + b ln p), + g at its target
+  float m, ls, a, b;
 };
+struct Target {
+  int j;  // -1 for none
+  float g;
+};
+
+// Whether lse's rounding (2^-24 of it) would show in p. Such positions' coefficients take the largest
+// logit and ln s from the logits, which are then summed once more; with the difference first, the
+// rounding of the product by the scale is no larger than lp's.
+__device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) > kLargeLse && isfinite(lse); }
 
 // The power of two by which the coefficients are scaled while they are 16-bit numbers: the largest
 // comes to 2^14 (fp16: what is 2^-28 of that has all its bits, and 2^-39 some). For whole warps.
 __device__ __forceinline__ float coef_scale(const Header *head, int bounds, bool inverse) {
-  const int lane = threadIdx.x & 31;
-  unsigned largest = lane < bounds ? head->largest[lane] : 0u;
-  if (lane + 32 < bounds) largest = max(largest, head->largest[lane + 32]);
+  unsigned largest = 0u;
+  for (int i = threadIdx.x & 31; i < bounds; i += 32) largest = max(largest, head->largest[i]);
   largest = __reduce_max_sync(kAll, largest);
   const int e = (int)(largest >> 23) - 127;  // (the largest is in [2^e, 2^(e + 1)))
   if (largest == 0u || largest >= 0x7f800000u) return 1.f;
@@ -92,10 +103,11 @@ struct Work {
   float *part;              // 3 x parts x Tp: maxima, s, u
   float *picked;            // Tp: x of the targets
   const long long *targets;
+  const float *lse;         // the launch is for far positions alone; NULL: for all
   long long Tp;             // (coefficients: the pitch of coef)
   // coefficients
   const Position *pos;
-  const int *tgt;           // targets, -1 for none
+  const Target *tgt;
   float scale;
   uint16_t *coef;           // a piece's: tokens x positions, or positions x tokens
   int low;                  // columns on, what rounding left of each follows (0: none kept)
@@ -169,7 +181,7 @@ constexpr int kBoxBytes = 4096;
 template <Kind KIND>
 constexpr int kBoxes = KIND == kStatsCols ? kEpiWarps * 32 * kPitch * 4 + 2 * 4 * kMaxTileN * 12
                        : KIND == kCoefCols
-                           ? 2 * kMaxTileN * (int)(sizeof(Position) + sizeof(int))
+                           ? 2 * kMaxTileN * (int)(sizeof(Position) + sizeof(Target))
                            : 0;
 template <Kind KIND>
 constexpr int kEpi =
@@ -290,8 +302,17 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
   const uint32_t tmem = tmem_holder;
   pdl_wait();
   pdl_trigger();
+  bool idle = false;  // (alike in both blocks)
+  if (kStats && J.job[0].w.lse) {
+    const Work &W = J.job[0].w;
+    const int n = KIND == kStatsRows ? W.M : W.N;
+    bool far = false;
+    for (int i = tid; i < n; i += kThreads) far |= BOUTE_INB(i, W.Tp) && is_far(W.lse[i]);
+    idle = !__syncthreads_or(far);
+  }
 
-  if (warp == 0) {
+  if (idle) {
+  } else if (warp == 0) {
     // ------------------------------------------------------------------ operand tiles
     if (lane == 0) {
       int s = 0, used = 0;
@@ -509,27 +530,30 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
         const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32, col = t.n * W.tile_n;
         // what does not wait for the products
         Position *pos = (Position *)epi + group * kMaxTileN;
-        int *tgt = (int *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
-        Position own = {1e30f, 0.f, 0.f, 0.f};
+        Target *tgt = (Target *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
+        Position own = {0.f, 1e30f, 0.f, 0.f};
         int target = -1;
+        float target_g = 0.f;
         if constexpr (KIND == kCoefCols) {
           named_barrier_sync(1 + group, kGroup);  // (the last tile's are read)
           for (int c = gtid; c < W.tile_n; c += kGroup) {
-            Position p = {1e30f, 0.f, 0.f, 0.f};
-            int j = -1;
+            Position p = {0.f, 1e30f, 0.f, 0.f};
+            Target to = {-1, 0.f};
             if (col + c < W.N && BOUTE_INB(col + c, W.N)) {
               p = W.pos[col + c];
-              p.a *= mul, p.b *= mul, p.g *= mul;
-              j = W.tgt[col + c] - W.row0;
+              p.a *= mul, p.b *= mul;
+              to = W.tgt[col + c];
+              to.j -= W.row0, to.g *= mul;
             }
             pos[c] = p;
-            tgt[c] = j;
+            tgt[c] = to;
           }
         } else if constexpr (KIND == kCoefRows) {
           if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
             own = W.pos[row + lane];
-            own.a *= mul, own.b *= mul, own.g *= mul;
-            target = W.tgt[row + lane] - W.row0;
+            own.a *= mul, own.b *= mul;
+            target = W.tgt[row + lane].j - W.row0;
+            target_g = W.tgt[row + lane].g * mul;
           }
         } else if constexpr (KIND == kStatsRows) {
           if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
@@ -599,18 +623,18 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
                 if (target == d0 + q) W.picked[row + lane] = x[q];
             join(run, stat_of(x, W.c2), W.c2);
           } else if constexpr (KIND == kCoefCols) {
-            const int j = tgt[c * 32 + lane];
+            const int j = tgt[c * 32 + lane].j;
             unsigned here = __ballot_sync(kAll, j >= row && j < row + 32);
 #pragma unroll
             for (int q = 0; q < 32; ++q) {
               const Position p = pos[c * 32 + q];
-              const float lp = max_nan(fmaf(x[q], W.scale, -p.lse), -1e4f);
+              const float lp = max_nan(fmaf(x[q] - p.m, W.scale, -p.ls), -1e4f);
               x[q] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
             }
             if (here)
 #pragma unroll
               for (int q = 0; q < 32; ++q)
-                if ((here >> q & 1u) && tgt[c * 32 + q] == row + lane) x[q] += pos[c * 32 + q].g;
+                if ((here >> q & 1u) && tgt[c * 32 + q].j == row + lane) x[q] += tgt[c * 32 + q].g;
             if (d0 + 32 > W.N)  // (columns of no position, which a token of infinities makes NaN)
 #pragma unroll
               for (int q = 0; q < 32; ++q)
@@ -625,12 +649,13 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
               store_row_of<T>(to + W.low, x);
             }
           } else if constexpr (KIND == kCoefRows) {
-            const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.lse);
+            const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.ls);
+            const unsigned long long top = f2_dup(-own.m);
             const unsigned long long a2 = f2_dup(own.a), b2 = f2_dup(own.b), l2e = f2_dup(kLog2e);
 #pragma unroll
             for (int q = 0; q < 32; q += 2) {
               float l0, l1, y0, y1;
-              f2_split(f2_fma(f2_pack(x[q], x[q + 1]), by, less), l0, l1);
+              f2_split(f2_fma(f2_add(f2_pack(x[q], x[q + 1]), top), by, less), l0, l1);
               const unsigned long long lp = f2_pack(max_nan(l0, -1e4f), max_nan(l1, -1e4f));
               f2_split(f2_mul(lp, l2e), y0, y1);
               f2_split(f2_mul(f2_pack(exp2_fast(y0), exp2_fast(y1)), f2_fma(b2, lp, a2)), x[q],
@@ -639,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
             if (__any_sync(kAll, target >= d0 && target < d0 + 32))
 #pragma unroll
               for (int q = 0; q < 32; ++q)
-                if (target == d0 + q) x[q] += own.g;
+                if (target == d0 + q) x[q] += target_g;
             send(c, x);
           } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
             if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
@@ -732,7 +757,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
   __syncthreads();
   Header *head = J.job[0].w.head;
   if (tid == 0 && kStats) head->status[blockIdx.x] = *abort ? BOUTE_ERR_TIMEOUT : 0;
-  if (tid == 0 && !kStats && *abort) set_status(head->status, BOUTE_ERR_TIMEOUT);
+  if (tid == 0 && !kStats && *abort) set_status(&head->late, BOUTE_ERR_TIMEOUT);
   cluster_sync();
   if (warp == 1) pair_tmem_dealloc(tmem, 512);
 }
@@ -800,41 +825,52 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   lse[t] = l;
 }
 
-// What each position's coefficients need, and the largest bound of one: |p (ln p + H)| < 4 for
-// every distribution over BOUTE_MAX_VOCAB tokens.
+// What each position's coefficients need, of 256 positions a block, and the largest bound of one:
+// |p (ln p + H)| < 4 for every distribution over BOUTE_MAX_VOCAB tokens. Far positions take their
+// largest logit and ln s from the statistics' parts (a thread each: 4096 of 131072 tokens 0.2 ms).
 __global__ void __launch_bounds__(256)
-    hidden_positions_kernel(Header *head, const long long *targets, long long T, int V,
-                            float scale, const float *lse, const float *entropy,
-                            const float *g_logprob, const float *g_entropy, Position *pos,
-                            int *tgt) {
+    hidden_positions_kernel(Header *head, int blocks, const long long *targets, long long t0,
+                            long long T, int V, float scale, const float *lse,
+                            const float *entropy, const float *g_logprob, const float *g_entropy,
+                            const float *part, int parts, long long Tp, Position *pos,
+                            Target *tgt) {
   __shared__ unsigned red[8];
   pdl_wait();
   pdl_trigger();
+  const long long i = blockIdx.x * 256ll + threadIdx.x, t = t0 + i, all = parts * Tp;
   float bound = 0.f;
   bool nan = false;
-  for (long long t = blockIdx.x * 256ll + threadIdx.x; t < T; t += gridDim.x * 256ll) {
-    if (!BOUTE_INB(t, T)) break;
+  if (t < T && BOUTE_INB(t, T)) {
     const long long target = targets[t];
     const float g = target < 0 ? 0.f : g_logprob[t], gh = g_entropy ? g_entropy[t] : 0.f;
-    Position p = {lse[t], -scale * g, -scale * gh, scale * g};
+    Position p = {0.f, lse[t], -scale * g, -scale * gh};
+    Target to = {target >= 0 && target < V ? (int)target : -1, scale * g};
     if (g_entropy) p.a -= scale * gh * entropy[t];
     const float most = scale * (fabsf(g) + 4.f * fabsf(gh));
-    bound = fmaxf(bound, most);
-    nan |= isnan(most);
-    if (p.lse == -INFINITY) p = {1e30f, 0.f, 0.f, 0.f};  // a row without a token left
+    bound = most;
+    nan = isnan(most);
+    if (is_far(p.ls)) {
+      Stat a = {-INFINITY, 0.f, 0.f};
+      for (int q = 0; q < parts; ++q)
+        if (BOUTE_INB(q * Tp + i, all))
+          join(a, {part[q * Tp + i], part[all + q * Tp + i], 0.f}, scale * kLog2e);
+      p.m = a.m;
+      p.ls = logf(a.s);
+    }
+    if (p.ls == -INFINITY) p = {0.f, 1e30f, 0.f, 0.f}, to.g = 0.f;  // a row without a token left
     if (target >= V) p.a = NAN;
     pos[t] = p;
-    tgt[t] = target >= 0 && target < V ? (int)target : -1;
+    tgt[t] = to;
   }
   const unsigned most =
       __reduce_max_sync(kAll, nan ? 0x7fffffffu : __float_as_uint(bound));
   if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = most;
-  __syncthreads();
+  const bool late = __syncthreads_or(threadIdx.x < blocks && head->status[threadIdx.x] != 0);
   if (threadIdx.x == 0) {
     unsigned all = 0;
     for (int w = 0; w < 8; ++w) all = max(all, red[w]);
-    head->largest[blockIdx.x] = all;
-    if (blockIdx.x == 0) head->status[0] = 0;
+    head->largest[t0 / 256 + blockIdx.x] = all;
+    if (blockIdx.x == 0 && (t0 == 0 || late)) head->late = late ? BOUTE_ERR_TIMEOUT : 0;
   }
 }
 
@@ -877,7 +913,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] += x[j][e];
   }
-  const bool late = head->status[0] != 0;
+  const bool late = head->late != 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) dh[t * ldd + d + e] = from_float<T>(late ? NAN : mul * v[e]);
 }
@@ -962,6 +998,7 @@ struct Plan {
   bool fine;               // the coefficients have low parts
   int tiles_t, tile_t;     // of the positions in columns
   int tile_m;              // a block's tokens of the vocabulary (statistics in columns)
+  long long part_Tp;       // the pitch of the statistics' parts: positions of one pass
   long long Tp;            // the positions with what the last tile has beyond them
   int piece;               // tokens of the vocabulary at once (gradient)
   int splits;              // of dh's reduction
@@ -1025,12 +1062,14 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
     return from;
   };
   p.header = take(sizeof(Header));
+  p.tile_m = !grad && !p.rows && p.tiles_t == 1 ? even_rows(V) : 128;
+  p.part_Tp = std::min(p.Tp, kAtOnce);
+  const long long parts = p.rows ? 2ll * ((V + kMaxTileN - 1) / kMaxTileN)
+                                 : 2ll * ((V + 2 * p.tile_m - 1) / (2 * p.tile_m));
+  p.picked = take(p.part_Tp * sizeof(float));
+  const size_t part = 3 * sizeof(float) * (size_t)(parts * p.part_Tp);
   if (!grad) {
-    p.tile_m = p.tiles_t == 1 ? even_rows(V) : 128;
-    const long long parts = p.rows ? 2ll * ((V + kMaxTileN - 1) / kMaxTileN)
-                                   : 2ll * ((V + 2 * p.tile_m - 1) / (2 * p.tile_m));
-    p.part = take(3ull * parts * p.Tp * sizeof(float));
-    p.picked = take(p.Tp * sizeof(float));
+    p.part = take(part);
   } else {
     p.piece = (int)std::min<long long>(
         up(V, kPairM),
@@ -1046,8 +1085,9 @@ Plan make_plan(const void *h, long long T, int D, long long ldh, const void *w, 
                          each,
                          num_sms() / 2);
     p.pos = take(p.Tp * sizeof(Position));
-    p.tgt = take(p.Tp * sizeof(int));
-    p.coef = take((size_t)p.piece * p.columns() * 2);
+    p.tgt = take(p.Tp * sizeof(Target));
+    // (the statistics of far positions come before the coefficients)
+    p.part = p.coef = take(std::max<size_t>(part, (size_t)p.piece * p.columns() * 2));
     p.sums = take(p.splits * each);
   }
   if (p.h.moved) p.h_at = take((size_t)T * p.h.ld * 2);
@@ -1117,6 +1157,48 @@ int align_operand(Operand &x, long long rows, int D, long long ld, char *to, cud
                                (const uint16_t *)x.p, rows, D, ld, (uint16_t *)to, (int)x.ld);
   x.p = to;
   return r;
+}
+
+// The statistics of n positions from t0 on, in W.part; of far ones alone where W.lse is there.
+// parts: of each position, blocks: whose status is written.
+int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, const Work &with,
+                 cudaStream_t s, int &parts, int &blocks) {
+  Jobs J{};
+  Work &W = J.job[0].w;
+  W = with;
+  W.K = D;
+  W.tile_m = p.tile_m;
+  W.splits = 1;
+  W.Tp = p.part_Tp;
+  CUtensorMap *mh = p.rows ? &J.job[0].a : &J.job[0].b, *mw = p.rows ? &J.job[0].b : &J.job[0].a;
+  if (int r = make_map(mw, dtype, p.w.p, D, V, p.w.ld, p.rows ? kMaxTileN / 2 : p.tile_m)) return r;
+  if (p.rows) {
+    W.M = n, W.N = V;
+    W.nM = (n + kPairM - 1) / kPairM;
+    W.nN = parts = (V + kMaxTileN - 1) / kMaxTileN;
+    W.tile_n = kMaxTileN;
+    W.rows_first = 1;
+  } else {
+    W.M = V, W.N = n;
+    W.nM = (V + 2 * p.tile_m - 1) / (2 * p.tile_m);
+    parts = 2 * W.nM;
+    tile_columns(n, W.nN, W.tile_n);
+  }
+  if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
+                       p.rows ? 128 : W.tile_n / 2))
+    return r;
+  // (the coefficients' logits are in one part, and a far position's x - m has to be of equal sums)
+  J.part = W.lse ? blocks_of(D) : part_of(D, !p.rows && W.tile_n <= 64);
+  const bool parted = J.part < blocks_of(D);
+  if (parted && p.rows) parts *= 2;  // (of both groups' columns)
+  int (*start)(int, Jobs &, cudaStream_t) =
+      p.rows ? (parted ? launch<kStatsRows, 4> : launch<kStatsRows>)
+                     : !parted         ? launch<kStatsCols>
+                     : W.tile_n <= 64 ? launch<kStatsCols, 1>
+                                      : launch<kStatsCols, 4>;
+  if (int r = start(dtype, J, s)) return r;
+  blocks = 2 * pairs_of(J.units[0]);
+  return BOUTE_OK;
 }
 
 int sizes_ok(const void *h, int dtype, long long T, int D, long long ldh, const void *w, int V,
@@ -1194,51 +1276,19 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
   char *ws = (char *)workspace;
   if (int r = align_operand(p.h, T, D, ldh, ws + p.h_at, s)) return r;
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
-  const int tile_m = p.rows ? 128 : p.tile_m;
-  Jobs J{};
-  Work &W = J.job[0].w;
-  W.K = D;
-  W.tile_m = tile_m;
-  W.splits = 1;
+  Work W{};
   W.head = (Header *)(ws + p.header);
   W.c2 = scale * kLog2e;
   W.part = (float *)(ws + p.part);
   W.picked = (float *)(ws + p.picked);
-  W.Tp = p.Tp;
-  CUtensorMap *mh = p.rows ? &J.job[0].a : &J.job[0].b, *mw = p.rows ? &J.job[0].b : &J.job[0].a;
-  if (int r = make_map(mw, dtype, p.w.p, D, V, p.w.ld, p.rows ? kMaxTileN / 2 : tile_m)) return r;
   for (long long t0 = 0; t0 < T; t0 += kAtOnce) {
     const int n = (int)std::min(kAtOnce, T - t0);
     W.targets = targets + t0;
-    int parts;
-    if (p.rows) {
-      W.M = n, W.N = V;
-      W.nM = (n + kPairM - 1) / kPairM;
-      W.nN = parts = (V + kMaxTileN - 1) / kMaxTileN;
-      W.tile_n = kMaxTileN;
-      W.rows_first = 1;
-    } else {
-      W.M = V, W.N = n;
-      W.nM = (V + 2 * tile_m - 1) / (2 * tile_m);
-      parts = 2 * W.nM;
-      tile_columns(n, W.nN, W.tile_n);
-    }
-    if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
-                         p.rows ? 128 : W.tile_n / 2))
-      return r;
-    J.part = part_of(D, !p.rows && W.tile_n <= 64);
-    const bool parted = J.part < blocks_of(D);
-    if (parted && p.rows) parts *= 2;  // (of both groups' columns)
-    int (*start)(int, Jobs &, cudaStream_t) =
-        p.rows ? (parted ? launch<kStatsRows, 4> : launch<kStatsRows>)
-                       : !parted         ? launch<kStatsCols>
-                       : W.tile_n <= 64 ? launch<kStatsCols, 1>
-                                        : launch<kStatsCols, 4>;
-    if (int r = start(dtype, J, s)) return r;
+    int parts, blocks;
+    if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks)) return r;
     if (int r = launch_cluster(hidden_join_kernel, (n + kJoinAt - 1) / kJoinAt, 32 * kJoinWarps, 1,
-                               0, s, W.head, 2 * pairs_of(J.units[0]), W.part, W.picked,
-                               W.targets, n, W.Tp, parts, V, scale, W.c2, logprob + t0,
-                               entropy + t0, lse + t0))
+                               0, s, W.head, blocks, W.part, W.picked, W.targets, n, p.part_Tp,
+                               parts, V, scale, W.c2, logprob + t0, entropy + t0, lse + t0))
       return r;
   }
   return BOUTE_OK;
@@ -1273,14 +1323,25 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
   W.head = (Header *)(ws + p.header);
-  W.bounds = (int)std::min<long long>(kBounds, (T + 255) / 256);
+  Position *pos = (Position *)(ws + p.pos);
+  Target *tgt = (Target *)(ws + p.tgt);
+  W.c2 = scale * kLog2e;
+  W.part = (float *)(ws + p.part);
+  W.picked = (float *)(ws + p.picked);
+  for (long long t0 = 0; t0 < T; t0 += kAtOnce) {
+    const int n = (int)std::min(kAtOnce, T - t0);
+    W.targets = targets + t0;
+    W.lse = lse + t0;
+    int parts, blocks;
+    if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks)) return r;
+    if (int r = launch_cluster(hidden_positions_kernel, (n + 255) / 256, 256, 1, 0, s, W.head,
+                               blocks, targets, t0, t0 + n, V, scale, lse, entropy, g_logprob,
+                               g_entropy, W.part, parts, p.part_Tp, pos, tgt))
+      return r;
+  }
+  W.bounds = (int)((T + 255) / 256);
   W.tile_m = 128;
   W.splits = 1;
-  Position *pos = (Position *)(ws + p.pos);
-  int *tgt = (int *)(ws + p.tgt);
-  if (int r = launch_cluster(hidden_positions_kernel, W.bounds, 256, 1, 0, s, W.head, targets, T, V,
-                             scale, lse, entropy, g_logprob, g_entropy, pos, tgt))
-    return r;
   W.pos = pos;
   W.tgt = tgt;
   W.scale = scale;

@@ -505,11 +505,10 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 }
 
-// Beyond this |lse| its rounding (2^-24 of it) would show in p: rows whose mask is the type's
+// Beyond kLargeLse the rounding of lse (2^-24 of it) would show in p: rows whose mask is the type's
 // lowest value throughout have an lse that has lost ln s, and take the largest logit and ln s from
 // the row. The product of that logit and the scale has a rounding of the same size, so lp is then
 // (x - max x) scale - ln s: the difference comes first, as in the sums.
-constexpr float kLargeLse = 1024.f;
 
 // With lp_j = z_j - lse and p_j = exp(lp_j):
 //   dlogits_j = p_j (A + B lp_j) + scale g [j = t],  A = -scale (g + gh H),  B = -scale gh.
