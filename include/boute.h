@@ -758,8 +758,8 @@ int boute_hidden_logprobs(const void *hidden, int dtype, long long T, int D, lon
  *   dhidden = dlogits weight (T rows of D, pitch lddh), dweight = dlogits^T hidden (V rows, lddw),
  * rounded once to the type from fp32 sums. The products take each dlogits_tj rounded to the type, of
  * up to 32 positions as the sum of two such numbers (times a power of two, by which the largest
- * coefficient that the gradients allow comes near 2^14; what is less than 2^-28 of it loses bits in
- * fp16). At most 256 MB of them are held at a time (512 bytes a position, if that is more). dhidden
+ * coefficient that the finite gradients allow comes near 2^14; what is less than 2^-28 of it loses
+ * bits in fp16; positions without a distribution do not count). At most 256 MB of them are held at a time (512 bytes a position, if that is more). dhidden
  * and dweight overlap no input. */
 int boute_hidden_logprobs_grad(const void *hidden, int dtype, long long T, int D, long long ldh,
                                const void *weight, int V, long long ldw, const long long *targets,

@@ -86,7 +86,7 @@ __device__ __forceinline__ float coef_scale(const Header *head, int bounds, bool
   for (int i = threadIdx.x & 31; i < bounds; i += 32) largest = max(largest, head->largest[i]);
   largest = __reduce_max_sync(kAll, largest);
   const int e = (int)(largest >> 23) - 127;  // (the largest is in [2^e, 2^(e + 1)))
-  if (largest == 0u || largest >= 0x7f800000u) return 1.f;
+  if (largest == 0u) return 1.f;
   const int k = min(max(13 - e, -126), 126);
   return exp2i(inverse ? -k : k);
 }
@@ -826,7 +826,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 }
 
 // What each position's coefficients need, of 256 positions a block, and the largest bound of one:
-// |p (ln p + H)| < 4 for every distribution over BOUTE_MAX_VOCAB tokens. Far positions take their
+// |p (ln p + H)| < 4 for every distribution over BOUTE_MAX_VOCAB tokens. Positions that have no
+// coefficients, or none that are numbers, set no bound: the scale is the others'. Far positions take their
 // largest logit and ln s from the statistics' parts (a thread each: 4096 of 131072 tokens 0.2 ms).
 __global__ void __launch_bounds__(256)
     hidden_positions_kernel(Header *head, int blocks, const long long *targets, long long t0,
@@ -839,16 +840,12 @@ __global__ void __launch_bounds__(256)
   pdl_trigger();
   const long long i = blockIdx.x * 256ll + threadIdx.x, t = t0 + i, all = parts * Tp;
   float bound = 0.f;
-  bool nan = false;
   if (t < T && BOUTE_INB(t, T)) {
     const long long target = targets[t];
     const float g = target < 0 ? 0.f : g_logprob[t], gh = g_entropy ? g_entropy[t] : 0.f;
     Position p = {0.f, lse[t], -scale * g, -scale * gh};
     Target to = {target >= 0 && target < V ? (int)target : -1, scale * g};
     if (g_entropy) p.a -= scale * gh * entropy[t];
-    const float most = scale * (fabsf(g) + 4.f * fabsf(gh));
-    bound = most;
-    nan = isnan(most);
     if (is_far(p.ls)) {
       Stat a = {-INFINITY, 0.f, 0.f};
       for (int q = 0; q < parts; ++q)
@@ -857,13 +854,14 @@ __global__ void __launch_bounds__(256)
       p.m = a.m;
       p.ls = logf(a.s);
     }
+    const float most = scale * (fabsf(g) + 4.f * fabsf(gh));
+    if (isfinite(most) && p.ls > -INFINITY && target < V) bound = most;
     if (p.ls == -INFINITY) p = {0.f, 1e30f, 0.f, 0.f}, to.g = 0.f;  // a row without a token left
     if (target >= V) p.a = NAN;
     pos[t] = p;
     tgt[t] = to;
   }
-  const unsigned most =
-      __reduce_max_sync(kAll, nan ? 0x7fffffffu : __float_as_uint(bound));
+  const unsigned most = __reduce_max_sync(kAll, __float_as_uint(bound));
   if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = most;
   const bool late = __syncthreads_or(threadIdx.x < blocks && head->status[threadIdx.x] != 0);
   if (threadIdx.x == 0) {
