@@ -298,9 +298,10 @@ __global__ void __launch_bounds__(kScanThreads) expert_scan_kernel(Order A) {
 
 // The choices are put in order within the block first: neighbours then write neighbouring sources
 // (1048576 choices of 256: 16.8 us with each lane's own store to its place).
+constexpr size_t sort_smem_bytes(int E) { return (size_t)(kSortWarps + 2) * (E + 1) * sizeof(int); }
 template <int STEPS>
-constexpr size_t place_smem(int E) {
-  return ((size_t)(kSortWarps + 2) * (E + 1) + 2 * kSortThreads * STEPS) * sizeof(int);
+constexpr size_t place_smem_bytes(int E) {
+  return sort_smem_bytes(E) + 2 * kSortThreads * STEPS * sizeof(int);
 }
 template <int STEPS>
 __global__ void __launch_bounds__(kSortThreads) expert_place_kernel(Order A) {
@@ -753,30 +754,29 @@ extern "C" int boute_expert_sort(const int *idx, long long T, int k, int E, int 
   const long long N = T * k;
   const cudaStream_t s = (cudaStream_t)stream;
   Order A{idx, N, E, 0, 0, 0, offsets, source, place};
-  const size_t hist = (size_t)kSortWarps * (E + 1) * sizeof(int);
-  auto allow = [](auto *kernel, size_t bytes) {
-    return bytes <= 48 * 1024 ||
-           cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)bytes) == cudaSuccess;
-  };
   auto go = [&](auto steps) -> int {
     constexpr int STEPS = decltype(steps)::value;
     A.blocks = (int)std::max(1ll, (N + kSortThreads * STEPS - 1) / (kSortThreads * STEPS));
     A.each = (int)(N / A.blocks);
     A.more = (int)(N % A.blocks);
     if (A.blocks <= kMaxCluster) {
-      const size_t smem = hist + 2 * (E + 1) * sizeof(int);
-      if (!allow(expert_sort_kernel<STEPS>, smem)) return last_launch_status();
-      return launch_cluster(expert_sort_kernel<STEPS>, A.blocks, kSortThreads, A.blocks, smem, s,
-                            A);
+      static std::atomic<unsigned long long> allowed{0};
+      if (int r = allow_smem((const void *)expert_sort_kernel<STEPS>,
+                             sort_smem_bytes(BOUTE_MAX_EXPERTS), allowed))
+        return r;
+      return launch_cluster(expert_sort_kernel<STEPS>, A.blocks, kSortThreads, A.blocks,
+                            sort_smem_bytes(E), s, A);
     }
-    const size_t smem = place_smem<STEPS>(E);
-    if (!allow(expert_place_kernel<STEPS>, smem)) return last_launch_status();
+    static std::atomic<unsigned long long> allowed{0};
+    if (int r = allow_smem((const void *)expert_place_kernel<STEPS>,
+                           place_smem_bytes<STEPS>(BOUTE_MAX_EXPERTS), allowed))
+      return r;
     if (int r = launch_cluster(expert_count_kernel<STEPS>, A.blocks, kSortThreads, 1, 0, s, A))
       return r;
     if (int r = launch_cluster(expert_scan_kernel, kMaxCluster, kScanThreads, kMaxCluster, 0, s, A))
       return r;
-    return launch_cluster(expert_place_kernel<STEPS>, A.blocks, kSortThreads, 1, smem, s, A);
+    return launch_cluster(expert_place_kernel<STEPS>, A.blocks, kSortThreads, 1,
+                          place_smem_bytes<STEPS>(E), s, A);
   };
   // One launch of a cluster as far as it goes (24594 choices: 6.7 us, 8.3 in three); behind it
   // small blocks that fill the SMs, but for many choices, of which the blocks' counts would be most

@@ -34,7 +34,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "pair_mma.cuh"
 
@@ -1130,17 +1129,8 @@ int launch(int dtype, Jobs &J, cudaStream_t s) {
     if constexpr (std::is_same<T, float>::value) {
       return (int)BOUTE_ERR_INVALID_ARG;
     } else {
-      static std::atomic<unsigned long long> allowed{0};  // of the first 64 devices
-      int dev = 0;
-      if (cudaGetDevice(&dev) != cudaSuccess) return last_launch_status();
-      const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
-      if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute((const void *)hidden_kernel<KIND, T, MINE>,
-                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)kSmem) != cudaSuccess)
-          return last_launch_status();
-        allowed.fetch_or(bit, std::memory_order_relaxed);
-      }
+      static std::atomic<unsigned long long> allowed{0};
+      if (int r = allow_smem((const void *)hidden_kernel<KIND, T, MINE>, kSmem, allowed)) return r;
       const size_t smem = 1024 + (size_t)J.stages * J.stage_bytes + kEpi<KIND>;
       return launch_cluster(hidden_kernel<KIND, T, MINE>, 2 * pairs, kThreads, 2, smem, s, J);
     }
