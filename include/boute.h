@@ -741,7 +741,7 @@ int boute_expert_combine_grad(const void *g_out, int dtype, long long T, int D, 
  *   gives for the same arguments (grad: for which of the calls); its contents need not be kept
  *   between calls. Calls that may run at the same time need one each.
  * A device-side wait that gives up (2 s; nothing hangs) makes all outputs of the call NaN, but for
- * dweight, of which a part is then not written.
+ * dweight, of which parts may then hold their gradient already, or not be written.
  * 0 <= T <= BOUTE_MAX_HIDDEN, 1 <= D <= BOUTE_MAX_HIDDEN_SIZE, 1 <= V <= BOUTE_MAX_VOCAB. */
 #define BOUTE_MAX_HIDDEN (1 << 20)
 #define BOUTE_MAX_HIDDEN_SIZE (1 << 16)

@@ -521,6 +521,8 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
     } else {
       float mul = 1.f;
       if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
+      // (of coefficients of which a wait left out some, no number is written)
+      if (KIND == kGrads && *(volatile int *)&J.job[0].w.head->late != 0) mul = NAN;
       for (int i = group;; i += 2) {
         const Unit t = unit_of<KIND>(J, pair, pairs, i);
         if (t.job < 0) break;
