@@ -90,6 +90,16 @@ __device__ __forceinline__ float coef_scale(const Header *head, int bounds, bool
   return exp2i(inverse ? -k : k);
 }
 
+// Powers of two of logits' differences: (x - m) k c, where k = 2 if c = scale log2 e would be infinite
+// (of a scale above 2.3e38: 0 times it would be NaN).
+struct Exponents {
+  float k, c;
+};
+Exponents exponents_of(float scale) {
+  return scale * kLog2e <= FLT_MAX ? Exponents{1.f, scale * kLog2e}
+                                   : Exponents{2.f, scale * 0.5f * kLog2e};
+}
+
 struct Work {
   int M, N, K;              // rows, columns, reduction
   int tile_m, tile_n, nM, nN, splits;  // (tile_m: rows of a block, 128 but for few positions)
@@ -98,7 +108,7 @@ struct Work {
   Header *head;
   int bounds;               // values of head->largest
   // statistics
-  float c2;
+  Exponents c2;
   float *part;              // 3 x parts x Tp: maxima, s, u
   float *picked;            // Tp: x of the targets
   const long long *targets;
@@ -190,18 +200,19 @@ constexpr int kEpi =
 struct Stat {
   float m, s, u;
 };
-// Of 32 logits; c2 > 0.
-__device__ __forceinline__ Stat stat_of(const float (&x)[32], float c2) {
+// Of 32 logits.
+__device__ __forceinline__ Stat stat_of(const float (&x)[32], Exponents c2) {
   float m = x[0];
 #pragma unroll
   for (int i = 1; i < 31; i += 2) m = max_nan(m, x[i], x[i + 1]);
   m = max_nan(m, x[31]);
   if (m == -INFINITY) return {m, 0.f, 0.f};
-  const unsigned long long zero = f2_dup(0.f), less = f2_dup(-m), by = f2_dup(c2);
+  const unsigned long long zero = f2_dup(0.f), less = f2_dup(-m * c2.k), k = f2_dup(c2.k),
+                           by = f2_dup(c2.c);
   unsigned long long s[2] = {zero, zero}, u[2] = {zero, zero};
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const unsigned long long y = f2_mul(f2_add(f2_pack(x[i], x[i + 1]), less), by);
+    const unsigned long long y = f2_mul(f2_fma(f2_pack(x[i], x[i + 1]), k, less), by);
     float y0, y1;
     f2_split(y, y0, y1);
     const unsigned long long e = f2_pack(exp2_fast(y0), exp2_fast(y1));
@@ -218,21 +229,22 @@ __device__ __forceinline__ Stat stat_of(const float (&x)[32], float c2) {
     float v = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      const float y = max_nan((x[i] - m) * c2, kLowest);
+      const float y = max_nan(fmaf(x[i], c2.k, -m * c2.k) * c2.c, kLowest);
       v = fmaf(y, exp2_fast(y), v);
     }
     r.u = v;
   }
   return r;
 }
-__device__ __forceinline__ void join(Stat &a, Stat b, float c2) {
+__device__ __forceinline__ void join(Stat &a, Stat b, Exponents c2) {
   if (b.m == -INFINITY) return;
   if (a.m == -INFINITY) {
     a = b;
     return;
   }
   const float m = max_nan(a.m, b.m);
-  const float da = max_nan((a.m - m) * c2, kLowest), db = max_nan((b.m - m) * c2, kLowest);
+  const float da = max_nan(fmaf(a.m, c2.k, -m * c2.k) * c2.c, kLowest);
+  const float db = max_nan(fmaf(b.m, c2.k, -m * c2.k) * c2.c, kLowest);
   const float fa = exp2_fast(da), fb = exp2_fast(db);
   a.u = fmaf(da, a.s, a.u) * fa + fmaf(db, b.s, b.u) * fb;
   a.s = a.s * fa + b.s * fb;
@@ -766,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
 // The pieces' sums of kJoinAt positions a block (a sector of each piece's): a warp's lanes are four
 // pieces of each, and its warps 32 times those.
 constexpr int kJoinWarps = 32, kJoinAt = 8;
-__device__ __forceinline__ Stat join_lanes(Stat a, int from, float c2) {
+__device__ __forceinline__ Stat join_lanes(Stat a, int from, Exponents c2) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     if (o >= from)
@@ -777,7 +789,7 @@ __device__ __forceinline__ Stat join_lanes(Stat a, int from, float c2) {
 __global__ void __launch_bounds__(32 * kJoinWarps)
     hidden_join_kernel(const Header *head, int blocks, const float *part, const float *picked,
                        const long long *targets, long long T, long long Tp, int parts, int V,
-                       float scale, float c2, float *logprob, float *entropy, float *lse) {
+                       float scale, Exponents c2, float *logprob, float *entropy, float *lse) {
   __shared__ Stat red[kJoinAt][kJoinWarps + 1];
   pdl_wait();
   pdl_trigger();
@@ -834,7 +846,7 @@ __global__ void __launch_bounds__(256)
     hidden_positions_kernel(Header *head, int blocks, const long long *targets, long long t0,
                             long long T, int V, float scale, const float *lse,
                             const float *entropy, const float *g_logprob, const float *g_entropy,
-                            const float *part, int parts, long long Tp, Position *pos,
+                            const float *part, int parts, long long Tp, Exponents c2, Position *pos,
                             Target *tgt) {
   __shared__ unsigned red[8];
   pdl_wait();
@@ -851,7 +863,7 @@ __global__ void __launch_bounds__(256)
       Stat a = {-INFINITY, 0.f, 0.f};
       for (int q = 0; q < parts; ++q)
         if (BOUTE_INB(q * Tp + i, all))
-          join(a, {part[q * Tp + i], part[all + q * Tp + i], 0.f}, scale * kLog2e);
+          join(a, {part[q * Tp + i], part[all + q * Tp + i], 0.f}, c2);
       p.m = a.m;
       p.ls = logf(a.s);
     }
@@ -1268,7 +1280,7 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
   W.head = (Header *)(ws + p.header);
-  W.c2 = scale * kLog2e;
+  W.c2 = exponents_of(scale);
   W.part = (float *)(ws + p.part);
   W.picked = (float *)(ws + p.picked);
   for (long long t0 = 0; t0 < T; t0 += kAtOnce) {
@@ -1315,7 +1327,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   W.head = (Header *)(ws + p.header);
   Position *pos = (Position *)(ws + p.pos);
   Target *tgt = (Target *)(ws + p.tgt);
-  W.c2 = scale * kLog2e;
+  W.c2 = exponents_of(scale);
   W.part = (float *)(ws + p.part);
   W.picked = (float *)(ws + p.picked);
   for (long long t0 = 0; t0 < T; t0 += kAtOnce) {
@@ -1326,7 +1338,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks)) return r;
     if (int r = launch_cluster(hidden_positions_kernel, (n + 255) / 256, 256, 1, 0, s, W.head,
                                blocks, targets, t0, t0 + n, V, scale, lse, entropy, g_logprob,
-                               g_entropy, W.part, parts, p.part_Tp, pos, tgt))
+                               g_entropy, W.part, parts, p.part_Tp, W.c2, pos, tgt))
       return r;
   }
   W.bounds = (int)((T + 255) / 256);
