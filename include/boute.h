@@ -696,8 +696,10 @@ int boute_route_grad(const void *logits, int dtype, long long T, int E, long lon
  *   offsets (E + 1 int32): expert e's places are offsets[e] .. offsets[e + 1] - 1, n = offsets[E];
  *   source (T k int32): the choice at a place, -1 for places >= n;
  *   place (T x k int32): the place of a choice, -1 for none.
- * The order is the same on every run. The outputs overlap no input. E <= BOUTE_MAX_EXPERTS, k <= BOUTE_MAX_CHOICES, 0 <= T k <
- * 2^31. */
+ * The order is the same on every run. The outputs overlap no input and no other output
+ * (BOUTE_ERR_INVALID_ARG, as for the calls over rows and hidden states below; rows that lie between
+ * another array's rows, at one pitch, do not overlap). E <= BOUTE_MAX_EXPERTS, k <=
+ * BOUTE_MAX_CHOICES, 0 <= T k < 2^31. */
 int boute_expert_sort(const int *idx, long long T, int k, int E, int *offsets, int *source,
                       int *place, void *stream);
 /* The rows of the choices, x_t at each of query t's places, and the gradient of x:
@@ -740,6 +742,7 @@ int boute_expert_combine_grad(const void *g_out, int dtype, long long T, int D, 
  *   workspace: device memory, 256-byte aligned, of the bytes that boute_hidden_logprobs_workspace
  *   gives for the same arguments (grad: for which of the calls); its contents need not be kept
  *   between calls. Calls that may run at the same time need one each.
+ * The outputs overlap no input, no other output and not the workspace, which holds no input.
  * A device-side wait that gives up (2 s; nothing hangs) makes all outputs of the call NaN, but for
  * dweight, of which parts may then hold their gradient already, or not be written.
  * 0 <= T <= BOUTE_MAX_HIDDEN, 1 <= D <= BOUTE_MAX_HIDDEN_SIZE, 1 <= V <= BOUTE_MAX_VOCAB. */
@@ -759,8 +762,8 @@ int boute_hidden_logprobs(const void *hidden, int dtype, long long T, int D, lon
  * rounded once to the type from fp32 sums. The products take each dlogits_tj rounded to the type, of
  * up to 32 positions as the sum of two such numbers (times a power of two, by which the largest
  * coefficient that the finite gradients allow comes near 2^14; what is less than 2^-28 of it loses
- * bits in fp16; positions without a distribution do not count). At most 256 MB of them are held at a time (512 bytes a position, if that is more). dhidden
- * and dweight overlap no input. */
+ * bits in fp16; positions without a distribution do not count). At most 256 MB of them are held at a
+ * time (512 bytes a position, if that is more). */
 int boute_hidden_logprobs_grad(const void *hidden, int dtype, long long T, int D, long long ldh,
                                const void *weight, int V, long long ldw, const long long *targets,
                                float scale, const float *lse, const float *entropy,

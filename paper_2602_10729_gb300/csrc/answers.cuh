@@ -8,6 +8,7 @@
 #include <atomic>
 
 #include "internal.h"
+#include "regions.h"
 #include "warp_select.cuh"
 
 namespace boute {

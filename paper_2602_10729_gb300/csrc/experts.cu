@@ -745,13 +745,16 @@ extern "C" int boute_expert_sort(const int *idx, long long T, int k, int E, int 
                                  int *source, int *place, void *stream) {
   BOUTE_TRACE();
   if (T < 0 || k < 1 || E < 1 || !array_ok(offsets, 4) ||
-      (T > 0 && (!array_ok(idx, 4) || !array_ok(source, 4) || !array_ok(place, 4) ||
-                 idx == source || idx == place)))  // (read again after they are written)
+      (T > 0 && (!array_ok(idx, 4) || !array_ok(source, 4) || !array_ok(place, 4))))
     return BOUTE_ERR_INVALID_ARG;
   if (T > 0x7fffffff || k > BOUTE_MAX_CHOICES || T * k > 0x7fffffff || E > BOUTE_MAX_EXPERTS)
     return BOUTE_ERR_UNSUPPORTED;
-  if (int r = device_ok()) return r;
   const long long N = T * k;
+  // (the choices are read again after the outputs are written)
+  if (outputs_overlap({array_of(offsets, E + 1, 4), array_of(source, N, 4), array_of(place, N, 4)},
+                      {array_of(idx, N, 4)}))
+    return BOUTE_ERR_INVALID_ARG;
+  if (int r = device_ok()) return r;
   const cudaStream_t s = (cudaStream_t)stream;
   Order A{idx, N, E, 0, 0, 0, offsets, source, place};
   auto go = [&](auto steps) -> int {
@@ -802,7 +805,7 @@ int rows_ok(int dtype, const void *x, long long T, int D, long long ldx, const v
   return T > 0x7fffffff || R > 0x7fffffff || k > BOUTE_MAX_CHOICES || T * k > 0x7fffffff ||
                  D > BOUTE_MAX_ROW
              ? BOUTE_ERR_UNSUPPORTED
-             : device_ok();
+             : BOUTE_OK;
 }
 
 // Whether rows of these addresses, pitches and lengths (in bytes) start and end on 16-byte
@@ -853,10 +856,13 @@ extern "C" int boute_expert_dispatch(const void *x, int dtype, long long T, int 
                                      const int *place, int k, void *rows, long long R,
                                      long long ldr, void *stream) {
   BOUTE_TRACE();
-  if (T > 0 && x == rows) return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, x, T, D, ldx, rows, R, ldr, place, k)) return r;
-  if (T == 0 || R == 0) return BOUTE_OK;
   const int size = (int)dtype_bytes(dtype), bytes = D * size;
+  if (outputs_overlap({rows_of(rows, R, D, ldr, size)},
+                      {rows_of(x, T, D, ldx, size), array_of(place, T * k, 4)}))
+    return BOUTE_ERR_INVALID_ARG;
+  if (int r = device_ok()) return r;
+  if (T == 0 || R == 0) return BOUTE_OK;
   const Rows A{T, R, k, D, ldx, ldr, place};
   const bool aligned = rows_aligned((uintptr_t)x | (uintptr_t)rows | (uint64_t)(ldx * size) |
                                     (uint64_t)(ldr * size) | (uint64_t)bytes);
@@ -883,8 +889,12 @@ extern "C" int boute_expert_dispatch_grad(const void *g_rows, int dtype, long lo
                                           long long ldr, const int *place, long long T, int k,
                                           void *dx, long long ldx, void *stream) {
   BOUTE_TRACE();
-  if (T > 0 && dx == g_rows) return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, dx, T, D, ldx, g_rows, R, ldr, place, k)) return r;
+  const size_t size = dtype_bytes(dtype);
+  if (outputs_overlap({rows_of(dx, T, D, ldx, size)},
+                      {rows_of(g_rows, R, D, ldr, size), array_of(place, T * k, 4)}))
+    return BOUTE_ERR_INVALID_ARG;
+  if (int r = device_ok()) return r;
   if (T == 0) return BOUTE_OK;
   return combine(g_rows, dtype, R, D, ldr, place, nullptr, T, k, dx, ldx, (cudaStream_t)stream);
 }
@@ -893,8 +903,14 @@ extern "C" int boute_expert_combine(const void *rows, int dtype, long long R, in
                                     const int *place, const float *weight, long long T, int k,
                                     void *out, long long ldo, void *stream) {
   BOUTE_TRACE();
-  if (T > 0 && (!array_ok(weight, 4) || out == rows)) return BOUTE_ERR_INVALID_ARG;
+  if (T > 0 && !array_ok(weight, 4)) return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, out, T, D, ldo, rows, R, ldr, place, k)) return r;
+  const size_t size = dtype_bytes(dtype);
+  if (outputs_overlap({rows_of(out, T, D, ldo, size)},
+                      {rows_of(rows, R, D, ldr, size), array_of(place, T * k, 4),
+                       array_of(weight, T * k, 4)}))
+    return BOUTE_ERR_INVALID_ARG;
+  if (int r = device_ok()) return r;
   if (T == 0) return BOUTE_OK;
   return combine(rows, dtype, R, D, ldr, place, weight, T, k, out, ldo, (cudaStream_t)stream);
 }
@@ -907,9 +923,17 @@ extern "C" int boute_expert_combine_grad(const void *g_out, int dtype, long long
   BOUTE_TRACE();
   const int size = (int)dtype_bytes(dtype);
   if ((T > 0 && (!array_ok(weight, 4) || !array_ok(g_weight, 4))) || ldg < D ||
-      (R > 0 && (!array_ok(g_rows, size) || g_rows == g_out || (g_rows == rows && ldg != ldr))))
+      (R > 0 && !array_ok(g_rows, size)))
     return BOUTE_ERR_INVALID_ARG;
   if (int r = rows_ok(dtype, g_out, T, D, ldo, rows, R, ldr, place, k)) return r;
+  const Region read = rows_of(rows, R, D, ldr, size), g_read = rows_of(g_out, T, D, ldo, size);
+  const Region written = rows_of(g_rows, R, D, ldg, size), g_w = array_of(g_weight, T * k, 4);
+  const Region places = array_of(place, T * k, 4), weights = array_of(weight, T * k, 4);
+  const bool in_place = g_rows == rows && (ldg == ldr || R <= 1);
+  if (outputs_overlap({written, g_w}, {g_read, places, weights}) || overlap(g_w, read) ||
+      (!in_place && overlap(written, read)))
+    return BOUTE_ERR_INVALID_ARG;
+  if (int r = device_ok()) return r;
   if (T == 0) return BOUTE_OK;
   const Rows A{T, R, k, D, ldo, ldr, place};
   const int bytes = D * size;

@@ -1272,6 +1272,11 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
   if (int r = sizes_ok(hidden, dtype, T, D, ldh, weight, V, ldw)) return r;
   Plan p = make_plan(hidden, T, D, ldh, weight, V, ldw, false);
   if (T > 0 && bytes < (long long)p.bytes) return BOUTE_ERR_INVALID_ARG;
+  if (T > 0 && outputs_overlap({array_of(logprob, T, 4), array_of(entropy, T, 4),
+                                array_of(lse, T, 4), array_of(workspace, p.bytes, 1)},
+                               {rows_of(hidden, T, D, ldh, 2), rows_of(weight, V, D, ldw, 2),
+                                array_of(targets, T, 8)}))
+    return BOUTE_ERR_INVALID_ARG;
   if (int r = device_ok()) return r;
   if (T == 0) return BOUTE_OK;
   const cudaStream_t s = (cudaStream_t)stream;
@@ -1307,12 +1312,18 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   if (!(scale > 0.f) || !isfinite(scale) || lddh < D || lddw < D || !array_ok(dweight, 2) ||
       !optional_ok(entropy, 4) || !optional_ok(g_entropy, 4) || (g_entropy && !entropy && T > 0) ||
       (T > 0 && (!array_ok(targets, 8) || !array_ok(lse, 4) || !array_ok(g_logprob, 4) ||
-                 !array_ok(dhidden, 2) || !array_ok(workspace, 256) || dhidden == hidden ||
-                 dweight == weight)))
+                 !array_ok(dhidden, 2) || !array_ok(workspace, 256))))
     return BOUTE_ERR_INVALID_ARG;
   if (int r = sizes_ok(hidden, dtype, T, D, ldh, weight, V, ldw)) return r;
   Plan p = make_plan(hidden, T, D, ldh, weight, V, ldw, true);
   if (T > 0 && bytes < (long long)p.bytes) return BOUTE_ERR_INVALID_ARG;
+  if (T > 0 && outputs_overlap({rows_of(dhidden, T, D, lddh, 2), rows_of(dweight, V, D, lddw, 2),
+                                array_of(workspace, p.bytes, 1)},
+                               {rows_of(hidden, T, D, ldh, 2), rows_of(weight, V, D, ldw, 2),
+                                array_of(targets, T, 8), array_of(lse, T, 4),
+                                array_of(entropy, T, 4), array_of(g_logprob, T, 4),
+                                array_of(g_entropy, T, 4)}))
+    return BOUTE_ERR_INVALID_ARG;
   if (int r = device_ok()) return r;
   const cudaStream_t s = (cudaStream_t)stream;
   if (T == 0)  // (no position: the weight's gradient is 0)
