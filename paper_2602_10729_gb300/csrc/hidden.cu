@@ -57,26 +57,28 @@ enum Kind { kStatsCols, kStatsRows, kCoefCols, kCoefRows, kGrads };
 constexpr int kBlocks = 256;  // of a launch at most
 constexpr int kBounds = BOUTE_MAX_HIDDEN / 256;
 struct Header {
-  // BOUTE_ERR_TIMEOUT where a wait ran out: in the gradient's launches, which clear it first; in each
-  // block of the statistics' launch, which writes its own
+  // BOUTE_ERR_TIMEOUT where a wait ran out: in the gradient's launches, which clear it first; in
+  // each block of the statistics' launch, which writes its own
   int late, status[kBlocks];
   // bits of the largest bound of a coefficient, of each 256 positions
   unsigned largest[kBounds];
 };
 // What the coefficients of a position need: p = e^lp, lp = (x - m) scale - ls, p (a + b lp), + g at
-// its target.
+// its target j (-1 for none). m is 0 but for far positions.
 struct Position {
-  float m, ls, a, b;
+  float ls, a, b, g;
 };
 struct Target {
-  int j;  // -1 for none
-  float g;
+  int j;
+  float m;
 };
 
-// Whether lse's rounding (2^-24 of it) would show in p. Such positions' coefficients take the largest
-// logit and ln s from the logits, which are then summed once more; with the difference first, the
-// rounding of the product by the scale is no larger than lp's.
-__device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) > kLargeLse && isfinite(lse); }
+// Whether lse's rounding (2^-24 of it) would show in p. Such positions' coefficients take the
+// largest logit and ln s from the logits, which are then summed once more; with the difference
+// first, the rounding of the product by the scale is no larger than lp's.
+__device__ __forceinline__ bool is_far(float lse) {
+  return fabsf(lse) > kLargeLse && isfinite(lse);
+}
 
 // The power of two by which the coefficients are scaled while they are 16-bit numbers: the largest
 // comes to 2^14 (fp16: what is 2^-28 of that has all its bits, and 2^-39 some). For whole warps.
@@ -90,15 +92,10 @@ __device__ __forceinline__ float coef_scale(const Header *head, int bounds, bool
   return exp2i(inverse ? -k : k);
 }
 
-// Powers of two of logits' differences: (x - m) k c, where k = 2 if c = scale log2 e would be infinite
-// (of a scale above 2.3e38: 0 times it would be NaN).
-struct Exponents {
-  float k, c;
-};
-Exponents exponents_of(float scale) {
-  return scale * kLog2e <= FLT_MAX ? Exponents{1.f, scale * kLog2e}
-                                   : Exponents{2.f, scale * 0.5f * kLog2e};
-}
+// The statistics are of logits times k, which is 2 where scale log2 e would be infinite (of a scale
+// above 2.3e38: 0 times it would be NaN).
+float logits_by(float scale) { return scale * kLog2e <= FLT_MAX ? 1.f : 2.f; }
+float exponents_of(float scale) { return scale / logits_by(scale) * kLog2e; }
 
 struct Work {
   int M, N, K;              // rows, columns, reduction
@@ -108,11 +105,11 @@ struct Work {
   Header *head;
   int bounds;               // values of head->largest
   // statistics
-  Exponents c2;
+  float k, c2;              // logits_by, exponents_of the scale
   float *part;              // 3 x parts x Tp: maxima, s, u
   float *picked;            // Tp: x of the targets
   const long long *targets;
-  const float *lse;         // the launch is for far positions alone; NULL: for all
+  const float *lse;         // (to ask for far positions)
   long long Tp;             // (coefficients: the pitch of coef)
   // coefficients
   const Position *pos;
@@ -137,6 +134,7 @@ struct Job {
 struct Jobs {
   Job job[2];
   int units[2], stages, stage_bytes;
+  int far;   // statistics of a pass that has far positions alone, else of none
   int part;  // blocks of the reduction that an accumulator takes (statistics in parts)
   // The pairs take the first set's units in turn; those that got one fewer (`light`, from pair
   // light_from on) take `ahead` of the second set first, then all take the rest in turn.
@@ -200,19 +198,18 @@ constexpr int kEpi =
 struct Stat {
   float m, s, u;
 };
-// Of 32 logits.
-__device__ __forceinline__ Stat stat_of(const float (&x)[32], Exponents c2) {
+// Of 32 logits; c2 > 0.
+__device__ __forceinline__ Stat stat_of(const float (&x)[32], float c2) {
   float m = x[0];
 #pragma unroll
   for (int i = 1; i < 31; i += 2) m = max_nan(m, x[i], x[i + 1]);
   m = max_nan(m, x[31]);
   if (m == -INFINITY) return {m, 0.f, 0.f};
-  const unsigned long long zero = f2_dup(0.f), less = f2_dup(-m * c2.k), k = f2_dup(c2.k),
-                           by = f2_dup(c2.c);
+  const unsigned long long zero = f2_dup(0.f), less = f2_dup(-m), by = f2_dup(c2);
   unsigned long long s[2] = {zero, zero}, u[2] = {zero, zero};
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const unsigned long long y = f2_mul(f2_fma(f2_pack(x[i], x[i + 1]), k, less), by);
+    const unsigned long long y = f2_mul(f2_add(f2_pack(x[i], x[i + 1]), less), by);
     float y0, y1;
     f2_split(y, y0, y1);
     const unsigned long long e = f2_pack(exp2_fast(y0), exp2_fast(y1));
@@ -229,22 +226,21 @@ __device__ __forceinline__ Stat stat_of(const float (&x)[32], Exponents c2) {
     float v = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      const float y = max_nan(fmaf(x[i], c2.k, -m * c2.k) * c2.c, kLowest);
+      const float y = max_nan((x[i] - m) * c2, kLowest);
       v = fmaf(y, exp2_fast(y), v);
     }
     r.u = v;
   }
   return r;
 }
-__device__ __forceinline__ void join(Stat &a, Stat b, Exponents c2) {
+__device__ __forceinline__ void join(Stat &a, Stat b, float c2) {
   if (b.m == -INFINITY) return;
   if (a.m == -INFINITY) {
     a = b;
     return;
   }
   const float m = max_nan(a.m, b.m);
-  const float da = max_nan(fmaf(a.m, c2.k, -m * c2.k) * c2.c, kLowest);
-  const float db = max_nan(fmaf(b.m, c2.k, -m * c2.k) * c2.c, kLowest);
+  const float da = max_nan((a.m - m) * c2, kLowest), db = max_nan((b.m - m) * c2, kLowest);
   const float fa = exp2_fast(da), fb = exp2_fast(db);
   a.u = fmaf(da, a.s, a.u) * fa + fmaf(db, b.s, b.u) * fb;
   a.s = a.s * fa + b.s * fb;
@@ -273,13 +269,12 @@ __device__ __forceinline__ void box_row(uint8_t *box, int half, const float (&x)
 }
 
 // ---- the kernel --------------------------------------------------------------------------
-// MINE > 0: statistics over a reduction of several parts, whose tiles both groups of warps take
-// together, up to MINE chunks of 32 columns each.
+// MINE > 0: reductions in several parts, whose tiles both groups of warps take together, up to MINE
+// chunks of 32 columns each.
 template <Kind KIND, class T, int MINE>
 __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_constant__ Jobs J) {
   constexpr bool kStats = KIND == kStatsCols || KIND == kStatsRows;
   constexpr bool kParted = MINE > 0;
-  static_assert(kStats || !kParted, "");
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2],
       drain;
@@ -291,39 +286,46 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
   uint8_t *ring = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   uint8_t *epi = ring + (size_t)J.stages * J.stage_bytes;
 
-  if (tid == 0) {
-    for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+  auto begin = [&]() {  // barriers and tensor memory
+    if (tid == 0) {
+      for (int s = 0; s < kMaxStages; ++s) {
+        mbar_init(&full[s], 1);
+        mbar_init(&empty[s], 1);
+      }
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&acc_full[i], 1);
+        // (the warps of both blocks that read it)
+        mbar_init(&acc_empty[i], kParted ? 2 * kEpiWarps : kEpiWarps);
+      }
+      mbar_init(&drain, 1);
+      abort_flag = 0;
+      fence_mbar_init();
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&acc_full[i], 1);
-      // (the warps of both blocks that read it)
-      mbar_init(&acc_empty[i], kParted ? 2 * kEpiWarps : kEpiWarps);
-    }
-    mbar_init(&drain, 1);
-    abort_flag = 0;
-    fence_mbar_init();
-  }
-  if (warp == 1) pair_tmem_alloc(&tmem_holder, 512);
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync();
-  tc_fence_after();
-  const uint32_t tmem = tmem_holder;
+    if (warp == 1) pair_tmem_alloc(&tmem_holder, 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+  };
+  // Where few launches find any work, what they need waits until they have.
+  const bool asks = kStats && J.far;
+  if (!asks) begin();
   pdl_wait();
   pdl_trigger();
-  bool idle = false;  // (alike in both blocks)
-  if (kStats && J.job[0].w.lse) {
+  if (asks) {
     const Work &W = J.job[0].w;
     const int n = KIND == kStatsRows ? W.M : W.N;
-    bool far = false;
+    bool far = false;  // (alike in both blocks)
     for (int i = tid; i < n; i += kThreads) far |= BOUTE_INB(i, W.Tp) && is_far(W.lse[i]);
-    idle = !__syncthreads_or(far);
+    if (!__syncthreads_or(far)) {
+      if (tid == 0) W.head->status[blockIdx.x] = 0;
+      return;
+    }
+    begin();
   }
+  const uint32_t tmem = tmem_holder;
 
-  if (idle) {
-  } else if (warp == 0) {
+  if (warp == 0) {
     // ------------------------------------------------------------------ operand tiles
     if (lane == 0) {
       int s = 0, used = 0;
@@ -430,26 +432,78 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
       __syncwarp();
       if (lane == 0) arrive_peer(&acc_empty[acc], 0);
     };
-    if constexpr (kParted) {
-      // Both groups take each tile, the first half of its columns one and the rest the other.
-      const Work &W = J.job[0].w;
-      const int half = (W.tile_n / 32 + 1) / 2, chunk0 = group * half;
-      const int chunks = group == 0 ? half : W.tile_n / 32 - half;
-      uint32_t seq = 0;
-      for (int i = 0;; ++i) {
-        const Unit t = unit_of<KIND>(J, pair, pairs, i);
-        if (t.job < 0) break;
-        const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32;
-        const int col = t.n * W.tile_n + chunk0 * 32;
-        // the token wanted of a position
-        auto wanted_at = [&](int at, int end) {
-          return at < end && BOUTE_INB(at, end)
-                     ? (int)min(max(W.targets[at], -1ll), (long long)INT_MAX)
-                     : -1;
-        };
-        float x[kParted ? MINE : 1][32];
-        bool ok = true;
-        for (int k0 = t.k0; k0 < t.k1; k0 += J.part, ++seq) {
+    float mul = 1.f;
+    if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
+    // (of coefficients of which a wait left out some, no number is written)
+    if (KIND == kGrads && *(volatile int *)&J.job[0].w.head->late != 0) mul = NAN;
+    uint32_t seq = 0;  // accumulators so far, where both groups take all
+    // The groups take the tiles in turn, or, in parts, the first half of each tile's columns one
+    // and the rest the other.
+    for (int i = kParted ? 0 : group;; i += kParted ? 1 : 2) {
+      const Unit t = unit_of<KIND>(J, pair, pairs, i);
+      if (t.job < 0) break;
+      const Work &W = J.job[KIND == kGrads ? t.job : 0].w;
+      const int half = (W.tile_n / 32 + 1) / 2, chunk0 = kParted ? group * half : 0;
+      const int chunks = !kParted ? W.tile_n / 32 : group == 0 ? half : W.tile_n / 32 - half;
+      const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32;
+      const int col = t.n * W.tile_n + chunk0 * 32;
+      // what does not wait for the products
+      Position *pos = (Position *)epi + group * kMaxTileN;
+      Target *tgt = (Target *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
+      Position own = {1e30f, 0.f, 0.f, 0.f};
+      int target = -1;
+      float own_m = 0.f;
+      if constexpr (KIND == kCoefCols) {
+        named_barrier_sync(1 + group, kGroup);  // (the last tile's are read)
+        for (int c = gtid; c < chunks * 32; c += kGroup) {
+          Position p = {1e30f, 0.f, 0.f, 0.f};
+          Target to = {-1, 0.f};
+          if (col + c < W.N && BOUTE_INB(col + c, W.N)) {
+            p = W.pos[col + c];
+            p.a *= mul, p.b *= mul, p.g *= mul;
+            to = W.tgt[col + c];
+            to.j -= W.row0;
+          }
+          pos[c] = p;
+          tgt[c] = to;
+        }
+      } else if constexpr (KIND == kCoefRows) {
+        if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+          own = W.pos[row + lane];
+          own.a *= mul, own.b *= mul, own.g *= mul;
+          target = W.tgt[row + lane].j - W.row0;
+          own_m = W.tgt[row + lane].m;
+        }
+      } else if constexpr (KIND == kStatsRows) {
+        if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+          const long long j = W.targets[row + lane];
+          target = j >= 0 && j < W.N ? (int)j : -1;
+        }
+      }
+      Stat run = {-INFINITY, 0.f, 0.f};
+      const int red0 = kParted ? chunk0 * 32 : group * 4 * kMaxTileN;
+      // 64 columns of 32 rows go out as a box (a row's bytes at once: 268 MB of dW took 77 us by
+      // each thread's 32 bytes of its row), a last half by the threads
+      uint8_t *box = epi + kBoxes<KIND> + (warp - 2) * kBoxBytes;
+      auto send = [&](int c, const float (&x)[32]) {
+        const CUtensorMap *out = &J.job[KIND == kGrads ? t.job : 0].out;
+        if (c % 2 == 0) {
+          if (lane == 0) bulk_wait_read();
+          __syncwarp();
+        }
+        box_row<T>(box, c & 1, x);
+        if (c % 2 == 0) return;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          store_box(out, box, col + (c - 1) * 32, row);
+          bulk_commit();
+        }
+      };
+      bool ok = true;
+      float sum[kParted ? MINE : 1][32];
+      if constexpr (kParted) {
+        for (int k0 = t.k0; k0 < t.k1 || k0 == t.k0; k0 += J.part, ++seq) {
           const int acc = seq & 1u;
           ok = __all_sync(kAll, pair_wait(&acc_full[acc], (seq >> 1) & 1u, abort));
           if (!ok) break;
@@ -463,17 +517,174 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
               tmem_ld16(from + acc * kMaxTileN + (chunk0 + c) * 32 + h, v);
               if (k0 == t.k0)
 #pragma unroll
-                for (int q = 0; q < 16; ++q) x[c][h + q] = 0.f;
+                for (int q = 0; q < 16; ++q) sum[c][h + q] = 0.f;
 #pragma unroll
-              for (int q = 0; q < 16; ++q) x[c][h + q] += v[q];
+              for (int q = 0; q < 16; ++q) sum[c][h + q] += v[q];
             }
           }
           release(acc);
         }
-        // (where the group meets at a barrier, it goes on or gives up as one)
-        if (KIND == kStatsCols) ok = group_all(1 + group, kGroup, ok);
-        if (!ok) break;
-        const long long parts = KIND == kStatsCols ? 2ll * W.nM : 2ll * W.nN, all = parts * W.Tp;
+      } else {
+        ok = __all_sync(kAll, pair_wait(&acc_full[group], (i >> 1) & 1u, abort));
+      }
+      // (where the group meets at a barrier, it goes on or gives up as one)
+      if (KIND == kStatsCols || KIND == kCoefCols) ok = group_all(1 + group, kGroup, ok);
+      if (!ok) break;
+      if (!kParted) tc_fence_after();
+#pragma unroll(kParted ? MINE : 1)
+      for (int c = 0; c < (kParted ? MINE : chunks); ++c) {
+        if (kParted && c >= chunks) continue;
+        float(&x)[32] = sum[kParted ? c : 0];
+        if (!kParted) {
+          tmem_ld32(from + group * kMaxTileN + c * 32, x);
+          if (c == chunks - 1) release(group);
+        }
+        const int d0 = col + c * 32;
+        const bool boxed = c < (chunks & ~1);
+        if constexpr (KIND == kStatsCols) {
+          float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
+          Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + red0;
+          const int at = d0 + lane;
+          long long wanted = -1;
+          if (at < W.N && BOUTE_INB(at, W.N)) wanted = W.targets[at];
+          // (rows of the accumulator beyond the block's hold what was in its shared memory)
+          const int rows = min(W.tile_m - quarter * 32, W.M - row);
+          if (lane >= rows || W.k != 1.f)
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] = lane >= rows ? -INFINITY : x[q] * W.k;
+#pragma unroll
+          for (int q = 0; q < 32; q += 4)
+            *(float4 *)(buf + lane * kPitch + q) = {x[q], x[q + 1], x[q + 2], x[q + 3]};
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 32; ++q) x[q] = buf[q * kPitch + lane];
+          if (wanted >= row && wanted < row + min(rows, 32))
+            W.picked[at] = buf[(int)(wanted - row) * kPitch + lane];
+          red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x, W.c2);
+          __syncwarp();
+        } else if constexpr (KIND == kStatsRows) {
+          if (d0 + 32 > W.N || W.k != 1.f)
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] = d0 + q >= W.N ? -INFINITY : x[q] * W.k;
+          if (__any_sync(kAll, target >= d0 && target < d0 + 32))
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (target == d0 + q) W.picked[row + lane] = x[q];
+          join(run, stat_of(x, W.c2), W.c2);
+        } else if constexpr (KIND == kCoefCols) {
+          const Target aim = tgt[c * 32 + lane];
+          const unsigned here = __ballot_sync(kAll, aim.j >= row && aim.j < row + 32);
+          if (__any_sync(kAll, aim.m != 0.f))
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] -= tgt[c * 32 + q].m;
+#pragma unroll
+          for (int q = 0; q < 32; ++q) {
+            const Position p = pos[c * 32 + q];
+            const float lp = max_nan(fmaf(x[q], W.scale, -p.ls), -1e4f);
+            x[q] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
+          }
+          if (here)
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if ((here >> q & 1u) && tgt[c * 32 + q].j == row + lane) x[q] += pos[c * 32 + q].g;
+          if (d0 + 32 > W.N)  // (columns of no position, which a token of infinities makes NaN)
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (d0 + q >= W.N) x[q] = 0.f;
+          uint16_t *to = W.coef + (row + lane) * W.Tp + d0;
+          const bool mine = row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp);
+          if (boxed) send(c, x);
+          else if (mine) store_row_of<T>(to, x);
+          if (W.low > 0 && mine && BOUTE_INB(d0 + W.low + 31, W.Tp)) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] -= to_float(from_float<T>(x[q]));
+            store_row_of<T>(to + W.low, x);
+          }
+        } else if constexpr (KIND == kCoefRows) {
+          const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.ls);
+          if (__any_sync(kAll, own_m != 0.f))
+#pragma unroll
+            for (int q = 0; q < 32; ++q) x[q] -= own_m;
+          const unsigned long long a2 = f2_dup(own.a), b2 = f2_dup(own.b), l2e = f2_dup(kLog2e);
+#pragma unroll
+          for (int q = 0; q < 32; q += 2) {
+            float l0, l1, y0, y1;
+            f2_split(f2_fma(f2_pack(x[q], x[q + 1]), by, less), l0, l1);
+            const unsigned long long lp = f2_pack(max_nan(l0, -1e4f), max_nan(l1, -1e4f));
+            f2_split(f2_mul(lp, l2e), y0, y1);
+            f2_split(f2_mul(f2_pack(exp2_fast(y0), exp2_fast(y1)), f2_fma(b2, lp, a2)), x[q],
+                     x[q + 1]);
+          }
+          if (__any_sync(kAll, target >= d0 && target < d0 + 32))
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (target == d0 + q) x[q] += own.g;
+          send(c, x);
+        } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
+          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
+            const int n = min(32, W.N - d0);
+            float *to = W.sums + ((long long)t.split * W.N + d0) * W.M + row + lane;
+            if (t.k0 == t.k1)  // (a short piece's empty part)
+#pragma unroll
+              for (int q = 0; q < 32; ++q) x[q] = 0.f;
+            if (W.add) {
+              float was[32];  // (all on their way at once)
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (q < n) was[q] = to[(long long)q * W.M];
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (q < n) x[q] += was[q];
+            }
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (q < n) to[(long long)q * W.M] = x[q];
+          }
+        } else {  // dW
+#pragma unroll
+          for (int q = 0; q < 32; ++q) x[q] *= mul;
+          T *to = (T *)W.out + (row + lane) * W.ldo + d0;
+          if (boxed && W.boxes) {
+            send(c, x);
+          } else if (boxed) {  // rows at any address: by way of the box, a row by its lanes
+            if (c % 2 == 0) __syncwarp();
+            box_row<T>(box, c & 1, x);
+            if (c % 2 == 1) {
+              __syncwarp();
+              const int rows = min(32, W.M - row);
+              for (int r = 0; r < rows; ++r) {
+                T *line = (T *)W.out + (row + r) * W.ldo + d0 - 32;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const int e = h * 32 + lane;
+                  const int at = r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2;
+                  const T v = *(const T *)(box + at);
+                  if (d0 - 32 + e < W.N && BOUTE_INB(row + r, W.M)) line[e] = v;
+                }
+              }
+            }
+          } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {
+            if (d0 + 32 <= W.N && W.width >= 32) {
+              store_row_of<T>((uint16_t *)to, x);
+            } else if (d0 + 32 <= W.N && W.width >= 16) {
+#pragma unroll
+              for (int q = 0; q < 32; q += 8)
+                *(uint4 *)(to + q) = {
+                    pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
+                    pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
+            } else {
+#pragma unroll
+              for (int q = 0; q < 32; ++q)
+                if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
+            }
+          }
+        }
+        __syncwarp();
+      }
+      if constexpr (kStats) {
+        constexpr int kOf = KIND == kStatsCols || kParted ? 2 : 1;  // (blocks', groups')
+        const long long parts = (long long)kOf * (KIND == kStatsCols ? W.nM : W.nN);
+        const long long all = parts * W.Tp;
         auto write = [&](Stat a, long long at) {
           if (!BOUTE_INB(at, all)) return;
           W.part[at] = a.m;
@@ -481,285 +692,15 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
           W.part[2 * all + at] = a.u;
         };
         if constexpr (KIND == kStatsCols) {
-          float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
-          Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + chunk0 * 32;
-          // (rows of the accumulator beyond the block's hold what was in its shared memory)
-          const int rows = min(W.tile_m - quarter * 32, W.M - row);
-#pragma unroll
-          for (int c = 0; c < MINE; ++c) {
-            if (c >= chunks) continue;
-            if (lane >= rows)
-#pragma unroll
-              for (int q = 0; q < 32; ++q) x[c][q] = -INFINITY;
-#pragma unroll
-            for (int q = 0; q < 32; q += 4)
-              *(float4 *)(buf + lane * kPitch + q) = {x[c][q], x[c][q + 1], x[c][q + 2],
-                                                      x[c][q + 3]};
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < 32; ++q) x[c][q] = buf[q * kPitch + lane];
-            const int wanted = wanted_at(col + c * 32 + lane, W.N);
-            if (wanted >= row && wanted < row + min(rows, 32))
-              W.picked[col + c * 32 + lane] = buf[(wanted - row) * kPitch + lane];
-            red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x[c], W.c2);
-            __syncwarp();
-          }
           named_barrier_sync(1 + group, kGroup);
-          if (gtid < chunks * 32 && col + gtid < W.N) {
-            Stat a = red[gtid];
-            for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + gtid], W.c2);
-            write(a, (2ll * t.m + rank) * W.Tp + col + gtid);
+          const Stat *red = (const Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + red0;
+          for (int c = gtid; c < chunks * 32; c += kGroup) {
+            Stat a = red[c];
+            for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + c], W.c2);
+            if (col + c < W.N) write(a, (2ll * t.m + rank) * W.Tp + col + c);
           }
-        } else {
-          Stat run = {-INFINITY, 0.f, 0.f};
-          const int wanted = wanted_at(row + lane, W.M);
-#pragma unroll
-          for (int c = 0; c < MINE; ++c) {
-            if (c >= chunks) continue;
-            const int d0 = col + c * 32;
-            if (d0 + 32 > W.N)
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (d0 + q >= W.N) x[c][q] = -INFINITY;
-            if (__any_sync(kAll, wanted >= d0 && wanted < d0 + 32))
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (wanted == d0 + q && d0 + q < W.N) W.picked[row + lane] = x[c][q];
-            join(run, stat_of(x[c], W.c2), W.c2);
-          }
-          if (row + lane < W.M) write(run, (2ll * t.n + group) * W.Tp + row + lane);
-        }
-      }
-    } else {
-      float mul = 1.f;
-      if (!kStats) mul = coef_scale(J.job[0].w.head, J.job[0].w.bounds, KIND == kGrads);
-      // (of coefficients of which a wait left out some, no number is written)
-      if (KIND == kGrads && *(volatile int *)&J.job[0].w.head->late != 0) mul = NAN;
-      for (int i = group;; i += 2) {
-        const Unit t = unit_of<KIND>(J, pair, pairs, i);
-        if (t.job < 0) break;
-        const Work &W = J.job[KIND == kGrads ? t.job : 0].w;
-        const int chunks = W.tile_n / 32;
-        const int row = (t.m * 2 + rank) * W.tile_m + quarter * 32, col = t.n * W.tile_n;
-        // what does not wait for the products
-        Position *pos = (Position *)epi + group * kMaxTileN;
-        Target *tgt = (Target *)(epi + 2 * kMaxTileN * sizeof(Position)) + group * kMaxTileN;
-        Position own = {0.f, 1e30f, 0.f, 0.f};
-        int target = -1;
-        float target_g = 0.f;
-        if constexpr (KIND == kCoefCols) {
-          named_barrier_sync(1 + group, kGroup);  // (the last tile's are read)
-          for (int c = gtid; c < W.tile_n; c += kGroup) {
-            Position p = {0.f, 1e30f, 0.f, 0.f};
-            Target to = {-1, 0.f};
-            if (col + c < W.N && BOUTE_INB(col + c, W.N)) {
-              p = W.pos[col + c];
-              p.a *= mul, p.b *= mul;
-              to = W.tgt[col + c];
-              to.j -= W.row0, to.g *= mul;
-            }
-            pos[c] = p;
-            tgt[c] = to;
-          }
-        } else if constexpr (KIND == kCoefRows) {
-          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
-            own = W.pos[row + lane];
-            own.a *= mul, own.b *= mul;
-            target = W.tgt[row + lane].j - W.row0;
-            target_g = W.tgt[row + lane].g * mul;
-          }
-        } else if constexpr (KIND == kStatsRows) {
-          if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
-            const long long j = W.targets[row + lane];
-            target = j >= 0 && j < W.N ? (int)j : -1;
-          }
-        }
-        // (where the group meets at a barrier, it goes on or gives up as one)
-        bool ok = __all_sync(kAll, pair_wait(&acc_full[group], (i >> 1) & 1u, abort));
-        if (KIND == kStatsCols || KIND == kCoefCols) ok = group_all(1 + group, kGroup, ok);
-        if (!ok) break;
-        tc_fence_after();
-        Stat run = {-INFINITY, 0.f, 0.f};
-        // 64 columns of 32 rows go out as a box (a row's bytes at once: 268 MB of dW took 77 us by
-        // each thread's 32 bytes of its row), a last half by the threads
-        uint8_t *box = epi + kBoxes<KIND> + (warp - 2) * kBoxBytes;
-        auto send = [&](int c, const float (&x)[32]) {
-          const CUtensorMap *out = &J.job[KIND == kGrads ? t.job : 0].out;
-          if (c % 2 == 0) {
-            if (lane == 0) bulk_wait_read();
-            __syncwarp();
-          }
-          box_row<T>(box, c & 1, x);
-          if (c % 2 == 0) return;
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            store_box(out, box, col + (c - 1) * 32, row);
-            bulk_commit();
-          }
-        };
-        for (int c = 0; c < chunks; ++c) {
-          float x[32];
-          tmem_ld32(from + group * kMaxTileN + c * 32, x);
-          if (c == chunks - 1) release(group);
-          const int d0 = col + c * 32;
-          const bool boxed = c < (chunks & ~1);
-          if constexpr (KIND == kStatsCols) {
-            float *buf = (float *)epi + (warp - 2) * 32 * kPitch;
-            Stat *red = (Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
-            const int at = d0 + lane;
-            long long wanted = -1;
-            if (at < W.N && BOUTE_INB(at, W.N)) wanted = W.targets[at];
-            // (rows of the accumulator beyond the block's hold what was in its shared memory)
-            const int rows = min(W.tile_m - quarter * 32, W.M - row);
-            if (lane >= rows)
-#pragma unroll
-              for (int q = 0; q < 32; ++q) x[q] = -INFINITY;
-#pragma unroll
-            for (int q = 0; q < 32; q += 4)
-              *(float4 *)(buf + lane * kPitch + q) = {x[q], x[q + 1], x[q + 2], x[q + 3]};
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < 32; ++q) x[q] = buf[q * kPitch + lane];
-            if (wanted >= row && wanted < row + min(rows, 32))
-              W.picked[at] = buf[(int)(wanted - row) * kPitch + lane];
-            red[quarter * kMaxTileN + c * 32 + lane] = stat_of(x, W.c2);
-            __syncwarp();
-          } else if constexpr (KIND == kStatsRows) {
-            if (d0 + 32 > W.N)
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (d0 + q >= W.N) x[q] = -INFINITY;
-            if (__any_sync(kAll, target >= d0 && target < d0 + 32))
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (target == d0 + q) W.picked[row + lane] = x[q];
-            join(run, stat_of(x, W.c2), W.c2);
-          } else if constexpr (KIND == kCoefCols) {
-            const int j = tgt[c * 32 + lane].j;
-            unsigned here = __ballot_sync(kAll, j >= row && j < row + 32);
-#pragma unroll
-            for (int q = 0; q < 32; ++q) {
-              const Position p = pos[c * 32 + q];
-              const float lp = max_nan(fmaf(x[q] - p.m, W.scale, -p.ls), -1e4f);
-              x[q] = exp2_fast(lp * kLog2e) * fmaf(p.b, lp, p.a);
-            }
-            if (here)
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if ((here >> q & 1u) && tgt[c * 32 + q].j == row + lane) x[q] += tgt[c * 32 + q].g;
-            if (d0 + 32 > W.N)  // (columns of no position, which a token of infinities makes NaN)
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (d0 + q >= W.N) x[q] = 0.f;
-            uint16_t *to = W.coef + (row + lane) * W.Tp + d0;
-            const bool mine = row + lane < W.M && BOUTE_INB(d0 + 31, W.Tp);
-            if (boxed) send(c, x);
-            else if (mine) store_row_of<T>(to, x);
-            if (W.low > 0 && mine && BOUTE_INB(d0 + W.low + 31, W.Tp)) {
-#pragma unroll
-              for (int q = 0; q < 32; ++q) x[q] -= to_float(from_float<T>(x[q]));
-              store_row_of<T>(to + W.low, x);
-            }
-          } else if constexpr (KIND == kCoefRows) {
-            const unsigned long long by = f2_dup(W.scale), less = f2_dup(-own.ls);
-            const unsigned long long top = f2_dup(-own.m);
-            const unsigned long long a2 = f2_dup(own.a), b2 = f2_dup(own.b), l2e = f2_dup(kLog2e);
-#pragma unroll
-            for (int q = 0; q < 32; q += 2) {
-              float l0, l1, y0, y1;
-              f2_split(f2_fma(f2_add(f2_pack(x[q], x[q + 1]), top), by, less), l0, l1);
-              const unsigned long long lp = f2_pack(max_nan(l0, -1e4f), max_nan(l1, -1e4f));
-              f2_split(f2_mul(lp, l2e), y0, y1);
-              f2_split(f2_mul(f2_pack(exp2_fast(y0), exp2_fast(y1)), f2_fma(b2, lp, a2)), x[q],
-                       x[q + 1]);
-            }
-            if (__any_sync(kAll, target >= d0 && target < d0 + 32))
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (target == d0 + q) x[q] += target_g;
-            send(c, x);
-          } else if (t.job == 0) {  // dh: rows of its elements, columns of the positions
-            if (row + lane < W.M && BOUTE_INB(row + lane, W.M)) {
-              const int n = min(32, W.N - d0);
-              float *to = W.sums + ((long long)t.split * W.N + d0) * W.M + row + lane;
-              if (t.k0 == t.k1)  // (a short piece's empty part)
-#pragma unroll
-                for (int q = 0; q < 32; ++q) x[q] = 0.f;
-              if (W.add) {
-                float was[32];  // (all on their way at once)
-#pragma unroll
-                for (int q = 0; q < 32; ++q)
-                  if (q < n) was[q] = to[(long long)q * W.M];
-#pragma unroll
-                for (int q = 0; q < 32; ++q)
-                  if (q < n) x[q] += was[q];
-              }
-#pragma unroll
-              for (int q = 0; q < 32; ++q)
-                if (q < n) to[(long long)q * W.M] = x[q];
-            }
-          } else {  // dW
-#pragma unroll
-            for (int q = 0; q < 32; ++q) x[q] *= mul;
-            T *to = (T *)W.out + (row + lane) * W.ldo + d0;
-            if (boxed && W.boxes) {
-              send(c, x);
-            } else if (boxed) {  // rows at any address: by way of the box, a row by its lanes
-              if (c % 2 == 0) __syncwarp();
-              box_row<T>(box, c & 1, x);
-              if (c % 2 == 1) {
-                __syncwarp();
-                const int rows = min(32, W.M - row);
-                for (int r = 0; r < rows; ++r) {
-                  T *line = (T *)W.out + (row + r) * W.ldo + d0 - 32;
-#pragma unroll
-                  for (int h = 0; h < 2; ++h) {
-                    const int e = h * 32 + lane;
-                    const int at = r * 128 + (((e / 8) ^ (r & 7)) << 4) + e % 8 * 2;
-                    const T v = *(const T *)(box + at);
-                    if (d0 - 32 + e < W.N && BOUTE_INB(row + r, W.M)) line[e] = v;
-                  }
-                }
-              }
-            } else if (row + lane < W.M && d0 < W.N && BOUTE_INB(row + lane, W.M)) {
-              if (d0 + 32 <= W.N && W.width >= 32) {
-                store_row_of<T>((uint16_t *)to, x);
-              } else if (d0 + 32 <= W.N && W.width >= 16) {
-#pragma unroll
-                for (int q = 0; q < 32; q += 8)
-                  *(uint4 *)(to + q) = {
-                      pack2(T{}, x[q], x[q + 1]), pack2(T{}, x[q + 2], x[q + 3]),
-                      pack2(T{}, x[q + 4], x[q + 5]), pack2(T{}, x[q + 6], x[q + 7])};
-              } else {
-#pragma unroll
-                for (int q = 0; q < 32; ++q)
-                  if (d0 + q < W.N) to[q] = from_float<T>(x[q]);
-              }
-            }
-          }
-          __syncwarp();
-        }
-        if constexpr (kStats) {
-          const long long parts = KIND == kStatsCols ? 2ll * W.nM : W.nN, all = parts * W.Tp;
-          auto write = [&](Stat a, long long at) {
-            if (!BOUTE_INB(at, all)) return;
-            W.part[at] = a.m;
-            W.part[all + at] = a.s;
-            W.part[2 * all + at] = a.u;
-          };
-          if constexpr (KIND == kStatsCols) {
-            named_barrier_sync(1 + group, kGroup);
-            const Stat *red =
-                (const Stat *)(epi + kEpiWarps * 32 * kPitch * 4) + group * 4 * kMaxTileN;
-            for (int c = gtid; c < W.tile_n; c += kGroup) {
-              Stat a = red[c];
-              for (int q = 1; q < 4; ++q) join(a, red[q * kMaxTileN + c], W.c2);
-              if (col + c < W.N) write(a, (2ll * t.m + rank) * W.Tp + col + c);
-            }
-          } else if (row + lane < W.M) {
-            write(run, t.n * W.Tp + row + lane);
-          }
+        } else if (row + lane < W.M) {
+          write(run, (kParted ? 2ll * t.n + group : t.n) * W.Tp + row + lane);
         }
       }
     }
@@ -778,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 1) hidden_kernel(const __grid_consta
 // The pieces' sums of kJoinAt positions a block (a sector of each piece's): a warp's lanes are four
 // pieces of each, and its warps 32 times those.
 constexpr int kJoinWarps = 32, kJoinAt = 8;
-__device__ __forceinline__ Stat join_lanes(Stat a, int from, Exponents c2) {
+__device__ __forceinline__ Stat join_lanes(Stat a, int from, float c2) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     if (o >= from)
@@ -789,7 +730,7 @@ __device__ __forceinline__ Stat join_lanes(Stat a, int from, Exponents c2) {
 __global__ void __launch_bounds__(32 * kJoinWarps)
     hidden_join_kernel(const Header *head, int blocks, const float *part, const float *picked,
                        const long long *targets, long long T, long long Tp, int parts, int V,
-                       float scale, Exponents c2, float *logprob, float *entropy, float *lse) {
+                       float scale, float k, float c2, float *logprob, float *entropy, float *lse) {
   __shared__ Stat red[kJoinAt][kJoinWarps + 1];
   pdl_wait();
   pdl_trigger();
@@ -821,9 +762,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   if (lane != 0 || t >= T || !BOUTE_INB(t, T)) return;
   const long long target = targets[t];
   const float ls = logf(a.s);
-  const float top = scale * a.m;  // (a scale may take it to an infinity)
+  const float back = k == 1.f ? 1.f : 0.5f;
+  const float top = scale * (a.m * back);  // (a scale may take it to an infinity)
   float l = top + ls, H = ls - kLn2 * (a.u / a.s), lp;
-  lp = target >= V ? NAN : target < 0 ? 0.f : scale * (picked[t] - a.m) - ls;
+  lp = target >= V ? NAN : target < 0 ? 0.f : scale * ((picked[t] - a.m) * back) - ls;
   if (top == -INFINITY) {
     l = -INFINITY;
     H = 0.f;
@@ -840,14 +782,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 
 // What each position's coefficients need, of 256 positions a block, and the largest bound of one:
 // |p (ln p + H)| < 4 for every distribution over BOUTE_MAX_VOCAB tokens. Positions that have no
-// coefficients, or none that are numbers, set no bound: the scale is the others'. Far positions take their
-// largest logit and ln s from the statistics' parts (a thread each: 4096 of 131072 tokens 0.2 ms).
+// coefficients, or none that are numbers, set no bound: the scale is the others'. Far positions take
+// their largest logit and ln s from the statistics' parts.
 __global__ void __launch_bounds__(256)
     hidden_positions_kernel(Header *head, int blocks, const long long *targets, long long t0,
                             long long T, int V, float scale, const float *lse,
                             const float *entropy, const float *g_logprob, const float *g_entropy,
-                            const float *part, int parts, long long Tp, Exponents c2, Position *pos,
-                            Target *tgt) {
+                            const float *part, int parts, long long Tp, float k, float c2,
+                            Position *pos, Target *tgt) {
   __shared__ unsigned red[8];
   pdl_wait();
   pdl_trigger();
@@ -856,20 +798,20 @@ __global__ void __launch_bounds__(256)
   if (t < T && BOUTE_INB(t, T)) {
     const long long target = targets[t];
     const float g = target < 0 ? 0.f : g_logprob[t], gh = g_entropy ? g_entropy[t] : 0.f;
-    Position p = {0.f, lse[t], -scale * g, -scale * gh};
-    Target to = {target >= 0 && target < V ? (int)target : -1, scale * g};
+    Position p = {lse[t], -scale * g, -scale * gh, scale * g};
+    Target to = {target >= 0 && target < V ? (int)target : -1, 0.f};
     if (g_entropy) p.a -= scale * gh * entropy[t];
     if (is_far(p.ls)) {
       Stat a = {-INFINITY, 0.f, 0.f};
       for (int q = 0; q < parts; ++q)
         if (BOUTE_INB(q * Tp + i, all))
           join(a, {part[q * Tp + i], part[all + q * Tp + i], 0.f}, c2);
-      p.m = a.m;
+      to.m = k == 1.f ? a.m : 0.5f * a.m;
       p.ls = logf(a.s);
     }
     const float most = scale * (fabsf(g) + 4.f * fabsf(gh));
     if (isfinite(most) && p.ls > -INFINITY && target < V) bound = most;
-    if (p.ls == -INFINITY) p = {0.f, 1e30f, 0.f, 0.f}, to.g = 0.f;  // a row without a token left
+    if (p.ls == -INFINITY) p = {1e30f, 0.f, 0.f, 0.f};  // a row without a token left
     if (target >= V) p.a = NAN;
     pos[t] = p;
     tgt[t] = to;
@@ -1035,6 +977,14 @@ int part_of(int D, bool few) {
   return (blocks + parts - 1) / parts;
 }
 
+// The same of dh's reduction over tokens and of dW's over positions, where one is of more than
+// grad_long blocks: up to there the steps cut off a quarter of what rounding to the type does, at
+// most, half of that on average. (512 tokens, dW of terms of one sign, without and with parts:
+// 131072 positions 8.4e-4 and 5e-5 off, 2^20 5.7e-3 and 5e-5; in parts throughout, 515 x 50021 x
+// 1000 took 181 us for 173.)
+constexpr int kGradPart = 64;
+constexpr int grad_long(int dtype) { return dtype == BOUTE_F16 ? 256 : 2048; }
+
 // The number of parts of dh's reduction over a piece, each a unit of its own of the pairs: the
 // fewest whose units are small beside a pair's share of the whole launch (other: dW's part of it),
 // so that dW's units even the pairs out.
@@ -1161,7 +1111,24 @@ int align_operand(Operand &x, long long rows, int D, long long ld, char *to, cud
   return r;
 }
 
-// The statistics of n positions from t0 on, in W.part; of far ones alone where W.lse is there.
+// A launch that takes logits, in parts; rows, columns: the positions'. The statistics and the
+// coefficients take them alike: a far position's x - m is of equal sums, and where all tokens share
+// a large term, what the steps beside it cut off is in lse as well. (One of 512, 4096 elements, in
+// one part: p 7e-3 off. 130 positions of 32768 tokens, 4096 elements: 2 % of the gradient's time,
+// 4096 1.)
+template <Kind ROWS, Kind COLUMNS>
+int launch_logits(const Plan &p, int dtype, int D, Jobs &J, cudaStream_t s, bool &parted) {
+  const bool few = !p.rows && J.job[0].w.tile_n <= 64;
+  J.part = part_of(D, few);
+  parted = J.part < blocks_of(D);
+  if (p.rows) return parted ? launch<ROWS, 4>(dtype, J, s) : launch<ROWS>(dtype, J, s);
+  return !parted ? launch<COLUMNS>(dtype, J, s)
+         : few   ? launch<COLUMNS, 1>(dtype, J, s)
+                 : launch<COLUMNS, 4>(dtype, J, s);
+}
+
+// The statistics of n positions from t0 on, in W.part; if W.lse is there, where it has far ones
+// alone.
 // parts: of each position, blocks: whose status is written.
 int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, const Work &with,
                  cudaStream_t s, int &parts, int &blocks) {
@@ -1172,6 +1139,7 @@ int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, co
   W.tile_m = p.tile_m;
   W.splits = 1;
   W.Tp = p.part_Tp;
+  J.far = W.lse != nullptr;
   CUtensorMap *mh = p.rows ? &J.job[0].a : &J.job[0].b, *mw = p.rows ? &J.job[0].b : &J.job[0].a;
   if (int r = make_map(mw, dtype, p.w.p, D, V, p.w.ld, p.rows ? kMaxTileN / 2 : p.tile_m)) return r;
   if (p.rows) {
@@ -1189,16 +1157,9 @@ int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, co
   if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
                        p.rows ? 128 : W.tile_n / 2))
     return r;
-  // (the coefficients' logits are in one part, and a far position's x - m has to be of equal sums)
-  J.part = W.lse ? blocks_of(D) : part_of(D, !p.rows && W.tile_n <= 64);
-  const bool parted = J.part < blocks_of(D);
+  bool parted;
+  if (int r = launch_logits<kStatsRows, kStatsCols>(p, dtype, D, J, s, parted)) return r;
   if (parted && p.rows) parts *= 2;  // (of both groups' columns)
-  int (*start)(int, Jobs &, cudaStream_t) =
-      p.rows ? (parted ? launch<kStatsRows, 4> : launch<kStatsRows>)
-                     : !parted         ? launch<kStatsCols>
-                     : W.tile_n <= 64 ? launch<kStatsCols, 1>
-                                      : launch<kStatsCols, 4>;
-  if (int r = start(dtype, J, s)) return r;
   blocks = 2 * pairs_of(J.units[0]);
   return BOUTE_OK;
 }
@@ -1285,6 +1246,7 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
   W.head = (Header *)(ws + p.header);
+  W.k = logits_by(scale);
   W.c2 = exponents_of(scale);
   W.part = (float *)(ws + p.part);
   W.picked = (float *)(ws + p.picked);
@@ -1295,7 +1257,7 @@ extern "C" int boute_hidden_logprobs(const void *hidden, int dtype, long long T,
     if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks)) return r;
     if (int r = launch_cluster(hidden_join_kernel, (n + kJoinAt - 1) / kJoinAt, 32 * kJoinWarps, 1,
                                0, s, W.head, blocks, W.part, W.picked, W.targets, n, p.part_Tp,
-                               parts, V, scale, W.c2, logprob + t0, entropy + t0, lse + t0))
+                               parts, V, scale, W.k, W.c2, logprob + t0, entropy + t0, lse + t0))
       return r;
   }
   return BOUTE_OK;
@@ -1338,6 +1300,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   W.head = (Header *)(ws + p.header);
   Position *pos = (Position *)(ws + p.pos);
   Target *tgt = (Target *)(ws + p.tgt);
+  W.k = logits_by(scale);
   W.c2 = exponents_of(scale);
   W.part = (float *)(ws + p.part);
   W.picked = (float *)(ws + p.picked);
@@ -1349,7 +1312,7 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks)) return r;
     if (int r = launch_cluster(hidden_positions_kernel, (n + 255) / 256, 256, 1, 0, s, W.head,
                                blocks, targets, t0, t0 + n, V, scale, lse, entropy, g_logprob,
-                               g_entropy, W.part, parts, p.part_Tp, W.c2, pos, tgt))
+                               g_entropy, W.part, parts, p.part_Tp, W.k, W.c2, pos, tgt))
       return r;
   }
   W.bounds = (int)((T + 255) / 256);
@@ -1388,7 +1351,8 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
       c.w.nM = tiles_v, c.w.nN = p.tiles_t, c.w.tile_n = p.tile_t;
     }
     if (int r = make_map(&c.out, dtype, W.coef, inner, outer, W.Tp, 32)) return r;
-    if (int r = p.rows ? launch<kCoefRows>(dtype, J, s) : launch<kCoefCols>(dtype, J, s)) return r;
+    bool parted;
+    if (int r = launch_logits<kCoefRows, kCoefCols>(p, dtype, D, J, s, parted)) return r;
     Job &g = J.job[0], &o = J.job[1];
     g.w = W;  // dh: rows of its elements, columns of the positions
     g.w.M = D, g.w.N = (int)both, g.w.K = n;
@@ -1413,7 +1377,11 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     o.w.width = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
     o.w.boxes = bits % 16 == 0;
     if (int r = o.w.boxes ? make_map(&o.out, dtype, o.w.out, D, n, lddw, 32) : 0) return r;
-    if (int r = launch<kGrads>(dtype, J, s)) return r;
+    J.part = kGradPart;
+    const bool lengthy =
+        std::max(blocks_of((int)both), (blocks_of(n) + p.splits - 1) / p.splits) >
+        grad_long(dtype);
+    if (int r = lengthy ? launch<kGrads, 4>(dtype, J, s) : launch<kGrads>(dtype, J, s)) return r;
   }
   return with_dtype(dtype, [&](auto t) {
     using E = decltype(t);

@@ -1,5 +1,5 @@
-// Whether arrays of rows share memory. (A header of its own, on the standard library alone, so that it
-// can be built without a device.)
+// Whether arrays of rows share memory. (A header of its own, on the standard library alone, so that
+// it can be built without a device.)
 #pragma once
 
 #include <cstddef>

@@ -1,0 +1,89 @@
+"""What long sums lose on the way to log-probabilities from hidden states and their gradient. The
+tensor cores cut off what fp32 does not hold beside the sum so far, 16 terms a step, up to a unit,
+2 U = 2^-23, each: sums are taken in parts, so that many steps do not add up to a bias."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_hidden import EPS, U, backward, forward, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("T", [5000, 16384, 16385, 40000, 131072, 1 << 20])
+def test_the_weights_gradient_of_many_positions(T):
+    """Each element is a sum over the positions of terms of one sign. Its relative error, averaged over
+    the elements, is the bias of the sum: the roundings to 16 bits, of the coefficients and of the result,
+    are apart by element or position. Up to 256 x 64 positions a sum has a step for 16 of them, beyond
+    that parts of 64 x 64 have 256; a step loses 2 U at most. p's own errors are 2 ulp of an exponential
+    and lse's rounding (lse < 8)."""
+    V, D = 300, 40
+    g = torch.Generator(device="cuda").manual_seed(T)
+    by = 1 + torch.rand((D,), generator=g, device="cuda")  # (sums apart, and with them their roundings)
+    h = (by + 0.25 * torch.rand((T, D), generator=g, device="cuda")).half()
+    w = (0.1 * torch.randn((V, D), generator=g, device="cuda")).half()
+    t = torch.full((T,), 7, dtype=torch.int64, device="cuda")
+    up = torch.rand((T,), generator=g, device="cuda") / T
+    lp, H, lse = forward(h, w, t, 1.0)
+    _, dw = backward(h, w, t, 1.0, lse, None, up, None)
+    want = torch.zeros((V, D), dtype=torch.float64, device="cuda")
+    for r in range(0, T, 1 << 16):
+        x = h[r:r + (1 << 16)].double()
+        c = -torch.softmax(x @ w.double().t(), 1)
+        c[:, 7] += 1
+        want += (c * up[r:r + (1 << 16), None].double()).t() @ x
+    error = (dw.double() - want) / want
+    # six deviations of the mean: the result's rounding (within EPS, uniform) and, by token, the
+    # coefficients'; and what elements below fp16's normal range lose
+    noise = 6 * EPS["f16"] / math.sqrt(3) * (1 / math.sqrt(V * D) + 1 / math.sqrt(V * T / 2))
+    tiny = (2.0 ** -25 / want.abs()).mean().item() * 6 / math.sqrt(V * D)
+    steps = T / 16 if T <= 16384 else 256
+    assert abs(error.mean().item()) <= steps * 2 * U + 16 * U + noise + tiny
+    assert (error.abs() <= 2 * EPS["f16"] + 2.0 ** -25 / want.abs()).all()
+
+
+@pytest.mark.parametrize("T", [3, 40, 130, 300, 600])
+@pytest.mark.parametrize("D", [2048, 4096])
+def test_gradient_of_logits_with_a_large_common_term(T, D):
+    """Each logit begins with 512, beside which fp32 holds multiples of 2^-14: 32 steps, which a part of
+    512 elements has, are off by 32 units at most and by their random half, 2^-14 sqrt(32 / 12), from
+    one token to another (of 16 blocks, sqrt(64 / 12)); all steps of 4096 elements were off by 255 2^-15
+    throughout. The entropy's gradient, whose coefficients p (ln p + H) show it, is otherwise off by its
+    roundings to 16 bits: EPS relative, and 2^-25 at least, as many of dw's elements are below 2^-14,
+    where fp16 has no finer step than 2^-24 (600 positions: elements of 9e-6, of which 2^-25 / sqrt(3),
+    uniform, is 2e-3)."""
+    V = 2000
+    h, w, t = inputs(T, V, D, "f16", seed=3)
+    h[:, :16], w[:, :16] = 0, 0
+    h[:, 0], w[:, 0] = 16.0, 32.0
+    gh = torch.randn((T,), device="cuda") / T
+    lp, H, lse = forward(h, w, t, 1.0)
+    dh, dw = backward(h, w, t, 1.0, lse, H, torch.zeros_like(gh), gh)
+    q = torch.log_softmax(h.double() @ w.double().t(), 1)
+    c = -gh.double()[:, None] * q.exp() * (q - (q.exp() * q).sum(1, keepdim=True))
+    p = 2.0 ** -14 * math.sqrt(64 / 12) + U * 512  # of ln p: in p, and beside 1 or so in ln p + H
+    tol = 2 * p + 2 * EPS["f16"] / math.sqrt(3)
+    for got, want in ((dh, c @ w.double()), (dw, c.t() @ h.double())):
+        got, want = got.double()[:, 16:], want[:, 16:]
+        least = 2.0 ** -25 / math.sqrt(3) * math.sqrt(want.numel())
+        assert (got - want).norm() <= tol * want.norm() + least, (got - want).norm() / want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,D", [(3, 700), (20, 1100), (64, 2048), (130, 1100), (300, 2048), (600, 1500)])
+def test_far_positions_coefficients_sum_to_0(T, D, dtype):
+    """Logits around 2^17, whose sums fp32 rounds to multiples of 2^-7 in an order of their own: the
+    coefficients' are those of which the largest and ln s were taken, so that p sums to 1. One element
+    of all tokens is 1 and adds a position's coefficients up: what they leave is their rounding (EPS
+    each; of the target's and of the others' together, g scale each) and that of p's sum."""
+    h, w, t = inputs(T, 1500, D, dtype, seed=8)
+    h[:, 0], w[:, 0] = 2.0 ** 9, 2.0 ** 8
+    h[:, -1], w[:, -1] = 0.0, 1.0
+    t = t.clamp_min(0)
+    g = torch.rand((T,), device="cuda") + 0.5
+    lp, H, lse = forward(h, w, t, 1.25)
+    assert (lse > 1e5).all()
+    dh, _ = backward(h, w, t, 1.25, lse, None, g, None)
+    tol = 1.25 * g.double() * (2 * EPS[dtype] + 64 * U)
+    assert (dh[:, -1].double().abs() <= tol).all()
