@@ -782,8 +782,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 
 // What each position's coefficients need, of 256 positions a block, and the largest bound of one:
 // |p (ln p + H)| < 4 for every distribution over BOUTE_MAX_VOCAB tokens. Positions that have no
-// coefficients, or none that are numbers, set no bound: the scale is the others'. Far positions take
-// their largest logit and ln s from the statistics' parts.
+// coefficients, or none that are numbers, set no bound: the scale is the others'. Far positions
+// take their largest logit and ln s from the statistics' parts.
 __global__ void __launch_bounds__(256)
     hidden_positions_kernel(Header *head, int blocks, const long long *targets, long long t0,
                             long long T, int V, float scale, const float *lse,
@@ -966,13 +966,15 @@ int pairs_of(long long units) {
 }
 int blocks_of(int k) { return (k + kBlockK - 1) / kBlockK; }
 
-// Blocks of the reduction that a logit of the statistics takes on the tensor cores at once, as even
-// as they come. Their sums cut off what fp32 does not hold, step by step; the parts are added up,
-// rounded, in registers. (4096 positions of 32768 tokens, 4096 elements: entropies in one part
-// 2.5e-6 off, in parts of 16 blocks 5.4e-7 for 1 % more time, of 8 2.4e-7 for another 1 to 3, at 515
-// positions 10, up to 64, where the weight is waited for, nothing.)
+// Blocks of the reduction that a logit takes on the tensor cores at once, as even as they come.
+// Their sums cut off what fp32 does not hold, step by step; the parts are added up, rounded, in
+// registers. (Entropies of 4096 positions, 5000 tokens: in parts of 16 blocks 3.5e-7 (bf16) and
+// 4.7e-7 (fp16) off, of 8 1.5e-7 and 2.1e-7, of 64 2.5e-6. 4096 x 131072 x 4096 takes 2411 us in
+// parts of 8, 2375 of 16, and the gradient with 4096 elements 2 % more; with 2048 elements it was
+// 2 % more for the statistics, at 515 positions 10, up to 64, where the weight is waited for,
+// nothing.)
 int part_of(int D, bool few) {
-  const int blocks = blocks_of(D), most = few ? 8 : 16;
+  const int blocks = blocks_of(D), most = few || blocks > 32 ? 8 : 16;
   const int parts = (blocks + most - 1) / most;
   return (blocks + parts - 1) / parts;
 }
@@ -980,7 +982,7 @@ int part_of(int D, bool few) {
 // The same of dh's reduction over tokens and of dW's over positions, where one is of more than
 // grad_long blocks: up to there the steps cut off a quarter of what rounding to the type does, at
 // most, half of that on average. (512 tokens, dW of terms of one sign, without and with parts:
-// 131072 positions 8.4e-4 and 5e-5 off, 2^20 5.7e-3 and 5e-5; in parts throughout, 515 x 50021 x
+// 131072 positions 8.4e-4 and 5e-5 off, 2^20 5.7e-3 and 1.1e-4; in parts throughout, 515 x 50021 x
 // 1000 took 181 us for 173.)
 constexpr int kGradPart = 64;
 constexpr int grad_long(int dtype) { return dtype == BOUTE_F16 ? 256 : 2048; }

@@ -87,3 +87,44 @@ def test_far_positions_coefficients_sum_to_0(T, D, dtype):
     dh, _ = backward(h, w, t, 1.25, lse, None, g, None)
     tol = 1.25 * g.double() * (2 * EPS[dtype] + 64 * U)
     assert (dh[:, -1].double().abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [60, 130, 600, 3000])
+@pytest.mark.parametrize("D", [512, 1024, 2048, 4096, 16384])
+def test_how_far_the_outputs_are_off(T, D, dtype):
+    """Relative 2-norms, at twice what is documented beside the parts: 2e-7 in parts of 512 elements, which
+    up to 64 positions and reductions of more than 2048 elements have, 4e-7 in others."""
+    h, w, t = inputs(T, 5000, D, dtype, seed=9)
+    lp, H, lse = forward(h, w, t, 1.0)
+    for r in range(0, T, 1000):
+        r = slice(r, r + 1000)
+        q = torch.log_softmax(h[r].double() @ w.double().t(), 1)
+        m = torch.logsumexp(h[r].double() @ w.double().t(), 1)
+        at = torch.where(t[r] >= 0, q.gather(1, t[r].clamp_min(0)[:, None])[:, 0], torch.zeros_like(m))
+        tol = 4e-7 if T <= 64 or D > 2048 or D <= 512 else 8e-7
+        for got, want in ((lp[r], at), (H[r], -(q.exp() * q).sum(1)), (lse[r], m)):
+            assert (got.double() - want).norm() <= tol * want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 20, 32, 33, 130, 600, 3000])
+@pytest.mark.parametrize("D", [512, 4096])
+def test_how_far_the_gradients_are_off(T, D, dtype):
+    """Relative 2-norms: one rounding to the type is EPS / sqrt(3) at most, its relative size being uniform
+    within EPS where a binade begins and half of that where it ends. Up to 32 positions that is all, with
+    more the coefficients' is there too, apart from the result's. (A tenth beyond: some hundred elements
+    at least, and logits' errors of 1e-6.)"""
+    h, w, t = inputs(T, 3000, D, dtype, seed=10)
+    g, gh = torch.randn((T,), device="cuda"), 0.3 * torch.randn((T,), device="cuda")
+    lp, H, lse = forward(h, w, t, 1.0)
+    dh, dw = backward(h, w, t, 1.0, lse, H, g, gh)
+    q = torch.log_softmax(h.double() @ w.double().t(), 1)
+    c = -q.exp() * (torch.where(t >= 0, g, 0 * g).double()[:, None]
+                    + gh.double()[:, None] * (q - (q.exp() * q).sum(1, keepdim=True)))
+    at = (t >= 0).nonzero()[:, 0]
+    c[at, t[at]] += g[at].double()
+    tol = 1.1 * EPS[dtype] / math.sqrt(3) * (1 if T <= 32 else math.sqrt(2))
+    tiny = 2.0 ** -25 if dtype == "f16" else 0.0  # (half of fp16's smallest step)
+    for got, want in ((dh, c @ w.double()), (dw, c.t() @ h.double())):
+        assert (got.double() - want).norm() <= tol * want.norm() + tiny * math.sqrt(want.numel() / 3)
