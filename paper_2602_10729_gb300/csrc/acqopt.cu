@@ -344,8 +344,7 @@ int launch_acq_optimize(const Gp *gp, const float *lower, const float *upper, co
     const size_t smem = (6 * n + (size_t)(T / 32) * std::min(n, panel) + 3 * (n + 1) +
                          (n > panel ? 2 * n : 0)) * sizeof(float);
     // (no shared-memory preference: what it leaves of the SM's memory caches W)
-    cudaFuncSetAttribute(acqopt_kernel<T, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                         (int)smem);
+    raise_smem(acqopt_kernel<T, R>, smem);
     launch_pdl(acqopt_kernel<T, R>, dim3(P, gp->B), dim3(T), smem, s, a);
   };
   // With at most 128 columns a row of W takes four registers of a lane, and starts beyond one

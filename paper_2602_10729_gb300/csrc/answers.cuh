@@ -5,8 +5,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <atomic>
-
 #include "internal.h"
 #include "regions.h"
 #include "warp_select.cuh"
@@ -179,21 +177,6 @@ inline int launch_cluster(void (*kernel)(KArgs...), long long blocks, int thread
   cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
   count_launch();
   return last_launch_status();
-}
-
-// Lets a kernel have `bytes` of dynamic shared memory, the most that any of its launches takes, once
-// on each device (allowed: those of the first 64 where it is done). The limit is the process's: set
-// to each call's own size, it would fail other threads' launches of more.
-inline int allow_smem(const void *kernel, size_t bytes, std::atomic<unsigned long long> &allowed) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return last_launch_status();
-  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
-  if (allowed.load(std::memory_order_relaxed) & bit) return BOUTE_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) !=
-      cudaSuccess)
-    return last_launch_status();
-  allowed.fetch_or(bit, std::memory_order_relaxed);
-  return BOUTE_OK;
 }
 
 }  // namespace boute

@@ -757,29 +757,27 @@ extern "C" int boute_expert_sort(const int *idx, long long T, int k, int E, int 
   if (int r = device_ok()) return r;
   const cudaStream_t s = (cudaStream_t)stream;
   Order A{idx, N, E, 0, 0, 0, offsets, source, place};
+  constexpr size_t kUnasked = 47 * 1024;  // of 48 KB that kernels have, beside static arrays
   auto go = [&](auto steps) -> int {
     constexpr int STEPS = decltype(steps)::value;
     A.blocks = (int)std::max(1ll, (N + kSortThreads * STEPS - 1) / (kSortThreads * STEPS));
     A.each = (int)(N / A.blocks);
     A.more = (int)(N % A.blocks);
     if (A.blocks <= kMaxCluster) {
-      static std::atomic<unsigned long long> allowed{0};
-      if (int r = allow_smem((const void *)expert_sort_kernel<STEPS>,
-                             sort_smem_bytes(BOUTE_MAX_EXPERTS), allowed))
-        return r;
-      return launch_cluster(expert_sort_kernel<STEPS>, A.blocks, kSortThreads, A.blocks,
-                            sort_smem_bytes(E), s, A);
+      const size_t smem = sort_smem_bytes(E);
+      if (smem > kUnasked && raise_smem(expert_sort_kernel<STEPS>, smem) != cudaSuccess)
+        return last_launch_status();
+      return launch_cluster(expert_sort_kernel<STEPS>, A.blocks, kSortThreads, A.blocks, smem, s,
+                            A);
     }
-    static std::atomic<unsigned long long> allowed{0};
-    if (int r = allow_smem((const void *)expert_place_kernel<STEPS>,
-                           place_smem_bytes<STEPS>(BOUTE_MAX_EXPERTS), allowed))
-      return r;
+    const size_t smem = place_smem_bytes<STEPS>(E);
+    if (smem > kUnasked && raise_smem(expert_place_kernel<STEPS>, smem) != cudaSuccess)
+      return last_launch_status();
     if (int r = launch_cluster(expert_count_kernel<STEPS>, A.blocks, kSortThreads, 1, 0, s, A))
       return r;
     if (int r = launch_cluster(expert_scan_kernel, kMaxCluster, kScanThreads, kMaxCluster, 0, s, A))
       return r;
-    return launch_cluster(expert_place_kernel<STEPS>, A.blocks, kSortThreads, 1,
-                          place_smem_bytes<STEPS>(E), s, A);
+    return launch_cluster(expert_place_kernel<STEPS>, A.blocks, kSortThreads, 1, smem, s, A);
   };
   // One launch of a cluster as far as it goes (24594 choices: 6.7 us, 8.3 in three); behind it
   // small blocks that fill the SMs, but for many choices, of which the blocks' counts would be most

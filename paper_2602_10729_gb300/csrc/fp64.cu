@@ -189,9 +189,7 @@ size_t post64_smem_bytes(int n, int d) {
 int launch_fit64(Gp *gp, const double *X, const double *Ys, const double *ls, const double *s2,
                  const double *noise, cudaStream_t s) {
   const size_t smem = fit64_smem_bytes(gp->n);
-  if (cudaFuncSetAttribute(fit64_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)smem) != cudaSuccess)
-    return last_launch_status();
+  if (raise_smem(fit64_kernel, smem) != cudaSuccess) return last_launch_status();
   fit64_kernel<<<gp->B * gp->m, kFit64Threads, smem, s>>>(X, Ys, ls, s2, noise, gp->n, gp->d,
                                                           gp->m, gp->W64, gp->a64, gp->xs64,
                                                           gp->status);
@@ -203,9 +201,7 @@ int launch_posterior64(const Gp *gp, const float *Xc, long long N, double *mean,
                        cudaStream_t s) {
   if (N <= 0) return BOUTE_OK;
   const size_t smem = post64_smem_bytes(gp->n, gp->d);
-  if (cudaFuncSetAttribute(posterior64_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)smem) != cudaSuccess)
-    return last_launch_status();
+  if (raise_smem(posterior64_kernel, smem) != cudaSuccess) return last_launch_status();
   const long long per = (N + kPost64Warps - 1) / kPost64Warps;
   const unsigned gx = (unsigned)std::max(1LL, std::min<long long>(per, 2LL * num_sms()));
   posterior64_kernel<<<dim3(gx, gp->B * gp->m), 32 * kPost64Warps, smem, s>>>(

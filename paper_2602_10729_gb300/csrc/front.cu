@@ -282,7 +282,7 @@ __global__ void front_fused_kernel(const double *Y, int n, int m, const double *
 int launch_pareto(const double *Ys, int B, int n, int m, const double *ref, unsigned char *mask,
                   double *front, int *P, cudaStream_t s) {
   const size_t smem = (size_t)n * m * sizeof(long long) + (size_t)n * sizeof(int) + 16;
-  cudaFuncSetAttribute(pareto_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  raise_smem(pareto_kernel, smem);
   pareto_kernel<<<B, 512, smem, s>>>(Ys, n, m, ref, mask, front, P);
   count_launch();
   return last_launch_status();
@@ -293,7 +293,7 @@ int launch_boxes(const double *front, const int *P, int B, int n, int m, const d
   size_t smem = 0;
   if (m == 3) smem = (size_t)13 * (n + 2) * sizeof(double);
   else if (m != 2) return BOUTE_ERR_UNSUPPORTED;
-  cudaFuncSetAttribute(boxes_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  raise_smem(boxes_kernel, smem);
   boxes_kernel<<<B, 256, smem, s>>>(front, P, n, m, ref, lower, upper, K);
   count_launch();
   return last_launch_status();
@@ -310,9 +310,7 @@ int launch_front_fused(const double *Y, int B, int n, int m, const double *ref, 
                        int *K, int want_boxes, cudaStream_t s) {
   const size_t smem = front_smem_bytes(n, m);
   prefer_shared(front_fused_kernel);
-  // (static arrays count against the same 48 KB default: always set)
-  cudaFuncSetAttribute(front_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                       (int)smem);
+  raise_smem(front_fused_kernel, smem);
   front_fused_kernel<<<B, 512, smem, s>>>(Y, n, m, ref, Ys, mask, front, P, lower, upper, K,
                                           want_boxes);
   count_launch();

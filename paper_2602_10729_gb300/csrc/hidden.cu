@@ -1095,8 +1095,8 @@ int launch(int dtype, Jobs &J, cudaStream_t s) {
     if constexpr (std::is_same<T, float>::value) {
       return (int)BOUTE_ERR_INVALID_ARG;
     } else {
-      static std::atomic<unsigned long long> allowed{0};
-      if (int r = allow_smem((const void *)hidden_kernel<KIND, T, MINE>, kSmem, allowed)) return r;
+      if (raise_smem(hidden_kernel<KIND, T, MINE>, kSmem) != cudaSuccess)
+        return last_launch_status();
       const size_t smem = 1024 + (size_t)J.stages * J.stage_bytes + kEpi<KIND>;
       return launch_cluster(hidden_kernel<KIND, T, MINE>, 2 * pairs, kThreads, 2, smem, s, J);
     }

@@ -376,15 +376,13 @@ int launch_insample(Gp *gp, const double *Ys, const double *s2, const double *no
   if (S < 1 || n > kInsMaxN) return BOUTE_ERR_UNSUPPORTED;
   const size_t smem = insample_smem_bytes(n);
   prefer_shared(insample_factor_kernel);
-  cudaFuncSetAttribute(insample_factor_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                       (int)smem);
+  raise_smem(insample_factor_kernel, smem);
   launch_pdl(insample_factor_kernel, dim3(BM), dim3(kInsThreads), smem, s,
              (const float *)gp->Wws, gp->plan.npad, gp->xt, gp->DP, gp->plan.nxt, Ys, s2, noise,
              n, gp->m, gp->iws, gp->bop, gp->plan, gp->status);
   const size_t smem2 = (2 * (size_t)n * ins_ld(n) + kInsDraws * kInsMaxN + kInsMaxN) * sizeof(float);
   prefer_shared(insample_draws_kernel);
-  cudaFuncSetAttribute(insample_draws_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                       (int)smem2);
+  raise_smem(insample_draws_kernel, smem2);
   launch_pdl(insample_draws_kernel, dim3((S + kInsDraws - 1) / kInsDraws, BM), dim3(kDrawThreads),
              smem2, s, n, S, z, Yin, gp->gws, gp->iws, (const int *)gp->status);
   const int kpairs = gp->plan.nchunk * (BOUTE_ACHUNK / 2);
@@ -631,7 +629,7 @@ int launch_nehvi2(const float *mean, const float *cvar, const float *shift, int 
   const bool vec = S % 4 == 0 && eps_stride % 4 == 0 && ((uintptr_t)eps & 15) == 0;
   auto go = [&](auto kern) {
     prefer_shared(kern);
-    cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    raise_smem(kern, smem);
     launch_pdl(kern, dim3(gx, B), dim3(kAcqThreads), smem, s, mean, cvar, shift, N, S, eps,
                eps_stride, (const float4 *)strips, counts, n, cons, acq);
   };

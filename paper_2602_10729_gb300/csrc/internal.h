@@ -6,6 +6,7 @@
 #include "bounds.cuh"
 #include "common.cuh"
 #include "device_info.h"
+#include "smem_limit.h"
 
 #include <nvtx3/nvToolsExt.h>
 

@@ -1172,7 +1172,7 @@ int launch_dp(const Gp *gp, const float *Xc, const float *kst, long long N, floa
   const int grid = std::max(1, std::min(a.tiles_total * a.m, num_sms()));  // (tile, objective) units
   auto go = [&](auto kern) {
     prefer_shared(kern);
-    cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    raise_smem(kern, smem);
     launch_pdl(kern, dim3(grid), dim3(Layout<DP>::kThreads), smem, s, a);
   };
   if (kst) {
@@ -1271,11 +1271,7 @@ int launch_kstar_dp(const Gp *gp, const float *Xc, long long N, float *kst, cuda
   const size_t smem = kstar_smem(gp);
   auto go = [&](auto kern) {
     prefer_shared(kern);
-    // (set on every launch: the kernel's static array counts against the same
-    // 48 KB default as the dynamic part)
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
-        cudaSuccess)
-      return last_launch_status();
+    if (raise_smem(kern, smem) != cudaSuccess) return last_launch_status();
     kern<<<units, Layout<DP>::kBld * 32, smem, s>>>(Xc, gp->xt, N, gp->d, gp->m, gp->n, tpp,
                                                     gp->plan.nxt, kst);
     return (int)BOUTE_OK;
