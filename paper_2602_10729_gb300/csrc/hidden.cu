@@ -1290,8 +1290,9 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     return BOUTE_ERR_INVALID_ARG;
   if (int r = device_ok()) return r;
   const cudaStream_t s = (cudaStream_t)stream;
+  const long long ldo = V > 1 ? lddw : up(D, 8);  // (one row has no pitch)
   if (T == 0)  // (no position: the weight's gradient is 0)
-    return cudaMemset2DAsync(dweight, lddw * 2, 0, (size_t)D * 2, V, s) == cudaSuccess
+    return cudaMemset2DAsync(dweight, ldo * 2, 0, (size_t)D * 2, V, s) == cudaSuccess
                ? BOUTE_OK
                : last_launch_status();
   char *ws = (char *)workspace;
@@ -1373,12 +1374,12 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     o.w.a_mn = p.rows, o.w.b_mn = 1;
     if (int r = make_map(&o.a, dtype, W.coef, inner, outer, W.Tp, p.rows ? kBlockK : 128)) return r;
     o.b = h_mn;
-    o.w.out = (char *)dweight + (size_t)v0 * lddw * 2;
-    o.w.ldo = lddw;
-    const uint64_t bits = (uintptr_t)dweight | (uint64_t)(lddw * 2);
+    o.w.out = (char *)dweight + (size_t)v0 * ldo * 2;
+    o.w.ldo = ldo;
+    const uint64_t bits = (uintptr_t)dweight | (uint64_t)(ldo * 2);
     o.w.width = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
     o.w.boxes = bits % 16 == 0;
-    if (int r = o.w.boxes ? make_map(&o.out, dtype, o.w.out, D, n, lddw, 32) : 0) return r;
+    if (int r = o.w.boxes ? make_map(&o.out, dtype, o.w.out, D, n, ldo, 32) : 0) return r;
     J.part = kGradPart;
     const bool lengthy =
         std::max(blocks_of((int)both), (blocks_of(n) + p.splits - 1) / p.splits) >
