@@ -803,9 +803,18 @@ __global__ void __launch_bounds__(256)
     if (g_entropy) p.a -= scale * gh * entropy[t];
     if (is_far(p.ls)) {
       Stat a = {-INFINITY, 0.f, 0.f};
-      for (int q = 0; q < parts; ++q)
-        if (BOUTE_INB(q * Tp + i, all))
-          join(a, {part[q * Tp + i], part[all + q * Tp + i], 0.f}, c2);
+      constexpr int kAtOnce = 8;  // on their way to a thread (one by one 392 took 260 us)
+      for (int q0 = 0; q0 < parts; q0 += kAtOnce) {
+        Stat b[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+          const long long at = (q0 + q) * Tp + i;
+          b[q] = {-INFINITY, 0.f, 0.f};
+          if (q0 + q < parts && BOUTE_INB(at, all)) b[q] = {part[at], part[all + at], 0.f};
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) join(a, b[q], c2);
+      }
       to.m = k == 1.f ? a.m : 0.5f * a.m;
       p.ls = logf(a.s);
     }
