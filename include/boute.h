@@ -732,10 +732,10 @@ int boute_expert_combine_grad(const void *g_out, int dtype, long long T, int D, 
                               const float *weight, int k, void *g_rows, long long ldg,
                               float *g_weight, void *stream);
 
-/* boute_token_logprobs for a caller who has the last hidden states and the vocabulary's weight:
- * logprob, entropy and lse for the logits hidden . weight^T (products of 16-bit numbers, summed in
- * fp32), which are never in memory, with its scale, its targets and its rules for what is masked,
- * NaN or infinite. The outputs are boute_answer_scores' inputs, its gradients this gradient's.
+/* boute_token_logprobs, but for its alternatives, for a caller who has the last hidden states and
+ * the vocabulary's weight: logprob, entropy and lse for the logits hidden . weight^T (products of
+ * 16-bit numbers, summed in fp32), which are never in memory, with its scale, its targets and its
+ * rules for what is masked, NaN or infinite. The outputs are boute_answer_scores' inputs, its gradients this gradient's.
  *   hidden: T rows of D (pitch ldh), weight: V rows of D (pitch ldw), both fp16 or both bf16 (fp32
  *   is refused: BOUTE_ERR_UNSUPPORTED); any 2-byte-aligned address and any pitch >= D, but rows at
  *   multiples of 16 bytes are read in place, others by way of an aligned copy in the workspace.
@@ -759,11 +759,13 @@ int boute_hidden_logprobs(const void *hidden, int dtype, long long T, int D, lon
  * forward call's lse and entropy and the outputs' gradients (g_entropy, and entropy with it, may be
  * NULL),
  *   dhidden = dlogits weight (T rows of D, pitch lddh), dweight = dlogits^T hidden (V rows, lddw),
- * rounded once to the type from fp32 sums. The products take each dlogits_tj rounded to the type, of
- * up to 32 positions as the sum of two such numbers (times a power of two, by which the largest
- * coefficient that the finite gradients allow comes near 2^14; what is less than 2^-28 of it loses
- * bits in fp16; positions without a distribution do not count). At most 256 MB of them are held at a
- * time (512 bytes a position, if that is more). */
+ * rounded once to the type from fp32 sums. Where |lse| > 1024, whose rounding would show in p, the
+ * row's largest logit and sum are taken once more (in the time of a forward call, if any is so). The
+ * products take each dlogits_tj rounded to the type, of up to 32 positions as the sum of two such
+ * numbers (times a power of two, by which the largest coefficient that the finite gradients allow
+ * comes near 2^14; what is less than 2^-28 of it loses bits in fp16; positions without a
+ * distribution do not count). At most 256 MB of them are held at a time (512 bytes a position, if
+ * that is more). */
 int boute_hidden_logprobs_grad(const void *hidden, int dtype, long long T, int D, long long ldh,
                                const void *weight, int V, long long ldw, const long long *targets,
                                float scale, const float *lse, const float *entropy,

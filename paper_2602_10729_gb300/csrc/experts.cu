@@ -2,8 +2,8 @@
 // rows copied there, the experts' rows summed back with the routing's weights, and the gradients.
 //
 // Memory bounds all but the smallest calls: 65536 queries of 2048 bf16, k = 8, are sorted and sent
-// to 256 experts in 383 us (0.94 of the copy rate) and their rows brought back in 343 (1.03); the
-// gradients of 32768 x 4096 take 994 (1.02). Rows that start anywhere go at 0.8 (sent), 0.65 (back)
+// to 256 experts in 370 us (0.97 of the copy rate) and their rows brought back in 345 (1.04); the
+// gradients of 32768 x 4096 take 995 (1.04). Rows that start anywhere go at 0.8 (sent), 0.65 (back)
 // and 0.6 to 0.9 (gradients) of it, short ones of those at 0.35. The order alone takes three
 // launches' latencies beyond 32768 choices (131072 of 64 experts: 8.6 us, 1048576 of 256: 20, of
 // which the scan of the blocks' counts is 6 and the places 10), a few queries the host's two calls

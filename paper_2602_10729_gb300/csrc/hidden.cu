@@ -16,19 +16,20 @@
 // one's products. The logits' pieces are as small as a tile (256 tokens), the coefficients' as
 // large as 256 MB: a piece's reductions and its tail of tiles are long beside what they wait for.
 //
-// Many positions are bound by the tensor cores (96 % of their cycles in the statistics, 94 and 83
+// Many positions are bound by the tensor cores (97 % of their cycles in the statistics, 91 and 78
 // in the gradient's two launches) and at that by power, which takes the clock to 1.7 GHz: 4096
-// positions x 131072 tokens, 4096 elements, bf16: 2.1 to 2.4 ms from machine to machine (1.86 to
-// 2.1 PFLOP/s; a library product that writes such logits 2.25); the gradient with 2048 elements 3.8
-// to 4.1 ms (1.62 to 1.74). In the gradient, what operands read by columns cost is not hidden
+// positions x 131072 tokens, 4096 elements, bf16: 2.38 to 2.52 ms from machine to machine (1.74 to
+// 1.85 PFLOP/s; a library product that writes such logits 2.25 ms); the gradient with 2048 elements
+// 4.1 to 4.23 ms (1.56 to 1.61). In the gradient, what operands read by columns cost is not hidden
 // (without their copies the launch took 508 us for 627). Few positions are bound by reading the
 // weight: one position of 50021 x 2048 takes 42 us (4.9 TB/s; 36 are the kernel's, the rest its
-// start, the last tile and the join), 64 of 32768 x 4096 51, and 157 for the gradient, which reads
+// start, the last tile and the join), 64 of 32768 x 4096 51, and 158 for the gradient, which reads
 // the weight twice and writes as much. Between them every 256 tokens ask as many bytes of the L2 as
-// it brings at the tensor cores' pace: 515 x 50021 x 1024 49 us (1.1 PFLOP/s). A weight whose rows
-// are no multiples of 128 bytes is read in pieces of two lines (515 x 50021 x 1000 fp16: gradient
-// 165 us, with 1024 elements 150), one of no multiples of 16 is copied first (64 x 32768 x 1001: 46
-// us, x 1000 22).
+// it brings at the tensor cores' pace: 515 x 50021 x 1024 47 to 50 us (1.1 PFLOP/s). A weight whose
+// rows are no multiples of 128 bytes is read in pieces of two lines (515 x 50021 x 1000 fp16:
+// gradient 167 to 178 us, with 1024 elements 157 to 161), one of no multiples of 16 is copied first
+// (64 x 32768 x 1001: 42 to 46 us, x 1000 18 to 22). Far positions cost what the statistics do (515
+// x 50021 x 1000: 265 us).
 #include <float.h>
 #include <limits.h>
 #include <math.h>
@@ -1139,10 +1140,11 @@ int launch_logits(const Plan &p, int dtype, int D, Jobs &J, cudaStream_t s, bool
 }
 
 // The statistics of n positions from t0 on, in W.part; if W.lse is there, where it has far ones
-// alone.
-// parts: of each position, blocks: whose status is written.
+// alone. parts: of each position, blocks: whose status is written. h_map, w_map: the operands', of
+// a caller who has them.
 int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, const Work &with,
-                 cudaStream_t s, int &parts, int &blocks) {
+                 cudaStream_t s, int &parts, int &blocks, const CUtensorMap *h_map = nullptr,
+                 const CUtensorMap *w_map = nullptr) {
   Jobs J{};
   Work &W = J.job[0].w;
   W = with;
@@ -1151,8 +1153,7 @@ int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, co
   W.splits = 1;
   W.Tp = p.part_Tp;
   J.far = W.lse != nullptr;
-  CUtensorMap *mh = p.rows ? &J.job[0].a : &J.job[0].b, *mw = p.rows ? &J.job[0].b : &J.job[0].a;
-  if (int r = make_map(mw, dtype, p.w.p, D, V, p.w.ld, p.rows ? kMaxTileN / 2 : p.tile_m)) return r;
+  CUtensorMap &mh = p.rows ? J.job[0].a : J.job[0].b, &mw = p.rows ? J.job[0].b : J.job[0].a;
   if (p.rows) {
     W.M = n, W.N = V;
     W.nM = (n + kPairM - 1) / kPairM;
@@ -1165,9 +1166,18 @@ int launch_stats(const Plan &p, int dtype, int D, int V, long long t0, int n, co
     parts = 2 * W.nM;
     tile_columns(n, W.nN, W.tile_n);
   }
-  if (int r = make_map(mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
-                       p.rows ? 128 : W.tile_n / 2))
+  if (w_map) {
+    mw = *w_map;
+  } else if (int r = make_map(&mw, dtype, p.w.p, D, V, p.w.ld,
+                              p.rows ? kMaxTileN / 2 : p.tile_m)) {
     return r;
+  }
+  if (h_map) {
+    mh = *h_map;
+  } else if (int r = make_map(&mh, dtype, (const char *)p.h.p + t0 * p.h.ld * 2, D, n, p.h.ld,
+                              p.rows ? 128 : W.tile_n / 2)) {
+    return r;
+  }
   bool parted;
   if (int r = launch_logits<kStatsRows, kStatsCols>(p, dtype, D, J, s, parted)) return r;
   if (parted && p.rows) parts *= 2;  // (of both groups' columns)
@@ -1310,6 +1320,11 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   if (int r = align_operand(p.w, V, D, ldw, ws + p.w_at, s)) return r;
   Work W{};
   W.head = (Header *)(ws + p.header);
+  CUtensorMap h_k, h_mn, w_k;
+  if (int r = make_map(&h_k, dtype, p.h.p, D, T, p.h.ld, p.rows ? 128 : p.tile_t / 2)) return r;
+  if (int r = make_map(&h_mn, dtype, p.h.p, D, T, p.h.ld, p.fine ? kBlockK / 2 : kBlockK))
+    return r;
+  if (int r = make_map(&w_k, dtype, p.w.p, D, V, p.w.ld, 128)) return r;
   Position *pos = (Position *)(ws + p.pos);
   Target *tgt = (Target *)(ws + p.tgt);
   W.k = logits_by(scale);
@@ -1321,7 +1336,9 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     W.targets = targets + t0;
     W.lse = lse + t0;
     int parts, blocks;
-    if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks)) return r;
+    if (int r = launch_stats(p, dtype, D, V, t0, n, W, s, parts, blocks, n == T ? &h_k : nullptr,
+                             &w_k))
+      return r;
     if (int r = launch_cluster(hidden_positions_kernel, (n + 255) / 256, 256, 1, 0, s, W.head,
                                blocks, targets, t0, t0 + n, V, scale, lse, entropy, g_logprob,
                                g_entropy, W.part, parts, p.part_Tp, W.k, W.c2, pos, tgt))
@@ -1339,10 +1356,6 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
   // other way round
   W.Tp = p.rows ? p.piece : p.columns();
   W.low = p.fine ? (int)p.Tp : 0;
-  CUtensorMap h_k, h_mn;
-  if (int r = make_map(&h_k, dtype, p.h.p, D, T, p.h.ld, p.rows ? 128 : p.tile_t / 2)) return r;
-  if (int r = make_map(&h_mn, dtype, p.h.p, D, T, p.h.ld, p.fine ? kBlockK / 2 : kBlockK))
-    return r;
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = std::min(p.piece, V - v0), tiles_v = (n + kPairM - 1) / kPairM;
     const char *w = (const char *)p.w.p + (size_t)v0 * p.w.ld * 2;
@@ -1351,8 +1364,9 @@ extern "C" int boute_hidden_logprobs_grad(const void *hidden, int dtype, long lo
     Job &c = J.job[0];
     c.w = W;
     c.w.K = D, c.w.row0 = v0;
-    CUtensorMap *mw = p.rows ? &c.b : &c.a;
-    if (int r = make_map(mw, dtype, w, D, n, p.w.ld, 128)) return r;
+    CUtensorMap &mw = p.rows ? c.b : c.a;
+    if (n == V) mw = w_k;
+    else if (int r = make_map(&mw, dtype, w, D, n, p.w.ld, 128)) return r;
     (p.rows ? c.a : c.b) = h_k;
     if (p.rows) {
       c.w.M = (int)T, c.w.N = n;
