@@ -14,7 +14,7 @@ namespace boute {
 // is set to the most that any call has asked for, under a lock; each time, as a reset of the device
 // takes it back; whatever the size, as static arrays count against the 48 KB that kernels have
 // unasked.
-inline cudaError_t raise_smem(const void *kernel, size_t bytes) {
+inline cudaError_t raise_smem(const void *kernel, size_t bytes) try {
   static std::mutex lock;
   static std::map<std::pair<const void *, int>, size_t> limits;
   int dev = 0;
@@ -26,6 +26,8 @@ inline cudaError_t raise_smem(const void *kernel, size_t bytes) {
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
   if (e == cudaSuccess) limit = most;
   return e;
+} catch (...) {  // (no memory for the table, or no lock: the callers are C entry points)
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 template <class... Args>
 inline cudaError_t raise_smem(void (*kernel)(Args...), size_t bytes) {

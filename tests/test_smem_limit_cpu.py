@@ -8,6 +8,8 @@ from paper_2602_10729_gb300 import build as bld
 HOST = r"""
 #include <atomic>
 #include <cstdio>
+#include <cstdlib>
+#include <new>
 #include <map>
 #include <thread>
 enum cudaError_t { cudaSuccess, cudaFailed };
@@ -22,12 +24,22 @@ static cudaError_t cudaFuncSetAttribute(const void *k, int, int bytes) {
   limit[device][(const int *)k - kernels] = bytes;
   return cudaSuccess;
 }
+static std::atomic<int> no_memory{0};
+void *operator new(size_t n) {
+  if (no_memory) throw std::bad_alloc();
+  return std::malloc(n);
+}
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, size_t) noexcept { std::free(p); }
 #include "smem_limit.h"
 using namespace boute;
 int main() {
   int bad = 0;
   auto want = [&](bool ok, const char *what) { if (!ok) ++bad, std::printf("%s\n", what); };
   const void *a = &kernels[0], *b = &kernels[1];
+  no_memory = 1;
+  want(raise_smem(a, 4000) == cudaSuccess && limit[0][0] == 4000, "no memory for the table: set all the same");
+  no_memory = 0;
   failing = 1;
   want(raise_smem(a, 5000) == cudaFailed, "a failure is told");
   failing = 0;
