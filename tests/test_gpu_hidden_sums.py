@@ -6,23 +6,25 @@ import math
 import pytest
 import torch
 
-from test_gpu_hidden import EPS, U, backward, forward, inputs
+from test_gpu_hidden import DT, EPS, U, backward, forward, inputs
 
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("T", [5000, 16384, 16385, 40000, 131072, 1 << 20])
-def test_the_weights_gradient_of_many_positions(T):
+@pytest.mark.parametrize("T,dtype", [
+    (5000, "f16"), (16384, "f16"), (16385, "f16"), (40000, "f16"), (131072, "f16"), (1 << 20, "f16"),
+    (5000, "bf16"), (131072, "bf16"), (131073, "bf16"), (1 << 20, "bf16")])
+def test_the_weights_gradient_of_many_positions(T, dtype):
     """Each element is a sum over the positions of terms of one sign. Its relative error, averaged over
     the elements, is the bias of the sum: the roundings to 16 bits, of the coefficients and of the result,
-    are apart by element or position. Up to 256 x 64 positions a sum has a step for 16 of them, beyond
-    that parts of 64 x 64 have 256; a step loses 2 U at most. p's own errors are 2 ulp of an exponential
+    are apart by element or position. Up to 256 x 64 positions (bf16: 2048 x 64) a sum has a step for 16 of
+    them, beyond that parts of 64 x 64 have 256; a step loses 2 U at most. p's own errors are 2 ulp of an exponential
     and lse's rounding (lse < 8)."""
     V, D = 300, 40
     g = torch.Generator(device="cuda").manual_seed(T)
     by = 1 + torch.rand((D,), generator=g, device="cuda")  # (sums apart, and with them their roundings)
-    h = (by + 0.25 * torch.rand((T, D), generator=g, device="cuda")).half()
-    w = (0.1 * torch.randn((V, D), generator=g, device="cuda")).half()
+    h = (by + 0.25 * torch.rand((T, D), generator=g, device="cuda")).to(DT[dtype])
+    w = (0.1 * torch.randn((V, D), generator=g, device="cuda")).to(DT[dtype])
     t = torch.full((T,), 7, dtype=torch.int64, device="cuda")
     up = torch.rand((T,), generator=g, device="cuda") / T
     lp, H, lse = forward(h, w, t, 1.0)
@@ -36,11 +38,12 @@ def test_the_weights_gradient_of_many_positions(T):
     error = (dw.double() - want) / want
     # six deviations of the mean: the result's rounding (within EPS, uniform) and, by token, the
     # coefficients'; and what elements below fp16's normal range lose
-    noise = 6 * EPS["f16"] / math.sqrt(3) * (1 / math.sqrt(V * D) + 1 / math.sqrt(V * T / 2))
-    tiny = (2.0 ** -25 / want.abs()).mean().item() * 6 / math.sqrt(V * D)
-    steps = T / 16 if T <= 16384 else 256
+    noise = 6 * EPS[dtype] / math.sqrt(3) * (1 / math.sqrt(V * D) + 1 / math.sqrt(V * T / 2))
+    least = 2.0 ** -25 if dtype == "f16" else 0.0
+    tiny = (least / want.abs()).mean().item() * 6 / math.sqrt(V * D)
+    steps = T / 16 if T <= (16384 if dtype == "f16" else 131072) else 256
     assert abs(error.mean().item()) <= steps * 2 * U + 16 * U + noise + tiny
-    assert (error.abs() <= 2 * EPS["f16"] + 2.0 ** -25 / want.abs()).all()
+    assert (error.abs() <= 2 * EPS[dtype] + least / want.abs()).all()
 
 
 @pytest.mark.parametrize("T", [3, 40, 130, 300, 600])
